@@ -254,6 +254,20 @@ dp_status dp_grad_sample_embedding(const int64_t *ids, const void *B, dp_dtype d
                                    int64_t cap, float *sqnorm, int32_t *status, void *ws,
                                    size_t ws_bytes, hipStream_t stream);
 
+/* The embedding layer's forward: rows of a table by token id, scaled,
+ *   Y[n][t][:] = s * E[ids[n][t]][:]
+ * (the product is formed in fp32 and rounded once to `dt_y`).  ids: int64
+ * [N][T]; E: [V][D] of `dt` (an fp32 master table may be read into bf16
+ * activations); Y: [N][T][D] of `dt_y`, overwritten, not overlapping E.  An id
+ * outside [0, V) sets DP_FLAG_BAD_INDEX and its row is written as zeros.
+ * N, T >= 0, V, D >= 1; needs N*T < 2^31 and D < 2^23 (else DP_EUNSUPPORTED)
+ * and V < 2^31.  Its gradient: dp_grad_sample_embedding (per sample),
+ * dp_clip_accumulate_tokens (the clipped sum, or, with norm NULL, the batch
+ * gradient), both with the same scale s. */
+dp_status dp_embedding_lookup(const int64_t *ids, const void *E, dp_dtype dt, int64_t N, int64_t T,
+                              int64_t V, int64_t D, float scale, void *Y, dp_dtype dt_y,
+                              int32_t *status, hipStream_t stream);
+
 /* LayerNorm's elementwise affine y = gamma * xhat + beta over D features at T
  * positions (the paper lists normalization layers among those supported):
  *   ggamma[n][k] = s * sum_t B[n][t][k] * xhat[n][t][k]
@@ -333,6 +347,53 @@ dp_status dp_grad_sample_groupnorm(const void *xhat, const void *B, dp_dtype dt,
 dp_status dp_lstm_backward(const float *gates, const float *c, const float *W_hh, const float *dh_out,
                            const float *dh_last, int64_t N, int64_t T, int64_t H, float *delta,
                            int32_t *status, hipStream_t stream);
+
+/* Activation of a gated feed-forward block:
+ *   DP_ACT_SILU       act(g) = g * sigmoid(g)
+ *   DP_ACT_GELU_TANH  act(g) = g/2 * (1 + tanh(sqrt(2/pi) * (g + 0.044715 g^3)))
+ * act'(g) below is the derivative of the same expression. */
+typedef enum dp_act { DP_ACT_SILU = 0, DP_ACT_GELU_TANH = 1 } dp_act;
+
+/* Gated feed-forward block, forward: both projections, the activation and
+ * the product in one call, over M rows (M = N*T positions, or 1 for a single
+ * token):
+ *   G = X Wg^T,  U = X Wu^T,  H = act(G) * U   (elementwise)
+ * X: [M][d_in]; Wg, Wu: [d_ff][d_in]; H: [M][d_ff]; all of `dt`, products
+ * summed in fp32.  H is formed from the fp32 sums and rounded once.  G and U:
+ * [M][d_ff] of `dt`, the projections rounded once, as the backward pass takes
+ * them; both NULL where no backward pass follows (one alone: DP_EINVAL).  The
+ * outputs overlap neither each other nor the inputs.  M >= 0, d_in, d_ff >= 1,
+ * each < 2^31 and M * d_ff, M * d_in, d_in * d_ff < 2^35 (else
+ * DP_EUNSUPPORTED).  A row of X that holds a NaN or an infinity makes its own
+ * rows of the outputs non-finite and no others.  The block's output
+ * projection is a Linear layer that takes H as its A.  Workspace:
+ * dp_gated_ffn_forward_workspace_bytes(M, d_in, d_ff, dt) bytes, 16-byte
+ * aligned. */
+size_t dp_gated_ffn_forward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt);
+dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const void *Wu, dp_dtype dt, int64_t M,
+                               int64_t d_in, int64_t d_ff, dp_act act, void *H, void *G, void *U,
+                               void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Gated feed-forward block, backward: from dH, the loss gradient at H, the
+ * backprops at the outputs of the two projections and the loss gradient at X:
+ *   BG = dH * U * act'(G),  BU = dH * act(G)   (elementwise)
+ *   dX = BG Wg + BU Wu
+ * BG and BU are what the per-sample gradients, ghost norms and clipped sums
+ * of the two weights take as B, with A = X (dp_grad_sample_linear,
+ * dp_ghost_norm_linear, dp_clip_accumulate_linear and their grouped forms).
+ * dH, G, U, BG, BU: [M][d_ff]; dX: [M][d_in] or NULL (not wanted; Wg and Wu
+ * may then be NULL); Wg, Wu: [d_ff][d_in]; all of `dt`.  BG and BU are formed
+ * in fp32 from the stored G and U and rounded once; dX is formed from BG and
+ * BU as stored, summed in fp32 and rounded once.  BG and BU may be the same
+ * arrays as dH, G or U (they then overwrite them), not the same as each other;
+ * otherwise outputs overlap nothing.  Sizes as for the forward.  Workspace:
+ * dp_gated_ffn_backward_workspace_bytes(M, d_in, d_ff, dt) bytes, 16-byte
+ * aligned. */
+size_t dp_gated_ffn_backward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt);
+dp_status dp_gated_ffn_backward(const void *dH, const void *G, const void *U, const void *Wg,
+                                const void *Wu, dp_dtype dt, int64_t M, int64_t d_in, int64_t d_ff,
+                                dp_act act, void *BG, void *BU, void *dX, void *ws, size_t ws_bytes,
+                                hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
  * Norms and clipping
@@ -494,6 +555,57 @@ dp_status dp_clip_accumulate_embedding(const int64_t *row_ptr, const int64_t *un
                                        int64_t N, int64_t V, int64_t D, float *sum,
                                        int32_t *status, void *ws, size_t ws_bytes,
                                        hipStream_t stream);
+
+/* Dense clipped sum of an Embedding layer from its ids and backprops, without
+ * the per-sample gradients (the embedding's counterpart of
+ * dp_clip_accumulate_linear):
+ *   sum[v][:] = s * sum over the positions (n, t) with ids[n][t] = v of c_n * B[n][t][:]
+ * with c_n = min(1, C / (norm[n] + 1e-6)) as in dp_clip_factors; norm NULL
+ * takes every c_n as 1 (the gradient of the whole batch; C is not used).  The
+ * positions are sorted by id and each id's rows are added in a fixed order
+ * (pieces of consecutive positions, then the pieces); rows v that no position
+ * holds are written as zeros.  ids: int64 [N][T]; B: [N][T][D] of `dt`; sum:
+ * fp32 [V][D].  The positions of a padding row (norm[n] < 0, see
+ * dp_per_sample_norms_active) are left out: neither their ids nor their
+ * backprops are looked at.  A NaN or infinite norm turns the rows of its
+ * sample's ids to NaN.  An id outside [0, V) sets DP_FLAG_BAD_INDEX and its
+ * position is left out.  N, T >= 0, V, D >= 1; needs N*T < 2^30, D < 2^22 and
+ * N*T*D < 2^37 (else DP_EUNSUPPORTED) and V < 2^31; there is no bound on T alone.
+ * Workspace: dp_clip_accumulate_tokens_workspace_bytes(N, T, V, D, dt) bytes,
+ * 16-byte aligned. */
+size_t dp_clip_accumulate_tokens_workspace_bytes(int64_t N, int64_t T, int64_t V, int64_t D, dp_dtype dt);
+dp_status dp_clip_accumulate_tokens(const int64_t *ids, const void *B, dp_dtype dt, int64_t N, int64_t T,
+                                    int64_t V, int64_t D, float scale, const float *norm, float C,
+                                    float *sum, int32_t *status, void *ws, size_t ws_bytes,
+                                    hipStream_t stream);
+
+/* One tensor of dp_clip_global_norm_many. */
+typedef struct dp_grad_tensor {
+    const void *g;   /* [numel] of `dtype`: a gradient */
+    void *out;       /* [numel] of `dtype`: the clipped gradient; may be g itself (in place), or NULL
+                        (the tensor counts in the norm only) */
+    int64_t numel;
+    int32_t dtype;   /* a dp_dtype; tensors of both types may be mixed */
+} dp_grad_tensor;
+
+/* The l2 norm of one gradient held in many tensors, and its clipping (the
+ * rule of dp_clip_factors, applied to the whole gradient instead of a
+ * sample's; for gradients that are not clipped per sample, or for bounding
+ * the noised average before an optimizer takes it):
+ *   norm[0] = sqrt(sum_k sum_e g_k[e]^2),  out_k[e] = c * g_k[e],
+ *   c = min(1, C / (norm[0] + 1e-6))
+ * Squares are formed and added in 64 bits, so no finite gradient overflows
+ * or underflows on the way; norm: fp32 [1], rounded once.  out_k is c times
+ * the value in fp32, rounded once to its type.  A norm that is NaN, or that
+ * fp32 cannot hold, sets DP_FLAG_NONFINITE and turns every out_k to NaN.  C =
+ * +inf gives c = 1.  items: a host array, read during the call only; count in
+ * [0, 65536] (0 writes norm = 0); a tensor's numel >= 0 is below 2^40.  The
+ * outs overlap nothing but their own g.  Workspace:
+ * dp_clip_global_norm_many_workspace_bytes(items, count) bytes, 16-byte
+ * aligned. */
+size_t dp_clip_global_norm_many_workspace_bytes(const dp_grad_tensor *items, int32_t count);
+dp_status dp_clip_global_norm_many(const dp_grad_tensor *items, int32_t count, float C, float *norm,
+                                   int32_t *status, void *ws, size_t ws_bytes, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
  * Grouped clipped sums and noise over many parameter tensors

@@ -5,7 +5,11 @@ marshals arguments: device pointers may be given as torch tensors (their
 ``data_ptr()``), raw integer addresses or None; ``ws_bytes`` is taken from the
 workspace tensor; ``stream`` defaults to torch's current HIP stream.  A status
 other than DP_OK raises :class:`DPError`.  There is no fallback: if the
-library is not built, loading fails loudly.
+library is not built, loading fails loudly.  The functions of the
+language-model operators (dp_embedding_lookup, dp_clip_accumulate_tokens,
+dp_gated_ffn_*, dp_clip_global_norm_many) also check their tensors: dense, on
+one GPU, of the declared type and at least the declared size, else ValueError
+or TypeError; they are enqueued on the tensors' GPU.
 """
 from __future__ import annotations
 
@@ -47,6 +51,11 @@ SIGNATURES = {
     "dp_grad_sample_embedding_workspace_bytes": (_SZ, [_I64, _I64]),
     "dp_grad_sample_embedding": (_ST, [_P, _P, _ST, _I64, _I64, _I64, _I64, _F, _P, _P, _P, _I64, _P,
                                        _P, _P, _SZ, _P]),
+    "dp_embedding_lookup": (_ST, [_P, _P, _ST, _I64, _I64, _I64, _I64, _F, _P, _ST, _P, _P]),
+    "dp_gated_ffn_forward_workspace_bytes": (_SZ, [_I64, _I64, _I64, _ST]),
+    "dp_gated_ffn_forward": (_ST, [_P, _P, _P, _ST, _I64, _I64, _I64, _ST, _P, _P, _P, _P, _SZ, _P]),
+    "dp_gated_ffn_backward_workspace_bytes": (_SZ, [_I64, _I64, _I64, _ST]),
+    "dp_gated_ffn_backward": (_ST, [_P, _P, _P, _P, _P, _ST, _I64, _I64, _I64, _ST, _P, _P, _P, _P, _SZ, _P]),
     "dp_grad_sample_layernorm_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
     "dp_grad_sample_layernorm": (_ST, [_P, _P, _ST, _I64, _I64, _I64, _F, _P, _P, _P, _P, _P, _SZ, _P]),
     "dp_grad_sample_groupnorm_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
@@ -71,6 +80,10 @@ SIGNATURES = {
     "dp_clip_accumulate_linear_many": (_ST, [_P, _I32, _ST, _I64, _P, _F, _P, _P, _SZ, _P]),
     "dp_clip_accumulate_embedding_workspace_bytes": (_SZ, [_I64, _I64]),
     "dp_clip_accumulate_embedding": (_ST, [_P, _P, _P, _I64, _P, _F, _I64, _I64, _I64, _P, _P, _P, _SZ, _P]),
+    "dp_clip_accumulate_tokens_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _ST]),
+    "dp_clip_accumulate_tokens": (_ST, [_P, _P, _ST, _I64, _I64, _I64, _I64, _F, _P, _F, _P, _P, _P, _SZ, _P]),
+    "dp_clip_global_norm_many_workspace_bytes": (_SZ, [_P, _I32]),
+    "dp_clip_global_norm_many": (_ST, [_P, _I32, _F, _P, _P, _P, _SZ, _P]),
     "dp_clip_noise_many_workspace_bytes": (_SZ, [_P, _I32, _I64]),
     "dp_clip_noise_many": (_ST, [_P, _I32, _I64, _P, _F, _U64, _U64, _P, _F, _F, _P, _P, _SZ, _P]),
     "dp_norms_clip_noise_workspace_bytes": (_SZ, [_P, _I32, _I64]),
@@ -211,6 +224,24 @@ def make_layernorm_layers(entries):
     return arr
 
 
+class DPGradTensor(ctypes.Structure):
+    """struct dp_grad_tensor of dpgrad.h."""
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+
+def make_grad_tensors(entries):
+    """A dp_grad_tensor array from (g, out, numel, dtype) tuples; out None: the tensor counts in the norm only."""
+    arr = (DPGradTensor * max(len(entries), 1))()
+    a = _Call("make_grad_tensors")
+    for i, (g, out, numel, dt) in enumerate(entries):
+        arr[i].g = a.ptr("g", g, _tdtype(dt), numel)
+        arr[i].out = a.ptr("out", out, _tdtype(dt), numel)
+        arr[i].numel = int(numel)
+        arr[i].dtype = int(dt)
+    return arr
+
+
 class DPError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -282,6 +313,51 @@ def dtype_of(t) -> int:
     if t.dtype == torch.bfloat16:
         return DP_BF16
     raise TypeError("unsupported dtype %s" % t.dtype)
+
+
+class _Call:
+    """Tensor arguments of one call: each must be dense, on one GPU, of its
+    type and at least its size (a host tensor's address, say, would fault the
+    GPU); addresses given as integers pass as they are.  The call is enqueued
+    on that GPU: on its current stream, unless the caller names one."""
+
+    def __init__(self, where):
+        self.where, self.device = where, None
+
+    def ptr(self, name, x, dtype, numel):
+        if x is None or isinstance(x, int):
+            return x
+        if not x.is_cuda:
+            raise ValueError("%s: %s is not on a GPU" % (self.where, name))
+        if self.device is None:
+            self.device = x.device
+        elif x.device != self.device:
+            raise ValueError("%s: %s is on %s, other arguments on %s" % (self.where, name, x.device, self.device))
+        if dtype is not None and x.dtype != dtype:
+            raise TypeError("%s: %s is %s, not %s" % (self.where, name, x.dtype, dtype))
+        if not x.is_contiguous():
+            raise ValueError("%s: %s is not contiguous" % (self.where, name))
+        if x.numel() < numel:
+            raise ValueError("%s: %s has %d elements, %d are needed" % (self.where, name, x.numel(), numel))
+        return x.data_ptr()
+
+    def run(self, fn, *args, stream):
+        dev = self.device
+        if dev is None:
+            _check(fn(*args, _stream(stream)), self.where)
+            return
+        import torch
+        if dev.index == torch.cuda.current_device():
+            _check(fn(*args, _stream(stream)), self.where)
+            return
+        with torch.cuda.device(dev):
+            _check(fn(*args, _stream(stream)), self.where)
+
+
+def _tdtype(dt):
+    """The torch type of a dp_dtype (None for an unknown one, which the call itself refuses)."""
+    import torch
+    return {DP_F32: torch.float32, DP_BF16: torch.bfloat16}.get(dt)
 
 
 def _check(code: int, where: str):
@@ -356,6 +432,40 @@ def dp_grad_sample_embedding(ids, B, dt, N, T, V, D, scale, row_ptr, uniq_ids, r
                                           _ptr(uniq_ids), _ptr(rows), cap, _ptr(sqnorm), _ptr(status),
                                           _ptr(ws), _nbytes(ws), _stream(stream)),
            "dp_grad_sample_embedding")
+
+
+def dp_embedding_lookup(ids, E, dt, N, T, V, D, scale, Y, dt_y, status=None, stream=None):
+    import torch
+    a = _Call("dp_embedding_lookup")
+    a.run(lib().dp_embedding_lookup, a.ptr("ids", ids, torch.int64, N * T), a.ptr("E", E, _tdtype(dt), V * D), dt, N, T,
+          V, D, scale, a.ptr("Y", Y, _tdtype(dt_y), N * T * D), dt_y, a.ptr("status", status, torch.int32, 1),
+          stream=stream)
+
+
+DP_ACT_SILU, DP_ACT_GELU_TANH = 0, 1
+
+
+def dp_gated_ffn_forward_workspace_bytes(M, d_in, d_ff, dt) -> int:
+    return lib().dp_gated_ffn_forward_workspace_bytes(M, d_in, d_ff, dt)
+
+
+def dp_gated_ffn_forward(X, Wg, Wu, dt, M, d_in, d_ff, act, H, G=None, U=None, ws=None, stream=None):
+    a, t = _Call("dp_gated_ffn_forward"), _tdtype(dt)
+    a.run(lib().dp_gated_ffn_forward, a.ptr("X", X, t, M * d_in), a.ptr("Wg", Wg, t, d_ff * d_in),
+          a.ptr("Wu", Wu, t, d_ff * d_in), dt, M, d_in, d_ff, act, a.ptr("H", H, t, M * d_ff),
+          a.ptr("G", G, t, M * d_ff), a.ptr("U", U, t, M * d_ff), a.ptr("ws", ws, None, 0), _nbytes(ws), stream=stream)
+
+
+def dp_gated_ffn_backward_workspace_bytes(M, d_in, d_ff, dt) -> int:
+    return lib().dp_gated_ffn_backward_workspace_bytes(M, d_in, d_ff, dt)
+
+
+def dp_gated_ffn_backward(dH, G, U, Wg, Wu, dt, M, d_in, d_ff, act, BG, BU, dX=None, ws=None, stream=None):
+    a, t = _Call("dp_gated_ffn_backward"), _tdtype(dt)
+    n, k = M * d_ff, d_ff * d_in
+    a.run(lib().dp_gated_ffn_backward, a.ptr("dH", dH, t, n), a.ptr("G", G, t, n), a.ptr("U", U, t, n),
+          a.ptr("Wg", Wg, t, k), a.ptr("Wu", Wu, t, k), dt, M, d_in, d_ff, act, a.ptr("BG", BG, t, n),
+          a.ptr("BU", BU, t, n), a.ptr("dX", dX, t, M * d_in), a.ptr("ws", ws, None, 0), _nbytes(ws), stream=stream)
 
 
 def dp_lstm_backward(gates, c, W_hh, dh_out, dh_last, N, T, H, delta, status=None, stream=None):
@@ -497,6 +607,30 @@ def dp_clip_accumulate_embedding(row_ptr, uniq_ids, rows, cap, norm, C, N, V, D,
                                               V, D, _ptr(sum), _ptr(status), _ptr(ws), _nbytes(ws),
                                               _stream(stream)),
            "dp_clip_accumulate_embedding")
+
+
+def dp_clip_accumulate_tokens_workspace_bytes(N, T, V, D, dt) -> int:
+    return lib().dp_clip_accumulate_tokens_workspace_bytes(N, T, V, D, dt)
+
+
+def dp_clip_accumulate_tokens(ids, B, dt, N, T, V, D, scale, norm, C, sum, status=None, ws=None, stream=None):
+    import torch
+    a = _Call("dp_clip_accumulate_tokens")
+    a.run(lib().dp_clip_accumulate_tokens, a.ptr("ids", ids, torch.int64, N * T), a.ptr("B", B, _tdtype(dt), N * T * D),
+          dt, N, T, V, D, scale, a.ptr("norm", norm, torch.float32, N), C, a.ptr("sum", sum, torch.float32, V * D),
+          a.ptr("status", status, torch.int32, 1), a.ptr("ws", ws, None, 0), _nbytes(ws), stream=stream)
+
+
+def dp_clip_global_norm_many_workspace_bytes(items, count) -> int:
+    return lib().dp_clip_global_norm_many_workspace_bytes(ctypes.cast(items, ctypes.c_void_p), count)
+
+
+def dp_clip_global_norm_many(items, count, C, norm, status=None, ws=None, stream=None):
+    import torch
+    a = _Call("dp_clip_global_norm_many")
+    a.run(lib().dp_clip_global_norm_many, ctypes.cast(items, ctypes.c_void_p), count, C,
+          a.ptr("norm", norm, torch.float32, 1), a.ptr("status", status, torch.int32, 1), a.ptr("ws", ws, None, 0),
+          _nbytes(ws), stream=stream)
 
 
 # ---------------------------------------------------------------------------

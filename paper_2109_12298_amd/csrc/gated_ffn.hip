@@ -1,0 +1,282 @@
+// Gated feed-forward block: both projections, the activation and the product
+// in one kernel, and its backward pass.
+//   forward:   G = X Wg^T, U = X Wu^T, H = act(G) * U
+//   backward:  BG = dH * U * act'(G), BU = dH * act(G), dX = BG Wg + BU Wu
+//
+// The forward computes a tile of G and the same tile of U in one workgroup
+// (each wave holds both accumulators of its positions and features), so that
+// H is formed from fp32 values in registers; G and U are written only where a
+// backward pass wants them.
+#include "gated_ffn.hpp"
+#include "mfma_tile.hpp"
+
+namespace dpg {
+namespace {
+
+using namespace ffn;
+
+constexpr int kThreads = 256;
+
+// ---------------------------------------------------------------------------
+// Any size, type and alignment: 64 x 64 tiles, element loads, fp32 MFMA
+// (products of bf16 values are exact in fp32).
+// ---------------------------------------------------------------------------
+constexpr int kTM = 64, kTN = 64, kTK = 16;
+constexpr int kLd = kTM + 1;              // LDS row: operands lie K-major, their loads come along K
+
+// rows r0 .. r0+63 of P [rows][K], columns k0 .. k0+kTK-1, into L [kTK][kLd]; zeros outside
+template <typename T>
+__device__ __forceinline__ void stage_rows(const T *__restrict__ P, i64 rows, i64 K, i64 r0, i64 k0, float *L)
+{
+#pragma unroll
+    for (int q = 0; q < kTM * kTK / kThreads; ++q) {
+        const int e = threadIdx.x + kThreads * q;
+        const int r = e / kTK, k = e % kTK;
+        L[k * kLd + r] = r0 + r < rows && k0 + k < K ? load_elem<T>(P, (r0 + r) * K + k0 + k) : 0.0f;
+    }
+}
+
+// rows k0 .. k0+kTK-1 of P [K][cols], columns c0 .. c0+63, into L [kTK][kLd]
+template <typename T>
+__device__ __forceinline__ void stage_cols(const T *__restrict__ P, i64 K, i64 cols, i64 k0, i64 c0, float *L)
+{
+#pragma unroll
+    for (int q = 0; q < kTN * kTK / kThreads; ++q) {
+        const int e = threadIdx.x + kThreads * q;
+        const int k = e / kTN, c = e % kTN;
+        L[k * kLd + c] = k0 + k < K && c0 + c < cols ? load_elem<T>(P, (k0 + k) * cols + c0 + c) : 0.0f;
+    }
+}
+
+template <typename T, int ACT>
+__global__ __launch_bounds__(kThreads) void ffn_forward_any_kernel(const T *__restrict__ X, const T *__restrict__ Wg,
+                                                                   const T *__restrict__ Wu, i64 M, i64 K, i64 F,
+                                                                   i64 tiles_f, T *__restrict__ H, T *__restrict__ G,
+                                                                   T *__restrict__ U)
+{
+    __shared__ float Xs[kTK * kLd], Gs[kTK * kLd], Us[kTK * kLd];
+    const i64 b = xcd_swizzle(blockIdx.x, gridDim.x);
+    const i64 m0 = b / tiles_f * kTM, f0 = b % tiles_f * kTN;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = (wave >> 1) * 32, wf = (wave & 1) * 32;
+    const int li = lane & 31, lk = lane >> 5;
+    f32x16 ag, au;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ag[r] = au[r] = 0.0f;
+    for (i64 k0 = 0; k0 < K; k0 += kTK) {
+        __syncthreads();
+        stage_rows(X, M, K, m0, k0, Xs);
+        stage_rows(Wg, F, K, f0, k0, Gs);
+        stage_rows(Wu, F, K, f0, k0, Us);
+        __syncthreads();
+#pragma unroll
+        for (int kk = 0; kk < kTK; kk += 2) {
+            const float x = Xs[(kk + lk) * kLd + wm + li];
+            ag = __builtin_amdgcn_mfma_f32_32x32x2f32(x, Gs[(kk + lk) * kLd + wf + li], ag, 0, 0, 0);
+            au = __builtin_amdgcn_mfma_f32_32x32x2f32(x, Us[(kk + lk) * kLd + wf + li], au, 0, 0, 0);
+        }
+    }
+    const i64 f = f0 + wf + li;
+    if (f >= F) return;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const i64 m = m0 + wm + 8 * (r >> 2) + 4 * lk + (r & 3);
+        if (m >= M) continue;
+        store_elem(H + m * F + f, act<ACT>(ag[r]) * au[r]);
+        if (G != nullptr) {
+            store_elem(G + m * F + f, ag[r]);
+            store_elem(U + m * F + f, au[r]);
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void ffn_dx_any_kernel(const T *__restrict__ BG, const T *__restrict__ BU,
+                                                              const T *__restrict__ Wg, const T *__restrict__ Wu, i64 M,
+                                                              i64 D, i64 F, i64 tiles_d, T *__restrict__ dX)
+{
+    __shared__ float Bs[kTK * kLd], Ws[kTK * kLd];
+    const i64 b = xcd_swizzle(blockIdx.x, gridDim.x);
+    const i64 m0 = b / tiles_d * kTM, d0 = b % tiles_d * kTN;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = (wave >> 1) * 32, wd = (wave & 1) * 32;
+    const int li = lane & 31, lk = lane >> 5;
+    f32x16 acc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+    for (int half = 0; half < 2; ++half) {
+        const T *P = half == 0 ? BG : BU, *W = half == 0 ? Wg : Wu;
+        for (i64 k0 = 0; k0 < F; k0 += kTK) {
+            __syncthreads();
+            stage_rows(P, M, F, m0, k0, Bs);
+            stage_cols(W, F, D, k0, d0, Ws);
+            __syncthreads();
+#pragma unroll
+            for (int kk = 0; kk < kTK; kk += 2)
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(Bs[(kk + lk) * kLd + wm + li], Ws[(kk + lk) * kLd + wd + li],
+                                                           acc, 0, 0, 0);
+        }
+    }
+    const i64 d = d0 + wd + li;
+    if (d >= D) return;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const i64 m = m0 + wm + 8 * (r >> 2) + 4 * lk + (r & 3);
+        if (m < M) store_elem(dX + m * D + d, acc[r]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The elementwise half of the backward pass: three arrays read, two written,
+// 16 bytes per lane and array where their alignment allows.
+// No __restrict__: BG and BU may be dH, G or U themselves (each element is
+// read before it is written, by the same thread).
+// ---------------------------------------------------------------------------
+template <typename T, int VEC>
+struct alignas(sizeof(T) * VEC) Pack {
+    T v[VEC];
+};
+
+template <typename T, int ACT, int VEC>
+__global__ __launch_bounds__(kThreads) void ffn_backprops_kernel(const T *dH, const T *G, const T *U, i64 n, T *BG,
+                                                                 T *BU)
+{
+    const i64 step = (i64)gridDim.x * kThreads * VEC;
+    for (i64 i = ((i64)blockIdx.x * kThreads + threadIdx.x) * VEC; i < n; i += step) {
+        if (VEC == 1 || i + VEC <= n) {
+            const Pack<T, VEC> h = *reinterpret_cast<const Pack<T, VEC> *>(dH + i);
+            const Pack<T, VEC> g = *reinterpret_cast<const Pack<T, VEC> *>(G + i);
+            const Pack<T, VEC> u = *reinterpret_cast<const Pack<T, VEC> *>(U + i);
+            Pack<T, VEC> bg, bu;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                float a, s;
+                act_and_slope<ACT>(load_elem<T>(g.v, j), a, s);
+                const float d = load_elem<T>(h.v, j);
+                store_elem(bg.v + j, d * load_elem<T>(u.v, j) * s);
+                store_elem(bu.v + j, d * a);
+            }
+            *reinterpret_cast<Pack<T, VEC> *>(BG + i) = bg;
+            *reinterpret_cast<Pack<T, VEC> *>(BU + i) = bu;
+        } else {
+            for (i64 e = i; e < n; ++e) {
+                float a, s;
+                act_and_slope<ACT>(load_elem<T>(G, e), a, s);
+                const float d = load_elem<T>(dH, e), u = load_elem<T>(U, e);
+                store_elem(BG + e, d * u * s);
+                store_elem(BU + e, d * a);
+            }
+        }
+    }
+}
+
+template <typename T, int ACT>
+void forward(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, void *H, void *G, void *U,
+             hipStream_t stream)
+{
+    const i64 tiles_f = ceil_div(F, kTN);
+    ffn_forward_any_kernel<T, ACT><<<(unsigned)(ceil_div(M, kTM) * tiles_f), kThreads, 0, stream>>>(
+        (const T *)X, (const T *)Wg, (const T *)Wu, M, K, F, tiles_f, (T *)H, (T *)G, (T *)U);
+}
+
+template <typename T, int ACT>
+void backprops(const void *dH, const void *G, const void *U, i64 n, void *BG, void *BU, hipStream_t stream)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    const bool vec = aligned(dH, 16) && aligned(G, 16) && aligned(U, 16) && aligned(BG, 16) && aligned(BU, 16);
+    const i64 blocks = ceil_div(n, (i64)kThreads * (vec ? VEC : 1));
+    const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
+    if (vec)
+        ffn_backprops_kernel<T, ACT, VEC><<<grid, kThreads, 0, stream>>>((const T *)dH, (const T *)G, (const T *)U, n,
+                                                                        (T *)BG, (T *)BU);
+    else
+        ffn_backprops_kernel<T, ACT, 1><<<grid, kThreads, 0, stream>>>((const T *)dH, (const T *)G, (const T *)U, n,
+                                                                      (T *)BG, (T *)BU);
+}
+
+template <typename T>
+void dx(const void *BG, const void *BU, const void *Wg, const void *Wu, i64 M, i64 D, i64 F, void *dX,
+        hipStream_t stream)
+{
+    const i64 tiles_d = ceil_div(D, kTN);
+    ffn_dx_any_kernel<T><<<(unsigned)(ceil_div(M, kTM) * tiles_d), kThreads, 0, stream>>>(
+        (const T *)BG, (const T *)BU, (const T *)Wg, (const T *)Wu, M, D, F, tiles_d, (T *)dX);
+}
+
+dp_status check_sizes(i64 M, i64 D, i64 F)
+{
+    DPG_REQUIRE(M >= 0 && D >= 1 && F >= 1, DP_EINVAL);
+    const i64 top = i64(1) << 31;
+    DPG_REQUIRE(M < top && D < top && F < top, DP_EUNSUPPORTED);
+    const i64 most = i64(1) << 35;       // a grid holds fewer than 2^24 workgroups, here of 64 x 64 values each
+    DPG_REQUIRE(M * D < most && M * F < most && D * F < most, DP_EUNSUPPORTED);
+    DPG_REQUIRE(ceil_div(M, kTM) * ceil_div(F > D ? F : D, kTN) < (i64(1) << 24), DP_EUNSUPPORTED);
+    return DP_OK;
+}
+
+bool act_ok(dp_act act) { return act == DP_ACT_SILU || act == DP_ACT_GELU_TANH; }
+
+}  // namespace
+}  // namespace dpg
+
+using namespace dpg;
+
+extern "C" size_t dp_gated_ffn_forward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt)
+{
+    (void)M; (void)d_in; (void)d_ff; (void)dt;
+    return 0;
+}
+
+extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const void *Wu, dp_dtype dt, int64_t M,
+                                          int64_t d_in, int64_t d_ff, dp_act act, void *H, void *G, void *U, void *ws,
+                                          size_t ws_bytes, hipStream_t stream)
+{
+    (void)ws; (void)ws_bytes;
+    DPG_REQUIRE(dtype_ok(dt), DP_EDTYPE);
+    DPG_REQUIRE(act_ok(act), DP_EINVAL);
+    const dp_status bad = check_sizes(M, d_in, d_ff);
+    if (bad != DP_OK) return bad;
+    if (M == 0) return DP_OK;
+    DPG_REQUIRE(X != nullptr && Wg != nullptr && Wu != nullptr && H != nullptr, DP_EINVAL);
+    DPG_REQUIRE((G == nullptr) == (U == nullptr), DP_EINVAL);
+    if (dt == DP_F32) {
+        if (act == DP_ACT_SILU) forward<float, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+        else forward<float, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+    } else {
+        if (act == DP_ACT_SILU) forward<uint16_t, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+        else forward<uint16_t, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+    }
+    return launch_status();
+}
+
+extern "C" size_t dp_gated_ffn_backward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt)
+{
+    (void)M; (void)d_in; (void)d_ff; (void)dt;
+    return 0;
+}
+
+extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const void *U, const void *Wg,
+                                           const void *Wu, dp_dtype dt, int64_t M, int64_t d_in, int64_t d_ff,
+                                           dp_act act, void *BG, void *BU, void *dX, void *ws, size_t ws_bytes,
+                                           hipStream_t stream)
+{
+    (void)ws; (void)ws_bytes;
+    DPG_REQUIRE(dtype_ok(dt), DP_EDTYPE);
+    DPG_REQUIRE(act_ok(act), DP_EINVAL);
+    const dp_status bad = check_sizes(M, d_in, d_ff);
+    if (bad != DP_OK) return bad;
+    if (M == 0) return DP_OK;
+    DPG_REQUIRE(dH != nullptr && G != nullptr && U != nullptr && BG != nullptr && BU != nullptr && BG != BU, DP_EINVAL);
+    DPG_REQUIRE(dX == nullptr || (Wg != nullptr && Wu != nullptr), DP_EINVAL);
+    const i64 n = M * d_ff;
+    if (dt == DP_F32) {
+        if (act == DP_ACT_SILU) backprops<float, DP_ACT_SILU>(dH, G, U, n, BG, BU, stream);
+        else backprops<float, DP_ACT_GELU_TANH>(dH, G, U, n, BG, BU, stream);
+        if (dX != nullptr) dx<float>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
+    } else {
+        if (act == DP_ACT_SILU) backprops<uint16_t, DP_ACT_SILU>(dH, G, U, n, BG, BU, stream);
+        else backprops<uint16_t, DP_ACT_GELU_TANH>(dH, G, U, n, BG, BU, stream);
+        if (dX != nullptr) dx<uint16_t>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
+    }
+    return launch_status();
+}
