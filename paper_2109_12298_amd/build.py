@@ -35,6 +35,7 @@ HIPFLAGS = ["-O3", "-std=c++17", "--offload-arch=" + ARCH, "-fPIC", "-Wall",
 EXTRA = {"clipsum_many.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
          "conv2d_split.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "conv2d_small.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+         "ffn_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
          "grad_many.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

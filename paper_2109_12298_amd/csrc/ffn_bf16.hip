@@ -1,0 +1,296 @@
+// Gated feed-forward block in bf16 on v_mfma_f32_32x32x16_bf16: tiles of G and U
+// (BM rows of X against BF rows of Wg and the same BF rows of Wu).
+//
+// Staging.  All three operands are K-major per row, so a stage is BK columns
+// of BM + 2 BF rows, copied straight to LDS (global_load_lds_dwordx4), NS
+// stages deep.  A staged row holds BK / 8 pieces of 16 bytes; piece q of row r
+// lies at piece q ^ f(r), so that the 16 rows that a quarter of a 16-byte LDS
+// read covers fall into 16 different pieces of the 256-byte bank window.
+// Operands are read one k-step (16 columns) ahead of the matrix instructions
+// that take them.
+//
+// MFMA rows run over features and columns over positions, so a lane's four
+// consecutive accumulators are four consecutive features of one position; G
+// and U of a (position, feature) sit in the same lane and register, and H is
+// formed there.  The results pass through LDS (each wave its own part) to be
+// stored by whole 16-byte pieces of rows.
+#include "ffn_bf16.hpp"
+
+#include "bf16_stage.hpp"
+#include "gated_ffn.hpp"
+
+namespace dpg {
+namespace {
+
+using namespace bf16s;
+using namespace ffn;
+
+// lane l's 16 bytes at base + off go to LDS byte lds + 16 l (see dma16)
+__device__ __forceinline__ void dma16_off(const void *base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base),
+                 "s"(__builtin_amdgcn_readfirstlane(lds))
+                 : "memory", "m0");
+}
+
+// wait until all but the last `later` (at most 2) stages' loads have landed, N loads each
+template <int N>
+__device__ __forceinline__ void wait_later(int later)
+{
+    if (later >= 2) wait_vmcnt<2 * N>();
+    else if (later == 1) wait_vmcnt<N>();
+    else wait_vmcnt<0>();
+}
+
+template <int BK>
+__device__ __forceinline__ int swizzle(int row)
+{
+    return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
+
+template <int BM_, int BF_, int WM_, int WF_, int BK_, int NS_>
+struct Shape {
+    static constexpr int BM = BM_, BF = BF_, WM = WM_, WF = WF_, BK = BK_, NS = NS_;
+    static constexpr int WAVES = WM * WF, THREADS = 64 * WAVES;
+    static constexpr int ROW = 2 * BK;                       // bytes of a staged row
+    static constexpr int ROWS = BM + 2 * BF;
+    static constexpr int STAGE = ROWS * ROW;
+    static constexpr int RPI = 1024 / ROW;                   // rows per load instruction
+    static constexpr int LOADS = ROWS / RPI / WAVES;         // per wave and stage
+    static constexpr int FM = BM / WM / 32, FF = BF / WF / 32;
+    static constexpr int LDT = FF * 64 + 16;                 // bytes of a row of the output transpose
+    static constexpr int LDS = NS * STAGE;
+    static_assert(LOADS * RPI * WAVES == ROWS && BM % RPI == 0 && BF % RPI == 0, "stage split");
+    static_assert(WAVES * 32 * LDT <= LDS, "the output transpose fits the stages");
+    static_assert(NS >= 2 && NS <= 4, "waits");
+    static_assert(BK / 16 % 2 == 0, "two sets of operands in turn");
+};
+
+// Tile order: workgroups go round robin over the XCDs; each XCD takes a run of
+// consecutive tiles, 8 tiles of positions by as many tiles of features as the
+// run holds, so that its L2 serves the operand rows that they share.
+__device__ __forceinline__ void tile_of(int b, int nb, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    constexpr int GM = 8;
+    const int t = (int)xcd_swizzle32((uint32_t)b, (uint32_t)nb);
+    const int group = t / (GM * tiles_n), m0 = group * GM;
+    const int gm = tiles_m - m0 < GM ? tiles_m - m0 : GM;
+    const int in = t - group * GM * tiles_n;
+    tm = m0 + in % gm;
+    tn = in / gm;
+}
+
+// 32 positions by FF * 32 features of one output, from LDS rows of LDT bytes
+template <int FF, int LDT>
+__device__ __forceinline__ void store_rows(const char *L, uint16_t *__restrict__ O, i64 M, i64 F, i64 m0, i64 f0,
+                                           bool vec, int lane)
+{
+    constexpr int LPR = FF * 4, RPS = 64 / LPR;              // lanes per row, rows per store
+#pragma unroll
+    for (int s = 0; s < 32 / RPS; ++s) {
+        const int row = s * RPS + lane / LPR, c = lane % LPR;
+        const uint4 v = *reinterpret_cast<const uint4 *>(L + row * LDT + 16 * c);
+        const i64 m = m0 + row, f = f0 + 8 * c;
+        if (m >= M) continue;
+        uint16_t *o = O + m * F + f;
+        if (vec) {
+            if (f < F) *reinterpret_cast<uint4 *>(o) = v;
+        } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (f + j < F) o[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        }
+    }
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    return (uint32_t)bf16_bits(a) | ((uint32_t)bf16_bits(b) << 16);
+}
+
+template <typename S, int ACT>
+__global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16_t *__restrict__ X,
+                                                                    const uint16_t *__restrict__ Wg,
+                                                                    const uint16_t *__restrict__ Wu, i64 M, i64 K, i64 F,
+                                                                    int tiles_m, int tiles_f, uint16_t *__restrict__ H,
+                                                                    uint16_t *__restrict__ G, uint16_t *__restrict__ U,
+                                                                    int vec)
+{
+    constexpr int FM = S::FM, FF = S::FF, BK = S::BK, NS = S::NS, ROW = S::ROW, KS = BK / 16;
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    int tm, tf;
+    tile_of((int)blockIdx.x, (int)gridDim.x, tiles_m, tiles_f, tm, tf);
+    const i64 m0 = (i64)tm * S::BM, f0 = (i64)tf * S::BF;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / S::WF * (FM * 32), wf = wave % S::WF * (FF * 32);
+    const uint32_t lds0 = lds_addr(smem);
+    const int nst = (int)((K + BK - 1) / BK);
+    const int tail = (int)(K - (i64)(nst - 1) * BK);         // columns of the last stage
+
+    // the wave's loads of a stage: rows past the end read the last row (their products are not stored)
+    const char *base[S::LOADS];
+    uint32_t off[S::LOADS];
+    int q[S::LOADS];
+#pragma unroll
+    for (int r = 0; r < S::LOADS; ++r) {
+        const int row = (wave + S::WAVES * r) * S::RPI + lane / (64 / S::RPI);
+        const int first = __builtin_amdgcn_readfirstlane(row);
+        const uint16_t *P = first < S::BM ? X + m0 * K : first < S::BM + S::BF ? Wg + f0 * K : Wu + f0 * K;
+        const int in = first < S::BM ? row : first < S::BM + S::BF ? row - S::BM : row - S::BM - S::BF;
+        const i64 left = first < S::BM ? M - m0 : F - f0;
+        base[r] = reinterpret_cast<const char *>(P);
+        q[r] = (lane % (64 / S::RPI)) ^ swizzle<BK>(row);
+        off[r] = (uint32_t)(in < left ? in : (int)left - 1) * (uint32_t)(2 * K) + 16u * q[r];
+    }
+    const auto issue = [&](int c) {
+        const uint32_t L = lds0 + (uint32_t)(c % NS) * S::STAGE;
+        const bool cut = c == nst - 1 && tail < BK;
+#pragma unroll
+        for (int r = 0; r < S::LOADS; ++r)
+            // columns past the end read the stage's first ones, and are zeroed in LDS
+            dma16_off(base[r] + (i64)c * (2 * BK), cut && 8 * q[r] >= tail ? off[r] - 16u * q[r] : off[r],
+                      L + 1024 * (wave + S::WAVES * r));
+    };
+    const auto zero_tail = [&](int c) {
+        if (c != nst - 1 || tail == BK) return;
+        char *L = smem + (c % NS) * S::STAGE;
+#pragma unroll
+        for (int r = 0; r < S::LOADS; ++r)
+            if (8 * q[r] >= tail)
+                *reinterpret_cast<uint4 *>(L + 1024 * (wave + S::WAVES * r) + 16 * lane) = make_uint4(0, 0, 0, 0);
+    };
+
+    f32x16_t ag[FM][FF], au[FM][FF];
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+        for (int y = 0; y < FF; ++y)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) ag[x][y][r] = au[x][y][r] = 0.0f;
+
+    struct Frag {
+        bf16x8_t x[FM], g[FF], u[FF];
+    };
+    const int li = lane & 31, lk = lane >> 5;
+    const int sw = swizzle<BK>(li);                          // of every row li + 32 n
+    const auto load_frag = [&](const char *L, int ks, Frag &f) {
+        const int at = 16 * ((2 * ks + lk) ^ sw) + li * ROW;
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+            f.x[x] = *reinterpret_cast<const bf16x8_t *>(L + (wm + 32 * x) * ROW + at);
+#pragma unroll
+        for (int y = 0; y < FF; ++y) {
+            f.g[y] = *reinterpret_cast<const bf16x8_t *>(L + (S::BM + wf + 32 * y) * ROW + at);
+            f.u[y] = *reinterpret_cast<const bf16x8_t *>(L + (S::BM + S::BF + wf + 32 * y) * ROW + at);
+        }
+    };
+    const auto mma = [&](const Frag &f) {
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+#pragma unroll
+            for (int y = 0; y < FF; ++y) {
+                ag[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.g[y], f.x[x], ag[x][y], 0, 0, 0);
+                au[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.u[y], f.x[x], au[x][y], 0, 0, 0);
+            }
+    };
+    // a k-step's operand reads between its matrix instructions
+    const auto interleave = [&]() {
+        constexpr int reads = FM + 2 * FF, mfma = 2 * FM * FF, per = (reads + mfma - 1) / mfma;
+#pragma unroll
+        for (int i = 0; i < reads / per; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       // a matrix instruction
+            __builtin_amdgcn_sched_group_barrier(0x100, per, 0);     // LDS reads
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, reads % per, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, mfma - reads / per, 0);
+    };
+
+#pragma unroll
+    for (int c = 0; c < NS - 1; ++c)
+        if (c < nst) issue(c);
+    {
+        const int later = (nst < NS - 1 ? nst : NS - 1) - 1;
+        wait_later<S::LOADS>(later);
+        zero_tail(0);
+        wait_lgkmcnt0();
+        stage_barrier();
+        if (NS - 1 < nst) issue(NS - 1);
+    }
+    // every trip is one straight run of blocks, so that the accumulators stay where they are: the last stage is peeled
+    Frag fa, fb;
+    load_frag(smem, 0, fa);
+    const auto inside = [&](const char *L) {
+#pragma unroll
+        for (int ks = 0; ks + 1 < KS; ++ks) {
+            load_frag(L, ks + 1, (ks & 1) == 0 ? fb : fa);
+            mma((ks & 1) == 0 ? fa : fb);
+            interleave();
+        }
+    };
+    for (int c = 0; c + 1 < nst; ++c) {
+        inside(smem + (c % NS) * S::STAGE);
+        // stage c + 1 has landed, and every wave has read the last of stage c: its buffer takes stage c + NS
+        wait_later<S::LOADS>(nst - 2 - c < NS - 2 ? nst - 2 - c : NS - 2);
+        zero_tail(c + 1);
+        wait_lgkmcnt0();
+        stage_barrier();
+        if (c + NS < nst) issue(c + NS);
+        load_frag(smem + ((c + 1) % NS) * S::STAGE, 0, fa);
+        mma(fb);
+        interleave();
+    }
+    inside(smem + ((nst - 1) % NS) * S::STAGE);
+    mma(fb);
+    __syncthreads();                                         // the stages become the output transposes
+
+    char *T = smem + wave * 32 * S::LDT;
+    const auto put = [&](int x, auto value, uint16_t *O) {
+#pragma unroll
+        for (int y = 0; y < FF; ++y)
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb) {
+                const uint2 v = make_uint2(pack2(value(y, 4 * rb), value(y, 4 * rb + 1)),
+                                           pack2(value(y, 4 * rb + 2), value(y, 4 * rb + 3)));
+                *reinterpret_cast<uint2 *>(T + li * S::LDT + 2 * (32 * y + 8 * rb + 4 * lk)) = v;
+            }
+        store_rows<FF, S::LDT>(T, O, M, F, m0 + wm + 32 * x, f0 + wf, vec != 0, lane);
+    };
+#pragma unroll
+    for (int x = 0; x < FM; ++x) {
+        put(x, [&](int y, int r) { return act_fast<ACT>(ag[x][y][r]) * au[x][y][r]; }, H);
+        if (G != nullptr) {
+            put(x, [&](int y, int r) { return ag[x][y][r]; }, G);
+            put(x, [&](int y, int r) { return au[x][y][r]; }, U);
+        }
+    }
+}
+
+template <typename S>
+void launch_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act,
+                    uint16_t *H, uint16_t *G, uint16_t *U, hipStream_t stream)
+{
+    const int tm = (int)ceil_div(M, S::BM), tf = (int)ceil_div(F, S::BF);
+    const int vec = F % 8 == 0 && aligned(H, 16) && aligned(G, 16) && aligned(U, 16);
+    const unsigned grid = (unsigned)((i64)tm * tf);
+    if (act == DP_ACT_SILU)
+        ffn_forward_kernel<S, DP_ACT_SILU><<<grid, S::THREADS, 0, stream>>>(X, Wg, Wu, M, K, F, tm, tf, H, G, U, vec);
+    else
+        ffn_forward_kernel<S, DP_ACT_GELU_TANH><<<grid, S::THREADS, 0, stream>>>(X, Wg, Wu, M, K, F, tm, tf, H, G, U,
+                                                                                 vec);
+}
+
+typedef Shape<256, 128, 4, 2, 64, 2> Large;
+typedef Shape<128, 64, 2, 2, 64, 2> Mid;
+
+}  // namespace
+
+void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act,
+                      uint16_t *H, uint16_t *G, uint16_t *U, hipStream_t stream)
+{
+    if (ceil_div(M, 256) * ceil_div(F, 128) >= 192) launch_forward<Large>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
+    else launch_forward<Mid>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
+}
+
+}  // namespace dpg

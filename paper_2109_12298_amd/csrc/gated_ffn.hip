@@ -8,6 +8,7 @@
 // H is formed from fp32 values in registers; G and U are written only where a
 // backward pass wants them.
 #include "gated_ffn.hpp"
+#include "ffn_bf16.hpp"
 #include "mfma_tile.hpp"
 
 namespace dpg {
@@ -242,6 +243,9 @@ extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const v
     if (dt == DP_F32) {
         if (act == DP_ACT_SILU) forward<float, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
         else forward<float, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+    } else if (M > 64 && ffn_rows_ok(X, d_in) && ffn_rows_ok(Wg, d_in) && ffn_rows_ok(Wu, d_in) && d_in < (1 << 21)) {
+        ffn_bf16_forward((const uint16_t *)X, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in, d_ff, act,
+                         (uint16_t *)H, (uint16_t *)G, (uint16_t *)U, stream);
     } else {
         if (act == DP_ACT_SILU) forward<uint16_t, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
         else forward<uint16_t, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
