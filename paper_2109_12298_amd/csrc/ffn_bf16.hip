@@ -284,6 +284,252 @@ void launch_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i
 typedef Shape<256, 128, 4, 2, 64, 2> Large;
 typedef Shape<128, 64, 2, 2, 64, 2> Mid;
 
+// ---------------------------------------------------------------------------
+// dX = BG Wg + BU Wu: one product whose K runs over BG's features, then BU's.
+// BG and BU are staged as X above; Wg and Wu lie K-major ([feature][d_in]),
+// so their operands come from transposing LDS reads (bf16_stage.hpp).
+// With several splits each takes a run of the stages and writes fp32 partial
+// tiles, which a second kernel adds in split order.
+// ---------------------------------------------------------------------------
+template <int BM_, int BD_, int WM_, int WD_, int BK_, int NS_>
+struct DxShape {
+    static constexpr int BM = BM_, BD = BD_, WM = WM_, WD = WD_, BK = BK_, NS = NS_;
+    static constexpr int WAVES = WM * WD, THREADS = 64 * WAVES;
+    static constexpr int A_ROW = 2 * BK, W_ROW = 2 * BD;         // bytes of a staged row
+    static constexpr int A_BYTES = BM * A_ROW, W_BYTES = BK * W_ROW, STAGE = A_BYTES + W_BYTES;
+    static constexpr int A_RPI = 1024 / A_ROW, W_RPI = 1024 / W_ROW;
+    static constexpr int A_LOADS = A_BYTES / 1024 / WAVES, W_LOADS = W_BYTES / 1024 / WAVES, LOADS = A_LOADS + W_LOADS;
+    static constexpr int FM = BM / WM / 32, FD = BD / WD / 32;
+    static constexpr int LDT = FD * 64 + 16;
+    static constexpr int LDS = NS * STAGE;
+    static_assert(A_LOADS * WAVES * 1024 == A_BYTES && W_LOADS * WAVES * 1024 == W_BYTES, "stage split");
+    static_assert(WAVES * 32 * LDT <= LDS, "the output transpose fits the stages");
+};
+
+template <typename S, bool SPLIT>
+__global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *__restrict__ BG,
+                                                               const uint16_t *__restrict__ BU,
+                                                               const uint16_t *__restrict__ Wg,
+                                                               const uint16_t *__restrict__ Wu, i64 M, i64 D, i64 F,
+                                                               int tiles_m, int tiles_d, int splits,
+                                                               uint16_t *__restrict__ dX, float *__restrict__ part,
+                                                               int vec)
+{
+    constexpr int FM = S::FM, FD = S::FD, BK = S::BK, NS = S::NS, KS = BK / 16;
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    int tm, td;
+    const int tiles = tiles_m * tiles_d, split = SPLIT ? (int)blockIdx.x / tiles : 0;
+    tile_of((int)blockIdx.x - split * tiles, tiles, tiles_m, tiles_d, tm, td);
+    const i64 m0 = (i64)tm * S::BM, d0 = (i64)td * S::BD;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / S::WD * (FM * 32), wd = wave % S::WD * (FD * 32);
+    const uint32_t lds0 = lds_addr(smem);
+    const int half = (int)((F + BK - 1) / BK);               // stages of each of the two products
+    const int tail = (int)(F - (i64)(half - 1) * BK);        // rows of W (columns of B) in the last of them
+    const int first = SPLIT ? (int)((i64)split * 2 * half / splits) : 0;
+    const int nst = (SPLIT ? (int)((i64)(split + 1) * 2 * half / splits) : 2 * half) - first;
+
+    uint32_t offA[S::A_LOADS], offW[S::W_LOADS];
+    int q[S::A_LOADS], kr[S::W_LOADS];
+#pragma unroll
+    for (int r = 0; r < S::A_LOADS; ++r) {
+        const int row = (wave + S::WAVES * r) * S::A_RPI + lane / (64 / S::A_RPI);
+        q[r] = (lane % (64 / S::A_RPI)) ^ swizzle<BK>(row);
+        offA[r] = (uint32_t)(row < M - m0 ? row : (int)(M - m0) - 1) * (uint32_t)(2 * F) + 16u * q[r];
+    }
+#pragma unroll
+    for (int r = 0; r < S::W_LOADS; ++r) {
+        kr[r] = (wave + S::WAVES * r) * S::W_RPI + lane / (64 / S::W_RPI);
+        const i64 d = 8 * ((lane % (64 / S::W_RPI)) ^ (4 * (kr[r] & 3)));
+        offW[r] = (uint32_t)kr[r] * (uint32_t)(2 * D) + (uint32_t)(2 * (d0 + d < D ? d : D - 8 - d0));
+    }
+    const auto issue = [&](int c) {
+        const uint32_t L = lds0 + (uint32_t)(c % NS) * S::STAGE;
+        const int g = first + c, u = g >= half, k = u ? g - half : g;
+        const bool cut = k == half - 1 && tail < BK;
+        const char *a = reinterpret_cast<const char *>((u ? BU : BG) + m0 * F) + (i64)k * (2 * BK);
+        const char *w = reinterpret_cast<const char *>((u ? Wu : Wg) + (i64)k * BK * D + d0);
+#pragma unroll
+        for (int r = 0; r < S::A_LOADS; ++r)
+            dma16_off(a, cut && 8 * q[r] >= tail ? offA[r] - 16u * q[r] : offA[r], L + 1024 * (wave + S::WAVES * r));
+#pragma unroll
+        for (int r = 0; r < S::W_LOADS; ++r)
+            dma16_off(w, cut && kr[r] >= tail ? offW[r] - (uint32_t)kr[r] * (uint32_t)(2 * D) : offW[r],
+                      L + S::A_BYTES + 1024 * (wave + S::WAVES * r));
+    };
+    // features past the end read the stage's first ones, and are zeroed in LDS on both sides
+    const auto zero_tail = [&](int c) {
+        const int g = first + c, k = g >= half ? g - half : g;
+        if (k != half - 1 || tail == BK) return;
+        char *L = smem + (c % NS) * S::STAGE;
+#pragma unroll
+        for (int r = 0; r < S::A_LOADS; ++r)
+            if (8 * q[r] >= tail)
+                *reinterpret_cast<uint4 *>(L + 1024 * (wave + S::WAVES * r) + 16 * lane) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < S::W_LOADS; ++r)
+            if (kr[r] >= tail)
+                *reinterpret_cast<uint4 *>(L + S::A_BYTES + 1024 * (wave + S::WAVES * r) + 16 * lane) =
+                    make_uint4(0, 0, 0, 0);
+    };
+
+    f32x16_t acc[FM][FD];
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+        for (int y = 0; y < FD; ++y)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.0f;
+
+    struct Frag {
+        bf16x8_t a[FM], w[FD];
+    };
+    const int li = lane & 31, lk = lane >> 5;
+    const int sw = swizzle<BK>(li);
+    const auto load_frag = [&](const char *L, int ks, Frag &f) {
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+            f.a[x] = *reinterpret_cast<const bf16x8_t *>(L + (wm + 32 * x + li) * S::A_ROW + 16 * ((2 * ks + lk) ^ sw));
+#pragma unroll
+        for (int y = 0; y < FD; ++y) f.w[y] = read_operand(L + S::A_BYTES, S::W_ROW, 16 * ks, wd + 32 * y, lane);
+    };
+    const auto mma = [&](const Frag &f) {
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+#pragma unroll
+            for (int y = 0; y < FD; ++y)
+                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[y], f.a[x], acc[x][y], 0, 0, 0);
+    };
+    const auto interleave = [&]() {
+        constexpr int reads = FM + 2 * FD, mfma = FM * FD, per = (reads + mfma - 1) / mfma;
+#pragma unroll
+        for (int i = 0; i < reads / per; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, per, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, reads % per, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, mfma - reads / per, 0);
+    };
+
+#pragma unroll
+    for (int c = 0; c < NS - 1; ++c)
+        if (c < nst) issue(c);
+    wait_later<S::LOADS>((nst < NS - 1 ? nst : NS - 1) - 1);
+    zero_tail(0);
+    wait_lgkmcnt0();
+    stage_barrier();
+    if (NS - 1 < nst) issue(NS - 1);
+    Frag fa, fb;
+    load_frag(smem, 0, fa);
+    const auto inside = [&](const char *L) {
+#pragma unroll
+        for (int ks = 0; ks + 1 < KS; ++ks) {
+            load_frag(L, ks + 1, (ks & 1) == 0 ? fb : fa);
+            mma((ks & 1) == 0 ? fa : fb);
+            interleave();
+        }
+    };
+    for (int c = 0; c + 1 < nst; ++c) {
+        inside(smem + (c % NS) * S::STAGE);
+        wait_later<S::LOADS>(nst - 2 - c < NS - 2 ? nst - 2 - c : NS - 2);
+        zero_tail(c + 1);
+        wait_lgkmcnt0();
+        stage_barrier();
+        if (c + NS < nst) issue(c + NS);
+        load_frag(smem + ((c + 1) % NS) * S::STAGE, 0, fa);
+        mma(fb);
+        interleave();
+    }
+    inside(smem + ((nst - 1) % NS) * S::STAGE);
+    mma(fb);
+
+    if constexpr (SPLIT) {
+        float *P = part + (i64)split * M * D;
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+#pragma unroll
+            for (int y = 0; y < FD; ++y)
+#pragma unroll
+                for (int rb = 0; rb < 4; ++rb) {
+                    const i64 m = m0 + wm + 32 * x + li, d = d0 + wd + 32 * y + 8 * rb + 4 * lk;
+                    if (m < M && d < D)                      // D % 8 == 0: the four are all in or all out
+                        *reinterpret_cast<float4 *>(P + m * D + d) =
+                            make_float4(acc[x][y][4 * rb], acc[x][y][4 * rb + 1], acc[x][y][4 * rb + 2],
+                                        acc[x][y][4 * rb + 3]);
+                }
+        return;
+    }
+    __syncthreads();
+    char *T = smem + wave * 32 * S::LDT;
+#pragma unroll
+    for (int x = 0; x < FM; ++x) {
+#pragma unroll
+        for (int y = 0; y < FD; ++y)
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb)
+                *reinterpret_cast<uint2 *>(T + li * S::LDT + 2 * (32 * y + 8 * rb + 4 * lk)) =
+                    make_uint2(pack2(acc[x][y][4 * rb], acc[x][y][4 * rb + 1]),
+                               pack2(acc[x][y][4 * rb + 2], acc[x][y][4 * rb + 3]));
+        store_rows<FD, S::LDT>(T, dX, M, D, m0 + wm + 32 * x, d0 + wd, vec != 0, lane);
+    }
+}
+
+// dX = the splits' partial sums, in split order
+__global__ __launch_bounds__(256) void ffn_dx_sum_kernel(const float *__restrict__ part, i64 n, int splits,
+                                                         uint16_t *__restrict__ dX)
+{
+    for (i64 i = ((i64)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (i64)gridDim.x * 1024) {
+        float4 s = *reinterpret_cast<const float4 *>(part + i);
+        for (int k = 1; k < splits; ++k) {
+            const float4 v = *reinterpret_cast<const float4 *>(part + (i64)k * n + i);
+            s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
+        }
+        const uint32_t w[2] = {pack2(s.x, s.y), pack2(s.z, s.w)};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dX[i + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+    }
+}
+
+typedef DxShape<256, 256, 2, 4, 64, 2> LargeDx;
+typedef DxShape<128, 128, 2, 2, 64, 2> MidDx;
+
+template <typename S>
+void launch_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
+               int splits, uint16_t *dX, float *part, hipStream_t stream)
+{
+    const int tm = (int)ceil_div(M, S::BM), td = (int)ceil_div(D, S::BD);
+    const int vec = aligned(dX, 16);
+    const unsigned grid = (unsigned)((i64)tm * td * splits);
+    if (splits == 1)
+        ffn_dx_kernel<S, false><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, tm, td, 1, dX, nullptr, vec);
+    else {
+        ffn_dx_kernel<S, true><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, tm, td, splits, dX, part, vec);
+        const i64 blocks = ceil_div(M * D, 1024);
+        ffn_dx_sum_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(part, M * D, splits, dX);
+    }
+}
+
+struct DxPlan {
+    bool large;
+    int splits;
+};
+
+DxPlan dx_plan(i64 M, i64 D, i64 F)
+{
+    DxPlan p;
+    p.large = ceil_div(M, 256) * ceil_div(D, 256) >= 192;
+    p.splits = 1;
+    if (!p.large) {
+        const i64 tiles = ceil_div(M, 128) * ceil_div(D, 128), stages = 2 * ceil_div(F, 64);
+        i64 s = 512 / tiles;
+        if (s > stages / 8) s = stages / 8;
+        if (s > 16) s = 16;
+        p.splits = s < 1 ? 1 : (int)s;
+    }
+    return p;
+}
+
 }  // namespace
 
 void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act,
@@ -291,6 +537,20 @@ void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu,
 {
     if (ceil_div(M, 256) * ceil_div(F, 128) >= 192) launch_forward<Large>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
     else launch_forward<Mid>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
+}
+
+size_t ffn_bf16_dx_workspace(i64 M, i64 D, i64 F)
+{
+    const DxPlan p = dx_plan(M, D, F);
+    return p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)(M * D) : 0;
+}
+
+void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
+                 uint16_t *dX, void *ws, hipStream_t stream)
+{
+    const DxPlan p = dx_plan(M, D, F);
+    if (p.large) launch_dx<LargeDx>(BG, BU, Wg, Wu, M, D, F, p.splits, dX, (float *)ws, stream);
+    else launch_dx<MidDx>(BG, BU, Wg, Wu, M, D, F, p.splits, dX, (float *)ws, stream);
 }
 
 }  // namespace dpg

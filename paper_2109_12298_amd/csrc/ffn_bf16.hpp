@@ -12,4 +12,10 @@ inline bool ffn_rows_ok(const void *p, i64 cols) { return cols % 8 == 0 && align
 void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act,
                       uint16_t *H, uint16_t *G, uint16_t *U, hipStream_t stream);
 
+// dX [M][D] = BG Wg + BU Wu from BG, BU [M][F] and Wg, Wu [F][D] (ffn_rows_ok
+// each); ws: ffn_bf16_dx_workspace bytes, 16-byte aligned
+size_t ffn_bf16_dx_workspace(i64 M, i64 D, i64 F);
+void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
+                 uint16_t *dX, void *ws, hipStream_t stream);
+
 }  // namespace dpg

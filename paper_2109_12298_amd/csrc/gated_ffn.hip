@@ -255,8 +255,8 @@ extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const v
 
 extern "C" size_t dp_gated_ffn_backward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt)
 {
-    (void)M; (void)d_in; (void)d_ff; (void)dt;
-    return 0;
+    if (!dtype_ok(dt) || check_sizes(M, d_in, d_ff) != DP_OK || M == 0) return 0;
+    return dt == DP_BF16 ? ffn_bf16_dx_workspace(M, d_in, d_ff) : 0;
 }
 
 extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const void *U, const void *Wg,
@@ -264,7 +264,6 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
                                            dp_act act, void *BG, void *BU, void *dX, void *ws, size_t ws_bytes,
                                            hipStream_t stream)
 {
-    (void)ws; (void)ws_bytes;
     DPG_REQUIRE(dtype_ok(dt), DP_EDTYPE);
     DPG_REQUIRE(act_ok(act), DP_EINVAL);
     const dp_status bad = check_sizes(M, d_in, d_ff);
@@ -272,6 +271,8 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
     if (M == 0) return DP_OK;
     DPG_REQUIRE(dH != nullptr && G != nullptr && U != nullptr && BG != nullptr && BU != nullptr && BG != BU, DP_EINVAL);
     DPG_REQUIRE(dX == nullptr || (Wg != nullptr && Wu != nullptr), DP_EINVAL);
+    const size_t need = dp_gated_ffn_backward_workspace_bytes(M, d_in, d_ff, dt);
+    DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
     const i64 n = M * d_ff;
     if (dt == DP_F32) {
         if (act == DP_ACT_SILU) backprops<float, DP_ACT_SILU>(dH, G, U, n, BG, BU, stream);
@@ -280,7 +281,13 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
     } else {
         if (act == DP_ACT_SILU) backprops<uint16_t, DP_ACT_SILU>(dH, G, U, n, BG, BU, stream);
         else backprops<uint16_t, DP_ACT_GELU_TANH>(dH, G, U, n, BG, BU, stream);
-        if (dX != nullptr) dx<uint16_t>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
+        if (dX == nullptr) return launch_status();
+        if (M > 64 && ffn_rows_ok(BG, d_ff) && ffn_rows_ok(BU, d_ff) && ffn_rows_ok(Wg, d_in) && ffn_rows_ok(Wu, d_in) &&
+            d_ff < (1 << 21) && d_in < (1 << 21))
+            ffn_bf16_dx((const uint16_t *)BG, (const uint16_t *)BU, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in,
+                        d_ff, (uint16_t *)dX, ws, stream);
+        else
+            dx<uint16_t>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
     }
     return launch_status();
 }
