@@ -281,9 +281,6 @@ void launch_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i
                                                                                  vec);
 }
 
-typedef Shape<256, 128, 4, 2, 64, 2> Large;
-typedef Shape<128, 64, 2, 2, 64, 2> Mid;
-
 // ---------------------------------------------------------------------------
 // dX = BG Wg + BU Wu: one product whose K runs over BG's features, then BU's.
 // BG and BU are staged as X above; Wg and Wu lie K-major ([feature][d_in]),
@@ -311,7 +308,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
                                                                const uint16_t *__restrict__ BU,
                                                                const uint16_t *__restrict__ Wg,
                                                                const uint16_t *__restrict__ Wu, i64 M, i64 D, i64 F,
-                                                               int tiles_m, int tiles_d, int splits,
+                                                               i64 lda, i64 ldw, int tiles_m, int tiles_d, int splits,
                                                                uint16_t *__restrict__ dX, float *__restrict__ part,
                                                                int vec)
 {
@@ -336,26 +333,26 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
     for (int r = 0; r < S::A_LOADS; ++r) {
         const int row = (wave + S::WAVES * r) * S::A_RPI + lane / (64 / S::A_RPI);
         q[r] = (lane % (64 / S::A_RPI)) ^ swizzle<BK>(row);
-        offA[r] = (uint32_t)(row < M - m0 ? row : (int)(M - m0) - 1) * (uint32_t)(2 * F) + 16u * q[r];
+        offA[r] = (uint32_t)(row < M - m0 ? row : (int)(M - m0) - 1) * (uint32_t)(2 * lda) + 16u * q[r];
     }
 #pragma unroll
     for (int r = 0; r < S::W_LOADS; ++r) {
         kr[r] = (wave + S::WAVES * r) * S::W_RPI + lane / (64 / S::W_RPI);
         const i64 d = 8 * ((lane % (64 / S::W_RPI)) ^ (4 * (kr[r] & 3)));
-        offW[r] = (uint32_t)kr[r] * (uint32_t)(2 * D) + (uint32_t)(2 * (d0 + d < D ? d : D - 8 - d0));
+        offW[r] = (uint32_t)kr[r] * (uint32_t)(2 * ldw) + (uint32_t)(2 * (d0 + d < ldw ? d : ldw - 8 - d0));
     }
     const auto issue = [&](int c) {
         const uint32_t L = lds0 + (uint32_t)(c % NS) * S::STAGE;
         const int g = first + c, u = g >= half, k = u ? g - half : g;
         const bool cut = k == half - 1 && tail < BK;
-        const char *a = reinterpret_cast<const char *>((u ? BU : BG) + m0 * F) + (i64)k * (2 * BK);
-        const char *w = reinterpret_cast<const char *>((u ? Wu : Wg) + (i64)k * BK * D + d0);
+        const char *a = reinterpret_cast<const char *>((u ? BU : BG) + m0 * lda) + (i64)k * (2 * BK);
+        const char *w = reinterpret_cast<const char *>((u ? Wu : Wg) + (i64)k * BK * ldw + d0);
 #pragma unroll
         for (int r = 0; r < S::A_LOADS; ++r)
             dma16_off(a, cut && 8 * q[r] >= tail ? offA[r] - 16u * q[r] : offA[r], L + 1024 * (wave + S::WAVES * r));
 #pragma unroll
         for (int r = 0; r < S::W_LOADS; ++r)
-            dma16_off(w, cut && kr[r] >= tail ? offW[r] - (uint32_t)kr[r] * (uint32_t)(2 * D) : offW[r],
+            dma16_off(w, cut && kr[r] >= tail ? offW[r] - (uint32_t)kr[r] * (uint32_t)(2 * ldw) : offW[r],
                       L + S::A_BYTES + 1024 * (wave + S::WAVES * r));
     };
     // features past the end read the stage's first ones, and are zeroed in LDS on both sides
@@ -445,7 +442,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
     mma(fb);
 
     if constexpr (SPLIT) {
-        float *P = part + (i64)split * M * D;
+        float *P = part + (i64)split * M * ldw;
 #pragma unroll
         for (int x = 0; x < FM; ++x)
 #pragma unroll
@@ -453,8 +450,8 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
 #pragma unroll
                 for (int rb = 0; rb < 4; ++rb) {
                     const i64 m = m0 + wm + 32 * x + li, d = d0 + wd + 32 * y + 8 * rb + 4 * lk;
-                    if (m < M && d < D)                      // D % 8 == 0: the four are all in or all out
-                        *reinterpret_cast<float4 *>(P + m * D + d) =
+                    if (m < M && d < ldw)                    // ldw % 8 == 0: the four are all in or all out
+                        *reinterpret_cast<float4 *>(P + m * ldw + d) =
                             make_float4(acc[x][y][4 * rb], acc[x][y][4 * rb + 1], acc[x][y][4 * rb + 2],
                                         acc[x][y][4 * rb + 3]);
                 }
@@ -475,10 +472,11 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
     }
 }
 
-// dX = the splits' partial sums, in split order
-__global__ __launch_bounds__(256) void ffn_dx_sum_kernel(const float *__restrict__ part, i64 n, int splits,
-                                                         uint16_t *__restrict__ dX)
+// dX = the splits' partial sums, in split order; rows of ld (a multiple of 8) there, of D here
+__global__ __launch_bounds__(256) void ffn_dx_sum_kernel(const float *__restrict__ part, i64 M, i64 D, i64 ld,
+                                                         int splits, uint16_t *__restrict__ dX)
 {
+    const i64 n = M * ld;
     for (i64 i = ((i64)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (i64)gridDim.x * 1024) {
         float4 s = *reinterpret_cast<const float4 *>(part + i);
         for (int k = 1; k < splits; ++k) {
@@ -486,55 +484,112 @@ __global__ __launch_bounds__(256) void ffn_dx_sum_kernel(const float *__restrict
             s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
         }
         const uint32_t w[2] = {pack2(s.x, s.y), pack2(s.z, s.w)};
+        if (D == ld) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) dX[i + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            for (int j = 0; j < 4; ++j) dX[i + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        } else {
+            const i64 m = i / ld, d = i - m * ld;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (d + j < D) dX[m * D + d + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        }
     }
 }
 
 typedef DxShape<256, 256, 2, 4, 64, 2> LargeDx;
 typedef DxShape<128, 128, 2, 2, 64, 2> MidDx;
+typedef DxShape<64, 128, 1, 4, 64, 3> Rows64Dx;
+typedef DxShape<32, 128, 1, 4, 64, 3> Rows32Dx;
 
 template <typename S>
 void launch_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
-               int splits, uint16_t *dX, float *part, hipStream_t stream)
+               i64 lda, i64 ldw, int splits, uint16_t *dX, float *part, hipStream_t stream)
 {
     const int tm = (int)ceil_div(M, S::BM), td = (int)ceil_div(D, S::BD);
-    const int vec = aligned(dX, 16);
+    const int vec = D % 8 == 0 && aligned(dX, 16);
     const unsigned grid = (unsigned)((i64)tm * td * splits);
-    if (splits == 1)
-        ffn_dx_kernel<S, false><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, tm, td, 1, dX, nullptr, vec);
-    else {
-        ffn_dx_kernel<S, true><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, tm, td, splits, dX, part, vec);
-        const i64 blocks = ceil_div(M * D, 1024);
-        ffn_dx_sum_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(part, M * D, splits, dX);
+    if (splits == 1) {
+        ffn_dx_kernel<S, false><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, lda, ldw, tm, td, 1, dX,
+                                                                 nullptr, vec);
+        return;
+    }
+    ffn_dx_kernel<S, true><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, lda, ldw, tm, td, splits, dX, part,
+                                                            vec);
+    const i64 blocks = ceil_div(M * ldw, 1024);
+    ffn_dx_sum_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(part, M, D, ldw, splits, dX);
+}
+
+// [rows][cols] into rows of ld > cols, zeros behind (16 bytes of the result per thread)
+__global__ __launch_bounds__(256) void ffn_pad_kernel(const uint16_t *__restrict__ P, i64 rows, i64 cols, i64 ld,
+                                                      uint16_t *__restrict__ O)
+{
+    const i64 per = ld / 8, n = rows * per;
+    for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < n; i += (i64)gridDim.x * 256) {
+        const i64 r = i / per, c = (i - r * per) * 8;
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t a = c + 2 * j < cols ? P[r * cols + c + 2 * j] : 0;
+            const uint32_t b = c + 2 * j + 1 < cols ? P[r * cols + c + 2 * j + 1] : 0;
+            w[j] = a | (b << 16);
+        }
+        *reinterpret_cast<uint4 *>(O + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
+i64 padded(i64 cols) { return (cols + 7) / 8 * 8; }
+
+size_t pad_bytes(i64 rows, i64 cols) { return cols % 8 == 0 ? 0 : align_up(sizeof(uint16_t) * (size_t)(rows * padded(cols)), 256); }
+
+// P itself, or its rows padded to 16 bytes in the workspace at ws, which is moved on
+const uint16_t *pad_rows(const uint16_t *P, i64 rows, i64 cols, char *&ws, hipStream_t stream)
+{
+    if (cols % 8 == 0) return P;
+    uint16_t *O = (uint16_t *)ws;
+    ws += pad_bytes(rows, cols);
+    const i64 blocks = ceil_div(rows * padded(cols) / 8, 256);
+    ffn_pad_kernel<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, stream>>>(P, rows, cols, padded(cols), O);
+    return O;
+}
+
+enum { kRows32, kRows64, kMid, kLarge };
+
 struct DxPlan {
-    bool large;
-    int splits;
+    int shape, splits;
 };
 
 DxPlan dx_plan(i64 M, i64 D, i64 F)
 {
     DxPlan p;
-    p.large = ceil_div(M, 256) * ceil_div(D, 256) >= 192;
     p.splits = 1;
-    if (!p.large) {
-        const i64 tiles = ceil_div(M, 128) * ceil_div(D, 128), stages = 2 * ceil_div(F, 64);
-        i64 s = 512 / tiles;
-        if (s > stages / 8) s = stages / 8;
-        if (s > 16) s = 16;
-        p.splits = s < 1 ? 1 : (int)s;
+    if (M > 64 && ceil_div(M, 256) * ceil_div(D, 256) >= 192) {
+        p.shape = kLarge;
+        return p;
     }
+    p.shape = M <= 32 ? kRows32 : M <= 64 ? kRows64 : kMid;
+    const i64 tiles = ceil_div(M, M <= 32 ? 32 : M <= 64 ? 64 : 128) * ceil_div(D, 128), stages = 2 * ceil_div(F, 64);
+    i64 s = 512 / tiles;
+    if (s > stages / 4) s = stages / 4;
+    if (s > 32) s = 32;
+    p.splits = s < 1 ? 1 : (int)s;
     return p;
 }
 
+typedef Shape<256, 128, 4, 2, 64, 2> Large;
+typedef Shape<128, 64, 2, 2, 64, 2> Mid;
+
 }  // namespace
 
+size_t ffn_bf16_forward_workspace(i64 M, i64 K, i64 F) { return pad_bytes(M, K) + 2 * pad_bytes(F, K); }
+
 void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act,
-                      uint16_t *H, uint16_t *G, uint16_t *U, hipStream_t stream)
+                      uint16_t *H, uint16_t *G, uint16_t *U, void *ws, hipStream_t stream)
 {
+    char *w = (char *)ws;
+    X = pad_rows(X, M, K, w, stream);
+    Wg = pad_rows(Wg, F, K, w, stream);
+    Wu = pad_rows(Wu, F, K, w, stream);
+    K = padded(K);
     if (ceil_div(M, 256) * ceil_div(F, 128) >= 192) launch_forward<Large>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
     else launch_forward<Mid>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
 }
@@ -542,15 +597,25 @@ void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu,
 size_t ffn_bf16_dx_workspace(i64 M, i64 D, i64 F)
 {
     const DxPlan p = dx_plan(M, D, F);
-    return p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)(M * D) : 0;
+    const size_t part = p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)(M * padded(D)) : 0;
+    return 2 * pad_bytes(M, F) + 2 * pad_bytes(F, D) + part;
 }
 
 void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
                  uint16_t *dX, void *ws, hipStream_t stream)
 {
     const DxPlan p = dx_plan(M, D, F);
-    if (p.large) launch_dx<LargeDx>(BG, BU, Wg, Wu, M, D, F, p.splits, dX, (float *)ws, stream);
-    else launch_dx<MidDx>(BG, BU, Wg, Wu, M, D, F, p.splits, dX, (float *)ws, stream);
+    char *w = (char *)ws;
+    BG = pad_rows(BG, M, F, w, stream);
+    BU = pad_rows(BU, M, F, w, stream);
+    Wg = pad_rows(Wg, F, D, w, stream);
+    Wu = pad_rows(Wu, F, D, w, stream);
+    const i64 lda = padded(F), ldw = padded(D);
+    float *part = (float *)w;
+    if (p.shape == kLarge) launch_dx<LargeDx>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, stream);
+    else if (p.shape == kMid) launch_dx<MidDx>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, stream);
+    else if (p.shape == kRows64) launch_dx<Rows64Dx>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, stream);
+    else launch_dx<Rows32Dx>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, stream);
 }
 
 }  // namespace dpg

@@ -5,14 +5,18 @@
 
 namespace dpg {
 
-// X, Wg and Wu as the tile kernels read them: rows of 16-byte pieces
-inline bool ffn_rows_ok(const void *p, i64 cols) { return cols % 8 == 0 && aligned(p, 16); }
+// Operands as the tile kernels take them: rows of any length from a 16-byte
+// boundary (rows that are no multiple of 16 bytes are padded into the
+// workspace first), row offsets of a tile in 32 bits.
+inline bool ffn_tiles_ok(const void *p, i64 cols) { return aligned(p, 16) && cols < (i64(1) << 21); }
 
-// H (and G, U unless NULL) from X [M][K], Wg, Wu [F][K] (ffn_rows_ok each)
+// H (and G, U unless NULL) from X [M][K], Wg, Wu [F][K] (ffn_tiles_ok each);
+// ws: ffn_bf16_forward_workspace bytes, 16-byte aligned
+size_t ffn_bf16_forward_workspace(i64 M, i64 K, i64 F);
 void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act,
-                      uint16_t *H, uint16_t *G, uint16_t *U, hipStream_t stream);
+                      uint16_t *H, uint16_t *G, uint16_t *U, void *ws, hipStream_t stream);
 
-// dX [M][D] = BG Wg + BU Wu from BG, BU [M][F] and Wg, Wu [F][D] (ffn_rows_ok
+// dX [M][D] = BG Wg + BU Wu from BG, BU [M][F] and Wg, Wu [F][D] (ffn_tiles_ok
 // each); ws: ffn_bf16_dx_workspace bytes, 16-byte aligned
 size_t ffn_bf16_dx_workspace(i64 M, i64 D, i64 F);
 void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,

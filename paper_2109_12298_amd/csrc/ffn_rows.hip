@@ -1,0 +1,219 @@
+// Gated feed-forward block over few rows (a decoding step's single token up
+// to 64 rows): bound by reading Wg and Wu once.
+//
+// A workgroup takes 16 features of Wg and Wu and all rows of X; its waves
+// split K in units of 128 bytes of a row, unit by unit in turn, so that the
+// workgroup reads each weight row front to back.  Weights go straight from
+// memory to registers in the operand layout of v_mfma_f32_16x16x32_bf16 (or
+// v_mfma_f32_16x16x4_f32): lane l holds 16 bytes of feature l % 16; the
+// matrix unit's columns are the rows of X (rows past M repeat the last one
+// and are not stored).  X comes from the caches.  The waves' sums meet in LDS,
+// added in wave order, where G, U and H are formed.
+//
+// For fp32 a lane's four consecutive values k .. k + 3 feed four products,
+// whose k index runs over the lane groups: any order of K serves, as long as
+// both operands use the same.
+#include "ffn_rows.hpp"
+
+#include "gated_ffn.hpp"
+
+#include <type_traits>
+
+namespace dpg {
+namespace {
+
+using namespace ffn;
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kFT = 16;                   // features per workgroup
+constexpr int kMaxWaves = 16;
+
+template <typename T>
+struct Piece {                            // a lane's share of one step: 16 bytes of a row
+    static constexpr int N = 16 / sizeof(T);
+    static constexpr int STEP = 4 * N;    // columns of a step (four lane groups); two steps are a unit of 128 bytes
+    alignas(16) T v[N];
+};
+
+// columns k .. k + N - 1 of the row at p, zeros at and past K
+template <typename T, bool VEC>
+__device__ __forceinline__ Piece<T> load_cut(const T *p, i64 k, i64 K)
+{
+    constexpr int N = Piece<T>::N;
+    Piece<T> r;
+    if constexpr (VEC) {                  // K is a multiple of N: all in or all out
+        r = *reinterpret_cast<const Piece<T> *>(p + (k < K ? k : 0));
+#pragma unroll
+        for (int j = 0; j < N; ++j) r.v[j] = k < K ? r.v[j] : T(0);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) r.v[j] = k + j < K ? p[k + j] : T(0);
+    }
+    return r;
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ Piece<T> load_full(const T *p, i64 k)
+{
+    Piece<T> r;
+    if constexpr (VEC) {
+        r = *reinterpret_cast<const Piece<T> *>(p + k);
+    } else {
+#pragma unroll
+        for (int j = 0; j < Piece<T>::N; ++j) r.v[j] = p[k + j];
+    }
+    return r;
+}
+
+__device__ __forceinline__ void mma(const Piece<uint16_t> &a, const Piece<uint16_t> &b, f32x4_t &c)
+{
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a.v), __builtin_bit_cast(bf16x8_t, b.v), c,
+                                                0, 0, 0);
+}
+__device__ __forceinline__ void mma(const Piece<float> &a, const Piece<float> &b, f32x4_t &c)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+}
+
+template <typename T, int ACT>
+__device__ __forceinline__ float act_of(float g)
+{
+    if constexpr (std::is_same<T, float>::value) return act<ACT>(g);
+    else return act_fast<ACT>(g);
+}
+
+// MB: blocks of 16 rows of X; UNITS: units whose loads a wave has in flight
+template <typename T, int ACT, int MB, int UNITS, bool VEC>
+__global__ __launch_bounds__(64 * kMaxWaves) void ffn_rows_kernel(const T *__restrict__ X, const T *__restrict__ Wg,
+                                                                  const T *__restrict__ Wu, int M, i64 K, i64 F,
+                                                                  T *__restrict__ H, T *__restrict__ G,
+                                                                  T *__restrict__ U)
+{
+    constexpr int STEP = Piece<T>::STEP, UNIT = 2 * STEP, N = Piece<T>::N;
+    extern __shared__ f32x4_t red[];      // [waves][2][MB][64]
+    const int lane = threadIdx.x & 63, waves = (int)blockDim.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const i64 f0 = (i64)blockIdx.x * kFT;
+    const int li = lane & 15, k0 = lane / 16 * N;
+    const i64 f = f0 + li < F ? f0 + li : F - 1;
+    const T *wg = Wg + f * K, *wu = Wu + f * K;
+    const T *x[MB];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) x[b] = X + (i64)(16 * b + li < M ? 16 * b + li : M - 1) * K;
+
+    f32x4_t ag[MB], au[MB];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) ag[b] = au[b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const i64 whole = K / UNIT;           // whole units; one cut unit may follow
+    i64 u = wave;
+    for (; u + (i64)(UNITS - 1) * waves < whole; u += (i64)UNITS * waves) {
+        Piece<T> pg[UNITS][2], pu[UNITS][2], px[UNITS][2][MB];
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const i64 k = (u + (i64)i * waves) * UNIT + s * STEP + k0;
+                pg[i][s] = load_full<T, VEC>(wg, k);
+                pu[i][s] = load_full<T, VEC>(wu, k);
+#pragma unroll
+                for (int b = 0; b < MB; ++b) px[i][s][b] = load_full<T, VEC>(x[b], k);
+            }
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int b = 0; b < MB; ++b) {
+                    mma(pg[i][s], px[i][s][b], ag[b]);
+                    mma(pu[i][s], px[i][s][b], au[b]);
+                }
+    }
+    for (; u * UNIT < K; u += waves) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const i64 k = u * UNIT + s * STEP + k0;
+            const Piece<T> pg = load_cut<T, VEC>(wg, k, K), pu = load_cut<T, VEC>(wu, k, K);
+#pragma unroll
+            for (int b = 0; b < MB; ++b) {
+                const Piece<T> px = load_cut<T, VEC>(x[b], k, K);
+                mma(pg, px, ag[b]);
+                mma(pu, px, au[b]);
+            }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+        red[(wave * 2 * MB + b) * 64 + lane] = ag[b];
+        red[(wave * 2 * MB + MB + b) * 64 + lane] = au[b];
+    }
+    __syncthreads();
+    // register r of lane l: feature 4 (l / 16) + r, row l % 16
+    const float *v = reinterpret_cast<const float *>(red);
+    for (int e = threadIdx.x; e < MB * 256; e += (int)blockDim.x) {
+        // consecutive threads take consecutive features of a row
+        const int b = e >> 8, i = (e & 255) >> 4, fe = e & 15;
+        const int row = 16 * b + i, src = (b * 64 + (fe >> 2) * 16 + i) * 4 + (fe & 3);
+        float g = 0.0f, uu = 0.0f;
+        for (int w = 0; w < waves; ++w) {
+            g += v[w * 2 * MB * 256 + src];
+            uu += v[w * 2 * MB * 256 + MB * 256 + src];
+        }
+        if (row >= M || f0 + fe >= F) continue;
+        const i64 o = (i64)row * F + f0 + fe;
+        store_elem(H + o, act_of<T, ACT>(g) * uu);
+        if (G != nullptr) {
+            store_elem(G + o, g);
+            store_elem(U + o, uu);
+        }
+    }
+}
+
+template <typename T, int ACT, int MB, int UNITS>
+void launch(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, void *H, void *G, void *U,
+            hipStream_t stream)
+{
+    const i64 groups = ceil_div(F, kFT), units = ceil_div(K, 2 * Piece<T>::STEP);
+    // four waves, or more where the features alone give too few waves to fill the GPU and K has units for them
+    int waves = 4;
+    constexpr int most = MB <= 2 ? kMaxWaves : kMaxWaves / 2;       // 64 KB of LDS
+    while (waves < most && groups * waves < 2048 && units >= 2 * waves * UNITS) waves *= 2;
+    const size_t lds = (size_t)waves * 2 * MB * 64 * sizeof(f32x4_t);
+    const bool vec = K % Piece<T>::N == 0 && aligned(X, 16) && aligned(Wg, 16) && aligned(Wu, 16);
+    if (vec)
+        ffn_rows_kernel<T, ACT, MB, UNITS, true><<<(unsigned)groups, 64 * waves, lds, stream>>>(
+            (const T *)X, (const T *)Wg, (const T *)Wu, (int)M, K, F, (T *)H, (T *)G, (T *)U);
+    else
+        ffn_rows_kernel<T, ACT, MB, UNITS, false><<<(unsigned)groups, 64 * waves, lds, stream>>>(
+            (const T *)X, (const T *)Wg, (const T *)Wu, (int)M, K, F, (T *)H, (T *)G, (T *)U);
+}
+
+template <typename T, int ACT>
+void by_rows(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, void *H, void *G, void *U,
+             hipStream_t stream)
+{
+    if (M <= 16) launch<T, ACT, 1, 2>(X, Wg, Wu, M, K, F, H, G, U, stream);
+    else if (M <= 32) launch<T, ACT, 2, 2>(X, Wg, Wu, M, K, F, H, G, U, stream);
+    else launch<T, ACT, 4, 1>(X, Wg, Wu, M, K, F, H, G, U, stream);
+}
+
+template <typename T>
+void by_act(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, dp_act act, void *H, void *G, void *U,
+            hipStream_t stream)
+{
+    if (act == DP_ACT_SILU) by_rows<T, DP_ACT_SILU>(X, Wg, Wu, M, K, F, H, G, U, stream);
+    else by_rows<T, DP_ACT_GELU_TANH>(X, Wg, Wu, M, K, F, H, G, U, stream);
+}
+
+}  // namespace
+
+void ffn_rows_forward(const void *X, const void *Wg, const void *Wu, dp_dtype dt, i64 M, i64 K, i64 F, dp_act act,
+                      void *H, void *G, void *U, hipStream_t stream)
+{
+    if (dt == DP_F32) by_act<float>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
+    else by_act<uint16_t>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
+}
+
+}  // namespace dpg

@@ -1,0 +1,14 @@
+// The forward of the gated feed-forward block over few rows (ffn_rows.hip).
+#pragma once
+
+#include "common.hpp"
+
+namespace dpg {
+
+constexpr i64 kFfnRowsMax = 64;      // rows of X
+
+// H (and G, U unless NULL) from X [M][K], Wg, Wu [F][K], M <= kFfnRowsMax
+void ffn_rows_forward(const void *X, const void *Wg, const void *Wu, dp_dtype dt, i64 M, i64 K, i64 F, dp_act act,
+                      void *H, void *G, void *U, hipStream_t stream);
+
+}  // namespace dpg

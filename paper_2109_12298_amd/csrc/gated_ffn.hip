@@ -9,6 +9,7 @@
 // backward pass wants them.
 #include "gated_ffn.hpp"
 #include "ffn_bf16.hpp"
+#include "ffn_rows.hpp"
 #include "mfma_tile.hpp"
 
 namespace dpg {
@@ -224,15 +225,14 @@ using namespace dpg;
 
 extern "C" size_t dp_gated_ffn_forward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt)
 {
-    (void)M; (void)d_in; (void)d_ff; (void)dt;
-    return 0;
+    if (!dtype_ok(dt) || check_sizes(M, d_in, d_ff) != DP_OK || M <= kFfnRowsMax) return 0;
+    return dt == DP_BF16 ? ffn_bf16_forward_workspace(M, d_in, d_ff) : 0;
 }
 
 extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const void *Wu, dp_dtype dt, int64_t M,
                                           int64_t d_in, int64_t d_ff, dp_act act, void *H, void *G, void *U, void *ws,
                                           size_t ws_bytes, hipStream_t stream)
 {
-    (void)ws; (void)ws_bytes;
     DPG_REQUIRE(dtype_ok(dt), DP_EDTYPE);
     DPG_REQUIRE(act_ok(act), DP_EINVAL);
     const dp_status bad = check_sizes(M, d_in, d_ff);
@@ -240,12 +240,16 @@ extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const v
     if (M == 0) return DP_OK;
     DPG_REQUIRE(X != nullptr && Wg != nullptr && Wu != nullptr && H != nullptr, DP_EINVAL);
     DPG_REQUIRE((G == nullptr) == (U == nullptr), DP_EINVAL);
-    if (dt == DP_F32) {
+    const size_t need = dp_gated_ffn_forward_workspace_bytes(M, d_in, d_ff, dt);
+    DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
+    if (M <= kFfnRowsMax) {
+        ffn_rows_forward(X, Wg, Wu, dt, M, d_in, d_ff, act, H, G, U, stream);
+    } else if (dt == DP_F32) {
         if (act == DP_ACT_SILU) forward<float, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
         else forward<float, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
-    } else if (M > 64 && ffn_rows_ok(X, d_in) && ffn_rows_ok(Wg, d_in) && ffn_rows_ok(Wu, d_in) && d_in < (1 << 21)) {
+    } else if (ffn_tiles_ok(X, d_in) && ffn_tiles_ok(Wg, d_in) && ffn_tiles_ok(Wu, d_in)) {
         ffn_bf16_forward((const uint16_t *)X, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in, d_ff, act,
-                         (uint16_t *)H, (uint16_t *)G, (uint16_t *)U, stream);
+                         (uint16_t *)H, (uint16_t *)G, (uint16_t *)U, ws, stream);
     } else {
         if (act == DP_ACT_SILU) forward<uint16_t, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
         else forward<uint16_t, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
@@ -282,8 +286,7 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
         if (act == DP_ACT_SILU) backprops<uint16_t, DP_ACT_SILU>(dH, G, U, n, BG, BU, stream);
         else backprops<uint16_t, DP_ACT_GELU_TANH>(dH, G, U, n, BG, BU, stream);
         if (dX == nullptr) return launch_status();
-        if (M > 64 && ffn_rows_ok(BG, d_ff) && ffn_rows_ok(BU, d_ff) && ffn_rows_ok(Wg, d_in) && ffn_rows_ok(Wu, d_in) &&
-            d_ff < (1 << 21) && d_in < (1 << 21))
+        if (ffn_tiles_ok(BG, d_ff) && ffn_tiles_ok(BU, d_ff) && ffn_tiles_ok(Wg, d_in) && ffn_tiles_ok(Wu, d_in))
             ffn_bf16_dx((const uint16_t *)BG, (const uint16_t *)BU, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in,
                         d_ff, (uint16_t *)dX, ws, stream);
         else
