@@ -126,10 +126,11 @@ def test_tensors_are_checked_before_the_call():
         dp.make_grad_tensors([(E, E, 40, dp.DP_F32)])
 
     class Fake:                                      # stands for a GPU tensor; only its description is read
-        is_cuda, device = True, torch.device("cuda:0")
+        def __init__(self, dtype, n, dense=True, device=0):
+            self.dtype, self.n, self.dense, self.device = dtype, n, dense, device
 
-        def __init__(self, dtype, n, dense=True, device="cuda:0"):
-            self.dtype, self.n, self.dense, self.device = dtype, n, dense, torch.device(device)
+        def get_device(self):
+            return self.device
 
         def is_contiguous(self):
             return self.dense
@@ -140,17 +141,16 @@ def test_tensors_are_checked_before_the_call():
         def data_ptr(self):
             return FAKE
 
-    def ptr(x):
-        return dp._Call("f").ptr("x", x, torch.float32, 40)
+    def ptr(*xs):
+        return dp._tensors("f", *[("x", x, torch.float32, 40) for x in xs])
 
-    assert ptr(Fake(torch.float32, 40)) == FAKE and ptr(None) is None and ptr(FAKE) == FAKE
+    assert ptr(Fake(torch.float32, 40), None, FAKE) == (0, [FAKE, None, FAKE])
+    assert ptr(None, FAKE) == (None, [None, FAKE])
     with pytest.raises(TypeError, match="not torch.float32"):
         ptr(Fake(torch.bfloat16, 40))
     with pytest.raises(ValueError, match="not contiguous"):
         ptr(Fake(torch.float32, 40, dense=False))
     with pytest.raises(ValueError, match="40 are needed"):
         ptr(Fake(torch.float32, 39))
-    call = dp._Call("f")
-    call.ptr("a", Fake(torch.float32, 40), torch.float32, 40)
-    with pytest.raises(ValueError, match="other arguments on"):
-        call.ptr("b", Fake(torch.float32, 40, device="cuda:1"), torch.float32, 40)
+    with pytest.raises(ValueError, match="other arguments on GPU 0"):
+        ptr(Fake(torch.float32, 40), Fake(torch.float32, 40, device=1))
