@@ -98,9 +98,10 @@ def token_ids(rng, kind, N, T, V):
     return rng.integers(0, V, (N, T))
 
 
-# one workgroup's sort ends at 8192 positions (2048: two items per thread), 64 tiles of 8192 at 524288
-SIZES = [(1, 1, 1, 1), (1, 2, 3, 5), (2, 8, 512, 64), (1, 17, 511, 257), (3, 683, 513, 12), (1, 2049, 40, 100),
-         (2, 4096, 100, 8), (8193, 1, 1000, 6), (33, 300, 70000, 16), (5, 2011, 600, 533), (64, 256, 1000, 100)]
+# one launch up to 2048 positions, one workgroup's sort up to 16384, 64 tiles of 8192 at 524288
+SIZES = [(1, 1, 1, 1), (1, 2, 3, 5), (2, 8, 512, 64), (1, 17, 511, 257), (3, 100, 9000, 200), (16, 128, 300, 100),
+         (3, 683, 513, 12), (1, 2049, 40, 100), (2, 4096, 100, 8), (8193, 1, 1000, 6), (33, 300, 70000, 16),
+         (5, 2011, 600, 533), (64, 256, 1000, 100), (1, 16385, 500, 40), (4, 5000, 90000, 20)]
 
 
 @pytest.mark.parametrize("N,T,V,D", SIZES)
@@ -140,7 +141,25 @@ def test_tokens_many_positions(M, D):
     R.within(got, want, bound)
 
 
-@pytest.mark.parametrize("T", [9, 5000])
+@pytest.mark.parametrize("M", [1, 300, 3000, 20000])
+def test_tokens_large_vocabulary(M):
+    """Ids of 27 bits: three digits."""
+    say("tokens vocabulary", M)
+    rng = np.random.default_rng(M)
+    V, D = 70_000_000, 1
+    ids = rng.integers(0, V, (1, M))
+    ids[0, M // 2:] = ids[0, :M - M // 2]
+    ids[0, 0] = V - 1
+    B = torch.from_numpy(rng.standard_normal((1, M, D))).float()
+    got = run_tokens(torch.from_numpy(ids).to(DEV), B.to(DEV), dp.DP_F32, V, 1.0, None, 1.0)
+    uniq, at = np.unique(ids[0], return_inverse=True)
+    want, bound = R.tokens(at.reshape(1, M), R.f64(B), len(uniq), 1.0, None, 1.0)
+    R.within(got[torch.from_numpy(uniq).to(DEV)], want, bound)
+    got[torch.from_numpy(uniq).to(DEV)] = 0.0
+    assert (got == 0).all()
+
+
+@pytest.mark.parametrize("T", [9, 700, 5000])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_tokens_left_out(T, dt):
     """Padding rows are not looked at, bad ids are flagged, a broken norm poisons its sample's ids alone."""
