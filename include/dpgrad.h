@@ -365,7 +365,10 @@ typedef enum dp_act { DP_ACT_SILU = 0, DP_ACT_GELU_TANH = 1 } dp_act;
  * outputs overlap neither each other nor the inputs.  M >= 0, d_in, d_ff >= 1,
  * each < 2^31 and M * d_ff, M * d_in, d_in * d_ff < 2^35 (else
  * DP_EUNSUPPORTED).  A row of X that holds a NaN or an infinity makes its own
- * rows of the outputs non-finite and no others.  The block's output
+ * rows of the outputs non-finite and no others.  (fp32 products over more than
+ * 64 rows run on the bf16 matrix units as three bf16 parts, which keep every
+ * bit, or, where some value is not finite or its magnitude is under 2^-100 or
+ * from 2^127 on, on the fp32 units: the results agree to rounding.)  The block's output
  * projection is a Linear layer that takes H as its A.  Workspace:
  * dp_gated_ffn_forward_workspace_bytes(M, d_in, d_ff, dt) bytes, 16-byte
  * aligned. */

@@ -58,10 +58,9 @@ struct Shape {
     static constexpr int RPI = 1024 / ROW;                   // rows per load instruction
     static constexpr int LOADS = ROWS / RPI / WAVES;         // per wave and stage
     static constexpr int FM = BM / WM / 32, FF = BF / WF / 32;
-    static constexpr int LDT = FF * 64 + 16;                 // bytes of a row of the output transpose
     static constexpr int LDS = NS * STAGE;
     static_assert(LOADS * RPI * WAVES == ROWS && BM % RPI == 0 && BF % RPI == 0, "stage split");
-    static_assert(WAVES * 32 * LDT <= LDS, "the output transpose fits the stages");
+    static_assert(WAVES * 32 * (FF * 128 + 16) <= LDS, "the output transpose fits the stages");
     static_assert(NS >= 2 && NS <= 4, "waits");
     static_assert(BK / 16 % 2 == 0, "two sets of operands in turn");
 };
@@ -80,26 +79,29 @@ __device__ __forceinline__ void tile_of(int b, int nb, int tiles_m, int tiles_n,
     tn = in / gm;
 }
 
-// 32 positions by FF * 32 features of one output, from LDS rows of LDT bytes
-template <int FF, int LDT>
-__device__ __forceinline__ void store_rows(const char *L, uint16_t *__restrict__ O, i64 M, i64 F, i64 m0, i64 f0,
-                                           bool vec, int lane)
+// 32 rows by COLS values of one output tile, from LDS rows of LDT bytes
+template <typename T, int COLS, int LDT>
+__device__ __forceinline__ void store_rows(const char *L, T *__restrict__ O, i64 rows, i64 cols, i64 r0, i64 c0, bool vec,
+                                           int lane)
 {
-    constexpr int LPR = FF * 4, RPS = 64 / LPR;              // lanes per row, rows per store
+    constexpr int N = 16 / sizeof(T), LPR = COLS / N, RPS = 64 / LPR;        // values per piece, lanes per row, rows per store
 #pragma unroll
     for (int s = 0; s < 32 / RPS; ++s) {
         const int row = s * RPS + lane / LPR, c = lane % LPR;
         const uint4 v = *reinterpret_cast<const uint4 *>(L + row * LDT + 16 * c);
-        const i64 m = m0 + row, f = f0 + 8 * c;
-        if (m >= M) continue;
-        uint16_t *o = O + m * F + f;
+        const i64 r = r0 + row, f = c0 + N * c;
+        if (r >= rows) continue;
+        T *o = O + r * cols + f;
         if (vec) {
-            if (f < F) *reinterpret_cast<uint4 *>(o) = v;
+            if (f < cols) *reinterpret_cast<uint4 *>(o) = v;
         } else {
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (f + j < F) o[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            for (int j = 0; j < N; ++j)
+                if (f + j < cols) {
+                    if constexpr (sizeof(T) == 4) o[j] = __uint_as_float(w[j]);
+                    else o[j] = (T)(w[j >> 1] >> (16 * (j & 1)));
+                }
         }
     }
 }
@@ -109,16 +111,38 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return (uint32_t)bf16_bits(a) | ((uint32_t)bf16_bits(b) << 16);
 }
 
-template <typename S, int ACT>
+// four consecutive values of a row to LDS
+__device__ __forceinline__ void put4(uint16_t *p, float a, float b, float c, float d)
+{
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(a, b), pack2(c, d));
+}
+__device__ __forceinline__ void put4(float *p, float a, float b, float c, float d)
+{
+    *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d);
+}
+
+// The products of an fp32 contraction from three bf16 parts of each operand
+// (x = x0 + x1 + x2, exact; see ffn_split_kernel), smallest first: part s of
+// the list is x's part X_PART >> 2 s & 3 times w's part W_PART >> 2 s & 3.
+// Left out are x1 w2, x2 w1 (2^-24 of the product at most) and x2 w2.
+constexpr uint32_t X_PART = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
+constexpr uint32_t W_PART = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
+constexpr int kParts = 6;
+
+// T = float: X, Wg and Wu are the three parts of each ([3][rows][K], K a
+// multiple of BK), and *flag != 0 leaves the call to another kernel.
+template <typename S, int ACT, typename T>
 __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16_t *__restrict__ X,
                                                                     const uint16_t *__restrict__ Wg,
                                                                     const uint16_t *__restrict__ Wu, i64 M, i64 K, i64 F,
-                                                                    int tiles_m, int tiles_f, uint16_t *__restrict__ H,
-                                                                    uint16_t *__restrict__ G, uint16_t *__restrict__ U,
-                                                                    int vec)
+                                                                    int tiles_m, int tiles_f, T *__restrict__ H,
+                                                                    T *__restrict__ G, T *__restrict__ U, int vec,
+                                                                    const int32_t *__restrict__ flag)
 {
+    constexpr bool PARTS = sizeof(T) == 4;
     constexpr int FM = S::FM, FF = S::FF, BK = S::BK, NS = S::NS, ROW = S::ROW, KS = BK / 16;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    if (PARTS && *flag != 0) return;
     int tm, tf;
     tile_of((int)blockIdx.x, (int)gridDim.x, tiles_m, tiles_f, tm, tf);
     const i64 m0 = (i64)tm * S::BM, f0 = (i64)tf * S::BF;
@@ -126,13 +150,15 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WF * (FM * 32), wf = wave % S::WF * (FF * 32);
     const uint32_t lds0 = lds_addr(smem);
-    const int nst = (int)((K + BK - 1) / BK);
-    const int tail = (int)(K - (i64)(nst - 1) * BK);         // columns of the last stage
+    const int per = (int)((K + BK - 1) / BK);
+    const int nst = PARTS ? kParts * per : per;
+    const int tail = (int)(K - (i64)(per - 1) * BK);         // columns of the last stage
 
     // the wave's loads of a stage: rows past the end read the last row (their products are not stored)
     const char *base[S::LOADS];
     uint32_t off[S::LOADS];
     int q[S::LOADS];
+    bool is_x[S::LOADS];
 #pragma unroll
     for (int r = 0; r < S::LOADS; ++r) {
         const int row = (wave + S::WAVES * r) * S::RPI + lane / (64 / S::RPI);
@@ -141,20 +167,28 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16
         const int in = first < S::BM ? row : first < S::BM + S::BF ? row - S::BM : row - S::BM - S::BF;
         const i64 left = first < S::BM ? M - m0 : F - f0;
         base[r] = reinterpret_cast<const char *>(P);
+        is_x[r] = first < S::BM;
         q[r] = (lane % (64 / S::RPI)) ^ swizzle<BK>(row);
         off[r] = (uint32_t)(in < left ? in : (int)left - 1) * (uint32_t)(2 * K) + 16u * q[r];
     }
     const auto issue = [&](int c) {
         const uint32_t L = lds0 + (uint32_t)(c % NS) * S::STAGE;
-        const bool cut = c == nst - 1 && tail < BK;
+        const bool cut = !PARTS && c == nst - 1 && tail < BK;
+        i64 xo = (i64)c * (2 * BK), wo = xo;
+        if (PARTS) {
+            const int p = c / per;
+            const i64 k = (i64)(c - p * per) * (2 * BK);
+            xo = k + (i64)((X_PART >> (2 * p)) & 3) * (2 * M * K);
+            wo = k + (i64)((W_PART >> (2 * p)) & 3) * (2 * F * K);
+        }
 #pragma unroll
         for (int r = 0; r < S::LOADS; ++r)
             // columns past the end read the stage's first ones, and are zeroed in LDS
-            dma16_off(base[r] + (i64)c * (2 * BK), cut && 8 * q[r] >= tail ? off[r] - 16u * q[r] : off[r],
+            dma16_off(base[r] + (is_x[r] ? xo : wo), cut && 8 * q[r] >= tail ? off[r] - 16u * q[r] : off[r],
                       L + 1024 * (wave + S::WAVES * r));
     };
     const auto zero_tail = [&](int c) {
-        if (c != nst - 1 || tail == BK) return;
+        if (PARTS || c != nst - 1 || tail == BK) return;
         char *L = smem + (c % NS) * S::STAGE;
 #pragma unroll
         for (int r = 0; r < S::LOADS; ++r)
@@ -245,21 +279,20 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16
     mma(fb);
     __syncthreads();                                         // the stages become the output transposes
 
-    char *T = smem + wave * 32 * S::LDT;
-    const auto put = [&](int x, auto value, uint16_t *O) {
+    constexpr int LDT = FF * 32 * (int)sizeof(T) + 16;
+    char *L = smem + wave * 32 * LDT;
+    const auto put = [&](int x, auto value, T *O) {
 #pragma unroll
         for (int y = 0; y < FF; ++y)
 #pragma unroll
-            for (int rb = 0; rb < 4; ++rb) {
-                const uint2 v = make_uint2(pack2(value(y, 4 * rb), value(y, 4 * rb + 1)),
-                                           pack2(value(y, 4 * rb + 2), value(y, 4 * rb + 3)));
-                *reinterpret_cast<uint2 *>(T + li * S::LDT + 2 * (32 * y + 8 * rb + 4 * lk)) = v;
-            }
-        store_rows<FF, S::LDT>(T, O, M, F, m0 + wm + 32 * x, f0 + wf, vec != 0, lane);
+            for (int rb = 0; rb < 4; ++rb)
+                put4(reinterpret_cast<T *>(L + li * LDT) + 32 * y + 8 * rb + 4 * lk, value(y, 4 * rb),
+                     value(y, 4 * rb + 1), value(y, 4 * rb + 2), value(y, 4 * rb + 3));
+        store_rows<T, FF * 32, LDT>(L, O, M, F, m0 + wm + 32 * x, f0 + wf, vec != 0, lane);
     };
 #pragma unroll
     for (int x = 0; x < FM; ++x) {
-        put(x, [&](int y, int r) { return act_fast<ACT>(ag[x][y][r]) * au[x][y][r]; }, H);
+        put(x, [&](int y, int r) { return act_for<ACT, T>(ag[x][y][r]) * au[x][y][r]; }, H);
         if (G != nullptr) {
             put(x, [&](int y, int r) { return ag[x][y][r]; }, G);
             put(x, [&](int y, int r) { return au[x][y][r]; }, U);
@@ -267,18 +300,19 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16
     }
 }
 
-template <typename S>
-void launch_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act,
-                    uint16_t *H, uint16_t *G, uint16_t *U, hipStream_t stream)
+template <typename S, typename T>
+void launch_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act, T *H,
+                    T *G, T *U, const int32_t *flag, hipStream_t stream)
 {
     const int tm = (int)ceil_div(M, S::BM), tf = (int)ceil_div(F, S::BF);
-    const int vec = F % 8 == 0 && aligned(H, 16) && aligned(G, 16) && aligned(U, 16);
+    const int vec = F * sizeof(T) % 16 == 0 && aligned(H, 16) && aligned(G, 16) && aligned(U, 16);
     const unsigned grid = (unsigned)((i64)tm * tf);
     if (act == DP_ACT_SILU)
-        ffn_forward_kernel<S, DP_ACT_SILU><<<grid, S::THREADS, 0, stream>>>(X, Wg, Wu, M, K, F, tm, tf, H, G, U, vec);
+        ffn_forward_kernel<S, DP_ACT_SILU, T><<<grid, S::THREADS, 0, stream>>>(X, Wg, Wu, M, K, F, tm, tf, H, G, U, vec,
+                                                                               flag);
     else
-        ffn_forward_kernel<S, DP_ACT_GELU_TANH><<<grid, S::THREADS, 0, stream>>>(X, Wg, Wu, M, K, F, tm, tf, H, G, U,
-                                                                                 vec);
+        ffn_forward_kernel<S, DP_ACT_GELU_TANH, T><<<grid, S::THREADS, 0, stream>>>(X, Wg, Wu, M, K, F, tm, tf, H, G, U,
+                                                                                    vec, flag);
 }
 
 // ---------------------------------------------------------------------------
@@ -297,23 +331,28 @@ struct DxShape {
     static constexpr int A_RPI = 1024 / A_ROW, W_RPI = 1024 / W_ROW;
     static constexpr int A_LOADS = A_BYTES / 1024 / WAVES, W_LOADS = W_BYTES / 1024 / WAVES, LOADS = A_LOADS + W_LOADS;
     static constexpr int FM = BM / WM / 32, FD = BD / WD / 32;
-    static constexpr int LDT = FD * 64 + 16;
     static constexpr int LDS = NS * STAGE;
     static_assert(A_LOADS * WAVES * 1024 == A_BYTES && W_LOADS * WAVES * 1024 == W_BYTES, "stage split");
-    static_assert(WAVES * 32 * LDT <= LDS, "the output transpose fits the stages");
+    static_assert(WAVES * 32 * (FD * 128 + 16) <= LDS, "the output transpose fits the stages");
 };
 
-template <typename S, bool SPLIT>
+// T = float: BG and Wg point to the parts of both products ([2][3][M][lda] and
+// [2][3][F][ldw], F = lda a multiple of BK), BU and Wu are not used, and
+// *flag != 0 leaves the call to another kernel.
+template <typename S, bool SPLIT, typename T>
 __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *__restrict__ BG,
                                                                const uint16_t *__restrict__ BU,
                                                                const uint16_t *__restrict__ Wg,
                                                                const uint16_t *__restrict__ Wu, i64 M, i64 D, i64 F,
                                                                i64 lda, i64 ldw, int tiles_m, int tiles_d, int splits,
-                                                               uint16_t *__restrict__ dX, float *__restrict__ part,
-                                                               int vec)
+                                                               T *__restrict__ dX, float *__restrict__ part, int vec,
+                                                               const int32_t *__restrict__ flag)
 {
+    constexpr bool PARTS = sizeof(T) == 4;
+    constexpr int RUNS = PARTS ? 2 * kParts : 2;             // products that the stages run through
     constexpr int FM = S::FM, FD = S::FD, BK = S::BK, NS = S::NS, KS = BK / 16;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    if (PARTS && *flag != 0) return;
     int tm, td;
     const int tiles = tiles_m * tiles_d, split = SPLIT ? (int)blockIdx.x / tiles : 0;
     tile_of((int)blockIdx.x - split * tiles, tiles, tiles_m, tiles_d, tm, td);
@@ -322,10 +361,10 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WD * (FM * 32), wd = wave % S::WD * (FD * 32);
     const uint32_t lds0 = lds_addr(smem);
-    const int half = (int)((F + BK - 1) / BK);               // stages of each of the two products
+    const int half = (int)((F + BK - 1) / BK);               // stages of each product
     const int tail = (int)(F - (i64)(half - 1) * BK);        // rows of W (columns of B) in the last of them
-    const int first = SPLIT ? (int)((i64)split * 2 * half / splits) : 0;
-    const int nst = (SPLIT ? (int)((i64)(split + 1) * 2 * half / splits) : 2 * half) - first;
+    const int first = SPLIT ? (int)((i64)split * RUNS * half / splits) : 0;
+    const int nst = (SPLIT ? (int)((i64)(split + 1) * RUNS * half / splits) : RUNS * half) - first;
 
     uint32_t offA[S::A_LOADS], offW[S::W_LOADS];
     int q[S::A_LOADS], kr[S::W_LOADS];
@@ -343,10 +382,16 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
     }
     const auto issue = [&](int c) {
         const uint32_t L = lds0 + (uint32_t)(c % NS) * S::STAGE;
-        const int g = first + c, u = g >= half, k = u ? g - half : g;
-        const bool cut = k == half - 1 && tail < BK;
-        const char *a = reinterpret_cast<const char *>((u ? BU : BG) + m0 * lda) + (i64)k * (2 * BK);
-        const char *w = reinterpret_cast<const char *>((u ? Wu : Wg) + (i64)k * BK * ldw + d0);
+        const int g = first + c, run = PARTS ? g / half : g >= half, k = g - run * half;
+        const bool cut = !PARTS && k == half - 1 && tail < BK;
+        const uint16_t *ab = run ? BU : BG, *wb = run ? Wu : Wg;
+        if (PARTS) {
+            const int u = run >= kParts, p = 2 * (u ? run - kParts : run);
+            ab = BG + (3 * u + (int)((X_PART >> p) & 3)) * (M * lda);
+            wb = Wg + (3 * u + (int)((W_PART >> p) & 3)) * (F * ldw);
+        }
+        const char *a = reinterpret_cast<const char *>(ab + m0 * lda) + (i64)k * (2 * BK);
+        const char *w = reinterpret_cast<const char *>(wb + (i64)k * BK * ldw + d0);
 #pragma unroll
         for (int r = 0; r < S::A_LOADS; ++r)
             dma16_off(a, cut && 8 * q[r] >= tail ? offA[r] - 16u * q[r] : offA[r], L + 1024 * (wave + S::WAVES * r));
@@ -358,7 +403,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
     // features past the end read the stage's first ones, and are zeroed in LDS on both sides
     const auto zero_tail = [&](int c) {
         const int g = first + c, k = g >= half ? g - half : g;
-        if (k != half - 1 || tail == BK) return;
+        if (PARTS || k != half - 1 || tail == BK) return;
         char *L = smem + (c % NS) * S::STAGE;
 #pragma unroll
         for (int r = 0; r < S::A_LOADS; ++r)
@@ -458,41 +503,48 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
         return;
     }
     __syncthreads();
-    char *T = smem + wave * 32 * S::LDT;
+    constexpr int LDT = FD * 32 * (int)sizeof(T) + 16;
+    char *L = smem + wave * 32 * LDT;
 #pragma unroll
     for (int x = 0; x < FM; ++x) {
 #pragma unroll
         for (int y = 0; y < FD; ++y)
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb)
-                *reinterpret_cast<uint2 *>(T + li * S::LDT + 2 * (32 * y + 8 * rb + 4 * lk)) =
-                    make_uint2(pack2(acc[x][y][4 * rb], acc[x][y][4 * rb + 1]),
-                               pack2(acc[x][y][4 * rb + 2], acc[x][y][4 * rb + 3]));
-        store_rows<FD, S::LDT>(T, dX, M, D, m0 + wm + 32 * x, d0 + wd, vec != 0, lane);
+                put4(reinterpret_cast<T *>(L + li * LDT) + 32 * y + 8 * rb + 4 * lk, acc[x][y][4 * rb],
+                     acc[x][y][4 * rb + 1], acc[x][y][4 * rb + 2], acc[x][y][4 * rb + 3]);
+        store_rows<T, FD * 32, LDT>(L, dX, M, D, m0 + wm + 32 * x, d0 + wd, vec != 0, lane);
     }
 }
 
-// dX = the splits' partial sums, in split order; rows of ld (a multiple of 8) there, of D here
+// dX = the splits' partial sums, in split order; rows of ld (a multiple of 4) there, of D here
+template <typename T>
 __global__ __launch_bounds__(256) void ffn_dx_sum_kernel(const float *__restrict__ part, i64 M, i64 D, i64 ld,
-                                                         int splits, uint16_t *__restrict__ dX)
+                                                         int splits, T *__restrict__ dX,
+                                                         const int32_t *__restrict__ flag)
 {
+    if (flag != nullptr && *flag != 0) return;
     const i64 n = M * ld;
     for (i64 i = ((i64)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (i64)gridDim.x * 1024) {
-        float4 s = *reinterpret_cast<const float4 *>(part + i);
-        for (int k = 1; k < splits; ++k) {
-            const float4 v = *reinterpret_cast<const float4 *>(part + (i64)k * n + i);
-            s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
-        }
-        const uint32_t w[2] = {pack2(s.x, s.y), pack2(s.z, s.w)};
-        if (D == ld) {
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < splits; k += 8) {
+            float4 p[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) dX[i + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-        } else {
-            const i64 m = i / ld, d = i - m * ld;
+            for (int j = 0; j < 8; ++j)
+                p[j] = k + j < splits ? *reinterpret_cast<const float4 *>(part + (i64)(k + j) * n + i)
+                                      : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (d + j < D) dX[m * D + d + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            for (int j = 0; j < 8; ++j) {
+                v[0] += p[j].x;
+                v[1] += p[j].y;
+                v[2] += p[j].z;
+                v[3] += p[j].w;
+            }
         }
+        const i64 m = D == ld ? 0 : i / ld, d = i - m * ld;  // D = ld: one row of all values
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (D == ld || d + j < D) store_elem(dX + m * D + d + j, v[j]);
     }
 }
 
@@ -501,22 +553,23 @@ typedef DxShape<128, 128, 2, 2, 64, 2> MidDx;
 typedef DxShape<64, 128, 1, 4, 64, 3> Rows64Dx;
 typedef DxShape<32, 128, 1, 4, 64, 3> Rows32Dx;
 
-template <typename S>
+template <typename S, typename T>
 void launch_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
-               i64 lda, i64 ldw, int splits, uint16_t *dX, float *part, hipStream_t stream)
+               i64 lda, i64 ldw, int splits, T *dX, float *part, const int32_t *flag, hipStream_t stream)
 {
     const int tm = (int)ceil_div(M, S::BM), td = (int)ceil_div(D, S::BD);
-    const int vec = D % 8 == 0 && aligned(dX, 16);
+    const int vec = D * sizeof(T) % 16 == 0 && aligned(dX, 16);
     const unsigned grid = (unsigned)((i64)tm * td * splits);
     if (splits == 1) {
-        ffn_dx_kernel<S, false><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, lda, ldw, tm, td, 1, dX,
-                                                                 nullptr, vec);
+        ffn_dx_kernel<S, false, T><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, lda, ldw, tm, td, 1, dX,
+                                                                    nullptr, vec, flag);
         return;
     }
-    ffn_dx_kernel<S, true><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, lda, ldw, tm, td, splits, dX, part,
-                                                            vec);
+    ffn_dx_kernel<S, true, T><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, lda, ldw, tm, td, splits, dX,
+                                                               part, vec, flag);
     const i64 blocks = ceil_div(M * ldw, 1024);
-    ffn_dx_sum_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(part, M, D, ldw, splits, dX);
+    ffn_dx_sum_kernel<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(part, M, D, ldw, splits, dX,
+                                                                                        flag);
 }
 
 // [rows][cols] into rows of ld > cols, zeros behind (16 bytes of the result per thread)
@@ -558,7 +611,8 @@ struct DxPlan {
     int shape, splits;
 };
 
-DxPlan dx_plan(i64 M, i64 D, i64 F)
+// runs: products of F features that the stages run through (2, or 12 for fp32 in parts)
+DxPlan dx_plan(i64 M, i64 D, i64 F, int runs)
 {
     DxPlan p;
     p.splits = 1;
@@ -567,7 +621,7 @@ DxPlan dx_plan(i64 M, i64 D, i64 F)
         return p;
     }
     p.shape = M <= 32 ? kRows32 : M <= 64 ? kRows64 : kMid;
-    const i64 tiles = ceil_div(M, M <= 32 ? 32 : M <= 64 ? 64 : 128) * ceil_div(D, 128), stages = 2 * ceil_div(F, 64);
+    const i64 tiles = ceil_div(M, M <= 32 ? 32 : M <= 64 ? 64 : 128) * ceil_div(D, 128), stages = runs * ceil_div(F, 64);
     i64 s = 512 / tiles;
     if (s > stages / 4) s = stages / 4;
     if (s > 32) s = 32;
@@ -590,13 +644,14 @@ void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu,
     Wg = pad_rows(Wg, F, K, w, stream);
     Wu = pad_rows(Wu, F, K, w, stream);
     K = padded(K);
-    if (ceil_div(M, 256) * ceil_div(F, 128) >= 192) launch_forward<Large>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
-    else launch_forward<Mid>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
+    if (ceil_div(M, 256) * ceil_div(F, 128) >= 192)
+        launch_forward<Large, uint16_t>(X, Wg, Wu, M, K, F, act, H, G, U, nullptr, stream);
+    else launch_forward<Mid, uint16_t>(X, Wg, Wu, M, K, F, act, H, G, U, nullptr, stream);
 }
 
 size_t ffn_bf16_dx_workspace(i64 M, i64 D, i64 F)
 {
-    const DxPlan p = dx_plan(M, D, F);
+    const DxPlan p = dx_plan(M, D, F, 2);
     const size_t part = p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)(M * padded(D)) : 0;
     return 2 * pad_bytes(M, F) + 2 * pad_bytes(F, D) + part;
 }
@@ -604,7 +659,7 @@ size_t ffn_bf16_dx_workspace(i64 M, i64 D, i64 F)
 void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
                  uint16_t *dX, void *ws, hipStream_t stream)
 {
-    const DxPlan p = dx_plan(M, D, F);
+    const DxPlan p = dx_plan(M, D, F, 2);
     char *w = (char *)ws;
     BG = pad_rows(BG, M, F, w, stream);
     BU = pad_rows(BU, M, F, w, stream);
@@ -612,10 +667,152 @@ void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, con
     Wu = pad_rows(Wu, F, D, w, stream);
     const i64 lda = padded(F), ldw = padded(D);
     float *part = (float *)w;
-    if (p.shape == kLarge) launch_dx<LargeDx>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, stream);
-    else if (p.shape == kMid) launch_dx<MidDx>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, stream);
-    else if (p.shape == kRows64) launch_dx<Rows64Dx>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, stream);
-    else launch_dx<Rows32Dx>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, stream);
+    if (p.shape == kLarge) launch_dx<LargeDx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, nullptr, stream);
+    else if (p.shape == kMid) launch_dx<MidDx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, nullptr, stream);
+    else if (p.shape == kRows64) launch_dx<Rows64Dx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, nullptr, stream);
+    else launch_dx<Rows32Dx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, nullptr, stream);
+}
+
+// ---------------------------------------------------------------------------
+// fp32 by parts
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr i64 kAlignK = 64;               // a whole stage
+i64 whole(i64 n) { return (n + kAlignK - 1) / kAlignK * kAlignK; }
+
+// x = p[0] + p[1] + p[2] exactly, each a bf16 value (8 bits each, rounded to
+// nearest, so that what the left-out products hold has no preferred sign).
+// Returns true where that fails: infinities and NaN, values so large that
+// they round to infinity, and values under 2^-100, whose last bits may lie
+// below the smallest normal bf16, which the matrix unit takes as zero.
+__device__ __forceinline__ bool split3(float x, uint32_t (&p)[3])
+{
+    const uint32_t e = (__float_as_uint(x) >> 23) & 255u;
+    p[0] = bf16_bits(x);
+    const float r1 = x - bf16_to_f32((uint16_t)p[0]);
+    p[1] = bf16_bits(r1);
+    p[2] = bf16_bits(r1 - bf16_to_f32((uint16_t)p[1]));
+    return x != 0.0f && (e >= 254u || e < 27u);
+}
+
+// The parts of P [rows][cols] as [3][rows_out][ld], zeros past rows and cols;
+// *flag is set where a value cannot be split.
+__device__ __forceinline__ bool split_rows(const float *__restrict__ P, i64 rows, i64 cols, i64 rows_out, i64 ld,
+                                           uint16_t *__restrict__ O, i64 first, i64 step)
+{
+    const i64 per = ld / 8, n = rows_out * per;
+    const bool wide = cols % 4 == 0 && (reinterpret_cast<uintptr_t>(P) & 15) == 0;
+    bool bad = false;
+    for (i64 i = first; i < n; i += step) {
+        const i64 r = i / per, c = (i - r * per) * 8;
+        float x[8];
+        if (wide) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool in = r < rows && c + 4 * h < cols;
+                const float4 v = in ? *reinterpret_cast<const float4 *>(P + r * cols + c + 4 * h)
+                                    : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = r < rows && c + j < cols ? P[r * cols + c + j] : 0.0f;
+        }
+        uint32_t w[3][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t a[3], b[3];
+            bad |= split3(x[2 * j], a);
+            bad |= split3(x[2 * j + 1], b);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) w[k][j] = a[k] | (b[k] << 16);
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            *reinterpret_cast<uint4 *>(O + (i64)k * rows_out * ld + 8 * i) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+    }
+    return bad;
+}
+
+struct SplitItem {
+    const float *P;
+    i64 rows, cols, rows_out, ld;
+    uint16_t *O;
+};
+
+struct SplitItems {
+    SplitItem it[4];
+};
+
+// blockIdx.y: the array
+__global__ __launch_bounds__(256) void ffn_split_kernel(SplitItems s, int32_t *__restrict__ flag)
+{
+    const SplitItem it = s.it[blockIdx.y];
+    if (split_rows(it.P, it.rows, it.cols, it.rows_out, it.ld, it.O, (i64)blockIdx.x * 256 + threadIdx.x,
+                   (i64)gridDim.x * 256))
+        atomicOr(flag, 1);
+}
+
+size_t part_bytes(i64 rows, i64 ld) { return align_up(3 * sizeof(uint16_t) * (size_t)(rows * ld), 256); }
+
+void split(const SplitItems &s, int count, int32_t *flag, hipStream_t stream)
+{
+    zero_fill((float *)flag, 1, stream);
+    i64 most = 0;
+    for (int k = 0; k < count; ++k) {
+        const i64 n = s.it[k].rows_out * s.it[k].ld / 8;
+        most = n > most ? n : most;
+    }
+    const i64 blocks = ceil_div(most, 256);
+    ffn_split_kernel<<<dim3((unsigned)(blocks < 2048 ? blocks : 2048), (unsigned)count), 256, 0, stream>>>(s, flag);
+}
+
+}  // namespace
+
+size_t ffn_parts_forward_workspace(i64 M, i64 K, i64 F)
+{
+    return 256 + part_bytes(M, whole(K)) + 2 * part_bytes(F, whole(K));
+}
+
+const int32_t *ffn_parts_forward(const float *X, const float *Wg, const float *Wu, i64 M, i64 K, i64 F, dp_act act,
+                                 float *H, float *G, float *U, void *ws, hipStream_t stream)
+{
+    const i64 ld = whole(K);
+    int32_t *flag = (int32_t *)ws;
+    uint16_t *x = (uint16_t *)((char *)ws + 256);
+    uint16_t *g = (uint16_t *)((char *)x + part_bytes(M, ld)), *u = (uint16_t *)((char *)g + part_bytes(F, ld));
+    split({{{X, M, K, M, ld, x}, {Wg, F, K, F, ld, g}, {Wu, F, K, F, ld, u}, {}}}, 3, flag, stream);
+    if (ceil_div(M, 256) * ceil_div(F, 128) >= 192)
+        launch_forward<Large, float>(x, g, u, M, ld, F, act, H, G, U, flag, stream);
+    else launch_forward<Mid, float>(x, g, u, M, ld, F, act, H, G, U, flag, stream);
+    return flag;
+}
+
+size_t ffn_parts_dx_workspace(i64 M, i64 D, i64 F)
+{
+    const DxPlan p = dx_plan(M, D, whole(F), 2 * kParts);
+    const i64 lda = whole(F), ldw = padded(D);
+    const size_t part = p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)(M * ldw) : 0;
+    return 256 + align_up(6 * sizeof(uint16_t) * (size_t)(M * lda), 256) +
+           align_up(6 * sizeof(uint16_t) * (size_t)(lda * ldw), 256) + part;
+}
+
+const int32_t *ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F,
+                            float *dX, void *ws, hipStream_t stream)
+{
+    const i64 lda = whole(F), ldw = padded(D);
+    const DxPlan p = dx_plan(M, D, lda, 2 * kParts);
+    int32_t *flag = (int32_t *)ws;
+    uint16_t *b = (uint16_t *)((char *)ws + 256);
+    uint16_t *w = (uint16_t *)((char *)b + align_up(6 * sizeof(uint16_t) * (size_t)(M * lda), 256));
+    float *part = (float *)((char *)w + align_up(6 * sizeof(uint16_t) * (size_t)(lda * ldw), 256));
+    split({{{BG, M, F, M, lda, b}, {BU, M, F, M, lda, b + 3 * M * lda}, {Wg, F, D, lda, ldw, w},
+            {Wu, F, D, lda, ldw, w + 3 * lda * ldw}}}, 4, flag, stream);
+    if (p.shape == kLarge)
+        launch_dx<LargeDx, float>(b, nullptr, w, nullptr, M, D, lda, lda, ldw, p.splits, dX, part, flag, stream);
+    else launch_dx<MidDx, float>(b, nullptr, w, nullptr, M, D, lda, lda, ldw, p.splits, dX, part, flag, stream);
+    return flag;
 }
 
 }  // namespace dpg

@@ -8,7 +8,8 @@ namespace dpg {
 // Operands as the tile kernels take them: rows of any length from a 16-byte
 // boundary (rows that are no multiple of 16 bytes are padded into the
 // workspace first), row offsets of a tile in 32 bits.
-inline bool ffn_tiles_ok(const void *p, i64 cols) { return aligned(p, 16) && cols < (i64(1) << 21); }
+constexpr i64 kFfnTilesMax = i64(1) << 21;
+inline bool ffn_tiles_ok(const void *p, i64 cols) { return aligned(p, 16) && cols < kFfnTilesMax; }
 
 // H (and G, U unless NULL) from X [M][K], Wg, Wu [F][K] (ffn_tiles_ok each);
 // ws: ffn_bf16_forward_workspace bytes, 16-byte aligned
@@ -21,5 +22,17 @@ void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu,
 size_t ffn_bf16_dx_workspace(i64 M, i64 D, i64 F);
 void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
                  uint16_t *dX, void *ws, hipStream_t stream);
+
+// The same for fp32 values, each as three bf16 parts and every product as six
+// bf16 products (what is left out is 2^-24 of a product), M > 64.  Values that
+// have no such parts (infinities, NaN, and magnitudes under 2^-100 or from
+// 2^127 on) set the returned word in device memory; the kernels launched here
+// then do nothing, and the caller's kernel, launched after them, does the work.
+size_t ffn_parts_forward_workspace(i64 M, i64 K, i64 F);
+const int32_t *ffn_parts_forward(const float *X, const float *Wg, const float *Wu, i64 M, i64 K, i64 F, dp_act act,
+                                 float *H, float *G, float *U, void *ws, hipStream_t stream);
+size_t ffn_parts_dx_workspace(i64 M, i64 D, i64 F);
+const int32_t *ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F,
+                            float *dX, void *ws, hipStream_t stream);
 
 }  // namespace dpg

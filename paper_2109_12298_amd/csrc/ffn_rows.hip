@@ -17,8 +17,6 @@
 
 #include "gated_ffn.hpp"
 
-#include <type_traits>
-
 namespace dpg {
 namespace {
 
@@ -76,13 +74,6 @@ __device__ __forceinline__ void mma(const Piece<float> &a, const Piece<float> &b
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
-}
-
-template <typename T, int ACT>
-__device__ __forceinline__ float act_of(float g)
-{
-    if constexpr (std::is_same<T, float>::value) return act<ACT>(g);
-    else return act_fast<ACT>(g);
 }
 
 // MB: blocks of 16 rows of X; UNITS: units whose loads a wave has in flight
@@ -163,7 +154,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void ffn_rows_kernel(const T *__res
         }
         if (row >= M || f0 + fe >= F) continue;
         const i64 o = (i64)row * F + f0 + fe;
-        store_elem(H + o, act_of<T, ACT>(g) * uu);
+        store_elem(H + o, act_for<ACT, T>(g) * uu);
         if (G != nullptr) {
             store_elem(G + o, g);
             store_elem(U + o, uu);
@@ -207,6 +198,143 @@ void by_act(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, 
     else by_rows<T, DP_ACT_GELU_TANH>(X, Wg, Wu, M, K, F, H, G, U, stream);
 }
 
+// ---------------------------------------------------------------------------
+// dX = BG Wg + BU Wu in fp32 over few rows: a workgroup takes 128 columns and a
+// run of the features of both products, its waves every fourth group of eight
+// features.  Weights go straight to the operands of v_mfma_f32_32x32x2_f32: a
+// lane loads 16 bytes of a weight row (columns 4 j .. 4 j + 3, j = lane % 32),
+// which feed four products with the same column index j, and features are
+// dealt to the k index so that a lane's share of BG is 16 consecutive bytes.
+// The waves' sums are added in LDS in wave order, the workgroups' from the
+// workspace in order.
+// ---------------------------------------------------------------------------
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kDxCols = 128, kDxWaves = 4, kDxGroup = 8;
+
+// four consecutive values of the row at p from index k on, zeros from `end` on
+template <bool VEC>
+__device__ __forceinline__ float4 load4(const float *p, i64 k, i64 end)
+{
+    if constexpr (VEC) {                  // end is a multiple of 4, p 16-byte aligned
+        const float4 v = *reinterpret_cast<const float4 *>(p + (k < end ? k : 0));
+        return k < end ? v : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    } else {
+        return make_float4(k < end ? p[k] : 0.0f, k + 1 < end ? p[k + 1] : 0.0f, k + 2 < end ? p[k + 2] : 0.0f,
+                           k + 3 < end ? p[k + 3] : 0.0f);
+    }
+}
+
+template <int MB, bool VEC>
+__global__ __launch_bounds__(64 * kDxWaves) void ffn_dx_rows_kernel(const float *__restrict__ BG,
+                                                                    const float *__restrict__ BU,
+                                                                    const float *__restrict__ Wg,
+                                                                    const float *__restrict__ Wu, int M, i64 D, i64 F,
+                                                                    int colblocks, int splits, float *__restrict__ out)
+{
+    constexpr int UNROLL = MB == 1 ? 4 : 2;
+    __shared__ __attribute__((aligned(16))) float red[MB * 4 * 1024];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 31, lk = lane >> 5;
+    const int cb = (int)blockIdx.x % colblocks, split = (int)blockIdx.x / colblocks;
+    const i64 d = (i64)cb * kDxCols + 4 * li;
+    f32x16_t acc[MB][4];
+#pragma unroll
+    for (int b = 0; b < MB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[b][i][r] = 0.0f;
+
+    // groups of eight features of BG, then of BU
+    const i64 half = (F + kDxGroup - 1) / kDxGroup;
+    const i64 g0 = (i64)split * 2 * half / splits, g1 = (i64)(split + 1) * 2 * half / splits;
+    for (i64 gb = g0 + wave; gb < g1; gb += UNROLL * kDxWaves) {
+        float4 w[UNROLL][4], a[UNROLL][MB];
+#pragma unroll
+        for (int n = 0; n < UNROLL; ++n) {
+            const i64 g = gb + n * kDxWaves;
+            const bool u = g >= half;
+            // features f .. f + 3 of this lane; past the end (of the run, too) zeros on both sides
+            const i64 f = (u ? g - half : g) * kDxGroup + 4 * lk, end = g < g1 ? F : 0;
+            const float *W = u ? Wu : Wg, *B = u ? BU : BG;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const bool in = f + s < end;
+                const float4 v = load4<VEC>(W + (in ? f + s : 0) * D, d, D);
+                w[n][s] = in ? v : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int b = 0; b < MB; ++b) a[n][b] = load4<VEC>(B + (i64)(32 * b + li < M ? 32 * b + li : M - 1) * F, f, end);
+        }
+#pragma unroll
+        for (int n = 0; n < UNROLL; ++n)
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int b = 0; b < MB; ++b) {
+                    const float x = s == 0 ? a[n][b].x : s == 1 ? a[n][b].y : s == 2 ? a[n][b].z : a[n][b].w;
+                    acc[b][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[n][s].x, x, acc[b][0], 0, 0, 0);
+                    acc[b][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[n][s].y, x, acc[b][1], 0, 0, 0);
+                    acc[b][2] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[n][s].z, x, acc[b][2], 0, 0, 0);
+                    acc[b][3] = __builtin_amdgcn_mfma_f32_32x32x2f32(w[n][s].w, x, acc[b][3], 0, 0, 0);
+                }
+    }
+    // acc[b][i][r] of lane l: row 32 b + l % 32, column 4 j + i, j = 8 (r / 4) + 4 (l / 32) + r % 4
+    for (int w = 0; w < kDxWaves; ++w) {
+        if (wave == w) {
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int j = 8 * (r >> 2) + 4 * lk + (r & 3);
+                    float4 *p = reinterpret_cast<float4 *>(red) + (32 * b + li) * 32 + (j ^ (li & 31));
+                    float4 v = make_float4(acc[b][0][r], acc[b][1][r], acc[b][2][r], acc[b][3][r]);
+                    if (w > 0) {
+                        const float4 o = *p;
+                        v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+                    }
+                    *p = v;
+                }
+        }
+        __syncthreads();
+    }
+    float *O = out + (i64)split * M * D;
+    for (int e = threadIdx.x; e < 32 * MB * 32; e += 64 * kDxWaves) {
+        const int row = e >> 5, j = e & 31;
+        const i64 c = (i64)cb * kDxCols + 4 * j;
+        if (row >= M || c >= D) continue;
+        const float4 v = reinterpret_cast<const float4 *>(red)[row * 32 + (j ^ (row & 31))];
+        const float x[4] = {v.x, v.y, v.z, v.w};
+        if (D % 4 == 0 && (reinterpret_cast<uintptr_t>(O) & 15) == 0) {
+            *reinterpret_cast<float4 *>(O + row * D + c) = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + i < D) O[row * D + c + i] = x[i];
+        }
+    }
+}
+
+// out = the splits' sums, in split order
+__global__ __launch_bounds__(256) void ffn_dx_rows_sum_kernel(const float *__restrict__ part, i64 n, int splits,
+                                                              float *__restrict__ out)
+{
+    for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < n; i += (i64)gridDim.x * 256)
+        out[i] = ordered_sum(part + i, n, splits);
+}
+
+// runs of features: 512 workgroups with the column blocks, each wave two groups of features at the least
+int dx_rows_splits(i64 D, i64 F)
+{
+    const i64 groups = 2 * ceil_div(F, kDxGroup);
+    i64 s = 512 / ceil_div(D, kDxCols);
+    if (s > groups / (2 * kDxWaves)) s = groups / (2 * kDxWaves);
+    if (s > 64) s = 64;
+    return s < 1 ? 1 : (int)s;
+}
+
 }  // namespace
 
 void ffn_rows_forward(const void *X, const void *Wg, const void *Wu, dp_dtype dt, i64 M, i64 K, i64 F, dp_act act,
@@ -214,6 +342,29 @@ void ffn_rows_forward(const void *X, const void *Wg, const void *Wu, dp_dtype dt
 {
     if (dt == DP_F32) by_act<float>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
     else by_act<uint16_t>(X, Wg, Wu, M, K, F, act, H, G, U, stream);
+}
+
+size_t ffn_rows_dx_workspace(i64 M, i64 D, i64 F)
+{
+    const int splits = dx_rows_splits(D, F);
+    return splits > 1 ? sizeof(float) * (size_t)splits * (size_t)(M * D) : 0;
+}
+
+void ffn_rows_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F, float *dX,
+                 void *ws, hipStream_t stream)
+{
+    const int splits = dx_rows_splits(D, F), cb = (int)ceil_div(D, kDxCols);
+    const bool vec = D % 4 == 0 && F % 4 == 0 && aligned(BG, 16) && aligned(BU, 16) && aligned(Wg, 16) && aligned(Wu, 16);
+    float *out = splits > 1 ? (float *)ws : dX;
+    const auto go = [&](auto kernel) {
+        kernel<<<(unsigned)((i64)cb * splits), 64 * kDxWaves, 0, stream>>>(BG, BU, Wg, Wu, (int)M, D, F, cb, splits, out);
+    };
+    if (M <= 32) go(vec ? ffn_dx_rows_kernel<1, true> : ffn_dx_rows_kernel<1, false>);
+    else go(vec ? ffn_dx_rows_kernel<2, true> : ffn_dx_rows_kernel<2, false>);
+    if (splits > 1) {
+        const i64 blocks = ceil_div(M * D, 256);
+        ffn_dx_rows_sum_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(out, M * D, splits, dX);
+    }
 }
 
 }  // namespace dpg

@@ -21,7 +21,8 @@ constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------------------
 // Any size, type and alignment: 64 x 64 tiles, element loads, fp32 MFMA
-// (products of bf16 values are exact in fp32).
+// (products of bf16 values are exact in fp32).  flag: a word in device memory
+// without which the work is already done, or NULL.
 // ---------------------------------------------------------------------------
 constexpr int kTM = 64, kTN = 64, kTK = 16;
 constexpr int kLd = kTM + 1;              // LDS row: operands lie K-major, their loads come along K
@@ -54,8 +55,9 @@ template <typename T, int ACT>
 __global__ __launch_bounds__(kThreads) void ffn_forward_any_kernel(const T *__restrict__ X, const T *__restrict__ Wg,
                                                                    const T *__restrict__ Wu, i64 M, i64 K, i64 F,
                                                                    i64 tiles_f, T *__restrict__ H, T *__restrict__ G,
-                                                                   T *__restrict__ U)
+                                                                   T *__restrict__ U, const int32_t *__restrict__ flag)
 {
+    if (flag != nullptr && *flag == 0) return;
     __shared__ float Xs[kTK * kLd], Gs[kTK * kLd], Us[kTK * kLd];
     const i64 b = xcd_swizzle(blockIdx.x, gridDim.x);
     const i64 m0 = b / tiles_f * kTM, f0 = b % tiles_f * kTN;
@@ -95,8 +97,10 @@ __global__ __launch_bounds__(kThreads) void ffn_forward_any_kernel(const T *__re
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ffn_dx_any_kernel(const T *__restrict__ BG, const T *__restrict__ BU,
                                                               const T *__restrict__ Wg, const T *__restrict__ Wu, i64 M,
-                                                              i64 D, i64 F, i64 tiles_d, T *__restrict__ dX)
+                                                              i64 D, i64 F, i64 tiles_d, T *__restrict__ dX,
+                                                              const int32_t *__restrict__ flag)
 {
+    if (flag != nullptr && *flag == 0) return;
     __shared__ float Bs[kTK * kLd], Ws[kTK * kLd];
     const i64 b = xcd_swizzle(blockIdx.x, gridDim.x);
     const i64 m0 = b / tiles_d * kTM, d0 = b % tiles_d * kTN;
@@ -174,11 +178,11 @@ __global__ __launch_bounds__(kThreads) void ffn_backprops_kernel(const T *dH, co
 
 template <typename T, int ACT>
 void forward(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, void *H, void *G, void *U,
-             hipStream_t stream)
+             const int32_t *flag, hipStream_t stream)
 {
     const i64 tiles_f = ceil_div(F, kTN);
     ffn_forward_any_kernel<T, ACT><<<(unsigned)(ceil_div(M, kTM) * tiles_f), kThreads, 0, stream>>>(
-        (const T *)X, (const T *)Wg, (const T *)Wu, M, K, F, tiles_f, (T *)H, (T *)G, (T *)U);
+        (const T *)X, (const T *)Wg, (const T *)Wu, M, K, F, tiles_f, (T *)H, (T *)G, (T *)U, flag);
 }
 
 template <typename T, int ACT>
@@ -198,11 +202,11 @@ void backprops(const void *dH, const void *G, const void *U, i64 n, void *BG, vo
 
 template <typename T>
 void dx(const void *BG, const void *BU, const void *Wg, const void *Wu, i64 M, i64 D, i64 F, void *dX,
-        hipStream_t stream)
+        const int32_t *flag, hipStream_t stream)
 {
     const i64 tiles_d = ceil_div(D, kTN);
     ffn_dx_any_kernel<T><<<(unsigned)(ceil_div(M, kTM) * tiles_d), kThreads, 0, stream>>>(
-        (const T *)BG, (const T *)BU, (const T *)Wg, (const T *)Wu, M, D, F, tiles_d, (T *)dX);
+        (const T *)BG, (const T *)BU, (const T *)Wg, (const T *)Wu, M, D, F, tiles_d, (T *)dX, flag);
 }
 
 dp_status check_sizes(i64 M, i64 D, i64 F)
@@ -226,7 +230,7 @@ using namespace dpg;
 extern "C" size_t dp_gated_ffn_forward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt)
 {
     if (!dtype_ok(dt) || check_sizes(M, d_in, d_ff) != DP_OK || M <= kFfnRowsMax) return 0;
-    return dt == DP_BF16 ? ffn_bf16_forward_workspace(M, d_in, d_ff) : 0;
+    return dt == DP_BF16 ? ffn_bf16_forward_workspace(M, d_in, d_ff) : ffn_parts_forward_workspace(M, d_in, d_ff);
 }
 
 extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const void *Wu, dp_dtype dt, int64_t M,
@@ -245,14 +249,18 @@ extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const v
     if (M <= kFfnRowsMax) {
         ffn_rows_forward(X, Wg, Wu, dt, M, d_in, d_ff, act, H, G, U, stream);
     } else if (dt == DP_F32) {
-        if (act == DP_ACT_SILU) forward<float, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
-        else forward<float, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+        const int32_t *flag = nullptr;
+        if (d_in < kFfnTilesMax)
+            flag = ffn_parts_forward((const float *)X, (const float *)Wg, (const float *)Wu, M, d_in, d_ff, act, (float *)H,
+                                     (float *)G, (float *)U, ws, stream);
+        if (act == DP_ACT_SILU) forward<float, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, flag, stream);
+        else forward<float, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, flag, stream);
     } else if (ffn_tiles_ok(X, d_in) && ffn_tiles_ok(Wg, d_in) && ffn_tiles_ok(Wu, d_in)) {
         ffn_bf16_forward((const uint16_t *)X, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in, d_ff, act,
                          (uint16_t *)H, (uint16_t *)G, (uint16_t *)U, ws, stream);
     } else {
-        if (act == DP_ACT_SILU) forward<uint16_t, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
-        else forward<uint16_t, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+        if (act == DP_ACT_SILU) forward<uint16_t, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, nullptr, stream);
+        else forward<uint16_t, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, nullptr, stream);
     }
     return launch_status();
 }
@@ -260,7 +268,8 @@ extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const v
 extern "C" size_t dp_gated_ffn_backward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt)
 {
     if (!dtype_ok(dt) || check_sizes(M, d_in, d_ff) != DP_OK || M == 0) return 0;
-    return dt == DP_BF16 ? ffn_bf16_dx_workspace(M, d_in, d_ff) : 0;
+    if (dt == DP_BF16) return ffn_bf16_dx_workspace(M, d_in, d_ff);
+    return M <= kFfnRowsMax ? ffn_rows_dx_workspace(M, d_in, d_ff) : ffn_parts_dx_workspace(M, d_in, d_ff);
 }
 
 extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const void *U, const void *Wg,
@@ -281,7 +290,17 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
     if (dt == DP_F32) {
         if (act == DP_ACT_SILU) backprops<float, DP_ACT_SILU>(dH, G, U, n, BG, BU, stream);
         else backprops<float, DP_ACT_GELU_TANH>(dH, G, U, n, BG, BU, stream);
-        if (dX != nullptr) dx<float>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
+        if (dX == nullptr) return launch_status();
+        if (M <= kFfnRowsMax) {
+            ffn_rows_dx((const float *)BG, (const float *)BU, (const float *)Wg, (const float *)Wu, M, d_in, d_ff,
+                        (float *)dX, ws, stream);
+        } else {
+            const int32_t *flag = nullptr;
+            if (d_in < kFfnTilesMax && d_ff < kFfnTilesMax)
+                flag = ffn_parts_dx((const float *)BG, (const float *)BU, (const float *)Wg, (const float *)Wu, M, d_in,
+                                    d_ff, (float *)dX, ws, stream);
+            dx<float>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, flag, stream);
+        }
     } else {
         if (act == DP_ACT_SILU) backprops<uint16_t, DP_ACT_SILU>(dH, G, U, n, BG, BU, stream);
         else backprops<uint16_t, DP_ACT_GELU_TANH>(dH, G, U, n, BG, BU, stream);
@@ -290,7 +309,7 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
             ffn_bf16_dx((const uint16_t *)BG, (const uint16_t *)BU, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in,
                         d_ff, (uint16_t *)dX, ws, stream);
         else
-            dx<uint16_t>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
+            dx<uint16_t>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, nullptr, stream);
     }
     return launch_status();
 }

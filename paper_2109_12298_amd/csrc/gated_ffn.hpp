@@ -38,6 +38,13 @@ __device__ __forceinline__ float act_fast(float g)
     return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * w));
 }
 
+// for results kept in T
+template <int ACT, typename T>
+__device__ __forceinline__ float act_for(float g)
+{
+    return sizeof(T) == 4 ? act<ACT>(g) : act_fast<ACT>(g);
+}
+
 // act(g) and act'(g) = p + g p (1 - p) w'(g), p = sigmoid(w(g)).  For large
 // |g| in the GELU form p (1 - p) is 0 while g w'(g) may be infinite: the term is 0.
 template <int ACT>

@@ -130,27 +130,59 @@ def test_unaligned(M, K, F, dt, by):
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
 def test_nonfinite_rows_stay_apart(M, K, F, dt, value):
-    """A NaN or infinity in one row reaches that row's outputs, all of them, and no other's."""
+    """A NaN or infinity in one row reaches that row's outputs, all of them, and no other's (whose sums may be formed
+    by another kernel then: both meet the bound)."""
     say("ffn nonfinite", M, K, F, dt, value)
     rng = np.random.default_rng(M)
     tt, _ = DT[dt]
-    X, (Wg, Wu) = torch.from_numpy(rng.standard_normal((M, K))).to(tt).to(DEV), weights(rng, F, K, tt)
+    X, (Wg, Wu) = torch.from_numpy(rng.standard_normal((M, K))).to(tt), weights(rng, F, K, tt)
+    want, bound = R.ffn_forward(dp.DP_ACT_SILU, R.f64(X), R.f64(Wg), R.f64(Wu), tt)
     Wg, Wu = Wg.to(DEV), Wu.to(DEV)
-    clean = forward(X, Wg, Wu, dp.DP_ACT_SILU)
     bad = M // 2
     Xb = X.clone()
     Xb[bad, K // 3] = value
     rest = [m for m in range(M) if m != bad]
-    for a, b in zip(forward(Xb, Wg, Wu, dp.DP_ACT_SILU)[1:], clean[1:]):
-        assert not a[bad].isfinite().any() and torch.equal(a[rest], b[rest])
-    dH = torch.from_numpy(rng.standard_normal((M, F))).to(tt).to(DEV)
-    _, G, U = clean
-    _, _, dX = backward(dH, G, U, Wg, Wu, dp.DP_ACT_SILU)
-    dHb = dH.clone()
-    dHb[bad, F // 3] = value
-    BG, BU, dXb = backward(dHb, G, U, Wg, Wu, dp.DP_ACT_SILU)
-    assert not dXb[bad].isfinite().any() and torch.equal(dXb[rest], dX[rest])
-    assert not BU[bad, F // 3].isfinite().any()
+    out = forward(Xb.to(DEV), Wg, Wu, dp.DP_ACT_SILU)
+    for g, w, b in zip(out, want, bound):
+        R.within(g[rest], w[rest], b[rest])
+    assert not out[1][bad].isfinite().any() and not out[2][bad].isfinite().any()
+    _, G, U = forward(X.to(DEV), Wg, Wu, dp.DP_ACT_SILU)
+    dH = torch.from_numpy(rng.standard_normal((M, F))).to(tt)
+    dH[bad, F // 3] = value
+    BG, BU, dX = backward(dH.to(DEV), G, U, Wg, Wu, dp.DP_ACT_SILU)
+    assert not dX[bad].isfinite().any() and not BU[bad, F // 3].isfinite().any()
+    wx, bx = R.ffn_dx(R.f64(BG[rest]), R.f64(BU[rest]), R.f64(Wg), R.f64(Wu), tt)
+    R.within(dX[rest], wx, bx)
+
+
+@pytest.mark.parametrize("value", [1e-36, 1e-31, 1e-30, 2e38])
+@pytest.mark.parametrize("M,K,F", [(70, 64, 40), (300, 264, 136)])
+def test_f32_values_without_parts(M, K, F, value):
+    """fp32 values of the ends of the range, which the three-part product leaves to another kernel: one of them in X, in
+    a weight, in a backprop."""
+    say("ffn range", M, K, F, value)
+    rng = np.random.default_rng(K)
+    X, (Wg, Wu) = torch.from_numpy(rng.standard_normal((M, K))).float(), weights(rng, F, K, torch.float32)
+    dH = torch.from_numpy(rng.standard_normal((M, F))).float()
+    for where in ("X", "Wu", "dH"):
+        x, wu, dh = X.clone(), Wu.clone(), dH.clone()
+        if where == "X":
+            x[3] = x[3] * value / x[3].abs().max() / 4
+            wu, dh = wu.clone(), dh.clone()
+        elif where == "Wu":
+            wu[F - 1] = wu[F - 1] * value / wu[F - 1].abs().max() / (4 * K)
+        else:
+            dh[M - 1] = dh[M - 1] * value / dh[M - 1].abs().max() / (16 * F)
+        out = forward(x.to(DEV), Wg.to(DEV), wu.to(DEV), dp.DP_ACT_SILU)
+        want, bound = R.ffn_forward(dp.DP_ACT_SILU, R.f64(x), R.f64(Wg), R.f64(wu), torch.float32)
+        fine = np.abs(want[0]) < 1e38                          # H = act(G) U may leave the range of fp32
+        for g, w, b in zip(out, want, bound):
+            R.within(g[torch.from_numpy(fine)], w[fine], b[fine])
+        G, U = torch.from_numpy(want[1]).float().clamp(-8, 8), torch.from_numpy(want[2]).float().clamp(-8, 8)
+        BG, BU, dX = backward(dh.to(DEV), G.to(DEV), U.to(DEV), Wg.to(DEV), wu.to(DEV), dp.DP_ACT_SILU)
+        wx, bx = R.ffn_dx(R.f64(BG), R.f64(BU), R.f64(Wg), R.f64(wu), torch.float32)
+        fine = np.abs(wx) + bx < 1e38
+        R.within(dX[torch.from_numpy(fine)], wx[fine], bx[fine])
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
