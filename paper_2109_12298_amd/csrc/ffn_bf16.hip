@@ -549,7 +549,7 @@ __global__ __launch_bounds__(256) void ffn_dx_sum_kernel(const float *__restrict
 }
 
 typedef DxShape<256, 256, 2, 4, 64, 2> LargeDx;
-typedef DxShape<128, 128, 2, 2, 64, 2> MidDx;
+typedef DxShape<128, 128, 2, 2, 64, 4> MidDx;
 typedef DxShape<64, 128, 1, 4, 64, 3> Rows64Dx;
 typedef DxShape<32, 128, 1, 4, 64, 3> Rows32Dx;
 
@@ -611,26 +611,69 @@ struct DxPlan {
     int shape, splits;
 };
 
+// Tile shape and splits by the time they take: rounds of 256 workgroups, each
+// of its stages at what one takes (256 x 256 tiles 1.75 us, 128 x 128 0.59:
+// measured at 8192 x 11008 -> 4096 and 4096 x 2048 -> 768), and the partial
+// tiles written and read.  4096 x 2048 -> 768 (192 tiles of 128): 53 us in one
+// split, 65 in two; 128 x 11008 -> 4096 (32 tiles): 206 us in one, 64 in eight.
 // runs: products of F features that the stages run through (2, or 12 for fp32 in parts)
 DxPlan dx_plan(i64 M, i64 D, i64 F, int runs)
 {
-    DxPlan p;
-    p.splits = 1;
-    if (M > 64 && ceil_div(M, 256) * ceil_div(D, 256) >= 192) {
-        p.shape = kLarge;
+    const i64 stages = runs * ceil_div(F, 64);
+    DxPlan p = {kMid, 1};
+    if (M <= 64) {                        // one row of tiles: the weights' bytes bound it, over two workgroups per CU
+        p.shape = M <= 32 ? kRows32 : kRows64;
+        i64 s = 512 / ceil_div(D, 128);
+        if (s > stages / 4) s = stages / 4;
+        if (s > 32) s = 32;
+        p.splits = s < 1 ? 1 : (int)s;
         return p;
     }
-    p.shape = M <= 32 ? kRows32 : M <= 64 ? kRows64 : kMid;
-    const i64 tiles = ceil_div(M, M <= 32 ? 32 : M <= 64 ? 64 : 128) * ceil_div(D, 128), stages = runs * ceil_div(F, 64);
-    i64 s = 512 / tiles;
-    if (s > stages / 4) s = stages / 4;
-    if (s > 32) s = 32;
-    p.splits = s < 1 ? 1 : (int)s;
+    double best = 1e30;
+    for (int shape = kMid; shape <= kLarge; ++shape) {
+        const i64 b = shape == kLarge ? 256 : 128, tiles = ceil_div(M, b) * ceil_div(D, b);
+        for (int s = 1; s <= 16 && s <= stages / 4 + 1; ++s) {
+            const double t = (double)ceil_div(tiles * s, 256) * (double)ceil_div(stages, s) * (shape == kLarge ? 1.75 : 0.59) +
+                             (s > 1 ? 4.0 + 8.0 * s * (double)M * (double)D / 4.5e6 : 0.0);
+            if (t < best) {
+                best = t;
+                p.shape = shape;
+                p.splits = s;
+            }
+        }
+    }
     return p;
 }
 
 typedef Shape<256, 128, 4, 2, 64, 2> Large;
-typedef Shape<128, 64, 2, 2, 64, 2> Mid;
+typedef Shape<128, 64, 2, 2, 64, 2> Mid;       // two workgroups per CU
+typedef Shape<128, 64, 2, 2, 64, 4> Deep;      // one
+typedef Shape<64, 64, 2, 2, 64, 4> Rows64;
+
+// Tiles by the rounds that they take: 256 large ones, or 512 middle ones, at
+// 0.64 of the time (4096 x 1024 -> 2752, 352 large tiles: 60.3 us large, 59.3
+// middle; 4096 x 768 -> 2048, 256 tiles: 30.5 and 37.3); up to 256 middle ones
+// run one to a CU with four stages in flight (128 x 4096 -> 11008: 53.3 us,
+// 64.5 with two).
+enum { kTilesRows64, kTilesDeep, kTilesMid, kTilesLarge };
+int forward_tiles(i64 M, i64 F)
+{
+    if (M <= 64) return kTilesRows64;
+    const i64 large = ceil_div(M, 256) * ceil_div(F, 128), mid = ceil_div(M, 128) * ceil_div(F, 64);
+    if ((double)ceil_div(large, 256) <= 0.64 * (double)ceil_div(mid, 512)) return kTilesLarge;
+    return mid <= 256 ? kTilesDeep : kTilesMid;
+}
+
+template <typename T>
+void forward_by_tiles(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act, T *H,
+                      T *G, T *U, const int32_t *flag, hipStream_t stream)
+{
+    const int tiles = forward_tiles(M, F);
+    if (tiles == kTilesLarge) launch_forward<Large, T>(X, Wg, Wu, M, K, F, act, H, G, U, flag, stream);
+    else if (tiles == kTilesMid) launch_forward<Mid, T>(X, Wg, Wu, M, K, F, act, H, G, U, flag, stream);
+    else if (tiles == kTilesDeep) launch_forward<Deep, T>(X, Wg, Wu, M, K, F, act, H, G, U, flag, stream);
+    else if constexpr (sizeof(T) == 2) launch_forward<Rows64, T>(X, Wg, Wu, M, K, F, act, H, G, U, flag, stream);
+}
 
 }  // namespace
 
@@ -644,9 +687,7 @@ void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu,
     Wg = pad_rows(Wg, F, K, w, stream);
     Wu = pad_rows(Wu, F, K, w, stream);
     K = padded(K);
-    if (ceil_div(M, 256) * ceil_div(F, 128) >= 192)
-        launch_forward<Large, uint16_t>(X, Wg, Wu, M, K, F, act, H, G, U, nullptr, stream);
-    else launch_forward<Mid, uint16_t>(X, Wg, Wu, M, K, F, act, H, G, U, nullptr, stream);
+    forward_by_tiles<uint16_t>(X, Wg, Wu, M, K, F, act, H, G, U, nullptr, stream);
 }
 
 size_t ffn_bf16_dx_workspace(i64 M, i64 D, i64 F)
@@ -783,9 +824,7 @@ const int32_t *ffn_parts_forward(const float *X, const float *Wg, const float *W
     uint16_t *x = (uint16_t *)((char *)ws + 256);
     uint16_t *g = (uint16_t *)((char *)x + part_bytes(M, ld)), *u = (uint16_t *)((char *)g + part_bytes(F, ld));
     split({{{X, M, K, M, ld, x}, {Wg, F, K, F, ld, g}, {Wu, F, K, F, ld, u}, {}}}, 3, flag, stream);
-    if (ceil_div(M, 256) * ceil_div(F, 128) >= 192)
-        launch_forward<Large, float>(x, g, u, M, ld, F, act, H, G, U, flag, stream);
-    else launch_forward<Mid, float>(x, g, u, M, ld, F, act, H, G, U, flag, stream);
+    forward_by_tiles<float>(x, g, u, M, ld, F, act, H, G, U, flag, stream);
     return flag;
 }
 

@@ -227,6 +227,17 @@ bool act_ok(dp_act act) { return act == DP_ACT_SILU || act == DP_ACT_GELU_TANH; 
 
 using namespace dpg;
 
+namespace {
+
+// few rows, and (bf16) up to kFfnRowsMax of them whose operands the tiles would have to pad
+bool by_rows(const void *X, const void *Wg, const void *Wu, dp_dtype dt, i64 M, i64 K)
+{
+    if (dt == DP_F32 || M <= kFfnRowsBf16) return M <= kFfnRowsMax;
+    return M <= kFfnRowsMax && !(K % 8 == 0 && ffn_tiles_ok(X, K) && ffn_tiles_ok(Wg, K) && ffn_tiles_ok(Wu, K));
+}
+
+}  // namespace
+
 extern "C" size_t dp_gated_ffn_forward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt)
 {
     if (!dtype_ok(dt) || check_sizes(M, d_in, d_ff) != DP_OK || M <= kFfnRowsMax) return 0;
@@ -246,7 +257,7 @@ extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const v
     DPG_REQUIRE((G == nullptr) == (U == nullptr), DP_EINVAL);
     const size_t need = dp_gated_ffn_forward_workspace_bytes(M, d_in, d_ff, dt);
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
-    if (M <= kFfnRowsMax) {
+    if (by_rows(X, Wg, Wu, dt, M, d_in)) {
         ffn_rows_forward(X, Wg, Wu, dt, M, d_in, d_ff, act, H, G, U, stream);
     } else if (dt == DP_F32) {
         const int32_t *flag = nullptr;
