@@ -640,8 +640,7 @@ def dp_clip_global_norm_many(items, count, C, norm, status=None, ws=None, stream
     import torch
     dev, p = _tensors("dp_clip_global_norm_many", ("norm", norm, torch.float32, 1), ("status", status, torch.int32, 1),
                       ("ws", ws, None, 0))
-    _run("dp_clip_global_norm_many", dev, lib().dp_clip_global_norm_many, ctypes.cast(items, ctypes.c_void_p), count, C,
-         p[0], p[1], p[2], _nbytes(ws), stream=stream)
+    _run("dp_clip_global_norm_many", dev, lib().dp_clip_global_norm_many, ctypes.addressof(items), count, C, p[0], p[1], p[2], _nbytes(ws), stream=stream)
 
 
 # ---------------------------------------------------------------------------

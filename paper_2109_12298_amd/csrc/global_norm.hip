@@ -3,15 +3,21 @@
 //
 // The norm needs every value before the first output can be written, so the
 // values are read twice and written once; both passes are bound by those
-// bytes.  The tensors are cut into chunks of one size (chosen so that a call
-// has about kTargetChunks of them); a workgroup takes one chunk.
+// bytes.  The tensors are cut into chunks of one size (chunk_size); a
+// workgroup takes one chunk.
 // 1. sumsq_kernel: each chunk's sum of squares, in 64 bits, to the workspace;
 // 2. norm_kernel: the chunks' sums, added in a fixed order by one workgroup,
 //    and the clip factor;
 // 3. scale_kernel: the outputs, chunks in descending order, so that what the
-//    first pass read last (and the caches still hold) is read first.
+//    caches still hold of the first pass is read first.
+// Calls of more than kCachedBytes load and store past the caches, and have
+// shorter chunks (fp32, cached and streamed): 37 MB 24 and 27 us, 75 MB 42.5
+// and 44, 150 MB 93 and 80, 1.3 GB (4.0 GB moved) 750 and 694, of which the
+// first pass takes 206 (6.5 TB/s) and the second, reading and writing, 485.
 // Calls of at most kFoldChunks chunks leave out 2.: every workgroup of 3. adds
-// the few sums itself.  Up to kBatch tensors go into a launch.
+// the few sums itself.  Up to kBatch tensors go into a launch.  Calls of a few
+// tens of thousands of values are one launch of one workgroup (tiny_kernel),
+// which keeps them in registers.
 //
 // Squares and sums are in fp64: the vector unit has the rate to spare (a
 // conversion and a multiply-add per value, against the 4 bytes that it is
@@ -22,10 +28,15 @@ namespace dpg {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 96;                // tensors per launch (their table is a kernel argument)
+constexpr int kBatch = 128;               // tensors per launch (their table is a kernel argument)
 constexpr int kMinChunk = 4096;           // elements
-constexpr i64 kTargetChunks = 4096;
+constexpr int kMidChunk = 32768, kStreamChunk = 8192;
+constexpr i64 kMostChunks = 16384;
 constexpr int kFoldChunks = 512;
+constexpr i64 kCachedBytes = i64(96) << 20;
+constexpr int kTinyChunk = 1024;          // elements of a wave's turn in tiny_kernel
+constexpr int kTinyTurns = 4;
+constexpr int kTinyChunks = 16 * kTinyTurns;
 constexpr int kHeader = 16;               // bytes of the workspace before the chunks' sums
 constexpr int kMaxCount = 65536;
 
@@ -33,13 +44,17 @@ struct Batch {
     int count;
     int chunk0;                           // the batch's first chunk among the call's
     int chunks;                           // all chunks of the call
+    int stream;                           // loads and stores past the caches
     i64 chunk;                            // elements
     const void *g[kBatch];
     void *out[kBatch];
-    i64 numel[kBatch];
+    i64 numel[kBatch];                    // times two, plus one for bf16
     int blk0[kBatch + 1];                 // first workgroup of each tensor in this launch
-    uint8_t bf16[kBatch];
 };
+// (No array of bytes or half words in a kernel argument beside pointers:
+// scalar loads drop the low bits of both parts of their address, and the
+// compiler has been seen to reuse such an array's address as one part of a
+// pointer's.)
 
 __device__ __forceinline__ int find_tensor(const Batch &b, int blk)
 {
@@ -123,7 +138,26 @@ __device__ __forceinline__ uint4 pack(const float (&v)[8])
 __device__ __forceinline__ void store_elem(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_elem(uint16_t *p, float v) { *p = (uint16_t)bf16_bits(v); }
 
-constexpr int kInFlight = 4;              // 16-byte loads of a thread in flight
+constexpr int kInFlight = 8;              // 16-byte loads of a thread in flight
+
+template <bool STREAM>
+__device__ __forceinline__ uint4 load16(const uint4 *p)
+{
+    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+    if constexpr (STREAM) {
+        const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    return *p;
+}
+
+template <bool STREAM>
+__device__ __forceinline__ void store16(uint4 *p, const uint4 &v)
+{
+    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+    if constexpr (STREAM) __builtin_nontemporal_store(u32x4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_t *>(p));
+    else *p = v;
+}
 
 // elements before the first 16-byte boundary of p, at most n
 template <typename T>
@@ -133,7 +167,7 @@ __device__ __forceinline__ i64 head_of(const T *p, i64 n)
     return h < n ? h : n;
 }
 
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ double chunk_sumsq(const T *__restrict__ p, i64 n)
 {
     constexpr int VN = Vec<T>::N;
@@ -141,24 +175,26 @@ __device__ __forceinline__ double chunk_sumsq(const T *__restrict__ p, i64 n)
     const i64 nv = (n - head) / VN;
     const uint4 *q = reinterpret_cast<const uint4 *>(p + head);
     double s[4] = {0.0, 0.0, 0.0, 0.0};
-    i64 i = threadIdx.x;
-    for (; i + (kInFlight - 1) * kThreads < nv; i += kInFlight * kThreads) {
-        uint4 r[kInFlight];
-#pragma unroll
-        for (int k = 0; k < kInFlight; ++k) r[k] = q[i + k * kThreads];
-#pragma unroll
-        for (int k = 0; k < kInFlight; ++k) {
-            float v[VN];
-            unpack(r[k], v);
-#pragma unroll
-            for (int j = 0; j < VN; ++j) s[j & 3] = fma((double)v[j], (double)v[j], s[j & 3]);
-        }
-    }
-    for (; i < nv; i += kThreads) {
+    const auto add = [&](const uint4 &r) {
         float v[VN];
-        unpack(q[i], v);
+        unpack(r, v);
 #pragma unroll
         for (int j = 0; j < VN; ++j) s[j & 3] = fma((double)v[j], (double)v[j], s[j & 3]);
+    };
+    i64 i = threadIdx.x;
+    uint4 r[kInFlight];
+    for (; i + (kInFlight - 1) * kThreads < nv; i += kInFlight * kThreads) {
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k) r[k] = load16<STREAM>(q + i + k * kThreads);
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k) add(r[k]);
+    }
+    if (i < nv) {                         // what is left, all in flight too
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k) r[k] = load16<STREAM>(q + (i + k * kThreads < nv ? i + k * kThreads : i));
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k)
+            if (i + k * kThreads < nv) add(r[k]);
     }
     // the elements before the first and after the last 16-byte piece (fewer than 2 VN)
     const i64 rest = n - VN * nv;
@@ -170,7 +206,7 @@ __device__ __forceinline__ double chunk_sumsq(const T *__restrict__ p, i64 n)
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ void chunk_scale(const T *p, T *o, i64 n, float c)
 {
     constexpr int VN = Vec<T>::N;
@@ -183,26 +219,27 @@ __device__ __forceinline__ void chunk_scale(const T *p, T *o, i64 n, float c)
     const i64 nv = (n - head) / VN;
     const uint4 *q = reinterpret_cast<const uint4 *>(p + head);
     uint4 *t = reinterpret_cast<uint4 *>(o + head);
-    i64 i = threadIdx.x;
-    for (; i + (kInFlight - 1) * kThreads < nv; i += kInFlight * kThreads) {
-        uint4 r[kInFlight];
-#pragma unroll
-        for (int k = 0; k < kInFlight; ++k) r[k] = q[i + k * kThreads];
-#pragma unroll
-        for (int k = 0; k < kInFlight; ++k) {
-            float v[VN];
-            unpack(r[k], v);
-#pragma unroll
-            for (int j = 0; j < VN; ++j) v[j] *= c;
-            t[i + k * kThreads] = pack(v);
-        }
-    }
-    for (; i < nv; i += kThreads) {
+    const auto put = [&](i64 at, const uint4 &r) {
         float v[VN];
-        unpack(q[i], v);
+        unpack(r, v);
 #pragma unroll
         for (int j = 0; j < VN; ++j) v[j] *= c;
-        t[i] = pack(v);
+        store16<STREAM>(t + at, pack(v));
+    };
+    i64 i = threadIdx.x;
+    uint4 r[kInFlight];
+    for (; i + (kInFlight - 1) * kThreads < nv; i += kInFlight * kThreads) {
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k) r[k] = load16<STREAM>(q + i + k * kThreads);
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k) put(i + k * kThreads, r[k]);
+    }
+    if (i < nv) {
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k) r[k] = load16<STREAM>(q + (i + k * kThreads < nv ? i + k * kThreads : i));
+#pragma unroll
+        for (int k = 0; k < kInFlight; ++k)
+            if (i + k * kThreads < nv) put(i + k * kThreads, r[k]);
     }
     const i64 rest = n - VN * nv;
     if (threadIdx.x < rest) {
@@ -211,12 +248,14 @@ __device__ __forceinline__ void chunk_scale(const T *p, T *o, i64 n, float c)
     }
 }
 
-// the chunk of workgroup blk: its tensor, first element and length
-__device__ __forceinline__ int chunk_of(const Batch &b, int blk, i64 &first, i64 &n)
+// the chunk of workgroup blk: its tensor, first element, length and type
+__device__ __forceinline__ int chunk_of(const Batch &b, int blk, i64 &first, i64 &n, bool &bf16)
 {
     const int k = find_tensor(b, blk);
+    const i64 numel = b.numel[k] >> 1;
+    bf16 = (b.numel[k] & 1) != 0;
     first = (i64)(blk - b.blk0[k]) * b.chunk;
-    n = b.numel[k] - first < b.chunk ? b.numel[k] - first : b.chunk;
+    n = numel - first < b.chunk ? numel - first : b.chunk;
     return k;
 }
 
@@ -224,9 +263,16 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(Batch b, double *__rest
 {
     __shared__ double red[kThreads / 64];
     i64 first, n;
-    const int k = chunk_of(b, (int)blockIdx.x, first, n);
-    const double s = b.bf16[k] ? chunk_sumsq((const uint16_t *)b.g[k] + first, n)
-                               : chunk_sumsq((const float *)b.g[k] + first, n);
+    bool bf16;
+    const int k = chunk_of(b, (int)blockIdx.x, first, n, bf16);
+    double s;
+    if (bf16) {
+        const uint16_t *p = (const uint16_t *)b.g[k] + first;
+        s = b.stream ? chunk_sumsq<true>(p, n) : chunk_sumsq<false>(p, n);
+    } else {
+        const float *p = (const float *)b.g[k] + first;
+        s = b.stream ? chunk_sumsq<true>(p, n) : chunk_sumsq<false>(p, n);
+    }
     const double t = block_sum64<kThreads>(s, red);
     if (threadIdx.x == 0) sums[b.chunk0 + blockIdx.x] = t;
 }
@@ -263,20 +309,107 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Batch b, const double *
         c = *factor;
     }
     i64 first, n;
-    const int k = chunk_of(b, (int)(gridDim.x - 1 - blockIdx.x), first, n);
+    bool bf16;
+    const int k = chunk_of(b, (int)(gridDim.x - 1 - blockIdx.x), first, n, bf16);
     if (b.out[k] == nullptr) return;
-    if (b.bf16[k]) chunk_scale((const uint16_t *)b.g[k] + first, (uint16_t *)b.out[k] + first, n, c);
-    else chunk_scale((const float *)b.g[k] + first, (float *)b.out[k] + first, n, c);
+    if (bf16) {
+        const uint16_t *p = (const uint16_t *)b.g[k] + first;
+        uint16_t *o = (uint16_t *)b.out[k] + first;
+        if (b.stream) chunk_scale<true>(p, o, n, c);
+        else chunk_scale<false>(p, o, n, c);
+    } else {
+        const float *p = (const float *)b.g[k] + first;
+        float *o = (float *)b.out[k] + first;
+        if (b.stream) chunk_scale<true>(p, o, n, c);
+        else chunk_scale<false>(p, o, n, c);
+    }
 }
 
-// elements per chunk: kMinChunk, doubled until the call has at most kTargetChunks of them (and one per tensor)
+// A wave's chunk: its values (loads of clamped addresses, so that none waits
+// for another), or c times them to their places.
+template <typename T>
+__device__ __forceinline__ void tiny_load(const T *__restrict__ p, i64 n, float (&v)[kTinyChunk / 64])
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < kTinyChunk / 64; ++j) v[j] = load_elem<T>(p, lane + 64 * j < n ? lane + 64 * j : 0);
+#pragma unroll
+    for (int j = 0; j < kTinyChunk / 64; ++j) v[j] = lane + 64 * j < n ? v[j] : 0.0f;
+}
+
+template <typename T>
+__device__ __forceinline__ void tiny_store(T *__restrict__ o, i64 n, float c, const float (&v)[kTinyChunk / 64])
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < kTinyChunk / 64; ++j)
+        if (lane + 64 * j < n) store_elem(o + lane + 64 * j, c * v[j]);
+}
+
+// The whole call in one workgroup: wave w takes chunks w, w + 16, ... of up to
+// kTinyChunk elements of one tensor, loaded once by single elements (any
+// alignment).
+struct Tiny {
+    int chunks;
+    struct {
+        const void *g;
+        void *out;
+        int32_t n, bf16;
+    } at[kTinyChunks];
+};
+
+__global__ __launch_bounds__(1024) void tiny_kernel(Tiny b, float C, float *__restrict__ norm, int32_t *status)
+{
+    __shared__ double red[16];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    float v[kTinyTurns][kTinyChunk / 64];
+#pragma unroll
+    for (int t = 0; t < kTinyTurns; ++t) {
+        const int k = wave + 16 * t;
+        if (k >= b.chunks) continue;
+        if (b.at[k].bf16) tiny_load((const uint16_t *)b.at[k].g, b.at[k].n, v[t]);
+        else tiny_load((const float *)b.at[k].g, b.at[k].n, v[t]);
+    }
+    double s = 0.0;
+#pragma unroll
+    for (int t = 0; t < kTinyTurns; ++t)
+        if (wave + 16 * t < b.chunks)
+#pragma unroll
+            for (int j = 0; j < kTinyChunk / 64; ++j) s = fma((double)v[t][j], (double)v[t][j], s);
+    const float x = (float)sqrt(block_sum64<1024>(s, red));
+    const float c = clip_factor(x, C);
+    if (threadIdx.x == 0) {
+        *norm = x;
+        if (!isfinite(x)) raise_flag(status, DP_FLAG_NONFINITE);
+    }
+#pragma unroll
+    for (int t = 0; t < kTinyTurns; ++t) {
+        const int k = wave + 16 * t;
+        if (k >= b.chunks || b.at[k].out == nullptr) continue;
+        if (b.at[k].bf16) tiny_store((uint16_t *)b.at[k].out, b.at[k].n, c, v[t]);
+        else tiny_store((float *)b.at[k].out, b.at[k].n, c, v[t]);
+    }
+}
+
+bool streamed(const dp_grad_tensor *items, int32_t count)
+{
+    i64 bytes = 0;
+    for (int32_t k = 0; k < count; ++k) bytes += items[k].numel * (i64)dtype_bytes((dp_dtype)items[k].dtype);
+    return bytes > kCachedBytes;
+}
+
+// Elements per chunk: doubled from kMinChunk up to a size for the workgroups'
+// loads (kMidChunk, kStreamChunk) while there are more than kFoldChunks of
+// them, and beyond it while there are more than kMostChunks (and one per
+// tensor).
 i64 chunk_size(const dp_grad_tensor *items, int32_t count)
 {
+    const int mid = streamed(items, count) ? kStreamChunk : kMidChunk;
     i64 chunk = kMinChunk;
     for (;; chunk *= 2) {
         i64 n = 0;
         for (int32_t k = 0; k < count; ++k) n += items[k].numel / chunk;
-        if (n <= kTargetChunks) return chunk;
+        if (n <= (chunk < mid ? (i64)kFoldChunks : kMostChunks)) return chunk;
     }
 }
 
@@ -322,38 +455,70 @@ extern "C" dp_status dp_clip_global_norm_many(const dp_grad_tensor *items, int32
     DPG_REQUIRE(ws != nullptr && aligned(ws, 16) && ws_bytes >= kHeader + sizeof(double) * (size_t)chunks, DP_EINVAL);
     float *factor = (float *)ws;
     double *sums = (double *)((char *)ws + kHeader);
+    const auto add = [](Batch &b, const dp_grad_tensor &x) {
+        const int j = b.count++;
+        b.g[j] = x.g;
+        b.out[j] = x.out;
+        b.numel[j] = 2 * x.numel + (x.dtype == DP_BF16 ? 1 : 0);
+        b.blk0[j + 1] = b.blk0[j] + (int)ceil_div(x.numel, b.chunk);
+    };
+    Batch b;
+    b.count = 0;
+    b.blk0[0] = 0;
+    b.chunk0 = 0;
     bool any_out = false;
-    for (int32_t k = 0; k < count; ++k) any_out |= items[k].out != nullptr && items[k].numel > 0;
-    const bool fold = any_out && chunks <= kFoldChunks;
-    for (int pass = 0; pass < 2; ++pass) {
-        if (pass == 1 && !fold) norm_kernel<<<1, 1024, 0, stream>>>(sums, chunks, C, factor, norm, status);
-        if (pass == 1 && !any_out) break;
-        int chunk0 = 0;
-        Batch b;
-        b.count = 0;
-        b.blk0[0] = 0;
-        b.chunks = chunks;
-        b.chunk = chunk;
-        for (int32_t k = 0; k <= count; ++k) {
-            if (b.count == kBatch || (k == count && b.count > 0)) {
-                b.chunk0 = chunk0;
-                const int blocks = b.blk0[b.count];
-                if (pass == 0) sumsq_kernel<<<(unsigned)blocks, kThreads, 0, stream>>>(b, sums);
-                else if (fold)
-                    scale_kernel<true><<<(unsigned)blocks, kThreads, 0, stream>>>(b, sums, factor, C, norm, status);
-                else scale_kernel<false><<<(unsigned)blocks, kThreads, 0, stream>>>(b, sums, factor, C, norm, status);
-                chunk0 += blocks;
-                b.count = 0;
+    i64 tiny = 0;
+    for (int32_t k = 0; k < count; ++k) {
+        any_out |= items[k].out != nullptr && items[k].numel > 0;
+        tiny += ceil_div(items[k].numel, kTinyChunk);
+    }
+    if (tiny <= kTinyChunks) {
+        Tiny t;
+        t.chunks = 0;
+        for (int32_t k = 0; k < count; ++k)
+            for (i64 first = 0; first < items[k].numel; first += kTinyChunk) {
+                const i64 left = items[k].numel - first, off = first * (i64)dtype_bytes((dp_dtype)items[k].dtype);
+                const int j = t.chunks++;
+                t.at[j].g = (const char *)items[k].g + off;
+                t.at[j].out = items[k].out != nullptr ? (char *)items[k].out + off : nullptr;
+                t.at[j].n = (int32_t)(left < kTinyChunk ? left : kTinyChunk);
+                t.at[j].bf16 = items[k].dtype == DP_BF16;
             }
-            if (k == count) break;
-            if (items[k].numel == 0) continue;
-            const int j = b.count++;
-            b.g[j] = items[k].g;
-            b.out[j] = items[k].out;
-            b.numel[j] = items[k].numel;
-            b.bf16[j] = items[k].dtype == DP_BF16;
-            b.blk0[j + 1] = b.blk0[j] + (int)ceil_div(items[k].numel, chunk);
+        tiny_kernel<<<1, 1024, 0, stream>>>(t, C, norm, status);
+        return launch_status();
+    }
+    b.chunks = chunks;
+    b.chunk = chunk;
+    b.stream = streamed(items, count);
+    const bool fold = any_out && chunks <= kFoldChunks;
+    // 1. over the tensors in order, in batches
+    for (int32_t k = 0; k <= count; ++k) {
+        if (b.count == kBatch || (k == count && b.count > 0)) {
+            sumsq_kernel<<<(unsigned)b.blk0[b.count], kThreads, 0, stream>>>(b, sums);
+            b.chunk0 += b.blk0[b.count];
+            b.count = 0;
         }
+        if (k < count && items[k].numel > 0) add(b, items[k]);
+    }
+    // 2.
+    if (!fold) norm_kernel<<<1, 1024, 0, stream>>>(sums, chunks, C, factor, norm, status);
+    if (!any_out) return launch_status();
+    // 3. over batches of the tensors from the last one back
+    int end = chunks;                     // chunks of the tensors not yet taken
+    for (int32_t hi = count; hi > 0;) {
+        int32_t lo = hi;
+        int n = 0;
+        while (lo > 0 && n < kBatch) n += items[--lo].numel > 0;
+        b.count = 0;
+        for (int32_t k = lo; k < hi; ++k)
+            if (items[k].numel > 0) add(b, items[k]);
+        hi = lo;
+        if (b.count == 0) continue;
+        end -= b.blk0[b.count];
+        b.chunk0 = end;
+        const unsigned blocks = (unsigned)b.blk0[b.count];
+        if (fold) scale_kernel<true><<<blocks, kThreads, 0, stream>>>(b, sums, factor, C, norm, status);
+        else scale_kernel<false><<<blocks, kThreads, 0, stream>>>(b, sums, factor, C, norm, status);
     }
     return launch_status();
 }
