@@ -174,7 +174,9 @@ struct Fill {
     i64 D;
 };
 
-__device__ __forceinline__ void fill_rows(const Fill &f, uint32_t w0, uint32_t nw)
+// (STREAM: stored past the caches)
+template <bool STREAM>
+__device__ __forceinline__ void fill_rows_as(const Fill &f, uint32_t w0, uint32_t nw)
 {
     const int lane = threadIdx.x & 63;
     const bool wide = f.D % 4 == 0 && (reinterpret_cast<uintptr_t>(f.sum) & 15) == 0;
@@ -185,12 +187,23 @@ __device__ __forceinline__ void fill_rows(const Fill &f, uint32_t w0, uint32_t n
             const int j = __ffs((int)empty) - 1;
             empty &= empty - 1;
             float *row = f.sum + (i64)(v0 + j) * f.D;
-            if (wide)
-                for (i64 c = 4 * lane; c < f.D; c += 256) *reinterpret_cast<float4 *>(row + c) = make_float4(0, 0, 0, 0);
-            else
+            if (wide) {
+                for (i64 c = 4 * lane; c < f.D; c += 256) {
+                    if constexpr (STREAM) store_stream4(row + c, 0.0f, 0.0f, 0.0f, 0.0f);
+                    else *reinterpret_cast<float4 *>(row + c) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
+            } else {
                 for (i64 c = lane; c < f.D; c += 64) row[c] = 0.0f;
+            }
         }
     }
+}
+
+// tables large enough for the flags are larger than the caches
+__device__ __forceinline__ void fill_rows(const Fill &f, uint32_t w0, uint32_t nw)
+{
+    if (f.present != nullptr) fill_rows_as<true>(f, w0, nw);
+    else fill_rows_as<false>(f, w0, nw);
 }
 
 // hist[d][tile] = the tile's keys of digit d.  FIRST: the keys are formed
@@ -338,8 +351,9 @@ struct alignas(VEC >= 4 ? 16 : 4 * VEC) Out {
 __device__ __forceinline__ float as_f32(float x) { return x; }
 __device__ __forceinline__ float as_f32(uint16_t x) { return bf16_to_f32(x); }
 
-// Workgroups below walk_blocks add rows; the others write zeros.
-template <typename T, int VEC>
+// Workgroups below walk_blocks add rows; the others write zeros.  STREAM: B and
+// the sums pass by the caches (65536 x 2048 of 50000: the call 189 us, 181 so).
+template <typename T, int VEC, bool STREAM>
 __global__ __launch_bounds__(kWalkThreads) void walk_kernel(
     const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos, const T *__restrict__ B, uint32_t M,
     uint32_t Tn, uint32_t V, i64 D, float scale, const float *__restrict__ norm, float C, uint32_t chunk,
@@ -367,7 +381,13 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(
         Out<VEC> o;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) o.v[i] = f * acc[i];
-        if (on) *reinterpret_cast<Out<VEC> *>(dst + col) = o;
+        if (!on) return;
+        if constexpr (STREAM && VEC >= 4) {
+#pragma unroll
+            for (int i = 0; i < VEC; i += 4) store_stream4(dst + col + i, o.v[i], o.v[i + 1], o.v[i + 2], o.v[i + 3]);
+        } else {
+            *reinterpret_cast<Out<VEC> *>(dst + col) = o;
+        }
     };
     bool open = false;                                       // the last position's id continues in the next chunk
     for (uint32_t q0 = lo; q0 < hi; q0 += 64) {
@@ -385,7 +405,13 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {               // past the end: position 0's row again, not added
                 const uint32_t pj = __builtin_amdgcn_readlane(p, b + j);
-                v[j] = *reinterpret_cast<const Row<T, VEC> *>(Bc + (i64)pj * D);
+                const Row<T, VEC> *row = reinterpret_cast<const Row<T, VEC> *>(Bc + (i64)pj * D);
+                if constexpr (STREAM && sizeof(*row) == 16) {
+                    typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+                    v[j] = __builtin_bit_cast(Row<T, VEC>, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(row)));
+                } else {
+                    v[j] = *row;
+                }
             }
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
@@ -795,9 +821,14 @@ void sums(const Plan &p, const void *B, i64 T_, i64 V, i64 D, float scale, const
     float *part = (float *)(ws + p.part);
     const uint32_t walk_blocks = (uint32_t)ceil_div(p.chunks * p.colblocks, kWalkWaves);
     const uint32_t blocks = walk_blocks + fill_blocks(fills.walk, kWalkWaves);
-    walk_kernel<T, VEC><<<blocks, kWalkThreads, 0, stream>>>(
-        keys, pos, (const T *)B, (uint32_t)p.M, (uint32_t)T_, (uint32_t)V, D, scale, norm, C, (uint32_t)p.chunk,
-        (uint32_t)p.chunks, (uint32_t)p.colblocks, walk_blocks, sum, part, fills.walk);
+    const auto walk = [&](auto kernel) {
+        kernel<<<blocks, kWalkThreads, 0, stream>>>(keys, pos, (const T *)B, (uint32_t)p.M, (uint32_t)T_, (uint32_t)V, D,
+                                                    scale, norm, C, (uint32_t)p.chunk, (uint32_t)p.chunks,
+                                                    (uint32_t)p.colblocks, walk_blocks, sum, part, fills.walk);
+    };
+    constexpr bool WIDE = sizeof(T) * VEC == 16;
+    if (WIDE && fills.flags) walk(walk_kernel<T, VEC, WIDE>);
+    else walk(walk_kernel<T, VEC, false>);
     if (p.chunks > 1) {
         const uint32_t fb = fill_blocks(fills.join, kWalkWaves);
         join_kernel<VEC><<<(unsigned)((p.chunks - 1) * p.colblocks) + fb, kWalkThreads, 0, stream>>>(

@@ -61,6 +61,21 @@ def test_lookup(N, T, V, D, te, ty, shift):
     assert (buf[:shift] == 7).all() and (buf[shift + N * T * D:] == 7).all()       # nothing beside the output
 
 
+@pytest.mark.parametrize("te,ty", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
+def test_lookup_large_output(te, ty):
+    """Outputs stored past the caches."""
+    say("lookup large", te, ty)
+    (tt, ct), (yt, cy) = DT[te], DT[ty]
+    N, T, V, D = 7, 3700, 900, 2056
+    g = torch.Generator(device=DEV).manual_seed(3)
+    E = torch.randn((V, D), generator=g, device=DEV).to(tt)
+    ids = torch.randint(0, V, (N, T), generator=g, device=DEV)
+    Y = torch.full((N, T, D), 7.0, dtype=yt, device=DEV)
+    assert Y.numel() * Y.element_size() > 96 << 20
+    dp.dp_embedding_lookup(ids, E, ct, N, T, V, D, 1.5, Y, cy)
+    assert torch.equal(Y, (E.float() * 1.5).to(yt)[ids])               # one product, one rounding: the same bits
+
+
 def test_lookup_bad_ids_and_empty():
     say("lookup bad ids")
     V, D = 6, 40
@@ -157,6 +172,29 @@ def test_tokens_large_vocabulary(M):
     R.within(got[torch.from_numpy(uniq).to(DEV)], want, bound)
     got[torch.from_numpy(uniq).to(DEV)] = 0.0
     assert (got == 0).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 520])
+def test_tokens_large_table(dt, D):
+    """A table over 128 MB: only rows without a token are zeroed, by their flags."""
+    say("tokens large table", dt, D)
+    rng = np.random.default_rng(D)
+    tt, ct = DT[dt]
+    M, V = 20000, 40_000_000 // D
+    assert 4 * V * D > 128 << 20
+    ids = token_ids(rng, "skewed", 4, M // 4, V)
+    ids[1] = rng.integers(0, V, M // 4)
+    ids[2, :100] = -1                                                              # left out: no row of their own
+    B = torch.from_numpy(rng.standard_normal((4, M // 4, D))).to(tt)
+    st = status()
+    got = run_tokens(torch.from_numpy(ids).to(DEV), B.to(DEV), ct, V, 1.0, None, 1.0, st=st)
+    uniq, at = np.unique(ids, return_inverse=True)
+    want, bound = R.tokens(at.reshape(ids.shape) - 1, R.f64(B), len(uniq) - 1, 1.0, None, 1.0)
+    rows = torch.from_numpy(uniq[1:]).to(DEV)
+    R.within(got[rows], want, bound)
+    got[rows] = 0.0
+    assert (got == 0).all() and st.item() == dp.DP_FLAG_BAD_INDEX
 
 
 @pytest.mark.parametrize("T", [9, 700, 5000])
