@@ -25,12 +25,19 @@ namespace {
 using namespace bf16s;
 using namespace ffn;
 
-// lane l's 16 bytes at base + off go to LDS byte lds + 16 l (see dma16)
+// lane l's 16 bytes at base + off go to LDS byte lds + 16 l (see dma16); STREAM:
+// past the caches
+template <bool STREAM = false>
 __device__ __forceinline__ void dma16_off(const void *base, uint32_t off, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base),
-                 "s"(__builtin_amdgcn_readfirstlane(lds))
-                 : "memory", "m0");
+    if constexpr (STREAM)
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base),
+                     "s"(__builtin_amdgcn_readfirstlane(lds))
+                     : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base),
+                     "s"(__builtin_amdgcn_readfirstlane(lds))
+                     : "memory", "m0");
 }
 
 // wait until all but the last `later` (at most 2) stages' loads have landed, N loads each
@@ -397,7 +404,8 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
             dma16_off(a, cut && 8 * q[r] >= tail ? offA[r] - 16u * q[r] : offA[r], L + 1024 * (wave + S::WAVES * r));
 #pragma unroll
         for (int r = 0; r < S::W_LOADS; ++r)
-            dma16_off(w, cut && kr[r] >= tail ? offW[r] - (uint32_t)kr[r] * (uint32_t)(2 * ldw) : offW[r],
+            // (one row of tiles reads each weight once)
+            dma16_off<(S::BM <= 64)>(w, cut && kr[r] >= tail ? offW[r] - (uint32_t)kr[r] * (uint32_t)(2 * ldw) : offW[r],
                       L + S::A_BYTES + 1024 * (wave + S::WAVES * r));
     };
     // features past the end read the stage's first ones, and are zeroed in LDS on both sides

@@ -206,18 +206,22 @@ void by_act(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, 
 // which feed four products with the same column index j, and features are
 // dealt to the k index so that a lane's share of BG is 16 consecutive bytes.
 // The waves' sums are added in LDS in wave order, the workgroups' from the
-// workspace in order.
+// workspace in order.  Weights are read once, past the caches (one row, 11008 ->
+// 4096: the call 86 us, 82 so, 360 MB; 11008 -> 4096 bf16 in the tiles of
+// ffn_bf16.hip likewise 41 and 37 us).
 // ---------------------------------------------------------------------------
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kDxCols = 128, kDxWaves = 4, kDxGroup = 8;
 
-// four consecutive values of the row at p from index k on, zeros from `end` on
-template <bool VEC>
+// four consecutive values of the row at p from index k on, zeros from `end`
+// on; STREAM: past the caches
+template <bool VEC, bool STREAM = false>
 __device__ __forceinline__ float4 load4(const float *p, i64 k, i64 end)
 {
     if constexpr (VEC) {                  // end is a multiple of 4, p 16-byte aligned
-        const float4 v = *reinterpret_cast<const float4 *>(p + (k < end ? k : 0));
+        const float *q = p + (k < end ? k : 0);
+        const float4 v = STREAM ? load_stream4(q) : *reinterpret_cast<const float4 *>(q);
         return k < end ? v : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     } else {
         return make_float4(k < end ? p[k] : 0.0f, k + 1 < end ? p[k + 1] : 0.0f, k + 2 < end ? p[k + 2] : 0.0f,
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(64 * kDxWaves) void ffn_dx_rows_kernel(const float 
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const bool in = f + s < end;
-                const float4 v = load4<VEC>(W + (in ? f + s : 0) * D, d, D);
+                const float4 v = load4<VEC, true>(W + (in ? f + s : 0) * D, d, D);
                 w[n][s] = in ? v : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
 #pragma unroll
