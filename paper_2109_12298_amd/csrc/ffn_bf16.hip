@@ -17,7 +17,7 @@
 #include "ffn_bf16.hpp"
 
 #include "bf16_stage.hpp"
-#include "gated_ffn.hpp"
+#include "ffn_any.hpp"
 
 namespace dpg {
 namespace {
@@ -91,24 +91,22 @@ template <typename T, int COLS, int LDT>
 __device__ __forceinline__ void store_rows(const char *L, T *__restrict__ O, i64 rows, i64 cols, i64 r0, i64 c0, bool vec,
                                            int lane)
 {
-    constexpr int N = 16 / sizeof(T), LPR = COLS / N, RPS = 64 / LPR;        // values per piece, lanes per row, rows per store
+    if (vec) {                            // 16-byte pieces
+        constexpr int N = 16 / sizeof(T), LPR = COLS / N, RPS = 64 / LPR;    // values per piece, lanes per row, rows per store
 #pragma unroll
-    for (int s = 0; s < 32 / RPS; ++s) {
-        const int row = s * RPS + lane / LPR, c = lane % LPR;
-        const uint4 v = *reinterpret_cast<const uint4 *>(L + row * LDT + 16 * c);
-        const i64 r = r0 + row, f = c0 + N * c;
-        if (r >= rows) continue;
-        T *o = O + r * cols + f;
-        if (vec) {
-            if (f < cols) *reinterpret_cast<uint4 *>(o) = v;
-        } else {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (f + j < cols) {
-                    if constexpr (sizeof(T) == 4) o[j] = __uint_as_float(w[j]);
-                    else o[j] = (T)(w[j >> 1] >> (16 * (j & 1)));
-                }
+        for (int s = 0; s < 32 / RPS; ++s) {
+            const int row = s * RPS + lane / LPR, c = lane % LPR;
+            const uint4 v = *reinterpret_cast<const uint4 *>(L + row * LDT + 16 * c);
+            const i64 r = r0 + row, f = c0 + N * c;
+            if (r < rows && f < cols) *reinterpret_cast<uint4 *>(O + r * cols + f) = v;
+        }
+    } else {                              // rows of any alignment: 64 consecutive values per store
+#pragma unroll 8
+        for (int s = 0; s < 32 * COLS / 64; ++s) {
+            const int row = (64 * s + lane) / COLS, c = (64 * s + lane) % COLS;
+            const T v = *reinterpret_cast<const T *>(L + row * LDT + (int)sizeof(T) * c);
+            const i64 r = r0 + row, f = c0 + c;
+            if (r < rows && f < cols) O[r * cols + f] = v;
         }
     }
 }
@@ -136,23 +134,49 @@ constexpr uint32_t X_PART = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
 constexpr uint32_t W_PART = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
 constexpr int kParts = 6;
 
+// What the kernels of an fp32 call need besides the parts: the values
+// themselves (K features in a row), and a word per workgroup of the splitting
+// kernel that is not 0 where it met a value without parts.
+struct Whole {
+    const float *a, *b, *wg, *wu;         // X (b unused), or BG and BU
+    i64 K;
+    const int32_t *flags;
+    int count;
+};
+
+// whether any of the words is set, in every thread of the workgroup
+__device__ __forceinline__ bool any_flag(const Whole &w)
+{
+    int bad = 0;
+    for (int i = threadIdx.x; i < w.count; i += blockDim.x) bad |= w.flags[i];
+    return __syncthreads_or(bad) != 0;
+}
+
 // T = float: X, Wg and Wu are the three parts of each ([3][rows][K], K a
-// multiple of BK), and *flag != 0 leaves the call to another kernel.
+// multiple of BK).
 template <typename S, int ACT, typename T>
 __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16_t *__restrict__ X,
                                                                     const uint16_t *__restrict__ Wg,
                                                                     const uint16_t *__restrict__ Wu, i64 M, i64 K, i64 F,
                                                                     int tiles_m, int tiles_f, T *__restrict__ H,
                                                                     T *__restrict__ G, T *__restrict__ U, int vec,
-                                                                    const int32_t *__restrict__ flag)
+                                                                    Whole whole)
 {
     constexpr bool PARTS = sizeof(T) == 4;
     constexpr int FM = S::FM, FF = S::FF, BK = S::BK, NS = S::NS, ROW = S::ROW, KS = BK / 16;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
-    if (PARTS && *flag != 0) return;
     int tm, tf;
     tile_of((int)blockIdx.x, (int)gridDim.x, tiles_m, tiles_f, tm, tf);
     const i64 m0 = (i64)tm * S::BM, f0 = (i64)tf * S::BF;
+    if constexpr (PARTS) {
+        if (any_flag(whole)) {
+            for (int t = 0; t < (S::BM / kTM) * (S::BF / kTN); ++t)
+                any_forward_tile<S::THREADS, ACT>(whole.a, whole.wg, whole.wu, M, whole.K, F,
+                                                  m0 + t / (S::BF / kTN) * kTM, f0 + t % (S::BF / kTN) * kTN, H, G, U,
+                                                  reinterpret_cast<float *>(smem));
+            return;
+        }
+    }
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WF * (FM * 32), wf = wave % S::WF * (FF * 32);
@@ -309,17 +333,17 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16
 
 template <typename S, typename T>
 void launch_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act, T *H,
-                    T *G, T *U, const int32_t *flag, hipStream_t stream)
+                    T *G, T *U, const Whole &whole, hipStream_t stream)
 {
     const int tm = (int)ceil_div(M, S::BM), tf = (int)ceil_div(F, S::BF);
     const int vec = F * sizeof(T) % 16 == 0 && aligned(H, 16) && aligned(G, 16) && aligned(U, 16);
     const unsigned grid = (unsigned)((i64)tm * tf);
     if (act == DP_ACT_SILU)
         ffn_forward_kernel<S, DP_ACT_SILU, T><<<grid, S::THREADS, 0, stream>>>(X, Wg, Wu, M, K, F, tm, tf, H, G, U, vec,
-                                                                               flag);
+                                                                               whole);
     else
         ffn_forward_kernel<S, DP_ACT_GELU_TANH, T><<<grid, S::THREADS, 0, stream>>>(X, Wg, Wu, M, K, F, tm, tf, H, G, U,
-                                                                                    vec, flag);
+                                                                                    vec, whole);
 }
 
 // ---------------------------------------------------------------------------
@@ -344,8 +368,7 @@ struct DxShape {
 };
 
 // T = float: BG and Wg point to the parts of both products ([2][3][M][lda] and
-// [2][3][F][ldw], F = lda a multiple of BK), BU and Wu are not used, and
-// *flag != 0 leaves the call to another kernel.
+// [2][3][F][ldw], F = lda a multiple of BK), BU and Wu are not used.
 template <typename S, bool SPLIT, typename T>
 __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *__restrict__ BG,
                                                                const uint16_t *__restrict__ BU,
@@ -353,17 +376,26 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
                                                                const uint16_t *__restrict__ Wu, i64 M, i64 D, i64 F,
                                                                i64 lda, i64 ldw, int tiles_m, int tiles_d, int splits,
                                                                T *__restrict__ dX, float *__restrict__ part, int vec,
-                                                               const int32_t *__restrict__ flag)
+                                                               Whole whole)
 {
     constexpr bool PARTS = sizeof(T) == 4;
     constexpr int RUNS = PARTS ? 2 * kParts : 2;             // products that the stages run through
     constexpr int FM = S::FM, FD = S::FD, BK = S::BK, NS = S::NS, KS = BK / 16;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
-    if (PARTS && *flag != 0) return;
     int tm, td;
     const int tiles = tiles_m * tiles_d, split = SPLIT ? (int)blockIdx.x / tiles : 0;
     tile_of((int)blockIdx.x - split * tiles, tiles, tiles_m, tiles_d, tm, td);
     const i64 m0 = (i64)tm * S::BM, d0 = (i64)td * S::BD;
+    if constexpr (PARTS) {
+        if (any_flag(whole)) {
+            if (split == 0)
+                for (int t = 0; t < (S::BM / kTM) * (S::BD / kTN); ++t)
+                    any_dx_tile<S::THREADS>(whole.a, whole.b, whole.wg, whole.wu, M, D, whole.K,
+                                            m0 + t / (S::BD / kTN) * kTM, d0 + t % (S::BD / kTN) * kTN, dX,
+                                            reinterpret_cast<float *>(smem));
+            return;
+        }
+    }
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / S::WD * (FM * 32), wd = wave % S::WD * (FD * 32);
@@ -528,10 +560,9 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
 // dX = the splits' partial sums, in split order; rows of ld (a multiple of 4) there, of D here
 template <typename T>
 __global__ __launch_bounds__(256) void ffn_dx_sum_kernel(const float *__restrict__ part, i64 M, i64 D, i64 ld,
-                                                         int splits, T *__restrict__ dX,
-                                                         const int32_t *__restrict__ flag)
+                                                         int splits, T *__restrict__ dX, Whole whole)
 {
-    if (flag != nullptr && *flag != 0) return;
+    if (sizeof(T) == 4 && any_flag(whole)) return;           // dX is there already
     const i64 n = M * ld;
     for (i64 i = ((i64)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (i64)gridDim.x * 1024) {
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -563,54 +594,76 @@ typedef DxShape<32, 128, 1, 4, 64, 3> Rows32Dx;
 
 template <typename S, typename T>
 void launch_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
-               i64 lda, i64 ldw, int splits, T *dX, float *part, const int32_t *flag, hipStream_t stream)
+               i64 lda, i64 ldw, int splits, T *dX, float *part, const Whole &whole, hipStream_t stream)
 {
     const int tm = (int)ceil_div(M, S::BM), td = (int)ceil_div(D, S::BD);
     const int vec = D * sizeof(T) % 16 == 0 && aligned(dX, 16);
     const unsigned grid = (unsigned)((i64)tm * td * splits);
     if (splits == 1) {
         ffn_dx_kernel<S, false, T><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, lda, ldw, tm, td, 1, dX,
-                                                                    nullptr, vec, flag);
+                                                                    nullptr, vec, whole);
         return;
     }
     ffn_dx_kernel<S, true, T><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, lda, ldw, tm, td, splits, dX,
-                                                               part, vec, flag);
+                                                               part, vec, whole);
     const i64 blocks = ceil_div(M * ldw, 1024);
     ffn_dx_sum_kernel<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(part, M, D, ldw, splits, dX,
-                                                                                        flag);
-}
-
-// [rows][cols] into rows of ld > cols, zeros behind (16 bytes of the result per thread)
-__global__ __launch_bounds__(256) void ffn_pad_kernel(const uint16_t *__restrict__ P, i64 rows, i64 cols, i64 ld,
-                                                      uint16_t *__restrict__ O)
-{
-    const i64 per = ld / 8, n = rows * per;
-    for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < n; i += (i64)gridDim.x * 256) {
-        const i64 r = i / per, c = (i - r * per) * 8;
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t a = c + 2 * j < cols ? P[r * cols + c + 2 * j] : 0;
-            const uint32_t b = c + 2 * j + 1 < cols ? P[r * cols + c + 2 * j + 1] : 0;
-            w[j] = a | (b << 16);
-        }
-        *reinterpret_cast<uint4 *>(O + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+                                                                                        whole);
 }
 
 i64 padded(i64 cols) { return (cols + 7) / 8 * 8; }
 
-size_t pad_bytes(i64 rows, i64 cols) { return cols % 8 == 0 ? 0 : align_up(sizeof(uint16_t) * (size_t)(rows * padded(cols)), 256); }
+size_t pad_bytes(i64 rows, i64 cols)
+{
+    return cols % 8 == 0 ? 0 : align_up(sizeof(uint16_t) * (size_t)(rows * padded(cols)), 256);
+}
 
-// P itself, or its rows padded to 16 bytes in the workspace at ws, which is moved on
-const uint16_t *pad_rows(const uint16_t *P, i64 rows, i64 cols, char *&ws, hipStream_t stream)
+// Arrays whose rows are padded to 16 bytes: [rows][cols] into rows of
+// padded(cols), zeros behind.  One launch for all of a call's (pieces of eight
+// values, first[k] the first of array k).
+struct Pads {
+    int count;
+    const uint16_t *P[4];
+    uint16_t *O[4];
+    i64 cols[4], first[5];
+};
+
+__global__ __launch_bounds__(256) void ffn_pad_kernel(Pads s)
+{
+    for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < s.first[s.count]; i += (i64)gridDim.x * 256) {
+        int k = 0;
+        while (k + 1 < s.count && i >= s.first[k + 1]) ++k;
+        const i64 cols = s.cols[k], per = (cols + 7) / 8, j = i - s.first[k], r = j / per, c = (j - r * per) * 8;
+        const uint16_t *p = s.P[k] + r * cols + c;
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t a = c + 2 * q < cols ? p[2 * q] : 0, b = c + 2 * q + 1 < cols ? p[2 * q + 1] : 0;
+            w[q] = a | (b << 16);
+        }
+        *reinterpret_cast<uint4 *>(s.O[k] + 8 * j) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// Adds P to the arrays to pad, if its rows need it; returns where its rows are
+// then (in the workspace at ws, which is moved on, or in P itself).
+const uint16_t *pad_rows(Pads &s, const uint16_t *P, i64 rows, i64 cols, char *&ws)
 {
     if (cols % 8 == 0) return P;
-    uint16_t *O = (uint16_t *)ws;
+    const int k = s.count++;
+    s.P[k] = P;
+    s.O[k] = (uint16_t *)ws;
+    s.cols[k] = cols;
+    s.first[k + 1] = s.first[k] + rows * (padded(cols) / 8);
     ws += pad_bytes(rows, cols);
-    const i64 blocks = ceil_div(rows * padded(cols) / 8, 256);
-    ffn_pad_kernel<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, stream>>>(P, rows, cols, padded(cols), O);
-    return O;
+    return s.O[k];
+}
+
+void pad(const Pads &s, hipStream_t stream)
+{
+    if (s.count == 0) return;
+    const i64 blocks = ceil_div(s.first[s.count], 256);
+    ffn_pad_kernel<<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, stream>>>(s);
 }
 
 enum { kRows32, kRows64, kMid, kLarge };
@@ -674,13 +727,13 @@ int forward_tiles(i64 M, i64 F)
 
 template <typename T>
 void forward_by_tiles(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, dp_act act, T *H,
-                      T *G, T *U, const int32_t *flag, hipStream_t stream)
+                      T *G, T *U, const Whole &whole, hipStream_t stream)
 {
     const int tiles = forward_tiles(M, F);
-    if (tiles == kTilesLarge) launch_forward<Large, T>(X, Wg, Wu, M, K, F, act, H, G, U, flag, stream);
-    else if (tiles == kTilesMid) launch_forward<Mid, T>(X, Wg, Wu, M, K, F, act, H, G, U, flag, stream);
-    else if (tiles == kTilesDeep) launch_forward<Deep, T>(X, Wg, Wu, M, K, F, act, H, G, U, flag, stream);
-    else if constexpr (sizeof(T) == 2) launch_forward<Rows64, T>(X, Wg, Wu, M, K, F, act, H, G, U, flag, stream);
+    if (tiles == kTilesLarge) launch_forward<Large, T>(X, Wg, Wu, M, K, F, act, H, G, U, whole, stream);
+    else if (tiles == kTilesMid) launch_forward<Mid, T>(X, Wg, Wu, M, K, F, act, H, G, U, whole, stream);
+    else if (tiles == kTilesDeep) launch_forward<Deep, T>(X, Wg, Wu, M, K, F, act, H, G, U, whole, stream);
+    else if constexpr (sizeof(T) == 2) launch_forward<Rows64, T>(X, Wg, Wu, M, K, F, act, H, G, U, whole, stream);
 }
 
 }  // namespace
@@ -691,11 +744,13 @@ void ffn_bf16_forward(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu,
                       uint16_t *H, uint16_t *G, uint16_t *U, void *ws, hipStream_t stream)
 {
     char *w = (char *)ws;
-    X = pad_rows(X, M, K, w, stream);
-    Wg = pad_rows(Wg, F, K, w, stream);
-    Wu = pad_rows(Wu, F, K, w, stream);
+    Pads s = {};
+    X = pad_rows(s, X, M, K, w);
+    Wg = pad_rows(s, Wg, F, K, w);
+    Wu = pad_rows(s, Wu, F, K, w);
+    pad(s, stream);
     K = padded(K);
-    forward_by_tiles<uint16_t>(X, Wg, Wu, M, K, F, act, H, G, U, nullptr, stream);
+    forward_by_tiles<uint16_t>(X, Wg, Wu, M, K, F, act, H, G, U, Whole{}, stream);
 }
 
 size_t ffn_bf16_dx_workspace(i64 M, i64 D, i64 F)
@@ -710,16 +765,18 @@ void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, con
 {
     const DxPlan p = dx_plan(M, D, F, 2);
     char *w = (char *)ws;
-    BG = pad_rows(BG, M, F, w, stream);
-    BU = pad_rows(BU, M, F, w, stream);
-    Wg = pad_rows(Wg, F, D, w, stream);
-    Wu = pad_rows(Wu, F, D, w, stream);
+    Pads s = {};
+    BG = pad_rows(s, BG, M, F, w);
+    BU = pad_rows(s, BU, M, F, w);
+    Wg = pad_rows(s, Wg, F, D, w);
+    Wu = pad_rows(s, Wu, F, D, w);
+    pad(s, stream);
     const i64 lda = padded(F), ldw = padded(D);
     float *part = (float *)w;
-    if (p.shape == kLarge) launch_dx<LargeDx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, nullptr, stream);
-    else if (p.shape == kMid) launch_dx<MidDx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, nullptr, stream);
-    else if (p.shape == kRows64) launch_dx<Rows64Dx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, nullptr, stream);
-    else launch_dx<Rows32Dx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, nullptr, stream);
+    if (p.shape == kLarge) launch_dx<LargeDx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, Whole{}, stream);
+    else if (p.shape == kMid) launch_dx<MidDx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, Whole{}, stream);
+    else if (p.shape == kRows64) launch_dx<Rows64Dx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, Whole{}, stream);
+    else launch_dx<Rows32Dx, uint16_t>(BG, BU, Wg, Wu, M, D, F, lda, ldw, p.splits, dX, part, Whole{}, stream);
 }
 
 // ---------------------------------------------------------------------------
@@ -745,95 +802,102 @@ __device__ __forceinline__ bool split3(float x, uint32_t (&p)[3])
     return x != 0.0f && (e >= 254u || e < 27u);
 }
 
-// The parts of P [rows][cols] as [3][rows_out][ld], zeros past rows and cols;
-// *flag is set where a value cannot be split.
-__device__ __forceinline__ bool split_rows(const float *__restrict__ P, i64 rows, i64 cols, i64 rows_out, i64 ld,
-                                           uint16_t *__restrict__ O, i64 first, i64 step)
+// Arrays to split: P [rows][cols] as O [3][rows_out][ld], zeros past rows and
+// cols.  One launch for all of a call's (pieces of eight values, first[k] the
+// first of array k), of at most kSplitBlocks workgroups, each leaving a word
+// that says whether it met a value that cannot be split.
+constexpr int kSplitBlocks = 1024;
+
+struct Splits {
+    int count;
+    const float *P[4];
+    uint16_t *O[4];
+    i64 rows[4], cols[4], ld[4], plane[4], first[5];
+};
+
+__global__ __launch_bounds__(256) void ffn_split_kernel(Splits s, int32_t *__restrict__ flags)
 {
-    const i64 per = ld / 8, n = rows_out * per;
-    const bool wide = cols % 4 == 0 && (reinterpret_cast<uintptr_t>(P) & 15) == 0;
     bool bad = false;
-    for (i64 i = first; i < n; i += step) {
-        const i64 r = i / per, c = (i - r * per) * 8;
+    for (i64 i = (i64)blockIdx.x * 256 + threadIdx.x; i < s.first[s.count]; i += (i64)gridDim.x * 256) {
+        int k = 0;
+        while (k + 1 < s.count && i >= s.first[k + 1]) ++k;
+        const i64 rows = s.rows[k], cols = s.cols[k], per = s.ld[k] / 8;
+        const i64 j = i - s.first[k], r = j / per, c = (j - r * per) * 8;
+        const float *p = s.P[k] + r * cols + c;
         float x[8];
-        if (wide) {
+        if (cols % 4 == 0 && (reinterpret_cast<uintptr_t>(s.P[k]) & 15) == 0) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const bool in = r < rows && c + 4 * h < cols;
-                const float4 v = in ? *reinterpret_cast<const float4 *>(P + r * cols + c + 4 * h)
-                                    : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                const float4 v = in ? *reinterpret_cast<const float4 *>(p + 4 * h) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = r < rows && c + j < cols ? P[r * cols + c + j] : 0.0f;
+            for (int q = 0; q < 8; ++q) x[q] = r < rows && c + q < cols ? p[q] : 0.0f;
         }
         uint32_t w[3][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int q = 0; q < 4; ++q) {
             uint32_t a[3], b[3];
-            bad |= split3(x[2 * j], a);
-            bad |= split3(x[2 * j + 1], b);
+            bad |= split3(x[2 * q], a);
+            bad |= split3(x[2 * q + 1], b);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) w[k][j] = a[k] | (b[k] << 16);
+            for (int n = 0; n < 3; ++n) w[n][q] = a[n] | (b[n] << 16);
         }
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
-            *reinterpret_cast<uint4 *>(O + (i64)k * rows_out * ld + 8 * i) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+        for (int n = 0; n < 3; ++n)
+            *reinterpret_cast<uint4 *>(s.O[k] + n * s.plane[k] + 8 * j) = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
     }
-    return bad;
+    const int any = __syncthreads_or(bad);
+    if (threadIdx.x == 0) flags[blockIdx.x] = any;
 }
 
-struct SplitItem {
-    const float *P;
-    i64 rows, cols, rows_out, ld;
-    uint16_t *O;
-};
+constexpr size_t kFlagBytes = sizeof(int32_t) * kSplitBlocks;
 
-struct SplitItems {
-    SplitItem it[4];
-};
-
-// blockIdx.y: the array
-__global__ __launch_bounds__(256) void ffn_split_kernel(SplitItems s, int32_t *__restrict__ flag)
+void add_split(Splits &s, const float *P, i64 rows, i64 cols, i64 rows_out, i64 ld, uint16_t *O)
 {
-    const SplitItem it = s.it[blockIdx.y];
-    if (split_rows(it.P, it.rows, it.cols, it.rows_out, it.ld, it.O, (i64)blockIdx.x * 256 + threadIdx.x,
-                   (i64)gridDim.x * 256))
-        atomicOr(flag, 1);
+    const int k = s.count++;
+    s.P[k] = P;
+    s.O[k] = O;
+    s.rows[k] = rows;
+    s.cols[k] = cols;
+    s.ld[k] = ld;
+    s.plane[k] = rows_out * ld;
+    s.first[k + 1] = s.first[k] + rows_out * (ld / 8);
+}
+
+// Splits the arrays; returns how many words were left at flags.
+int split(const Splits &s, int32_t *flags, hipStream_t stream)
+{
+    const i64 blocks = ceil_div(s.first[s.count], 256);
+    const int n = (int)(blocks < kSplitBlocks ? blocks : kSplitBlocks);
+    ffn_split_kernel<<<(unsigned)n, 256, 0, stream>>>(s, flags);
+    return n;
 }
 
 size_t part_bytes(i64 rows, i64 ld) { return align_up(3 * sizeof(uint16_t) * (size_t)(rows * ld), 256); }
-
-void split(const SplitItems &s, int count, int32_t *flag, hipStream_t stream)
-{
-    zero_fill((float *)flag, 1, stream);
-    i64 most = 0;
-    for (int k = 0; k < count; ++k) {
-        const i64 n = s.it[k].rows_out * s.it[k].ld / 8;
-        most = n > most ? n : most;
-    }
-    const i64 blocks = ceil_div(most, 256);
-    ffn_split_kernel<<<dim3((unsigned)(blocks < 2048 ? blocks : 2048), (unsigned)count), 256, 0, stream>>>(s, flag);
-}
 
 }  // namespace
 
 size_t ffn_parts_forward_workspace(i64 M, i64 K, i64 F)
 {
-    return 256 + part_bytes(M, whole(K)) + 2 * part_bytes(F, whole(K));
+    return kFlagBytes + part_bytes(M, whole(K)) + 2 * part_bytes(F, whole(K));
 }
 
-const int32_t *ffn_parts_forward(const float *X, const float *Wg, const float *Wu, i64 M, i64 K, i64 F, dp_act act,
-                                 float *H, float *G, float *U, void *ws, hipStream_t stream)
+void ffn_parts_forward(const float *X, const float *Wg, const float *Wu, i64 M, i64 K, i64 F, dp_act act, float *H,
+                       float *G, float *U, void *ws, hipStream_t stream)
 {
     const i64 ld = whole(K);
-    int32_t *flag = (int32_t *)ws;
-    uint16_t *x = (uint16_t *)((char *)ws + 256);
+    int32_t *flags = (int32_t *)ws;
+    uint16_t *x = (uint16_t *)((char *)ws + kFlagBytes);
     uint16_t *g = (uint16_t *)((char *)x + part_bytes(M, ld)), *u = (uint16_t *)((char *)g + part_bytes(F, ld));
-    split({{{X, M, K, M, ld, x}, {Wg, F, K, F, ld, g}, {Wu, F, K, F, ld, u}, {}}}, 3, flag, stream);
-    forward_by_tiles<float>(x, g, u, M, ld, F, act, H, G, U, flag, stream);
-    return flag;
+    Splits s = {};
+    add_split(s, X, M, K, M, ld, x);
+    add_split(s, Wg, F, K, F, ld, g);
+    add_split(s, Wu, F, K, F, ld, u);
+    const int n = split(s, flags, stream);
+    forward_by_tiles<float>(x, g, u, M, ld, F, act, H, G, U, Whole{X, nullptr, Wg, Wu, K, flags, n}, stream);
 }
 
 size_t ffn_parts_dx_workspace(i64 M, i64 D, i64 F)
@@ -841,25 +905,28 @@ size_t ffn_parts_dx_workspace(i64 M, i64 D, i64 F)
     const DxPlan p = dx_plan(M, D, whole(F), 2 * kParts);
     const i64 lda = whole(F), ldw = padded(D);
     const size_t part = p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)(M * ldw) : 0;
-    return 256 + align_up(6 * sizeof(uint16_t) * (size_t)(M * lda), 256) +
+    return kFlagBytes + align_up(6 * sizeof(uint16_t) * (size_t)(M * lda), 256) +
            align_up(6 * sizeof(uint16_t) * (size_t)(lda * ldw), 256) + part;
 }
 
-const int32_t *ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F,
-                            float *dX, void *ws, hipStream_t stream)
+void ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F, float *dX,
+                  void *ws, hipStream_t stream)
 {
     const i64 lda = whole(F), ldw = padded(D);
     const DxPlan p = dx_plan(M, D, lda, 2 * kParts);
-    int32_t *flag = (int32_t *)ws;
-    uint16_t *b = (uint16_t *)((char *)ws + 256);
+    int32_t *flags = (int32_t *)ws;
+    uint16_t *b = (uint16_t *)((char *)ws + kFlagBytes);
     uint16_t *w = (uint16_t *)((char *)b + align_up(6 * sizeof(uint16_t) * (size_t)(M * lda), 256));
     float *part = (float *)((char *)w + align_up(6 * sizeof(uint16_t) * (size_t)(lda * ldw), 256));
-    split({{{BG, M, F, M, lda, b}, {BU, M, F, M, lda, b + 3 * M * lda}, {Wg, F, D, lda, ldw, w},
-            {Wu, F, D, lda, ldw, w + 3 * lda * ldw}}}, 4, flag, stream);
+    Splits s = {};
+    add_split(s, BG, M, F, M, lda, b);
+    add_split(s, BU, M, F, M, lda, b + 3 * M * lda);
+    add_split(s, Wg, F, D, lda, ldw, w);
+    add_split(s, Wu, F, D, lda, ldw, w + 3 * lda * ldw);
+    const Whole whole_ = {BG, BU, Wg, Wu, F, flags, split(s, flags, stream)};
     if (p.shape == kLarge)
-        launch_dx<LargeDx, float>(b, nullptr, w, nullptr, M, D, lda, lda, ldw, p.splits, dX, part, flag, stream);
-    else launch_dx<MidDx, float>(b, nullptr, w, nullptr, M, D, lda, lda, ldw, p.splits, dX, part, flag, stream);
-    return flag;
+        launch_dx<LargeDx, float>(b, nullptr, w, nullptr, M, D, lda, lda, ldw, p.splits, dX, part, whole_, stream);
+    else launch_dx<MidDx, float>(b, nullptr, w, nullptr, M, D, lda, lda, ldw, p.splits, dX, part, whole_, stream);
 }
 
 }  // namespace dpg

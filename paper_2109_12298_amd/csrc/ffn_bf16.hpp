@@ -24,15 +24,15 @@ void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, con
                  uint16_t *dX, void *ws, hipStream_t stream);
 
 // The same for fp32 values, each as three bf16 parts and every product as six
-// bf16 products (what is left out is 2^-24 of a product), M > 64.  Values that
-// have no such parts (infinities, NaN, and magnitudes under 2^-100 or from
-// 2^127 on) set the returned word in device memory; the kernels launched here
-// then do nothing, and the caller's kernel, launched after them, does the work.
+// bf16 products (what is left out is 2^-24 of a product), M > kFfnRowsMax.
+// Values that have no such parts (infinities, NaN, and magnitudes under 2^-100
+// or from 2^127 on) turn the whole call over to the fp32 units (ffn_any.hpp),
+// inside the same launches.
 size_t ffn_parts_forward_workspace(i64 M, i64 K, i64 F);
-const int32_t *ffn_parts_forward(const float *X, const float *Wg, const float *Wu, i64 M, i64 K, i64 F, dp_act act,
-                                 float *H, float *G, float *U, void *ws, hipStream_t stream);
+void ffn_parts_forward(const float *X, const float *Wg, const float *Wu, i64 M, i64 K, i64 F, dp_act act, float *H,
+                       float *G, float *U, void *ws, hipStream_t stream);
 size_t ffn_parts_dx_workspace(i64 M, i64 D, i64 F);
-const int32_t *ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F,
-                            float *dX, void *ws, hipStream_t stream);
+void ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F, float *dX,
+                  void *ws, hipStream_t stream);
 
 }  // namespace dpg

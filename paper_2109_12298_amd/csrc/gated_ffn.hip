@@ -7,10 +7,9 @@
 // (each wave holds both accumulators of its positions and features), so that
 // H is formed from fp32 values in registers; G and U are written only where a
 // backward pass wants them.
-#include "gated_ffn.hpp"
+#include "ffn_any.hpp"
 #include "ffn_bf16.hpp"
 #include "ffn_rows.hpp"
-#include "mfma_tile.hpp"
 
 namespace dpg {
 namespace {
@@ -20,116 +19,27 @@ using namespace ffn;
 constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------------------
-// Any size, type and alignment: 64 x 64 tiles, element loads, fp32 MFMA
-// (products of bf16 values are exact in fp32).  flag: a word in device memory
-// without which the work is already done, or NULL.
+// Any size, type and alignment (ffn_any.hpp): a workgroup per 64 x 64 tile.
 // ---------------------------------------------------------------------------
-constexpr int kTM = 64, kTN = 64, kTK = 16;
-constexpr int kLd = kTM + 1;              // LDS row: operands lie K-major, their loads come along K
-
-// rows r0 .. r0+63 of P [rows][K], columns k0 .. k0+kTK-1, into L [kTK][kLd]; zeros outside
-template <typename T>
-__device__ __forceinline__ void stage_rows(const T *__restrict__ P, i64 rows, i64 K, i64 r0, i64 k0, float *L)
-{
-#pragma unroll
-    for (int q = 0; q < kTM * kTK / kThreads; ++q) {
-        const int e = threadIdx.x + kThreads * q;
-        const int r = e / kTK, k = e % kTK;
-        L[k * kLd + r] = r0 + r < rows && k0 + k < K ? load_elem<T>(P, (r0 + r) * K + k0 + k) : 0.0f;
-    }
-}
-
-// rows k0 .. k0+kTK-1 of P [K][cols], columns c0 .. c0+63, into L [kTK][kLd]
-template <typename T>
-__device__ __forceinline__ void stage_cols(const T *__restrict__ P, i64 K, i64 cols, i64 k0, i64 c0, float *L)
-{
-#pragma unroll
-    for (int q = 0; q < kTN * kTK / kThreads; ++q) {
-        const int e = threadIdx.x + kThreads * q;
-        const int k = e / kTN, c = e % kTN;
-        L[k * kLd + c] = k0 + k < K && c0 + c < cols ? load_elem<T>(P, (k0 + k) * cols + c0 + c) : 0.0f;
-    }
-}
-
 template <typename T, int ACT>
 __global__ __launch_bounds__(kThreads) void ffn_forward_any_kernel(const T *__restrict__ X, const T *__restrict__ Wg,
                                                                    const T *__restrict__ Wu, i64 M, i64 K, i64 F,
                                                                    i64 tiles_f, T *__restrict__ H, T *__restrict__ G,
-                                                                   T *__restrict__ U, const int32_t *__restrict__ flag)
+                                                                   T *__restrict__ U)
 {
-    if (flag != nullptr && *flag == 0) return;
-    __shared__ float Xs[kTK * kLd], Gs[kTK * kLd], Us[kTK * kLd];
+    __shared__ float lds[kAnyFloats];
     const i64 b = xcd_swizzle(blockIdx.x, gridDim.x);
-    const i64 m0 = b / tiles_f * kTM, f0 = b % tiles_f * kTN;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wm = (wave >> 1) * 32, wf = (wave & 1) * 32;
-    const int li = lane & 31, lk = lane >> 5;
-    f32x16 ag, au;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) ag[r] = au[r] = 0.0f;
-    for (i64 k0 = 0; k0 < K; k0 += kTK) {
-        __syncthreads();
-        stage_rows(X, M, K, m0, k0, Xs);
-        stage_rows(Wg, F, K, f0, k0, Gs);
-        stage_rows(Wu, F, K, f0, k0, Us);
-        __syncthreads();
-#pragma unroll
-        for (int kk = 0; kk < kTK; kk += 2) {
-            const float x = Xs[(kk + lk) * kLd + wm + li];
-            ag = __builtin_amdgcn_mfma_f32_32x32x2f32(x, Gs[(kk + lk) * kLd + wf + li], ag, 0, 0, 0);
-            au = __builtin_amdgcn_mfma_f32_32x32x2f32(x, Us[(kk + lk) * kLd + wf + li], au, 0, 0, 0);
-        }
-    }
-    const i64 f = f0 + wf + li;
-    if (f >= F) return;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const i64 m = m0 + wm + 8 * (r >> 2) + 4 * lk + (r & 3);
-        if (m >= M) continue;
-        store_elem(H + m * F + f, act<ACT>(ag[r]) * au[r]);
-        if (G != nullptr) {
-            store_elem(G + m * F + f, ag[r]);
-            store_elem(U + m * F + f, au[r]);
-        }
-    }
+    any_forward_tile<kThreads, ACT>(X, Wg, Wu, M, K, F, b / tiles_f * kTM, b % tiles_f * kTN, H, G, U, lds);
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ffn_dx_any_kernel(const T *__restrict__ BG, const T *__restrict__ BU,
                                                               const T *__restrict__ Wg, const T *__restrict__ Wu, i64 M,
-                                                              i64 D, i64 F, i64 tiles_d, T *__restrict__ dX,
-                                                              const int32_t *__restrict__ flag)
+                                                              i64 D, i64 F, i64 tiles_d, T *__restrict__ dX)
 {
-    if (flag != nullptr && *flag == 0) return;
-    __shared__ float Bs[kTK * kLd], Ws[kTK * kLd];
+    __shared__ float lds[kAnyFloats];
     const i64 b = xcd_swizzle(blockIdx.x, gridDim.x);
-    const i64 m0 = b / tiles_d * kTM, d0 = b % tiles_d * kTN;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wm = (wave >> 1) * 32, wd = (wave & 1) * 32;
-    const int li = lane & 31, lk = lane >> 5;
-    f32x16 acc;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
-    for (int half = 0; half < 2; ++half) {
-        const T *P = half == 0 ? BG : BU, *W = half == 0 ? Wg : Wu;
-        for (i64 k0 = 0; k0 < F; k0 += kTK) {
-            __syncthreads();
-            stage_rows(P, M, F, m0, k0, Bs);
-            stage_cols(W, F, D, k0, d0, Ws);
-            __syncthreads();
-#pragma unroll
-            for (int kk = 0; kk < kTK; kk += 2)
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(Bs[(kk + lk) * kLd + wm + li], Ws[(kk + lk) * kLd + wd + li],
-                                                           acc, 0, 0, 0);
-        }
-    }
-    const i64 d = d0 + wd + li;
-    if (d >= D) return;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const i64 m = m0 + wm + 8 * (r >> 2) + 4 * lk + (r & 3);
-        if (m < M) store_elem(dX + m * D + d, acc[r]);
-    }
+    any_dx_tile<kThreads>(BG, BU, Wg, Wu, M, D, F, b / tiles_d * kTM, b % tiles_d * kTN, dX, lds);
 }
 
 // ---------------------------------------------------------------------------
@@ -178,11 +88,11 @@ __global__ __launch_bounds__(kThreads) void ffn_backprops_kernel(const T *dH, co
 
 template <typename T, int ACT>
 void forward(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, void *H, void *G, void *U,
-             const int32_t *flag, hipStream_t stream)
+             hipStream_t stream)
 {
     const i64 tiles_f = ceil_div(F, kTN);
     ffn_forward_any_kernel<T, ACT><<<(unsigned)(ceil_div(M, kTM) * tiles_f), kThreads, 0, stream>>>(
-        (const T *)X, (const T *)Wg, (const T *)Wu, M, K, F, tiles_f, (T *)H, (T *)G, (T *)U, flag);
+        (const T *)X, (const T *)Wg, (const T *)Wu, M, K, F, tiles_f, (T *)H, (T *)G, (T *)U);
 }
 
 template <typename T, int ACT>
@@ -202,11 +112,11 @@ void backprops(const void *dH, const void *G, const void *U, i64 n, void *BG, vo
 
 template <typename T>
 void dx(const void *BG, const void *BU, const void *Wg, const void *Wu, i64 M, i64 D, i64 F, void *dX,
-        const int32_t *flag, hipStream_t stream)
+        hipStream_t stream)
 {
     const i64 tiles_d = ceil_div(D, kTN);
     ffn_dx_any_kernel<T><<<(unsigned)(ceil_div(M, kTM) * tiles_d), kThreads, 0, stream>>>(
-        (const T *)BG, (const T *)BU, (const T *)Wg, (const T *)Wu, M, D, F, tiles_d, (T *)dX, flag);
+        (const T *)BG, (const T *)BU, (const T *)Wg, (const T *)Wu, M, D, F, tiles_d, (T *)dX);
 }
 
 dp_status check_sizes(i64 M, i64 D, i64 F)
@@ -259,19 +169,18 @@ extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const v
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
     if (by_rows(X, Wg, Wu, dt, M, d_in)) {
         ffn_rows_forward(X, Wg, Wu, dt, M, d_in, d_ff, act, H, G, U, stream);
+    } else if (dt == DP_F32 && d_in < kFfnTilesMax) {
+        ffn_parts_forward((const float *)X, (const float *)Wg, (const float *)Wu, M, d_in, d_ff, act, (float *)H, (float *)G,
+                          (float *)U, ws, stream);
     } else if (dt == DP_F32) {
-        const int32_t *flag = nullptr;
-        if (d_in < kFfnTilesMax)
-            flag = ffn_parts_forward((const float *)X, (const float *)Wg, (const float *)Wu, M, d_in, d_ff, act, (float *)H,
-                                     (float *)G, (float *)U, ws, stream);
-        if (act == DP_ACT_SILU) forward<float, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, flag, stream);
-        else forward<float, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, flag, stream);
+        if (act == DP_ACT_SILU) forward<float, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+        else forward<float, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
     } else if (ffn_tiles_ok(X, d_in) && ffn_tiles_ok(Wg, d_in) && ffn_tiles_ok(Wu, d_in)) {
         ffn_bf16_forward((const uint16_t *)X, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in, d_ff, act,
                          (uint16_t *)H, (uint16_t *)G, (uint16_t *)U, ws, stream);
     } else {
-        if (act == DP_ACT_SILU) forward<uint16_t, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, nullptr, stream);
-        else forward<uint16_t, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, nullptr, stream);
+        if (act == DP_ACT_SILU) forward<uint16_t, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+        else forward<uint16_t, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
     }
     return launch_status();
 }
@@ -305,12 +214,11 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
         if (M <= kFfnRowsMax) {
             ffn_rows_dx((const float *)BG, (const float *)BU, (const float *)Wg, (const float *)Wu, M, d_in, d_ff,
                         (float *)dX, ws, stream);
+        } else if (d_in < kFfnTilesMax && d_ff < kFfnTilesMax) {
+            ffn_parts_dx((const float *)BG, (const float *)BU, (const float *)Wg, (const float *)Wu, M, d_in, d_ff,
+                         (float *)dX, ws, stream);
         } else {
-            const int32_t *flag = nullptr;
-            if (d_in < kFfnTilesMax && d_ff < kFfnTilesMax)
-                flag = ffn_parts_dx((const float *)BG, (const float *)BU, (const float *)Wg, (const float *)Wu, M, d_in,
-                                    d_ff, (float *)dX, ws, stream);
-            dx<float>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, flag, stream);
+            dx<float>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
         }
     } else {
         if (act == DP_ACT_SILU) backprops<uint16_t, DP_ACT_SILU>(dH, G, U, n, BG, BU, stream);
@@ -320,7 +228,7 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
             ffn_bf16_dx((const uint16_t *)BG, (const uint16_t *)BU, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in,
                         d_ff, (uint16_t *)dX, ws, stream);
         else
-            dx<uint16_t>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, nullptr, stream);
+            dx<uint16_t>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
     }
     return launch_status();
 }
