@@ -363,7 +363,7 @@ typedef enum dp_act { DP_ACT_SILU = 0, DP_ACT_GELU_TANH = 1 } dp_act;
  * [M][d_ff] of `dt`, the projections rounded once, as the backward pass takes
  * them; both NULL where no backward pass follows (one alone: DP_EINVAL).  The
  * outputs overlap neither each other nor the inputs.  M >= 0, d_in, d_ff >= 1,
- * each < 2^31 and M * d_ff, M * d_in, d_in * d_ff < 2^35 (else
+ * each < 2^27 and M * d_ff, M * d_in, d_in * d_ff < 2^35 (else
  * DP_EUNSUPPORTED).  A row of X that holds a NaN or an infinity makes its own
  * rows of the outputs non-finite and no others.  (fp32 products over more than
  * 64 rows run on the bf16 matrix units as three bf16 parts, which keep every
@@ -572,8 +572,9 @@ dp_status dp_clip_accumulate_embedding(const int64_t *row_ptr, const int64_t *un
  * dp_per_sample_norms_active) are left out: neither their ids nor their
  * backprops are looked at.  A NaN or infinite norm turns the rows of its
  * sample's ids to NaN.  An id outside [0, V) sets DP_FLAG_BAD_INDEX and its
- * position is left out.  N, T >= 0, V, D >= 1; needs N*T < 2^30, D < 2^22 and
- * N*T*D < 2^37 (else DP_EUNSUPPORTED) and V < 2^31; there is no bound on T alone.
+ * position is left out.  N, T >= 0, V, D >= 1; needs N*T < 2^30, D < 2^22,
+ * N*T*D < 2^37 and V*D < 2^38 (else DP_EUNSUPPORTED) and V < 2^31; there is no
+ * bound on T alone.
  * Workspace: dp_clip_accumulate_tokens_workspace_bytes(N, T, V, D, dt) bytes,
  * 16-byte aligned. */
 size_t dp_clip_accumulate_tokens_workspace_bytes(int64_t N, int64_t T, int64_t V, int64_t D, dp_dtype dt);

@@ -122,9 +122,9 @@ void dx(const void *BG, const void *BU, const void *Wg, const void *Wu, i64 M, i
 dp_status check_sizes(i64 M, i64 D, i64 F)
 {
     DPG_REQUIRE(M >= 0 && D >= 1 && F >= 1, DP_EINVAL);
-    const i64 top = i64(1) << 31;
+    // a grid holds fewer than 2^32 threads: 256 per 64 x 64 values, or per 16 features
+    const i64 top = i64(1) << 27, most = i64(1) << 35;
     DPG_REQUIRE(M < top && D < top && F < top, DP_EUNSUPPORTED);
-    const i64 most = i64(1) << 35;       // a grid holds fewer than 2^24 workgroups, here of 64 x 64 values each
     DPG_REQUIRE(M * D < most && M * F < most && D * F < most, DP_EUNSUPPORTED);
     DPG_REQUIRE(ceil_div(M, kTM) * ceil_div(F > D ? F : D, kTN) < (i64(1) << 24), DP_EUNSUPPORTED);
     return DP_OK;

@@ -897,8 +897,9 @@ dp_status check_sizes(i64 N, i64 T, i64 V, i64 D)
     // 32-bit sorted positions, with room for a chunk past the last one
     DPG_REQUIRE(N < (i64(1) << 30) && T < (i64(1) << 30) && N * T < (i64(1) << 30), DP_EUNSUPPORTED);
     DPG_REQUIRE(D < (i64(1) << 22), DP_EUNSUPPORTED);
-    // a grid holds fewer than 2^24 workgroups of 256: one per 256 positions and 64 columns at the most
-    DPG_REQUIRE(N * T * D < (i64(1) << 37), DP_EUNSUPPORTED);
+    // a grid holds fewer than 2^24 workgroups of 256: one per 256 positions and 64 columns at the most, or (one_kernel)
+    // 2^22 of 1024: one per 8192 ids and 64 columns
+    DPG_REQUIRE(N * T * D < (i64(1) << 37) && V * D < (i64(1) << 38), DP_EUNSUPPORTED);
     return DP_OK;
 }
 

@@ -1,0 +1,103 @@
+"""The language-model operators where element offsets pass 32 bits: tables, sums, activations and tensors of more than
+2^31 elements."""
+import math
+import sys
+
+import pytest
+import torch
+
+from paper_2109_12298_amd import binding as dp
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def say(*a):
+    print("[case]", *a, file=sys.stderr, flush=True)
+
+
+def ws(n):
+    return torch.empty(max(int(n), 16), dtype=torch.uint8, device=DEV)
+
+
+@pytest.fixture(autouse=True)
+def free():
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_lookup_and_tokens_of_a_large_table():
+    say("large table")
+    V, D, T = 2_200_000, 1024, 3000                                   # 2.25e9 elements
+    E = torch.empty((V, D), dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    ids = torch.randint(V - 50, V, (1, T), generator=g, device=DEV)
+    ids[0, :4] = torch.tensor([0, V - 1, 2 ** 21, V // 2], device=DEV)
+    uniq = torch.unique(ids)
+    E[uniq] = torch.randn((len(uniq), D), generator=g, device=DEV).to(torch.bfloat16)
+    Y = torch.empty((1, T, D), dtype=torch.bfloat16, device=DEV)
+    dp.dp_embedding_lookup(ids, E, dp.DP_BF16, 1, T, V, D, 2.0, Y, dp.DP_BF16)
+    assert torch.equal(Y[0], (E[ids[0]].float() * 2.0).to(torch.bfloat16))
+    del E
+    for n in (T, 500):                                                # both paths of the gradient
+        S = torch.full((V, D), 7.0, device=DEV)                       # 9 GB
+        B = Y[:, :n].contiguous()
+        dp.dp_clip_accumulate_tokens(ids[:, :n].contiguous(), B, dp.DP_BF16, 1, n, V, D, 1.0, None, 1.0, S, None,
+                                     ws(dp.dp_clip_accumulate_tokens_workspace_bytes(1, n, V, D, dp.DP_BF16)))
+        want = torch.zeros((60, D), dtype=torch.float64, device=DEV)
+        tail = ids[0, :n] >= V - 60
+        want.index_add_(0, ids[0, :n][tail] - (V - 60), B[0][tail].double())
+        # at most n fp32 additions of values of order 10: n 2^-23 of the sum of the terms, under n / 2^23 * 10 n / 50
+        assert (S[V - 60:].double() - want).abs().max() <= n * 2.0 ** -23 * 10 * (n / 40)
+        for i, v in enumerate((0, None, 2 ** 21, V // 2)):
+            if v is not None:
+                assert torch.equal(S[v], B[0, i].float())
+        assert S[1:V // 2].abs().max() == 0
+        assert float(S.abs().sum(1).ne(0).sum()) == len(torch.unique(ids[0, :n]))
+        del S
+
+
+@pytest.mark.parametrize("M,K,F", [(280_000, 64, 8192)])
+def test_ffn_of_many_positions(M, K, F):
+    say("large ffn", M, K, F)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    bf = torch.bfloat16
+    X = torch.randn((M, K), generator=g, device=DEV).to(bf)
+    Wg, Wu = [(torch.randn((F, K), generator=g, device=DEV) / math.sqrt(K)).to(bf) for _ in range(2)]
+    H, G, U = [torch.full((M, F), 7.0, dtype=bf, device=DEV) for _ in range(3)]
+    assert H.numel() > 2 ** 31
+    dp.dp_gated_ffn_forward(X, Wg, Wu, dp.DP_BF16, M, K, F, dp.DP_ACT_SILU, H, G, U,
+                            ws(dp.dp_gated_ffn_forward_workspace_bytes(M, K, F, dp.DP_BF16)))
+    some = torch.tensor([0, 1, 255, 256, M // 2, 262143, 262144, M - 257, M - 1], device=DEV)
+    g64, u64 = X[some].double() @ Wg.double().t(), X[some].double() @ Wu.double().t()
+    # one rounding to bf16, and sums of 64 terms in fp32 of values of order 1
+    tol = lambda w: 2.0 ** -8 * w.abs() * 1.01 + 1e-4  # noqa: E731
+    for got, want in ((G, g64), (U, u64), (H, g64 * torch.sigmoid(g64) * u64)):
+        assert ((got[some].double() - want).abs() <= tol(want)).all()
+    dX = torch.full((M, K), 7.0, dtype=bf, device=DEV)
+    rows = [G[some].double(), U[some].double(), H[some].double()]
+    dp.dp_gated_ffn_backward(H, G, U, Wg, Wu, dp.DP_BF16, M, K, F, dp.DP_ACT_SILU, G, U, dX,
+                             ws(dp.dp_gated_ffn_backward_workspace_bytes(M, K, F, dp.DP_BF16)))     # BG in G, BU in U
+    p = torch.sigmoid(rows[0])
+    for got, want in ((G, rows[2] * rows[1] * (p + rows[0] * p * (1 - p))), (U, rows[2] * rows[0] * p)):
+        assert ((got[some].double() - want).abs() <= tol(want)).all()
+    want = G[some].double() @ Wg.double() + U[some].double() @ Wu.double()
+    size = G[some].double().abs() @ Wg.double().abs() + U[some].double().abs() @ Wu.double().abs()
+    assert ((dX[some].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2 * (2 * F + 1) * 2.0 ** -24 * size).all()
+
+
+def test_norm_of_a_large_tensor():
+    say("large norm")
+    n = 2 ** 31 + 12345
+    g = torch.full((n,), 0.5, dtype=torch.bfloat16, device=DEV)
+    g[-7:] = 3.0
+    out = torch.zeros_like(g)
+    norm = torch.zeros(1, device=DEV)
+    items = dp.make_grad_tensors([(g, out, n, dp.DP_BF16)])
+    dp.dp_clip_global_norm_many(items, 1, 1.0, norm, None, ws(dp.dp_clip_global_norm_many_workspace_bytes(items, 1)))
+    want = math.sqrt((n - 7) * 0.25 + 63.0)
+    assert abs(norm.item() - want) <= 2.0 ** -24 * want * 1.01
+    c = 1.0 / (want + 1e-6)
+    for at, v in ((0, 0.5), (2 ** 31 - 1, 0.5), (2 ** 31, 0.5), (n - 8, 0.5), (n - 7, 3.0), (n - 1, 3.0)):
+        assert abs(out[at].item() - c * v) <= (2.0 ** -8 + 2.0 ** -21) * c * v
+    assert out[:-7].min() == out[:-7].max()

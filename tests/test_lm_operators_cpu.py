@@ -45,7 +45,7 @@ def test_tokens_refusals():
                 dict(C=0.0), dict(C=-1.0), dict(C=math.nan), dict(ws=None), dict(ws=FAKE + 4), dict(ws_bytes=need - 1)):
         assert call(**bad) == dp.DP_EINVAL, bad
     for much in (dict(N=2 ** 15, T=2 ** 15), dict(N=2 ** 40, T=2 ** 40), dict(D=2 ** 22),
-                 dict(N=2 ** 14, T=2 ** 14, D=2 ** 10)):
+                 dict(N=2 ** 14, T=2 ** 14, D=2 ** 10), dict(V=2 ** 30, D=2 ** 10)):
         assert call(**much) == dp.DP_EUNSUPPORTED, much
     w = dp.dp_clip_accumulate_tokens_workspace_bytes
     assert w(0, 3, 10, 4, 0) == 0 and w(3, 0, 10, 4, 0) == 0 and w(-1, 3, 10, 4, 0) == 0 and w(2, 3, 10, 4, 9) == 0
@@ -77,7 +77,7 @@ def test_ffn_refusals():
         assert call(dt=2) == dp.DP_EDTYPE
         for bad in [dict(M=-1), dict(D=0), dict(F=0), dict(act=2), dict(act=-1)] + [{k: None} for k in outs]:
             assert call(**bad) == dp.DP_EINVAL, bad
-        for much in (dict(M=2 ** 31), dict(F=2 ** 31), dict(M=2 ** 20, F=2 ** 16), dict(D=2 ** 18, F=2 ** 18),
+        for much in (dict(M=2 ** 31), dict(F=2 ** 27), dict(D=2 ** 27), dict(M=2 ** 20, F=2 ** 16), dict(D=2 ** 18, F=2 ** 18),
                      dict(M=2 ** 62, D=2 ** 62)):
             assert call(**much) == dp.DP_EUNSUPPORTED, much
         assert call(M=0) == dp.DP_OK
