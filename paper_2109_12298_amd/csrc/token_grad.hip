@@ -3,13 +3,14 @@
 //
 // Few positions (one_rule): one launch (one_kernel, below).  Beyond:
 // 1. The positions are sorted by id (stable, so equal ids keep ascending
-//    positions): a least-significant-digit radix sort of (id, position) with
-//    digits of up to 9 bits, per digit a count launch and a scatter launch.  A
-//    position that is left out (a bad id, a sample outside the active batch)
-//    takes the key V and sorts behind all others.  The first count clears a
-//    byte per id, the first scatter sets those of the ids it meets, so that
-//    only rows without a token are zeroed, by workgroups that the launches
-//    after it have to spare.
+//    positions; a position that is left out, for a bad id or a sample outside
+//    the active batch, takes the key V and stands last).  Up to kGroupMax of
+//    them in one launch (group_kernel), more by a least-significant-digit
+//    radix sort of (id, position) with digits of up to 9 bits, per digit a
+//    count launch and a scatter launch.  For a large table the first count
+//    clears a byte per id and the first scatter sets those of the ids it
+//    meets, so that only rows without a token are zeroed, by workgroups that
+//    the launches after it have to spare.
 // 2. walk_kernel: the sorted positions in chunks; a wave adds a chunk's rows
 //    of one block of columns, kBatch row loads in flight, and writes each id's
 //    sum where the id's positions start and end inside the chunk.  A piece
@@ -29,6 +30,16 @@ constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kOneMax = 2048;             // positions of the one-launch path
 constexpr int kOneIds = 16384;            // ids of one of its workgroups, at most
+constexpr int kPosBits = 11;
+constexpr int kOneItems = kOneMax / kSortThreads;
+constexpr int kGroupMax = 16384;          // positions that one launch sorts
+constexpr int kGroups = 128;              // its workgroups
+constexpr int kGroupPosBits = 14;
+constexpr int kGroupItems = kGroupMax / kSortThreads;
+constexpr i64 kGroupIds = i64(1) << 24;   // ids it sorts, at most
+constexpr int kCompareMax = 128;          // kept positions ranked by comparing each with each
+static_assert(kOneMax == 1 << kPosBits && kOneIds <= 1 << (32 - kPosBits - 1), "(id, position) in 31 bits");
+static_assert(kGroupMax == 1 << kGroupPosBits && kGroupIds / kGroups <= 1 << (32 - kGroupPosBits - 1), "likewise");
 constexpr int kScanTiles = 64;            // tiles whose counts a scatter workgroup adds up itself
 constexpr i64 kFillBytes = i64(48) << 20; // zeros that a launch bound by latency writes beside its work
 constexpr i64 kFillAllBytes = i64(128) << 20;
@@ -45,6 +56,7 @@ int items_for(i64 M) { return M <= (i64)kScanTiles * 2 * kSortThreads ? 2 : 8; }
 struct Plan {
     i64 M, tiles, hist_ld, chunk, chunks, colblocks;
     int items, passes, bits, vec;         // bits per digit; columns per lane
+    bool grouped;                         // sorted in one launch
     size_t keys[2], pos[2], hist, tot, present, part, bytes;    // workspace offsets
 };
 
@@ -59,6 +71,9 @@ Plan make_plan(i64 N, i64 T, i64 V, i64 D, int vec)
     p.passes = (key_bits + kDigitBits - 1) / kDigitBits;
     p.bits = (key_bits + p.passes - 1) / p.passes;
     p.vec = vec;
+    // (ids of one digit take two launches by digits, and a large table is better zeroed beside more launches: 16384
+    // positions of 500 x 4096 48.0 us by digits, 49.7 grouped; 50000 x 1024 69.7 and 73.9)
+    p.grouped = p.M <= kGroupMax && V <= kGroupIds && p.passes > 1 && 4 * V * D <= kFillAllBytes;
     p.colblocks = ceil_div(D, 64 * (i64)vec);
     // chunks of 16 to 256 sorted positions, as long as 4096 waves remain
     p.chunk = 16;
@@ -336,6 +351,187 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(const uint32_t *_
     }
 }
 
+// The n keys (id, position) of list, kept in ascending position, grouped by the
+// digit of their id at `shift` (stable), in place: per-wave counts of each digit,
+// prefixes over the waves and the digits.
+template <int ITEMS, int POS_BITS>
+__device__ __forceinline__ void group_list(uint32_t *list, int n, int shift, int bits, int (*cnt)[kDigits], int *wsum)
+{
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rounds = (n + 64 * kSortWaves - 1) / (64 * kSortWaves);       // of each wave, on consecutive keys
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+    for (int i = lane; i < kDigits; i += 64) cnt[wave][i] = 0;
+    uint32_t key[ITEMS];
+    int rank[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        if (i >= rounds) continue;
+        const int e = (wave * rounds + i) * 64 + lane;
+        const bool on = e < n;
+        key[i] = on ? list[e] : 0;
+        const uint32_t d = (key[i] >> (POS_BITS + shift)) & ((1u << bits) - 1u);
+        uint64_t same = __ballot(on);
+        for (int b = 0; b < bits; ++b) {
+            const bool bit = (d >> b) & 1u;
+            const uint64_t m = __ballot(bit);
+            same &= bit ? m : ~m;
+        }
+        rank[i] = 0;
+        if (on) {
+            const int before = __popcll(same & below);
+            const int base = cnt[wave][d];
+            rank[i] = base + before;
+            if (before == 0) cnt[wave][d] = base + __popcll(same);
+        }
+    }
+    __syncthreads();
+    int total = 0;
+    if (threadIdx.x < kDigits) {
+#pragma unroll
+        for (int k = 0; k < kSortWaves; ++k) {
+            const int t = cnt[k][threadIdx.x];
+            cnt[k][threadIdx.x] = total;
+            total += t;
+        }
+    }
+    const int base = scan_1024(total, wsum);
+    if (threadIdx.x < kDigits) {
+#pragma unroll
+        for (int k = 0; k < kSortWaves; ++k) cnt[k][threadIdx.x] += base;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        if (i >= rounds) continue;
+        if ((wave * rounds + i) * 64 + lane < n)
+            list[cnt[wave][(key[i] >> (POS_BITS + shift)) & ((1u << bits) - 1u)] + rank[i]] = key[i];
+    }
+    __syncthreads();
+}
+
+// Groups the n keys of list by id (the ids below own): few by comparing each with each, more by digits.
+template <int ITEMS, int POS_BITS>
+__device__ __forceinline__ void group_ids(uint32_t *list, int n, uint32_t own, int (*cnt)[kDigits], int *wsum)
+{
+    const int tid = threadIdx.x;
+    if (n <= kCompareMax) {               // unique keys: a key's place is the number of smaller ones
+        const uint32_t k = tid < n ? list[tid] : 0;
+        if (tid >= n && tid < kCompareMax) list[tid] = ~0u;
+        __syncthreads();
+        int r = 0;
+        if (tid < n)
+            for (int j = 0; j < n; j += 4) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(list + j);
+                r += (x.x < k) + (x.y < k) + (x.z < k) + (x.w < k);
+            }
+        __syncthreads();
+        if (tid < n) list[r] = k;
+        __syncthreads();
+    } else {
+        int bits = 1;
+        while (((own - 1) >> bits) != 0) ++bits;
+        for (int shift = 0; shift < bits; shift += kDigitBits)
+            group_list<ITEMS, POS_BITS>(list, n, shift, bits - shift < kDigitBits ? bits - shift : kDigitBits, cnt, wsum);
+    }
+}
+
+// The whole sort of up to kGroupMax positions in one launch.  Any order of the
+// ids serves, as long as equal ids stand together: workgroup g takes the ids
+// v = g mod kGroups, looks at every position, keeps those of its ids in
+// order, groups them by id, and writes them behind the positions of the
+// workgroups before it, which it has counted on the way.  Workgroups past
+// kGroups write zeros.  Launches and the trips to memory between them bound
+// the sort of so few (16384 positions of 10000 x 100: 14 us, and the call 24.6;
+// by digits, four launches, the call 30.0.  4096 of 32000 x 768: 27.1 and 39.2).
+__global__ __launch_bounds__(kSortThreads) void group_kernel(const int64_t *__restrict__ ids, int M, uint32_t T, i64 V,
+                                                             const float *__restrict__ norm,
+                                                             uint32_t *__restrict__ keys, uint32_t *__restrict__ pos,
+                                                             int32_t *status, Fill fill)
+{
+    __shared__ __attribute__((aligned(16))) uint32_t list[kGroupMax];                         // (id / kGroups, position)
+    __shared__ int cnt[kSortWaves][kDigits];
+    __shared__ int wsum[kSortWaves], wbelow[kSortWaves], wvalid[kSortWaves];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (blockIdx.x >= kGroups) {
+        fill_rows(fill, (blockIdx.x - kGroups) * kSortWaves + wave, (gridDim.x - kGroups) * kSortWaves);
+        return;
+    }
+    const uint32_t g = blockIdx.x;
+    const uint32_t own = (uint32_t)((V - g + kGroups - 1) / kGroups);
+    const int rounds = (M + kSortThreads - 1) / kSortThreads;    // of each wave, on consecutive positions
+    const int m0 = wave * rounds * 64 + lane;
+    int64_t id[kGroupItems];              // all loads in flight
+#pragma unroll
+    for (int i = 0; i < kGroupItems; ++i) {
+        const int m = m0 + i * 64;
+        id[i] = i < rounds && m < M ? ids[m] : 0;
+    }
+    uint32_t key[kGroupItems];
+    int mine_n = 0, below_n = 0, valid_n = 0;
+    bool bad = false;
+    // the position's sample, by steps of 64 positions
+    uint32_t q = (uint32_t)m0 / T, r = (uint32_t)m0 - q * T;
+    const uint32_t dq = 64 / T, dr = 64 % T;
+#pragma unroll
+    for (int i = 0; i < kGroupItems; ++i) {
+        key[i] = ~0u;
+        if (i >= rounds) continue;
+        const int m = m0 + i * 64;
+        const bool in = m < M && (norm == nullptr || !(norm[m < M ? q : 0] < 0.0f));
+        const uint32_t v = (uint32_t)id[i], its = v % kGroups;
+        const bool valid = in && (uint32_t)((uint64_t)id[i] >> 32) == 0 && v < (uint32_t)V;
+        bad |= in && !valid;
+        const bool mine = valid && its == g;
+        if (mine) key[i] = (v / kGroups) << kGroupPosBits | (uint32_t)m;
+        mine_n += __popcll(__ballot(mine));
+        below_n += __popcll(__ballot(valid && its < g));
+        if (g == 0) valid_n += __popcll(__ballot(valid));
+        q += dq;
+        r += dr;
+        if (r >= T) {
+            r -= T;
+            ++q;
+        }
+    }
+    if (bad && g == 0) raise_flag(status, DP_FLAG_BAD_INDEX);
+    if (lane == 0) {
+        wsum[wave] = mine_n;
+        wbelow[wave] = below_n;
+        wvalid[wave] = valid_n;
+    }
+    __syncthreads();
+    int at = 0, n = 0, base = 0, kept = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        at += w < wave ? wsum[w] : 0;
+        n += wsum[w];
+        base += wbelow[w];
+        kept += wvalid[w];
+    }
+    n = __builtin_amdgcn_readfirstlane(n);
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < kGroupItems; ++i) {
+        const bool mine = key[i] != ~0u;
+        const uint64_t in = __ballot(mine);
+        if (in == 0) continue;
+        if (mine) list[at + __popcll(in & below)] = key[i];
+        at += __popcll(in);
+    }
+    __syncthreads();
+    group_ids<kGroupItems, kGroupPosBits>(list, n, own, cnt, wsum);
+    for (int e = tid; e < n; e += kSortThreads) {
+        const uint32_t k = list[e];
+        keys[base + e] = (k >> kGroupPosBits) * kGroups + g;
+        pos[base + e] = k & ((1u << kGroupPosBits) - 1u);
+    }
+    // positions left out stand last
+    if (g == 0)
+        for (int e = kept + tid; e < M; e += kSortThreads) keys[e] = (uint32_t)V;
+}
+
 // ---------------------------------------------------------------------------
 // sums
 // ---------------------------------------------------------------------------
@@ -455,17 +651,17 @@ __global__ __launch_bounds__(kWalkThreads) void join_kernel(const uint32_t *__re
     const uint32_t lo = ck * chunk, hi = lo + chunk;         // the grid leaves out the last chunk: hi < M
     const uint32_t key = keys[hi - 1];
     if (key >= V || keys[hi] != key || (lo > 0 && keys[lo - 1] == key)) return;
-    // the following chunks that hold the id up to their end and behind it
-    uint32_t n = 0;
-    for (;;) {
-        const uint32_t h = (ck + 2 + n + lane) * chunk;      // end of chunk ck + 1 + n + lane
-        const bool full = h < M && keys[h - 1] == key && keys[h] == key;
-        const uint64_t stop = ~__ballot(full);
-        if (stop != 0) {
-            n += __ffsll((unsigned long long)stop) - 1;
-            break;
-        }
-        n += 64;
+    // n, the following chunks that hold the id up to their end and behind it: between lo_n and hi_n, 64 places looked
+    // at together, first the next 64
+    uint32_t n = 0, hi_n = (M - 1) / chunk - (ck + 1), step = 1;
+    while (n < hi_n) {
+        const uint32_t x = n + (lane + 1) * step;            // chunk ck + x is full
+        const uint32_t h = (ck + 1 + x) * chunk;             // its end
+        const uint64_t stop = ~__ballot(x <= hi_n && keys[h] == key);
+        const uint32_t full = stop != 0 ? __ffsll((unsigned long long)stop) - 1 : 64;
+        if (full < 64 && n + (full + 1) * step - 1 < hi_n) hi_n = n + (full + 1) * step - 1;
+        n += full * step;
+        step = (hi_n - n + 63) / 64;
     }
     ++n;                                                     // and the one in which it ends
     const i64 col = (i64)(unit % colblocks) * 64 * VEC + lane * VEC;
@@ -481,13 +677,13 @@ __global__ __launch_bounds__(kWalkThreads) void join_kernel(const uint32_t *__re
 #pragma unroll
         for (int i = 0; i < VEC; ++i) acc[i] = o.v[i];
     }
-    for (uint32_t x = x0; x < x1; x += 8) {
-        Out<VEC> v[8];
+    for (uint32_t x = x0; x < x1; x += kBatch) {
+        Out<VEC> v[kBatch];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < kBatch; ++j)
             v[j] = *reinterpret_cast<const Out<VEC> *>(P + (i64)(2 * (x + j < x1 ? x + j : x)) * D);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < kBatch; ++j)
             if (x + j < x1) {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) acc[i] += v[j].v[i];
@@ -515,76 +711,13 @@ __global__ __launch_bounds__(kWalkThreads) void join_kernel(const uint32_t *__re
 // id, and adds the rows: each wave a run of the grouped positions, an id that
 // crosses waves joined through LDS in wave order.
 // ---------------------------------------------------------------------------
-constexpr int kPosBits = 11;
-constexpr int kOneItems = kOneMax / kSortThreads;
-constexpr int kCompareMax = 128;          // kept positions ranked by comparing each with each
-static_assert(kOneMax == 1 << kPosBits && kOneIds <= 1 << (32 - kPosBits - 1), "(id, position) in 31 bits");
-
-// The n keys of list, kept in ascending position, grouped by the digit of
-// their id at `shift` (stable), in place: per-wave counts of each digit,
-// prefixes over the waves and the digits.
-__device__ __forceinline__ void group_list(uint32_t *list, int n, int shift, int bits, int (*cnt)[kDigits], int *wsum)
-{
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rounds = (n + 64 * kSortWaves - 1) / (64 * kSortWaves);       // of each wave, on consecutive keys
-    const uint64_t below = (uint64_t(1) << lane) - 1;
-    for (int i = lane; i < kDigits; i += 64) cnt[wave][i] = 0;
-    uint32_t key[kOneItems];
-    int rank[kOneItems];
-#pragma unroll
-    for (int i = 0; i < kOneItems; ++i) {
-        if (i >= rounds) continue;
-        const int e = (wave * rounds + i) * 64 + lane;
-        const bool on = e < n;
-        key[i] = on ? list[e] : 0;
-        const uint32_t d = (key[i] >> (kPosBits + shift)) & ((1u << bits) - 1u);
-        uint64_t same = __ballot(on);
-        for (int b = 0; b < bits; ++b) {
-            const bool bit = (d >> b) & 1u;
-            const uint64_t m = __ballot(bit);
-            same &= bit ? m : ~m;
-        }
-        rank[i] = 0;
-        if (on) {
-            const int before = __popcll(same & below);
-            const int base = cnt[wave][d];
-            rank[i] = base + before;
-            if (before == 0) cnt[wave][d] = base + __popcll(same);
-        }
-    }
-    __syncthreads();
-    int total = 0;
-    if (threadIdx.x < kDigits) {
-#pragma unroll
-        for (int k = 0; k < kSortWaves; ++k) {
-            const int t = cnt[k][threadIdx.x];
-            cnt[k][threadIdx.x] = total;
-            total += t;
-        }
-    }
-    const int base = scan_1024(total, wsum);
-    if (threadIdx.x < kDigits) {
-#pragma unroll
-        for (int k = 0; k < kSortWaves; ++k) cnt[k][threadIdx.x] += base;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kOneItems; ++i) {
-        if (i >= rounds) continue;
-        if ((wave * rounds + i) * 64 + lane < n)
-            list[cnt[wave][(key[i] >> (kPosBits + shift)) & ((1u << bits) - 1u)] + rank[i]] = key[i];
-    }
-    __syncthreads();
-}
-
 template <typename T, int VEC>
 __global__ __launch_bounds__(kSortThreads) void one_kernel(const int64_t *__restrict__ ids, const T *__restrict__ B,
                                                            int M, uint32_t Tn, i64 V, i64 D, float scale,
                                                            const float *__restrict__ norm, float C, int log_g,
                                                            float *__restrict__ sum, int32_t *status)
 {
-    __shared__ uint32_t ranked[kOneMax];            // (id / G, position)
+    __shared__ __attribute__((aligned(16))) uint32_t ranked[kOneMax];            // (id / G, position)
     __shared__ int cnt[kSortWaves][kDigits];
     __shared__ uint32_t seen[kOneIds / 32];                      // ids of the workgroup that hold a token
     __shared__ Out<VEC> head[kSortWaves][64];                    // pieces of an id that started in an earlier wave
@@ -643,20 +776,7 @@ __global__ __launch_bounds__(kSortThreads) void one_kernel(const int64_t *__rest
             if (((seen[v >> 5] >> (v & 31)) & 1u) == 0)
                 *reinterpret_cast<Out<VEC> *>(sum + (((i64)v << log_g) + g) * D + col) = z;
     }
-    if (n <= kCompareMax) {               // unique keys: a key's place is the number of smaller ones
-        const uint32_t k = tid < n ? ranked[tid] : 0;
-        int r = 0;
-        if (tid < n)
-            for (int j = 0; j < n; ++j) r += ranked[j] < k ? 1 : 0;
-        __syncthreads();
-        if (tid < n) ranked[r] = k;
-        __syncthreads();
-    } else {
-        int bits = 1;
-        while (((own - 1) >> bits) != 0) ++bits;
-        for (int shift = 0; shift < bits; shift += kDigitBits)
-            group_list(ranked, n, shift, bits - shift < kDigitBits ? bits - shift : kDigitBits, cnt, wsum);
-    }
+    group_ids<kOneItems, kPosBits>(ranked, n, own, cnt, wsum);
 
     const int run = (n + kSortWaves - 1) / kSortWaves;
     const int lo = wave * run < n ? wave * run : n, hi = lo + run < n ? lo + run : n;
@@ -774,12 +894,13 @@ int vec_for(const void *B, const float *sum, dp_dtype dt, i64 D)
 
 // The groups of rows that each launch zeroes beside its work.  A table of up
 // to kFillAllBytes is zeroed whole by the sort's launches, which are bound by
-// latency (8192 positions, 32000 x 768: the call 34 us, 46 with the flags);
-// of a larger one only the rows without a token are, once their flags are
+// latency (4096 positions, 32000 x 768: the call 27 us, 35 with the flags;
+// 16640, sorted by digits: 50 and 48, where all ids are alike 66 and 80); of
+// a larger one only the rows without a token are, once their flags are
 // there (65536 positions, 50000 x 2048): up to kFillBytes by each later
 // launch that is bound by latency, the rest by the walk.
 struct Fills {
-    Fill count[4], scatter[4], walk, join;
+    Fill group, count[4], scatter[4], walk, join;
     bool flags;
 };
 
@@ -797,6 +918,7 @@ Fills split_fill(const Plan &p, float *sum, char *ws, i64 V, i64 D)
         return r;
     };
     const i64 part = f.flags ? kFillBytes / (4 * D * kFillRows) + 1 : ceil_div(groups, 2 * p.passes);
+    f.group = next(p.grouped ? groups : 0);
     for (int i = 0; i < p.passes; ++i) {
         f.count[i] = next(f.flags && i == 0 ? 0 : part);
         f.scatter[i] = next(f.flags && i == 0 ? 0 : part);
@@ -943,8 +1065,14 @@ extern "C" dp_status dp_clip_accumulate_tokens(const int64_t *ids, const void *B
     const Plan p = make_plan(N, T, V, D, vec);
     char *w = (char *)ws;
     const Fills fills = split_fill(p, sum, w, V, D);
-    const int buf = p.items == 2 ? sort<2>(p, ids, T, V, norm, status, w, fills, stream)
-                                 : sort<8>(p, ids, T, V, norm, status, w, fills, stream);
+    int buf = 0;
+    if (p.grouped)
+        group_kernel<<<kGroups + fill_blocks(fills.group, kSortWaves), kSortThreads, 0, stream>>>(
+            ids, (int)p.M, (uint32_t)T, V, norm, (uint32_t *)(w + p.keys[0]), (uint32_t *)(w + p.pos[0]),
+            status, fills.group);
+    else
+        buf = p.items == 2 ? sort<2>(p, ids, T, V, norm, status, w, fills, stream)
+                           : sort<8>(p, ids, T, V, norm, status, w, fills, stream);
     if (dt == DP_F32) sums_by_vec<float>(p, B, T, V, D, scale, norm, C, sum, w, buf, fills, stream);
     else sums_by_vec<uint16_t>(p, B, T, V, D, scale, norm, C, sum, w, buf, fills, stream);
     return launch_status();

@@ -113,10 +113,11 @@ def token_ids(rng, kind, N, T, V):
     return rng.integers(0, V, (N, T))
 
 
-# one launch up to 2048 positions, one workgroup's sort up to 16384, 64 tiles of 8192 at 524288
+# one launch up to 2048 positions, sorted in one up to 16384 where the ids have 10 bits, 64 tiles of 8192 at 524288
 SIZES = [(1, 1, 1, 1), (1, 2, 3, 5), (2, 8, 512, 64), (1, 17, 511, 257), (3, 100, 9000, 200), (16, 128, 300, 100),
          (3, 683, 513, 12), (1, 2049, 40, 100), (2, 4096, 100, 8), (8193, 1, 1000, 6), (33, 300, 70000, 16),
-         (5, 2011, 600, 533), (64, 256, 1000, 100), (1, 16385, 500, 40), (4, 5000, 90000, 20)]
+         (5, 2011, 600, 533), (64, 256, 1000, 100), (1, 16385, 500, 40), (4, 5000, 90000, 20), (4, 4096, 512, 8), (16384, 1, 513, 4), (37, 63, 700, 130), (41, 65, 511, 24),
+         (150, 100, 130000, 40)]
 
 
 @pytest.mark.parametrize("N,T,V,D", SIZES)
@@ -197,14 +198,15 @@ def test_tokens_large_table(dt, D):
     assert (got == 0).all() and st.item() == dp.DP_FLAG_BAD_INDEX
 
 
-@pytest.mark.parametrize("T", [9, 700, 5000])
+@pytest.mark.parametrize("T", [9, 700, 3000, 5000])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-def test_tokens_left_out(T, dt):
+@pytest.mark.parametrize("V", [64, 5000])
+def test_tokens_left_out(V, T, dt):
     """Padding rows are not looked at, bad ids are flagged, a broken norm poisons its sample's ids alone."""
-    say("tokens left out", T, dt)
+    say("tokens left out", V, T, dt)
     rng = np.random.default_rng(T)
     tt, ct = DT[dt]
-    N, V, D = 5, 64, 24
+    N, D = 5, 24
     ids = rng.integers(0, V // 2, (N, T))
     ids[3] = V - 1 - rng.integers(0, 3, T)                                         # ids of the broken sample alone
     B = rng.standard_normal((N, T, D)).astype(np.float32)
@@ -225,18 +227,19 @@ def test_tokens_left_out(T, dt):
     assert st.item() == dp.DP_FLAG_BAD_INDEX
 
 
-@pytest.mark.parametrize("N,T", [(0, 5), (4, 0), (2, 3), (1, 9000)])
-def test_tokens_nothing_left(N, T):
+@pytest.mark.parametrize("N,T", [(0, 5), (4, 0), (2, 3), (1, 9000), (1, 17000)])
+@pytest.mark.parametrize("V", [33, 900])
+def test_tokens_nothing_left(V, N, T):
     """No positions, or none that counts: zeros."""
     say("tokens nothing", N, T)
     ids = torch.full((N, T), -1, device=DEV)
     B = torch.full((N, T, 20), math.nan, device=DEV)
     st = status()
-    assert (run_tokens(ids, B, dp.DP_F32, 33, 1.0, None, 1.0, st=st) == 0).all()
+    assert (run_tokens(ids, B, dp.DP_F32, V, 1.0, None, 1.0, st=st) == 0).all()
     assert st.item() == (dp.DP_FLAG_BAD_INDEX if N * T else 0)
     st = status()
     norm = torch.full((N,), -1.0, device=DEV)
-    assert (run_tokens(ids, B, dp.DP_F32, 33, 1.0, norm, 1.0, st=st) == 0).all()
+    assert (run_tokens(ids, B, dp.DP_F32, V, 1.0, norm, 1.0, st=st) == 0).all()
     assert st.item() == 0
 
 
