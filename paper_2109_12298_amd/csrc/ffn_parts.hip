@@ -1,0 +1,592 @@
+// Gated feed-forward block in fp32 on v_mfma_f32_32x32x16_bf16: every value as
+// three bf16 parts (ffn_split_kernel), every product as six bf16 products
+//   x w = x0 w0 + (x1 w0 + x0 w1 + x1 w1 + x2 w0 + x0 w2)
+// What is left out (x1 w2, x2 w1: 2^-24 of the product at most, and x2 w2) is
+// within the rounding of an fp32 product.  The first product and the others
+// have accumulators of their own, so that the small ones are not rounded to
+// the large sum's last bit.
+//
+// A stage holds 32 columns of all three parts of each operand, so that a part
+// is staged once and read from LDS once for all the products that take it:
+// 12 operand reads for 24 matrix instructions (the parts as six products one
+// after another, each with stages of its own, take 32 for 24, and twice the
+// stage loads: MEASURED).
+//
+// Operands, swizzles and the output's way are those of ffn_bf16.hip; one
+// workgroup of four waves per CU, three stages.
+#include "ffn_any.hpp"
+#include "ffn_bf16.hpp"
+#include "ffn_tiles.hpp"
+
+#include <type_traits>
+
+namespace dpg {
+namespace {
+
+constexpr int kBK = 32, kNS = 3, kPlanes = 3, kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kRow = 2 * kBK;             // bytes of a staged row of X, Wg, Wu, BG or BU
+constexpr int kRpi = 1024 / kRow;         // such rows per load instruction
+constexpr int kCols = 128;                // columns of a staged row of Wg and Wu in the backward pass
+constexpr int kWRpi = 1024 / (2 * kCols); // such rows per load instruction
+constexpr int kWLoads = kBK / kWRpi;      // load instructions per part and stage
+constexpr int kSplitBlocks = 1024;        // workgroups of the splitting kernel, at most
+constexpr int kProducts = 6;              // the last one the large one
+constexpr int kXPart[kProducts] = {0, 2, 1, 0, 1, 0}, kWPart[kProducts] = {2, 0, 1, 1, 0, 0};
+
+// whether a value has no parts, from this thread's words
+__device__ __forceinline__ int own_flags(const Whole &w)
+{
+    int bad = 0;
+#pragma unroll
+    for (int k = 0; k < kSplitBlocks / kThreads; ++k) {      // past the end the first word again
+        const int i = threadIdx.x + k * kThreads;
+        bad |= w.flags[i < w.count ? i : 0];
+    }
+    return bad;
+}
+
+// The parts lie in memory as they do in LDS: a load instruction copies 1 KB of
+// consecutive bytes (16 rows of 64 bytes from a row-major array, half a cache
+// line each, took MEASURED2).  Rows of X, Wg, Wu, BG and BU: [group of kRpi
+// rows][stage][part] of 1 KB.
+struct Parts {
+    const char *p;
+    i64 groups, stages;
+    __device__ __forceinline__ const char *at(i64 group, i64 part) const
+    {
+        return p + ((group < groups ? group : groups - 1) * stages * kPlanes + part) * 1024;
+    }
+};
+constexpr i64 kStageBytes = kPlanes * 1024;                  // from a group's stage to its next
+
+constexpr int kOperands = 12;             // of a wave and k-step
+constexpr int kMfma = 24;                 // matrix instructions of a wave and k-step
+constexpr int kLoads = 12;                // loads of a wave and stage
+
+// The run of stages 0 .. nst-1.  issue(c, r): load r of stage c; read(c, ks, j,
+// f): operand j of its k-step ks; mma(i, f): matrix instruction i.  One wave
+// per SIMD: the loads and reads of what comes next are issued in the shadow of
+// the matrix instructions (32 clocks each), in this order.
+template <typename Issue>
+__device__ __forceinline__ void start_stages(int nst, const Issue &issue)
+{
+    static_assert(kNS == 3, "two stages ahead");
+#pragma unroll
+    for (int c = 0; c < kNS; ++c)
+        if (c < nst)
+#pragma unroll
+            for (int r = 0; r < kLoads; ++r) issue(c, r);
+}
+
+template <typename Frag, typename Issue, typename Read, typename Mma>
+__device__ __forceinline__ void run_stages(int nst, const Issue &issue, const Read &read, const Mma &mma)
+{
+    static_assert(kBK == 32, "two k-steps in turn");
+    // f's products; meanwhile the operands of k-step ks of stage c (READ) and the loads of stage `ahead` (ISSUE)
+    const auto step = [&](auto READ, auto ISSUE, const Frag &f, int c, int ks, Frag &next, int ahead) {
+#pragma unroll
+        for (int i = 0; i < kMfma; ++i) {
+            mma(i, f);
+            if constexpr (decltype(READ)::value)
+                if (i < kOperands) read(c, ks, i, next);
+            if constexpr (decltype(ISSUE)::value)
+                if (i % (kMfma / kLoads) == 1) issue(ahead, i / (kMfma / kLoads));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    wait_later<kLoads>(nst - 1);
+    stage_barrier();
+    Frag fa, fb;
+#pragma unroll
+    for (int j = 0; j < kOperands; ++j) read(0, 0, j, fa);
+    int c = 0;
+    for (; c + kNS < nst; ++c) {
+        step(yes, no, fa, c, 1, fb, 0);
+        // stage c + 1 has landed, and every wave has read the last of stage c: its buffer takes stage c + kNS
+        wait_vmcnt<kLoads>();
+        wait_lgkmcnt0();
+        stage_barrier();
+        step(yes, yes, fb, c + 1, 0, fa, c + kNS);
+    }
+    for (; c + 1 < nst; ++c) {
+        step(yes, no, fa, c, 1, fb, 0);
+        wait_later<kLoads>(nst - 2 - c < 1 ? 0 : 1);
+        wait_lgkmcnt0();
+        stage_barrier();
+        step(yes, no, fb, c + 1, 0, fa, 0);
+    }
+    step(yes, no, fa, c, 1, fb, 0);
+    step(no, no, fb, 0, 0, fa, 0);
+}
+
+// ---------------------------------------------------------------------------
+// forward: tiles of BM positions by BF features of both G and U, each wave half
+// of either
+// ---------------------------------------------------------------------------
+template <int BM_, int BF_>
+struct Shape {
+    static constexpr int BM = BM_, BF = BF_, ROWS = BM + 2 * BF;
+    static constexpr int STAGE = kPlanes * ROWS * kRow, LDS = kNS * STAGE;
+    static constexpr int LOADS = kPlanes * ROWS / kRpi / kWaves;
+    static constexpr int FM = BM / 64, FF = BF / 64;
+    static_assert(kPlanes * (FM + 2 * FF) == kOperands && kProducts * 2 * FM * FF == kMfma && LOADS == kLoads, "steps");
+    static_assert(LOADS * kRpi * kWaves == kPlanes * ROWS && BM % kRpi == 0 && BF % kRpi == 0, "stage split");
+    static_assert(kWaves * 32 * (FF * 128 + 16) <= LDS && 4 * kAnyFloats <= LDS, "the outputs' and the fallback's LDS");
+};
+
+template <typename S, int ACT>
+__global__ __launch_bounds__(kThreads, 1) void ffn_parts_forward_kernel(Parts X, Parts Wg, Parts Wu, i64 M, i64 F,
+                                                                        int tiles_m, int tiles_f,
+                                                                        float *__restrict__ H, float *__restrict__ G,
+                                                                        float *__restrict__ U, int vec, Whole whole)
+{
+    constexpr int FM = S::FM, FF = S::FF;
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    int tm, tf;
+    tile_of((int)blockIdx.x, (int)gridDim.x, tiles_m, tiles_f, tm, tf);
+    const i64 m0 = (i64)tm * S::BM, f0 = (i64)tf * S::BF;
+    const int bad = own_flags(whole);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / 2 * (FM * 32), wf = wave % 2 * (FF * 32);
+    const uint32_t lds0 = lds_addr(smem);
+
+    // the wave's loads of a stage: [part][group of rows] of X, then of Wg, then of Wu; groups past the end read the last
+    // one (their products are not stored)
+    const char *base[S::LOADS];
+#pragma unroll
+    for (int r = 0; r < S::LOADS; ++r) {
+        const int i = wave + kWaves * r;
+        constexpr int GX = S::BM / kRpi, GW = S::BF / kRpi;
+        if (i < kPlanes * GX) {
+            base[r] = X.at(m0 / kRpi + i % GX, i / GX);
+        } else {
+            const int w = i - kPlanes * GX, v = w < kPlanes * GW ? w : w - kPlanes * GW;
+            base[r] = (w < kPlanes * GW ? Wg : Wu).at(f0 / kRpi + v % GW, v / GW);
+        }
+    }
+    f32x16_t ag[2][FM][FF], au[2][FM][FF];                   // the small products, the large one
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+#pragma unroll
+            for (int y = 0; y < FF; ++y)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) ag[n][x][y][r] = au[n][x][y][r] = 0.0f;
+
+    struct Frag {
+        bf16x8_t x[kPlanes][FM], g[kPlanes][FF], u[kPlanes][FF];
+    };
+    const int li = lane & 31, lk = lane >> 5;
+    const int sw = swizzle<kBK>(li);                         // of every row li + 32 n
+    const auto issue = [&](int c, int r) {
+        dma16_off(base[r] + c * kStageBytes, 16u * lane, lds0 + (uint32_t)(c % kNS) * S::STAGE + 1024 * (wave + kWaves * r));
+    };
+    const auto read = [&](int c, int ks, int j, Frag &f) {
+        const char *L = smem + (c % kNS) * S::STAGE + 16 * ((2 * ks + lk) ^ sw) + li * kRow;
+        const int p = j % kPlanes, n = j / kPlanes;
+        if (n < FM) {
+            f.x[p][n] = *reinterpret_cast<const bf16x8_t *>(L + (p * S::BM + wm + 32 * n) * kRow);
+        } else if (n < FM + FF) {
+            f.g[p][n - FM] =
+                *reinterpret_cast<const bf16x8_t *>(L + (kPlanes * S::BM + p * S::BF + wf + 32 * (n - FM)) * kRow);
+        } else {
+            f.u[p][n - FM - FF] = *reinterpret_cast<const bf16x8_t *>(
+                L + (kPlanes * (S::BM + S::BF) + p * S::BF + wf + 32 * (n - FM - FF)) * kRow);
+        }
+    };
+    const auto mma = [&](int i, const Frag &f) {
+        const int n = i / (2 * FM * FF), x = i / 2 / FF % FM, y = i / 2 % FF;
+        if (i % 2 == 0) {
+            f32x16_t &g = ag[n == kProducts - 1][x][y];
+            g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.g[kWPart[n]][y], f.x[kXPart[n]][x], g, 0, 0, 0);
+        } else {
+            f32x16_t &u = au[n == kProducts - 1][x][y];
+            u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.u[kWPart[n]][y], f.x[kXPart[n]][x], u, 0, 0, 0);
+        }
+    };
+    const int nst = (int)X.stages;
+    start_stages(nst, issue);
+    if (__syncthreads_or(bad)) {
+        wait_vmcnt<0>();
+        __syncthreads();
+        for (int t = 0; t < (S::BM / kTM) * (S::BF / kTN); ++t)
+            any_forward_tile<kThreads, ACT>(whole.a, whole.wg, whole.wu, M, whole.K, F, m0 + t / (S::BF / kTN) * kTM,
+                                            f0 + t % (S::BF / kTN) * kTN, H, G, U, reinterpret_cast<float *>(smem));
+        return;
+    }
+    run_stages<Frag>(nst, issue, read, mma);
+    __syncthreads();                                         // the stages become the output transposes
+
+    constexpr int LDT = FF * 128 + 16;
+    char *L = smem + wave * 32 * LDT;
+    const auto put = [&](int x, auto value, float *O) {
+#pragma unroll
+        for (int y = 0; y < FF; ++y)
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb)
+                put4(reinterpret_cast<float *>(L + li * LDT) + 32 * y + 8 * rb + 4 * lk, value(y, 4 * rb),
+                     value(y, 4 * rb + 1), value(y, 4 * rb + 2), value(y, 4 * rb + 3));
+        store_rows<float, FF * 32, LDT>(L, O, M, F, m0 + wm + 32 * x, f0 + wf, vec != 0, lane);
+    };
+#pragma unroll
+    for (int x = 0; x < FM; ++x) {
+#pragma unroll
+        for (int y = 0; y < FF; ++y)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                ag[1][x][y][r] += ag[0][x][y][r];
+                au[1][x][y][r] += au[0][x][y][r];
+            }
+        put(x, [&](int y, int r) { return act_for<ACT, float>(ag[1][x][y][r]) * au[1][x][y][r]; }, H);
+        if (G != nullptr) {
+            put(x, [&](int y, int r) { return ag[1][x][y][r]; }, G);
+            put(x, [&](int y, int r) { return au[1][x][y][r]; }, U);
+        }
+    }
+}
+
+typedef Shape<128, 64> Tile;
+
+// ---------------------------------------------------------------------------
+// dX = BG Wg + BU Wu: tiles of 128 positions by 128 columns, the stages through
+// both products' features, with several splits each a run of them.
+// W: the parts of Wg, then of Wu, each [block of kCols columns][stage][part][rows
+// of the stage], kCols columns of a row.
+// ---------------------------------------------------------------------------
+struct DxTile {
+    static constexpr int BM = 128, BD = kCols, W_ROW = 2 * BD;
+    static constexpr int A_BYTES = kPlanes * BM * kRow, W_PLANE = kBK * W_ROW, W_BYTES = kPlanes * W_PLANE;
+    static constexpr int STAGE = A_BYTES + W_BYTES, LDS = kNS * STAGE;
+    static constexpr int A_LOADS = A_BYTES / 1024 / kWaves, W_LOADS = W_BYTES / 1024 / kWaves, LOADS = A_LOADS + W_LOADS;
+    static constexpr int FM = BM / 64, FD = BD / 64;
+    static_assert(kPlanes * (FM + FD) == kOperands && kProducts * FM * FD == kMfma && LOADS == kLoads, "steps");
+    static_assert(A_LOADS * kWaves * 1024 == A_BYTES && W_LOADS * kWaves * 1024 == W_BYTES, "stage split");
+    static_assert(kWaves * 32 * (FD * 128 + 16) <= LDS && 4 * kAnyFloats <= LDS, "the outputs' and the fallback's LDS");
+};
+
+template <bool SPLIT>
+__global__ __launch_bounds__(kThreads, 1) void ffn_parts_dx_kernel(Parts BG, Parts BU, const char *__restrict__ W, i64 M,
+                                                                   i64 D, i64 ldw, int tiles_m, int tiles_d, int splits,
+                                                                   float *__restrict__ dX, float *__restrict__ part,
+                                                                   int vec, Whole whole)
+{
+    typedef DxTile S;
+    constexpr int FM = S::FM, FD = S::FD;
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    int tm, td;
+    const int tiles = tiles_m * tiles_d, split = SPLIT ? (int)blockIdx.x / tiles : 0;
+    tile_of((int)blockIdx.x - split * tiles, tiles, tiles_m, tiles_d, tm, td);
+    const i64 m0 = (i64)tm * S::BM, d0 = (i64)td * S::BD;
+    const int bad = own_flags(whole);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / 2 * (FM * 32), wd = wave % 2 * (FD * 32);
+    const uint32_t lds0 = lds_addr(smem);
+    const int half = (int)BG.stages;                         // of each product
+    const int first = SPLIT ? (int)((i64)split * 2 * half / splits) : 0;
+    const int nst = (SPLIT ? (int)((i64)(split + 1) * 2 * half / splits) : 2 * half) - first;
+
+    // groups past the end read the last one (their products are not stored)
+    const char *baseA[2][S::A_LOADS];
+#pragma unroll
+    for (int r = 0; r < S::A_LOADS; ++r) {
+        constexpr int GA = S::BM / kRpi;
+        const int i = wave + kWaves * r;
+        baseA[0][r] = BG.at(m0 / kRpi + i % GA, i / GA);
+        baseA[1][r] = BU.at(m0 / kRpi + i % GA, i / GA);
+    }
+    const i64 w_run = (i64)tiles_d * half * S::W_BYTES;
+    const char *baseW = W + (i64)td * half * S::W_BYTES + 1024 * wave;
+    f32x16_t acc[2][FM][FD];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+#pragma unroll
+            for (int y = 0; y < FD; ++y)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[n][x][y][r] = 0.0f;
+
+    struct Frag {
+        bf16x8_t a[kPlanes][FM], w[kPlanes][FD];
+    };
+    const int li = lane & 31, lk = lane >> 5;
+    const int sw = swizzle<kBK>(li);
+    const auto issue = [&](int c, int r) {
+        const uint32_t L = lds0 + (uint32_t)(c % kNS) * S::STAGE;
+        const int g = first + c, run = g >= half, k = g - run * half;
+        if (r < S::A_LOADS)
+            dma16_off((run ? baseA[1][r] : baseA[0][r]) + k * kStageBytes, 16u * lane, L + 1024 * (wave + kWaves * r));
+        else
+            dma16_off(baseW + run * w_run + (i64)k * S::W_BYTES + 1024 * kWaves * (r - S::A_LOADS), 16u * lane,
+                      L + S::A_BYTES + 1024 * (wave + kWaves * (r - S::A_LOADS)));
+    };
+    const auto read = [&](int c, int ks, int j, Frag &f) {
+        const char *L = smem + (c % kNS) * S::STAGE;
+        const int p = j % kPlanes, n = j / kPlanes;
+        if (n < FM)
+            f.a[p][n] = *reinterpret_cast<const bf16x8_t *>(L + (p * S::BM + wm + 32 * n + li) * kRow +
+                                                            16 * ((2 * ks + lk) ^ sw));
+        else
+            f.w[p][n - FM] = read_operand(L + S::A_BYTES + p * S::W_PLANE, S::W_ROW, 16 * ks, wd + 32 * (n - FM), lane);
+    };
+    const auto mma = [&](int i, const Frag &f) {
+        const int n = i / (FM * FD), x = i / FD % FM, y = i % FD;
+        f32x16_t &a = acc[n == kProducts - 1][x][y];
+        a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[kWPart[n]][y], f.a[kXPart[n]][x], a, 0, 0, 0);
+    };
+    start_stages(nst, issue);
+    if (__syncthreads_or(bad)) {
+        wait_vmcnt<0>();
+        __syncthreads();
+        if (split == 0)
+            for (int t = 0; t < (S::BM / kTM) * (S::BD / kTN); ++t)
+                any_dx_tile<kThreads>(whole.a, whole.b, whole.wg, whole.wu, M, D, whole.K, m0 + t / (S::BD / kTN) * kTM,
+                                      d0 + t % (S::BD / kTN) * kTN, dX, reinterpret_cast<float *>(smem));
+        return;
+    }
+    run_stages<Frag>(nst, issue, read, mma);
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+        for (int y = 0; y < FD; ++y)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[1][x][y][r] += acc[0][x][y][r];
+
+    if constexpr (SPLIT) {
+        float *P = part + (i64)split * M * ldw;
+#pragma unroll
+        for (int x = 0; x < FM; ++x)
+#pragma unroll
+            for (int y = 0; y < FD; ++y)
+#pragma unroll
+                for (int rb = 0; rb < 4; ++rb) {
+                    const i64 m = m0 + wm + 32 * x + li, d = d0 + wd + 32 * y + 8 * rb + 4 * lk;
+                    if (m < M && d < ldw)                    // ldw % 8 == 0: the four are all in or all out
+                        put4(P + m * ldw + d, acc[1][x][y][4 * rb], acc[1][x][y][4 * rb + 1], acc[1][x][y][4 * rb + 2],
+                             acc[1][x][y][4 * rb + 3]);
+                }
+        return;
+    }
+    __syncthreads();
+    constexpr int LDT = FD * 128 + 16;
+    char *L = smem + wave * 32 * LDT;
+#pragma unroll
+    for (int x = 0; x < FM; ++x) {
+#pragma unroll
+        for (int y = 0; y < FD; ++y)
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb)
+                put4(reinterpret_cast<float *>(L + li * LDT) + 32 * y + 8 * rb + 4 * lk, acc[1][x][y][4 * rb],
+                     acc[1][x][y][4 * rb + 1], acc[1][x][y][4 * rb + 2], acc[1][x][y][4 * rb + 3]);
+        store_rows<float, FD * 32, LDT>(L, dX, M, D, m0 + wm + 32 * x, d0 + wd, vec != 0, lane);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// the parts
+// ---------------------------------------------------------------------------
+// x = p[0] + p[1] + p[2] exactly, each a bf16 value (8 bits each, rounded to
+// nearest, so that what the left-out products hold has no preferred sign).
+// Returns true where that fails: infinities and NaN, values so large that
+// they round to infinity, and values under 2^-100, whose last bits may lie
+// below the smallest normal bf16, which the matrix unit takes as zero.
+__device__ __forceinline__ bool split3(float x, uint32_t (&p)[3])
+{
+    const uint32_t e = (__float_as_uint(x) >> 23) & 255u;
+    p[0] = bf16_bits(x);
+    const float r1 = x - bf16_to_f32((uint16_t)p[0]);
+    p[1] = bf16_bits(r1);
+    p[2] = bf16_bits(r1 - bf16_to_f32((uint16_t)p[1]));
+    return x != 0.0f && (e >= 254u || e < 27u);
+}
+
+// Arrays to split: P [rows][cols] as the kilobytes of its parts at O (Parts,
+// or, by_cols, as W of ffn_parts_dx_kernel), zeros past rows and cols.  One
+// launch for all of a call's, a wave per kilobyte of values' worth (the three
+// parts of 64 pieces of eight), first[k] the first of array k, of at most
+// kSplitBlocks workgroups, each leaving a word that says whether it met a
+// value that cannot be split.
+struct Splits {
+    int count;
+    const float *P[4];
+    char *O[4];
+    i64 rows[4], cols[4], stages[4], first[5];
+    int by_cols[4];
+};
+
+__global__ __launch_bounds__(256) void ffn_split_kernel(Splits s, int32_t *__restrict__ flags)
+{
+    const int lane = threadIdx.x & 63;
+    const i64 wave = (i64)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    bool bad = false;
+    for (i64 i = wave; i < s.first[s.count]; i += (i64)gridDim.x * 4) {
+        int k = 0;
+        while (k + 1 < s.count && i >= s.first[k + 1]) ++k;
+        const i64 rows = s.rows[k], cols = s.cols[k], t = i - s.first[k];
+        i64 r, c, at, step;               // the piece's place in P; the first part's kilobyte and the way to the next
+        if (s.by_cols[k]) {
+            const i64 g = t % kWLoads, cs = t / kWLoads, cb = cs / s.stages[k], st = cs - cb * s.stages[k];
+            const int row = lane / 16;
+            r = st * kBK + g * kWRpi + row;
+            c = cb * kCols + 8 * ((lane % 16) ^ (4 * (row & 3)));
+            at = cs * kPlanes * kWLoads + g;
+            step = kWLoads;
+        } else {
+            const i64 group = t / s.stages[k], st = t - group * s.stages[k];
+            const int row = lane / (64 / kRpi);
+            r = group * kRpi + row;
+            c = st * kBK + 8 * ((lane % (64 / kRpi)) ^ swizzle<kBK>(row));
+            at = t * kPlanes;
+            step = 1;
+        }
+        const float *p = s.P[k] + r * cols + c;
+        float x[8];
+        if (cols % 4 == 0 && (reinterpret_cast<uintptr_t>(s.P[k]) & 15) == 0) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool in = r < rows && c + 4 * h < cols;
+                const float4 v = in ? *reinterpret_cast<const float4 *>(p + 4 * h) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) x[q] = r < rows && c + q < cols ? p[q] : 0.0f;
+        }
+        uint32_t w[3][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint32_t a[3], b[3];
+            bad |= split3(x[2 * q], a);
+            bad |= split3(x[2 * q + 1], b);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) w[n][q] = a[n] | (b[n] << 16);
+        }
+#pragma unroll
+        for (int n = 0; n < 3; ++n)
+            *reinterpret_cast<uint4 *>(s.O[k] + (at + n * step) * 1024 + 16 * lane) =
+                make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
+    }
+    const int any = __syncthreads_or(bad);
+    if (threadIdx.x == 0) flags[blockIdx.x] = any;
+}
+
+constexpr size_t kFlagBytes = sizeof(int32_t) * kSplitBlocks;
+
+i64 stages_of(i64 features) { return ceil_div(features, kBK); }
+
+// kilobytes of one part of [rows][features], and of [features][cols] by columns
+i64 row_parts(i64 rows, i64 features) { return ceil_div(rows, kRpi) * stages_of(features); }
+i64 col_parts(i64 features, i64 cols) { return ceil_div(cols, kCols) * stages_of(features) * kWLoads; }
+
+// Adds P's split at ws, which is moved on; returns where.
+char *add_split(Splits &s, const float *P, i64 rows, i64 cols, bool by_cols, char *&ws)
+{
+    const int k = s.count++;
+    const i64 n = by_cols ? col_parts(rows, cols) : row_parts(rows, cols);
+    s.P[k] = P;
+    s.O[k] = ws;
+    s.rows[k] = rows;
+    s.cols[k] = cols;
+    s.stages[k] = stages_of(by_cols ? rows : cols);
+    s.by_cols[k] = by_cols;
+    s.first[k + 1] = s.first[k] + n;
+    ws += kPlanes * 1024 * n;
+    return s.O[k];
+}
+
+Parts add_rows(Splits &s, const float *P, i64 rows, i64 cols, char *&ws)
+{
+    const char *p = add_split(s, P, rows, cols, false, ws);
+    return Parts{p, ceil_div(rows, kRpi), stages_of(cols)};
+}
+
+// Splits the arrays; returns how many words were left at flags.
+int split(const Splits &s, int32_t *flags, hipStream_t stream)
+{
+    const i64 blocks = ceil_div(s.first[s.count], 4);
+    const int n = (int)(blocks < kSplitBlocks ? blocks : kSplitBlocks);
+    ffn_split_kernel<<<(unsigned)n, 256, 0, stream>>>(s, flags);
+    return n;
+}
+
+// Splits of the features: rounds of 256 workgroups, each of its stages at 0.85
+// us, and the partial tiles written and read.
+int dx_splits(i64 M, i64 D, i64 F)
+{
+    const i64 stages = 2 * stages_of(F), tiles = ceil_div(M, DxTile::BM) * ceil_div(D, DxTile::BD);
+    double best = 1e30;
+    int splits = 1;
+    for (int s = 1; s <= 16 && s <= stages / 4 + 1; ++s) {
+        const double t = (double)ceil_div(tiles * s, 256) * (5.0 + 0.85 * (double)ceil_div(stages, s)) +
+                         (s > 1 ? 4.0 + 8.0 * s * (double)M * (double)D / 4.5e6 : 0.0);
+        if (t < best) {
+            best = t;
+            splits = s;
+        }
+    }
+    return splits;
+}
+
+}  // namespace
+
+size_t ffn_parts_forward_workspace(i64 M, i64 K, i64 F)
+{
+    return kFlagBytes + kPlanes * 1024 * (size_t)(row_parts(M, K) + 2 * row_parts(F, K));
+}
+
+void ffn_parts_forward(const float *X, const float *Wg, const float *Wu, i64 M, i64 K, i64 F, dp_act act, float *H,
+                       float *G, float *U, void *ws, hipStream_t stream)
+{
+    int32_t *flags = (int32_t *)ws;
+    char *w = (char *)ws + kFlagBytes;
+    Splits s = {};
+    const Parts x = add_rows(s, X, M, K, w), g = add_rows(s, Wg, F, K, w), u = add_rows(s, Wu, F, K, w);
+    const Whole whole = {X, nullptr, Wg, Wu, K, flags, split(s, flags, stream)};
+    const int tm = (int)ceil_div(M, Tile::BM), tf = (int)ceil_div(F, Tile::BF);
+    const int vec = F % 4 == 0 && aligned(H, 16) && aligned(G, 16) && aligned(U, 16);
+    const unsigned grid = (unsigned)((i64)tm * tf);
+    if (act == DP_ACT_SILU)
+        ffn_parts_forward_kernel<Tile, DP_ACT_SILU><<<grid, kThreads, 0, stream>>>(x, g, u, M, F, tm, tf, H, G, U, vec,
+                                                                                  whole);
+    else
+        ffn_parts_forward_kernel<Tile, DP_ACT_GELU_TANH><<<grid, kThreads, 0, stream>>>(x, g, u, M, F, tm, tf, H, G, U,
+                                                                                       vec, whole);
+}
+
+size_t ffn_parts_dx_workspace(i64 M, i64 D, i64 F)
+{
+    const int splits = dx_splits(M, D, F);
+    const size_t part = splits > 1 ? sizeof(float) * (size_t)splits * (size_t)(M * padded(D)) : 0;
+    return kFlagBytes + kPlanes * 1024 * (size_t)(2 * row_parts(M, F) + 2 * col_parts(F, D)) + part;
+}
+
+void ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F, float *dX,
+                  void *ws, hipStream_t stream)
+{
+    const i64 ldw = padded(D);
+    const int splits = dx_splits(M, D, F);
+    int32_t *flags = (int32_t *)ws;
+    char *w = (char *)ws + kFlagBytes;
+    Splits s = {};
+    const Parts g = add_rows(s, BG, M, F, w), u = add_rows(s, BU, M, F, w);
+    const char *W = add_split(s, Wg, F, D, true, w);
+    add_split(s, Wu, F, D, true, w);                         // behind Wg's
+    float *part = (float *)w;
+    const Whole whole = {BG, BU, Wg, Wu, F, flags, split(s, flags, stream)};
+    const int tm = (int)ceil_div(M, DxTile::BM), td = (int)ceil_div(D, DxTile::BD);
+    const int vec = D % 4 == 0 && aligned(dX, 16);
+    const unsigned grid = (unsigned)((i64)tm * td * splits);
+    if (splits == 1) {
+        ffn_parts_dx_kernel<false><<<grid, kThreads, 0, stream>>>(g, u, W, M, D, ldw, tm, td, 1, dX, nullptr, vec, whole);
+        return;
+    }
+    ffn_parts_dx_kernel<true><<<grid, kThreads, 0, stream>>>(g, u, W, M, D, ldw, tm, td, splits, dX, part, vec, whole);
+    sum_splits(part, M, D, ldw, splits, dX, whole, stream);
+}
+
+}  // namespace dpg
