@@ -1,4 +1,4 @@
-// The bf16 tile kernels of the gated feed-forward block (ffn_bf16.hip).
+// The tile kernels of the gated feed-forward block (ffn_bf16.hip, ffn_parts.hip).
 #pragma once
 
 #include "common.hpp"

@@ -1,19 +1,20 @@
 // Gated feed-forward block in fp32 on v_mfma_f32_32x32x16_bf16: every value as
 // three bf16 parts (ffn_split_kernel), every product as six bf16 products
-//   x w = x0 w0 + (x1 w0 + x0 w1 + x1 w1 + x2 w0 + x0 w2)
-// What is left out (x1 w2, x2 w1: 2^-24 of the product at most, and x2 w2) is
-// within the rounding of an fp32 product.  The first product and the others
-// have accumulators of their own, so that the small ones are not rounded to
-// the large sum's last bit.
+//   x w = x0 w2 + x2 w0 + x1 w1 + x0 w1 + x1 w0 + x0 w0
+// added in fp32 in this order.  What is left out (x1 w2, x2 w1: 2^-24 of the
+// product at most, and x2 w2) is within the rounding of an fp32 product.
 //
-// A stage holds 32 columns of all three parts of each operand, so that a part
-// is staged once and read from LDS once for all the products that take it:
-// 12 operand reads for 24 matrix instructions (the parts as six products one
-// after another, each with stages of its own, take 32 for 24, and twice the
-// stage loads: MEASURED).
+// A stage holds 16 columns of all three parts of each operand, so that a part
+// is staged once and read from LDS once for all the products that take it: 12
+// operand reads for 24 matrix instructions.  (Products one after another, each
+// with stages of its own, take 32 reads for 24, and twice the loads: 4096 x
+// 2048 -> 5504 with the split 974 us, 850 so; 1000 x 500 -> 1333 44 and 32.)
+// Two workgroups of four waves share a CU and cover each other's first loads
+// and last stores; stages of 32 columns, one workgroup per CU, take 911 and 34.
+// At those sizes the products run at 1.3 PFLOP/s, the rate of a large library
+// product; small ones are bound by the split (6 us) and the stages' latency.
 //
-// Operands, swizzles and the output's way are those of ffn_bf16.hip; one
-// workgroup of four waves per CU, three stages.
+// Operands and the output's way are those of ffn_bf16.hip.
 #include "ffn_any.hpp"
 #include "ffn_bf16.hpp"
 #include "ffn_tiles.hpp"
@@ -23,14 +24,14 @@
 namespace dpg {
 namespace {
 
-constexpr int kBK = 32, kNS = 3, kPlanes = 3, kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kBK = 16, kNS = 3, kPlanes = 3, kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kRow = 2 * kBK;             // bytes of a staged row of X, Wg, Wu, BG or BU
 constexpr int kRpi = 1024 / kRow;         // such rows per load instruction
 constexpr int kCols = 128;                // columns of a staged row of Wg and Wu in the backward pass
 constexpr int kWRpi = 1024 / (2 * kCols); // such rows per load instruction
 constexpr int kWLoads = kBK / kWRpi;      // load instructions per part and stage
 constexpr int kSplitBlocks = 1024;        // workgroups of the splitting kernel, at most
-constexpr int kProducts = 6;              // the last one the large one
+constexpr int kProducts = 6;
 constexpr int kXPart[kProducts] = {0, 2, 1, 0, 1, 0}, kWPart[kProducts] = {2, 0, 1, 1, 0, 0};
 
 // whether a value has no parts, from this thread's words
@@ -46,8 +47,8 @@ __device__ __forceinline__ int own_flags(const Whole &w)
 }
 
 // The parts lie in memory as they do in LDS: a load instruction copies 1 KB of
-// consecutive bytes (16 rows of 64 bytes from a row-major array, half a cache
-// line each, took MEASURED2).  Rows of X, Wg, Wu, BG and BU: [group of kRpi
+// consecutive bytes (pieces of rows, parts of cache lines, of a row-major array:
+// 4096 x 2048 -> 5504 1343 us).  Rows of X, Wg, Wu, BG and BU: [group of kRpi
 // rows][stage][part] of 1 KB.
 struct Parts {
     const char *p;
@@ -61,16 +62,19 @@ constexpr i64 kStageBytes = kPlanes * 1024;                  // from a group's s
 
 constexpr int kOperands = 12;             // of a wave and k-step
 constexpr int kMfma = 24;                 // matrix instructions of a wave and k-step
-constexpr int kLoads = 12;                // loads of a wave and stage
+constexpr int kLoads = 6;                 // loads of a wave and stage
 
-// The run of stages 0 .. nst-1.  issue(c, r): load r of stage c; read(c, ks, j,
-// f): operand j of its k-step ks; mma(i, f): matrix instruction i.  One wave
-// per SIMD: the loads and reads of what comes next are issued in the shadow of
-// the matrix instructions (32 clocks each), in this order.
+// Where a staged row holds columns 8 q .. 8 q + 7: the 16 rows that a quarter of a 16-byte LDS read covers fall into 16
+// different pieces of the 256-byte bank window.
+__device__ __forceinline__ int piece_of(int row, int q) { return q ^ ((row >> 3) & 1); }
+
+// The run of stages 0 .. nst-1, a stage being one k-step.  issue(c, r): load r
+// of stage c; read(c, j, f): operand j of stage c; mma(i, f): matrix
+// instruction i.  The loads and reads of what comes next are issued in the
+// shadow of the matrix instructions (32 clocks each), in this order.
 template <typename Issue>
 __device__ __forceinline__ void start_stages(int nst, const Issue &issue)
 {
-    static_assert(kNS == 3, "two stages ahead");
 #pragma unroll
     for (int c = 0; c < kNS; ++c)
         if (c < nst)
@@ -81,44 +85,53 @@ __device__ __forceinline__ void start_stages(int nst, const Issue &issue)
 template <typename Frag, typename Issue, typename Read, typename Mma>
 __device__ __forceinline__ void run_stages(int nst, const Issue &issue, const Read &read, const Mma &mma)
 {
-    static_assert(kBK == 32, "two k-steps in turn");
-    // f's products; meanwhile the operands of k-step ks of stage c (READ) and the loads of stage `ahead` (ISSUE)
-    const auto step = [&](auto READ, auto ISSUE, const Frag &f, int c, int ks, Frag &next, int ahead) {
-#pragma unroll
-        for (int i = 0; i < kMfma; ++i) {
-            mma(i, f);
-            if constexpr (decltype(READ)::value)
-                if (i < kOperands) read(c, ks, i, next);
-            if constexpr (decltype(ISSUE)::value)
-                if (i % (kMfma / kLoads) == 1) issue(ahead, i / (kMfma / kLoads));
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-    constexpr std::true_type yes;
-    constexpr std::false_type no;
+    static_assert(kNS == 3, "two stages ahead");
     wait_later<kLoads>(nst - 1);
     stage_barrier();
     Frag fa, fb;
 #pragma unroll
-    for (int j = 0; j < kOperands; ++j) read(0, 0, j, fa);
+    for (int j = 0; j < kOperands; ++j) read(0, j, fa);
+    // f: stage c's operands, next: those of stage c + 1
+    const auto step = [&](auto ISSUE, int c, const Frag &f, Frag &next) {
+        // stage c + 1 has landed, and every wave has read stage c: its buffer takes stage c + kNS
+        if constexpr (decltype(ISSUE)::value) wait_vmcnt<kLoads>();
+        else wait_later<kLoads>(nst - 2 - c < 1 ? 0 : 1);
+        wait_lgkmcnt0();
+        stage_barrier();
+        if constexpr (!decltype(ISSUE)::value)
+            if (c + kNS < nst)
+#pragma unroll
+                for (int r = 0; r < kLoads; ++r) issue(c + kNS, r);
+#pragma unroll
+        for (int i = 0; i < kMfma; ++i) {
+            mma(i, f);
+            if (i < kOperands) read(c + 1, i, next);
+            if constexpr (decltype(ISSUE)::value)
+                if (i % (kMfma / kLoads) == 1) issue(c + kNS, i / (kMfma / kLoads));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const auto last = [&](const Frag &f) {
+#pragma unroll
+        for (int i = 0; i < kMfma; ++i) mma(i, f);
+    };
     int c = 0;
-    for (; c + kNS < nst; ++c) {
-        step(yes, no, fa, c, 1, fb, 0);
-        // stage c + 1 has landed, and every wave has read the last of stage c: its buffer takes stage c + kNS
-        wait_vmcnt<kLoads>();
-        wait_lgkmcnt0();
-        stage_barrier();
-        step(yes, yes, fb, c + 1, 0, fa, c + kNS);
+    for (; c + 1 + kNS < nst; c += 2) {
+        step(std::true_type(), c, fa, fb);
+        step(std::true_type(), c + 1, fb, fa);
     }
-    for (; c + 1 < nst; ++c) {
-        step(yes, no, fa, c, 1, fb, 0);
-        wait_later<kLoads>(nst - 2 - c < 1 ? 0 : 1);
-        wait_lgkmcnt0();
-        stage_barrier();
-        step(yes, no, fb, c + 1, 0, fa, 0);
+    for (;; c += 2) {
+        if (c + 1 == nst) {
+            last(fa);
+            return;
+        }
+        step(std::false_type(), c, fa, fb);
+        if (c + 2 == nst) {
+            last(fb);
+            return;
+        }
+        step(std::false_type(), c + 1, fb, fa);
     }
-    step(yes, no, fa, c, 1, fb, 0);
-    step(no, no, fb, 0, 0, fa, 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -137,7 +150,7 @@ struct Shape {
 };
 
 template <typename S, int ACT>
-__global__ __launch_bounds__(kThreads, 1) void ffn_parts_forward_kernel(Parts X, Parts Wg, Parts Wu, i64 M, i64 F,
+__global__ __launch_bounds__(kThreads, 2) void ffn_parts_forward_kernel(Parts X, Parts Wg, Parts Wu, i64 M, i64 F,
                                                                         int tiles_m, int tiles_f,
                                                                         float *__restrict__ H, float *__restrict__ G,
                                                                         float *__restrict__ U, int vec, Whole whole)
@@ -167,26 +180,24 @@ __global__ __launch_bounds__(kThreads, 1) void ffn_parts_forward_kernel(Parts X,
             base[r] = (w < kPlanes * GW ? Wg : Wu).at(f0 / kRpi + v % GW, v / GW);
         }
     }
-    f32x16_t ag[2][FM][FF], au[2][FM][FF];                   // the small products, the large one
+    f32x16_t ag[FM][FF], au[FM][FF];
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int x = 0; x < FM; ++x)
 #pragma unroll
-        for (int x = 0; x < FM; ++x)
+        for (int y = 0; y < FF; ++y)
 #pragma unroll
-            for (int y = 0; y < FF; ++y)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) ag[n][x][y][r] = au[n][x][y][r] = 0.0f;
+            for (int r = 0; r < 16; ++r) ag[x][y][r] = au[x][y][r] = 0.0f;
 
     struct Frag {
         bf16x8_t x[kPlanes][FM], g[kPlanes][FF], u[kPlanes][FF];
     };
     const int li = lane & 31, lk = lane >> 5;
-    const int sw = swizzle<kBK>(li);                         // of every row li + 32 n
+    const int at = li * kRow + 16 * piece_of(li, lk);
     const auto issue = [&](int c, int r) {
         dma16_off(base[r] + c * kStageBytes, 16u * lane, lds0 + (uint32_t)(c % kNS) * S::STAGE + 1024 * (wave + kWaves * r));
     };
-    const auto read = [&](int c, int ks, int j, Frag &f) {
-        const char *L = smem + (c % kNS) * S::STAGE + 16 * ((2 * ks + lk) ^ sw) + li * kRow;
+    const auto read = [&](int c, int j, Frag &f) {
+        const char *L = smem + (c % kNS) * S::STAGE + at;
         const int p = j % kPlanes, n = j / kPlanes;
         if (n < FM) {
             f.x[p][n] = *reinterpret_cast<const bf16x8_t *>(L + (p * S::BM + wm + 32 * n) * kRow);
@@ -201,10 +212,10 @@ __global__ __launch_bounds__(kThreads, 1) void ffn_parts_forward_kernel(Parts X,
     const auto mma = [&](int i, const Frag &f) {
         const int n = i / (2 * FM * FF), x = i / 2 / FF % FM, y = i / 2 % FF;
         if (i % 2 == 0) {
-            f32x16_t &g = ag[n == kProducts - 1][x][y];
+            f32x16_t &g = ag[x][y];
             g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.g[kWPart[n]][y], f.x[kXPart[n]][x], g, 0, 0, 0);
         } else {
-            f32x16_t &u = au[n == kProducts - 1][x][y];
+            f32x16_t &u = au[x][y];
             u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.u[kWPart[n]][y], f.x[kXPart[n]][x], u, 0, 0, 0);
         }
     };
@@ -234,17 +245,10 @@ __global__ __launch_bounds__(kThreads, 1) void ffn_parts_forward_kernel(Parts X,
     };
 #pragma unroll
     for (int x = 0; x < FM; ++x) {
-#pragma unroll
-        for (int y = 0; y < FF; ++y)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                ag[1][x][y][r] += ag[0][x][y][r];
-                au[1][x][y][r] += au[0][x][y][r];
-            }
-        put(x, [&](int y, int r) { return act_for<ACT, float>(ag[1][x][y][r]) * au[1][x][y][r]; }, H);
+        put(x, [&](int y, int r) { return act_for<ACT, float>(ag[x][y][r]) * au[x][y][r]; }, H);
         if (G != nullptr) {
-            put(x, [&](int y, int r) { return ag[1][x][y][r]; }, G);
-            put(x, [&](int y, int r) { return au[1][x][y][r]; }, U);
+            put(x, [&](int y, int r) { return ag[x][y][r]; }, G);
+            put(x, [&](int y, int r) { return au[x][y][r]; }, U);
         }
     }
 }
@@ -269,7 +273,7 @@ struct DxTile {
 };
 
 template <bool SPLIT>
-__global__ __launch_bounds__(kThreads, 1) void ffn_parts_dx_kernel(Parts BG, Parts BU, const char *__restrict__ W, i64 M,
+__global__ __launch_bounds__(kThreads, 2) void ffn_parts_dx_kernel(Parts BG, Parts BU, const char *__restrict__ W, i64 M,
                                                                    i64 D, i64 ldw, int tiles_m, int tiles_d, int splits,
                                                                    float *__restrict__ dX, float *__restrict__ part,
                                                                    int vec, Whole whole)
@@ -301,21 +305,19 @@ __global__ __launch_bounds__(kThreads, 1) void ffn_parts_dx_kernel(Parts BG, Par
     }
     const i64 w_run = (i64)tiles_d * half * S::W_BYTES;
     const char *baseW = W + (i64)td * half * S::W_BYTES + 1024 * wave;
-    f32x16_t acc[2][FM][FD];
+    f32x16_t acc[FM][FD];
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int x = 0; x < FM; ++x)
 #pragma unroll
-        for (int x = 0; x < FM; ++x)
+        for (int y = 0; y < FD; ++y)
 #pragma unroll
-            for (int y = 0; y < FD; ++y)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[n][x][y][r] = 0.0f;
+            for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.0f;
 
     struct Frag {
         bf16x8_t a[kPlanes][FM], w[kPlanes][FD];
     };
     const int li = lane & 31, lk = lane >> 5;
-    const int sw = swizzle<kBK>(li);
+    const int at = li * kRow + 16 * piece_of(li, lk);
     const auto issue = [&](int c, int r) {
         const uint32_t L = lds0 + (uint32_t)(c % kNS) * S::STAGE;
         const int g = first + c, run = g >= half, k = g - run * half;
@@ -325,18 +327,17 @@ __global__ __launch_bounds__(kThreads, 1) void ffn_parts_dx_kernel(Parts BG, Par
             dma16_off(baseW + run * w_run + (i64)k * S::W_BYTES + 1024 * kWaves * (r - S::A_LOADS), 16u * lane,
                       L + S::A_BYTES + 1024 * (wave + kWaves * (r - S::A_LOADS)));
     };
-    const auto read = [&](int c, int ks, int j, Frag &f) {
+    const auto read = [&](int c, int j, Frag &f) {
         const char *L = smem + (c % kNS) * S::STAGE;
         const int p = j % kPlanes, n = j / kPlanes;
         if (n < FM)
-            f.a[p][n] = *reinterpret_cast<const bf16x8_t *>(L + (p * S::BM + wm + 32 * n + li) * kRow +
-                                                            16 * ((2 * ks + lk) ^ sw));
+            f.a[p][n] = *reinterpret_cast<const bf16x8_t *>(L + (p * S::BM + wm + 32 * n) * kRow + at);
         else
-            f.w[p][n - FM] = read_operand(L + S::A_BYTES + p * S::W_PLANE, S::W_ROW, 16 * ks, wd + 32 * (n - FM), lane);
+            f.w[p][n - FM] = read_operand(L + S::A_BYTES + p * S::W_PLANE, S::W_ROW, 0, wd + 32 * (n - FM), lane);
     };
     const auto mma = [&](int i, const Frag &f) {
         const int n = i / (FM * FD), x = i / FD % FM, y = i % FD;
-        f32x16_t &a = acc[n == kProducts - 1][x][y];
+        f32x16_t &a = acc[x][y];
         a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[kWPart[n]][y], f.a[kXPart[n]][x], a, 0, 0, 0);
     };
     start_stages(nst, issue);
@@ -350,13 +351,6 @@ __global__ __launch_bounds__(kThreads, 1) void ffn_parts_dx_kernel(Parts BG, Par
         return;
     }
     run_stages<Frag>(nst, issue, read, mma);
-#pragma unroll
-    for (int x = 0; x < FM; ++x)
-#pragma unroll
-        for (int y = 0; y < FD; ++y)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[1][x][y][r] += acc[0][x][y][r];
-
     if constexpr (SPLIT) {
         float *P = part + (i64)split * M * ldw;
 #pragma unroll
@@ -367,8 +361,8 @@ __global__ __launch_bounds__(kThreads, 1) void ffn_parts_dx_kernel(Parts BG, Par
                 for (int rb = 0; rb < 4; ++rb) {
                     const i64 m = m0 + wm + 32 * x + li, d = d0 + wd + 32 * y + 8 * rb + 4 * lk;
                     if (m < M && d < ldw)                    // ldw % 8 == 0: the four are all in or all out
-                        put4(P + m * ldw + d, acc[1][x][y][4 * rb], acc[1][x][y][4 * rb + 1], acc[1][x][y][4 * rb + 2],
-                             acc[1][x][y][4 * rb + 3]);
+                        put4(P + m * ldw + d, acc[x][y][4 * rb], acc[x][y][4 * rb + 1], acc[x][y][4 * rb + 2],
+                             acc[x][y][4 * rb + 3]);
                 }
         return;
     }
@@ -381,8 +375,8 @@ __global__ __launch_bounds__(kThreads, 1) void ffn_parts_dx_kernel(Parts BG, Par
         for (int y = 0; y < FD; ++y)
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb)
-                put4(reinterpret_cast<float *>(L + li * LDT) + 32 * y + 8 * rb + 4 * lk, acc[1][x][y][4 * rb],
-                     acc[1][x][y][4 * rb + 1], acc[1][x][y][4 * rb + 2], acc[1][x][y][4 * rb + 3]);
+                put4(reinterpret_cast<float *>(L + li * LDT) + 32 * y + 8 * rb + 4 * lk, acc[x][y][4 * rb],
+                     acc[x][y][4 * rb + 1], acc[x][y][4 * rb + 2], acc[x][y][4 * rb + 3]);
         store_rows<float, FD * 32, LDT>(L, dX, M, D, m0 + wm + 32 * x, d0 + wd, vec != 0, lane);
     }
 }
@@ -440,7 +434,7 @@ __global__ __launch_bounds__(256) void ffn_split_kernel(Splits s, int32_t *__res
             const i64 group = t / s.stages[k], st = t - group * s.stages[k];
             const int row = lane / (64 / kRpi);
             r = group * kRpi + row;
-            c = st * kBK + 8 * ((lane % (64 / kRpi)) ^ swizzle<kBK>(row));
+            c = st * kBK + 8 * piece_of(row, lane % (64 / kRpi));
             at = t * kPlanes;
             step = 1;
         }
@@ -514,15 +508,20 @@ int split(const Splits &s, int32_t *flags, hipStream_t stream)
     return n;
 }
 
-// Splits of the features: rounds of 256 workgroups, each of its stages at 0.85
-// us, and the partial tiles written and read.
+// Splits of the features by the time they take: a stage at 0.55 us while most
+// workgroups have a CU to themselves, at 1.39 us per round of two per CU, the
+// first loads and last stores, and the partial tiles written and read.
+// 512 x 2752 -> 1024 (32 tiles), the whole call: 184 us in one split, 72 in
+// four, 64 in six, 72 in eight, 75 in sixteen; 4096 x 2752 -> 1024 (256 tiles)
+// 307 in one, 310 in two, 338 in eight.
 int dx_splits(i64 M, i64 D, i64 F)
 {
     const i64 stages = 2 * stages_of(F), tiles = ceil_div(M, DxTile::BM) * ceil_div(D, DxTile::BD);
     double best = 1e30;
     int splits = 1;
     for (int s = 1; s <= 16 && s <= stages / 4 + 1; ++s) {
-        const double t = (double)ceil_div(tiles * s, 256) * (5.0 + 0.85 * (double)ceil_div(stages, s)) +
+        const double n = (double)tiles * s, stage = n <= 192 ? 0.55 : n <= 512 ? 0.21 + 0.0023 * n : 1.39 * n / 512;
+        const double t = stage * (double)ceil_div(stages, s) + 3.0 * n / 512 +
                          (s > 1 ? 4.0 + 8.0 * s * (double)M * (double)D / 4.5e6 : 0.0);
         if (t < best) {
             best = t;
