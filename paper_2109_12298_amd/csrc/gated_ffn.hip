@@ -19,23 +19,25 @@ using namespace ffn;
 constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------------------
-// Any size, type and alignment (ffn_any.hpp): a workgroup per 64 x 64 tile.
+// bf16 of any size and alignment (ffn_any.hpp): a workgroup per 64 x 64 tile.
 // ---------------------------------------------------------------------------
-template <typename T, int ACT>
-__global__ __launch_bounds__(kThreads) void ffn_forward_any_kernel(const T *__restrict__ X, const T *__restrict__ Wg,
-                                                                   const T *__restrict__ Wu, i64 M, i64 K, i64 F,
-                                                                   i64 tiles_f, T *__restrict__ H, T *__restrict__ G,
-                                                                   T *__restrict__ U)
+template <int ACT>
+__global__ __launch_bounds__(kThreads) void ffn_forward_any_kernel(const uint16_t *__restrict__ X,
+                                                                   const uint16_t *__restrict__ Wg,
+                                                                   const uint16_t *__restrict__ Wu, i64 M, i64 K, i64 F,
+                                                                   i64 tiles_f, uint16_t *__restrict__ H,
+                                                                   uint16_t *__restrict__ G, uint16_t *__restrict__ U)
 {
     __shared__ float lds[kAnyFloats];
     const i64 b = xcd_swizzle(blockIdx.x, gridDim.x);
     any_forward_tile<kThreads, ACT>(X, Wg, Wu, M, K, F, b / tiles_f * kTM, b % tiles_f * kTN, H, G, U, lds);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void ffn_dx_any_kernel(const T *__restrict__ BG, const T *__restrict__ BU,
-                                                              const T *__restrict__ Wg, const T *__restrict__ Wu, i64 M,
-                                                              i64 D, i64 F, i64 tiles_d, T *__restrict__ dX)
+__global__ __launch_bounds__(kThreads) void ffn_dx_any_kernel(const uint16_t *__restrict__ BG,
+                                                              const uint16_t *__restrict__ BU,
+                                                              const uint16_t *__restrict__ Wg,
+                                                              const uint16_t *__restrict__ Wu, i64 M, i64 D, i64 F,
+                                                              i64 tiles_d, uint16_t *__restrict__ dX)
 {
     __shared__ float lds[kAnyFloats];
     const i64 b = xcd_swizzle(blockIdx.x, gridDim.x);
@@ -86,13 +88,13 @@ __global__ __launch_bounds__(kThreads) void ffn_backprops_kernel(const T *dH, co
     }
 }
 
-template <typename T, int ACT>
-void forward(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, void *H, void *G, void *U,
-             hipStream_t stream)
+template <int ACT>
+void forward_any(const uint16_t *X, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 K, i64 F, uint16_t *H, uint16_t *G,
+                 uint16_t *U, hipStream_t stream)
 {
     const i64 tiles_f = ceil_div(F, kTN);
-    ffn_forward_any_kernel<T, ACT><<<(unsigned)(ceil_div(M, kTM) * tiles_f), kThreads, 0, stream>>>(
-        (const T *)X, (const T *)Wg, (const T *)Wu, M, K, F, tiles_f, (T *)H, (T *)G, (T *)U);
+    ffn_forward_any_kernel<ACT><<<(unsigned)(ceil_div(M, kTM) * tiles_f), kThreads, 0, stream>>>(X, Wg, Wu, M, K, F, tiles_f,
+                                                                                                H, G, U);
 }
 
 template <typename T, int ACT>
@@ -110,13 +112,11 @@ void backprops(const void *dH, const void *G, const void *U, i64 n, void *BG, vo
                                                                       (T *)BG, (T *)BU);
 }
 
-template <typename T>
-void dx(const void *BG, const void *BU, const void *Wg, const void *Wu, i64 M, i64 D, i64 F, void *dX,
-        hipStream_t stream)
+void dx_any(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const uint16_t *Wu, i64 M, i64 D, i64 F,
+            uint16_t *dX, hipStream_t stream)
 {
     const i64 tiles_d = ceil_div(D, kTN);
-    ffn_dx_any_kernel<T><<<(unsigned)(ceil_div(M, kTM) * tiles_d), kThreads, 0, stream>>>(
-        (const T *)BG, (const T *)BU, (const T *)Wg, (const T *)Wu, M, D, F, tiles_d, (T *)dX);
+    ffn_dx_any_kernel<<<(unsigned)(ceil_div(M, kTM) * tiles_d), kThreads, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, tiles_d, dX);
 }
 
 dp_status check_sizes(i64 M, i64 D, i64 F)
@@ -169,18 +169,16 @@ extern "C" dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const v
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
     if (by_rows(X, Wg, Wu, dt, M, d_in)) {
         ffn_rows_forward(X, Wg, Wu, dt, M, d_in, d_ff, act, H, G, U, stream);
-    } else if (dt == DP_F32 && d_in < kFfnTilesMax) {
+    } else if (dt == DP_F32) {
         ffn_parts_forward((const float *)X, (const float *)Wg, (const float *)Wu, M, d_in, d_ff, act, (float *)H, (float *)G,
                           (float *)U, ws, stream);
-    } else if (dt == DP_F32) {
-        if (act == DP_ACT_SILU) forward<float, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
-        else forward<float, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
-    } else if (ffn_tiles_ok(X, d_in) && ffn_tiles_ok(Wg, d_in) && ffn_tiles_ok(Wu, d_in)) {
-        ffn_bf16_forward((const uint16_t *)X, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in, d_ff, act,
-                         (uint16_t *)H, (uint16_t *)G, (uint16_t *)U, ws, stream);
     } else {
-        if (act == DP_ACT_SILU) forward<uint16_t, DP_ACT_SILU>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
-        else forward<uint16_t, DP_ACT_GELU_TANH>(X, Wg, Wu, M, d_in, d_ff, H, G, U, stream);
+        const uint16_t *x = (const uint16_t *)X, *wg = (const uint16_t *)Wg, *wu = (const uint16_t *)Wu;
+        uint16_t *h = (uint16_t *)H, *g = (uint16_t *)G, *u = (uint16_t *)U;
+        if (ffn_tiles_ok(X, d_in) && ffn_tiles_ok(Wg, d_in) && ffn_tiles_ok(Wu, d_in))
+            ffn_bf16_forward(x, wg, wu, M, d_in, d_ff, act, h, g, u, ws, stream);
+        else if (act == DP_ACT_SILU) forward_any<DP_ACT_SILU>(x, wg, wu, M, d_in, d_ff, h, g, u, stream);
+        else forward_any<DP_ACT_GELU_TANH>(x, wg, wu, M, d_in, d_ff, h, g, u, stream);
     }
     return launch_status();
 }
@@ -214,21 +212,20 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
         if (M <= kFfnRowsMax) {
             ffn_rows_dx((const float *)BG, (const float *)BU, (const float *)Wg, (const float *)Wu, M, d_in, d_ff,
                         (float *)dX, ws, stream);
-        } else if (d_in < kFfnTilesMax && d_ff < kFfnTilesMax) {
+        } else {
             ffn_parts_dx((const float *)BG, (const float *)BU, (const float *)Wg, (const float *)Wu, M, d_in, d_ff,
                          (float *)dX, ws, stream);
-        } else {
-            dx<float>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
         }
     } else {
         if (act == DP_ACT_SILU) backprops<uint16_t, DP_ACT_SILU>(dH, G, U, n, BG, BU, stream);
         else backprops<uint16_t, DP_ACT_GELU_TANH>(dH, G, U, n, BG, BU, stream);
         if (dX == nullptr) return launch_status();
+        const uint16_t *bg = (const uint16_t *)BG, *bu = (const uint16_t *)BU;
+        const uint16_t *wg = (const uint16_t *)Wg, *wu = (const uint16_t *)Wu;
         if (ffn_tiles_ok(BG, d_ff) && ffn_tiles_ok(BU, d_ff) && ffn_tiles_ok(Wg, d_in) && ffn_tiles_ok(Wu, d_in))
-            ffn_bf16_dx((const uint16_t *)BG, (const uint16_t *)BU, (const uint16_t *)Wg, (const uint16_t *)Wu, M, d_in,
-                        d_ff, (uint16_t *)dX, ws, stream);
+            ffn_bf16_dx(bg, bu, wg, wu, M, d_in, d_ff, (uint16_t *)dX, ws, stream);
         else
-            dx<uint16_t>(BG, BU, Wg, Wu, M, d_in, d_ff, dX, stream);
+            dx_any(bg, bu, wg, wu, M, d_in, d_ff, (uint16_t *)dX, stream);
     }
     return launch_status();
 }

@@ -86,6 +86,35 @@ def test_ffn_of_many_positions(M, K, F):
     assert ((dX[some].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2 * (2 * F + 1) * 2.0 ** -24 * size).all()
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_ffn_of_long_sums(dt):
+    """Rows of more than 2^21 values on either side of the block."""
+    say("long sums", dt)
+    tt, ct = (torch.float32, dp.DP_F32) if dt == "f32" else (torch.bfloat16, dp.DP_BF16)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    n, M, few = 2 ** 21 + 8, 66, 3
+    # additions in any order (six products to a term in fp32), each rounded to 2^-24 of a partial sum, which stays under
+    # 5 standard deviations: sqrt(n) forward, under 3 sqrt(n) backward (2 n terms of deviation under 2); and the result's
+    eps = 2.0 ** -24 if dt == "f32" else 2.0 ** -8
+    randn = lambda *s: torch.randn(s, generator=g, device=DEV).to(tt)  # noqa: E731
+    X, Wg, Wu = randn(M, n), randn(few, n), randn(few, n)
+    H, G, U = [torch.full((M, few), 7.0, dtype=tt, device=DEV) for _ in range(3)]
+    dp.dp_gated_ffn_forward(X, Wg, Wu, ct, M, n, few, dp.DP_ACT_SILU, H, G, U,
+                            ws(dp.dp_gated_ffn_forward_workspace_bytes(M, n, few, ct)))
+    for got, W in ((G, Wg), (U, Wu)):
+        want = X.double() @ W.double().t()
+        assert ((got.double() - want).abs() <= eps * want.abs() + 6 * n * 2.0 ** -24 * 5 * math.sqrt(n)).all()
+    del X, Wg, Wu
+    dH, G, U = randn(M, n), randn(M, n), randn(M, n)
+    Wg, Wu = randn(n, few), randn(n, few)
+    dX = torch.full((M, few), 7.0, dtype=tt, device=DEV)
+    dp.dp_gated_ffn_backward(dH, G, U, Wg, Wu, ct, M, few, n, dp.DP_ACT_SILU, G, U, dX,
+                             ws(dp.dp_gated_ffn_backward_workspace_bytes(M, few, n, ct)))
+    want = G.double() @ Wg.double() + U.double() @ Wu.double()
+    assert G.isfinite().all() and U.isfinite().all() and want.abs().min() > 0
+    assert ((dX.double() - want).abs() <= eps * want.abs() + 12 * n * 2.0 ** -24 * 15 * math.sqrt(n)).all()
+
+
 def test_norm_of_a_large_tensor():
     say("large norm")
     n = 2 ** 31 + 12345
