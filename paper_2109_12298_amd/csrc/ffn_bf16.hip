@@ -494,10 +494,20 @@ DxPlan dx_plan(i64 M, i64 D, i64 F)
     DxPlan p = {kMid, 1};
     if (M <= 64) {                        // one row of tiles: the weights' bytes bound it, over two workgroups per CU
         p.shape = M <= 32 ? kRows32 : kRows64;
-        i64 s = 512 / ceil_div(D, 128);
-        if (s > stages / 4) s = stages / 4;
-        if (s > 32) s = 32;
-        p.splits = s < 1 ? 1 : (int)s;
+        i64 most = 512 / ceil_div(D, 128);
+        if (most > stages / 4) most = stages / 4;
+        if (most > 32) most = 32;
+        // one stage after another at 0.5 us, or one more launch, and the partial tiles beside the weights (16 x 512 ->
+        // 256: 10.7 us in one split, 13.1 in four; 16 x 1024 -> 1024: 17.4 and 13.1; 64 x 4096 -> 4096: 67 in one, 24.5
+        // in eight, 28 in sixteen)
+        double best = 0.5 * (double)stages;
+        for (int s = 2; s <= most; ++s) {
+            const double t = 0.5 * (double)ceil_div(stages, s) + 7.0 + 16.0 * s * (double)M * (double)D / 4.5e6;
+            if (t < best) {
+                best = t;
+                p.splits = s;
+            }
+        }
         return p;
     }
     double best = 1e30;

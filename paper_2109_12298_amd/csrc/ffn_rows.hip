@@ -334,13 +334,26 @@ __global__ __launch_bounds__(256) void ffn_dx_rows_sum_kernel(const float *__res
 }
 
 // runs of features: 512 workgroups with the column blocks, each wave two groups of features at the least
-int dx_rows_splits(i64 D, i64 F)
+// Runs of features by the time they take: 32 features at 0.75 us (1.35 over 32
+// rows) per round of 256 workgroups; more than one run takes one more launch
+// and writes and reads partial sums.  64 x 4096 -> 4096: 182 us in two runs, 59
+// in eight, 81 in twelve, 69 in sixteen; one row of 100 -> 256: 12.5 in one,
+// 14.3 in two.
+int dx_rows_splits(i64 M, i64 D, i64 F)
 {
-    const i64 groups = 2 * ceil_div(F, kDxGroup);
-    i64 s = 512 / ceil_div(D, kDxCols);
-    if (s > groups / (2 * kDxWaves)) s = groups / (2 * kDxWaves);
-    if (s > 64) s = 64;
-    return s < 1 ? 1 : (int)s;
+    const i64 units = ceil_div(2 * ceil_div(F, kDxGroup), kDxWaves), cols = ceil_div(D, kDxCols);
+    const double unit = M <= 32 ? 0.75 : 1.35;
+    double best = unit * (double)(units * ceil_div(cols, 256));
+    int splits = 1;
+    for (int s = 2; s <= 64 && 2 * s <= units; ++s) {
+        const double t = unit * (double)(ceil_div(units, s) * ceil_div(cols * s, 256)) + 7.0 +
+                         16.0 * s * (double)M * (double)D / 4.5e6;
+        if (t < best) {
+            best = t;
+            splits = s;
+        }
+    }
+    return splits;
 }
 
 }  // namespace
@@ -354,14 +367,14 @@ void ffn_rows_forward(const void *X, const void *Wg, const void *Wu, dp_dtype dt
 
 size_t ffn_rows_dx_workspace(i64 M, i64 D, i64 F)
 {
-    const int splits = dx_rows_splits(D, F);
+    const int splits = dx_rows_splits(M, D, F);
     return splits > 1 ? sizeof(float) * (size_t)splits * (size_t)(M * D) : 0;
 }
 
 void ffn_rows_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F, float *dX,
                  void *ws, hipStream_t stream)
 {
-    const int splits = dx_rows_splits(D, F), cb = (int)ceil_div(D, kDxCols);
+    const int splits = dx_rows_splits(M, D, F), cb = (int)ceil_div(D, kDxCols);
     const bool vec = D % 4 == 0 && F % 4 == 0 && aligned(BG, 16) && aligned(BU, 16) && aligned(Wg, 16) && aligned(Wu, 16);
     float *out = splits > 1 ? (float *)ws : dX;
     const auto go = [&](auto kernel) {
