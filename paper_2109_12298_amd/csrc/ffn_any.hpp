@@ -1,7 +1,7 @@
 // Tiles of the gated feed-forward block for any size, type and alignment: 64 x
 // 64, element loads, fp32 MFMA (products of bf16 values are exact in fp32).
-// The work of the calls and values that the tile kernels of ffn_bf16.hip do
-// not take.  THREADS threads stage, the first four waves multiply.
+// The work of the calls and values that the tile kernels of ffn_bf16.hip and
+// ffn_parts.hip do not take.  THREADS threads stage, the first four waves multiply.
 #pragma once
 
 #include "gated_ffn.hpp"
