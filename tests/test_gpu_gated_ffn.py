@@ -56,7 +56,9 @@ def weights(rng, F, K, tt):
 SIZES = [(1, 1, 1), (1, 64, 64), (1, 500, 77), (2, 256, 136), (3, 5, 7), (4, 8, 8), (5, 1032, 40), (8, 96, 256),
          (15, 72, 24), (16, 512, 130), (17, 40, 264), (31, 128, 128), (33, 128, 200), (48, 264, 96), (64, 64, 64),
          (65, 100, 130), (100, 192, 328), (127, 136, 72), (128, 256, 128), (129, 320, 129), (200, 77, 300),
-         (256, 256, 256), (257, 136, 264), (300, 1000, 520), (520, 72, 1000), (1000, 512, 264)]
+         (256, 256, 256), (257, 136, 264), (300, 1000, 520), (520, 72, 1000), (1000, 512, 264),
+         (70, 1, 2), (66, 16, 3), (90, 17, 33), (130, 33, 50), (70, 50, 17), (97, 65, 80), (260, 82, 97), (150, 140, 3000),
+         (90, 2000, 70), (20, 700, 900), (64, 130, 2100)]
 
 
 @pytest.mark.parametrize("M,K,F", SIZES)
