@@ -11,8 +11,8 @@
 // 2048 -> 5504 with the split 974 us, 850 so; 1000 x 500 -> 1333 44 and 32.)
 // Two workgroups of four waves share a CU and cover each other's first loads
 // and last stores; stages of 32 columns, one workgroup per CU, take 911 and 34.
-// At those sizes the products run at 1.3 PFLOP/s, the rate of a large library
-// product; small ones are bound by the split (6 us) and the stages' latency.
+// The first of these sizes runs at about 1.4 PFLOP/s, a large library product's
+// rate; small ones are bound by the split (6 us) and the stages' latency.
 //
 // Operands and the output's way are those of ffn_bf16.hip.
 #include "ffn_any.hpp"
