@@ -239,6 +239,7 @@ def make_grad_tensors(entries):
         arr[i].g, arr[i].out = ptrs[2 * i], ptrs[2 * i + 1]
         arr[i].numel = int(numel)
         arr[i].dtype = int(dt)
+    arr.dev = dev                         # the tensors' GPU
     return arr
 
 
@@ -632,15 +633,28 @@ def dp_clip_accumulate_tokens(ids, B, dt, N, T, V, D, scale, norm, C, sum, statu
          p[3], p[4], p[5], _nbytes(ws), stream=stream)
 
 
+def _grad_tensors(where, items, count):
+    """Address of a dp_grad_tensor array that holds `count` of them (None: of none)."""
+    if count > (0 if items is None else len(items)):
+        raise ValueError("%s: %d tensors of an array of %d" % (where, count, 0 if items is None else len(items)))
+    return None if items is None else ctypes.addressof(items)
+
+
 def dp_clip_global_norm_many_workspace_bytes(items, count) -> int:
-    return lib().dp_clip_global_norm_many_workspace_bytes(ctypes.cast(items, ctypes.c_void_p), count)
+    return lib().dp_clip_global_norm_many_workspace_bytes(
+        _grad_tensors("dp_clip_global_norm_many_workspace_bytes", items, count), count)
 
 
 def dp_clip_global_norm_many(items, count, C, norm, status=None, ws=None, stream=None):
     import torch
     dev, p = _tensors("dp_clip_global_norm_many", ("norm", norm, torch.float32, 1), ("status", status, torch.int32, 1),
                       ("ws", ws, None, 0))
-    _run("dp_clip_global_norm_many", dev, lib().dp_clip_global_norm_many, ctypes.addressof(items), count, C, p[0], p[1], p[2], _nbytes(ws), stream=stream)
+    where = "dp_clip_global_norm_many"
+    at, on = _grad_tensors(where, items, count), getattr(items, "dev", None)
+    if dev is not None and on is not None and dev != on:
+        raise ValueError("%s: norm, status or ws is on GPU %d, the tensors on GPU %d" % (where, dev, on))
+    _run(where, on if dev is None else dev, lib().dp_clip_global_norm_many, at, count, C, p[0], p[1], p[2], _nbytes(ws),
+         stream=stream)
 
 
 # ---------------------------------------------------------------------------

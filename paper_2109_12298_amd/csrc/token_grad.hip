@@ -990,9 +990,8 @@ int sort(const Plan &p, const int64_t *ids, i64 T, i64 V, const float *norm, int
         uint32_t *pi = (uint32_t *)(ws + p.pos[buf]), *po = (uint32_t *)(ws + p.pos[buf ^ 1]);
         const Fill &fc = fills.count[i], &fs = fills.scatter[i];
         if (i == 0)
-            count_kernel<ITEMS, true><<<tiles + fill_blocks(fc, kSortWaves), kSortThreads, 0, stream>>>(ids, (uint32_t)p.M, (uint32_t)T, V, norm, ki,
-                                                                         0, p.bits, hist, (int)tiles, p.hist_ld, present,
-                                                                         status, fc);
+            count_kernel<ITEMS, true><<<tiles + fill_blocks(fc, kSortWaves), kSortThreads, 0, stream>>>(
+                ids, (uint32_t)p.M, (uint32_t)T, V, norm, ki, 0, p.bits, hist, (int)tiles, p.hist_ld, present, status, fc);
         else
             count_kernel<ITEMS, false><<<tiles + fill_blocks(fc, kSortWaves), kSortThreads, 0, stream>>>(
                 ids, (uint32_t)p.M, (uint32_t)T, V, norm, ki, i * p.bits, p.bits, hist, (int)tiles, p.hist_ld, present,

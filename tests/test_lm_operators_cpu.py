@@ -154,3 +154,13 @@ def test_tensors_are_checked_before_the_call():
         ptr(Fake(torch.float32, 39))
     with pytest.raises(ValueError, match="other arguments on GPU 0"):
         ptr(Fake(torch.float32, 40), Fake(torch.float32, 40, device=1))
+
+    items = dp.make_grad_tensors([(Fake(torch.float32, 40, device=1), None, 40, dp.DP_F32)])
+    with pytest.raises(ValueError, match="on GPU 0, the tensors on GPU 1"):
+        dp.dp_clip_global_norm_many(items, 1, 1.0, Fake(torch.float32, 1), None, FAKE, stream=0)
+    for call in (dp.dp_clip_global_norm_many_workspace_bytes,
+                 lambda items, n: dp.dp_clip_global_norm_many(items, n, 1.0, FAKE, None, FAKE, stream=0)):
+        for few, n in ((items, 2), (None, 1)):       # more tensors than the array holds
+            with pytest.raises(ValueError, match="tensors of an array of"):
+                call(few, n)
+    assert dp.dp_clip_global_norm_many_workspace_bytes(None, 0) == dp.dp_clip_global_norm_many_workspace_bytes(items, 0)
