@@ -16,16 +16,15 @@ constexpr float kGeluA = 1.5957691216057308f;       // 2 sqrt(2 / pi)
 constexpr float kGeluB = 0.044715f;
 
 template <int ACT>
-__device__ __forceinline__ float gate_of(float g)
+__device__ __forceinline__ float exponent_of(float g)
 {
-    const float w = ACT == DP_ACT_SILU ? g : kGeluA * (g + kGeluB * g * g * g);
-    return 1.0f / (1.0f + expf(-w));
+    return ACT == DP_ACT_SILU ? g : kGeluA * (g + kGeluB * g * g * g);
 }
 
 template <int ACT>
 __device__ __forceinline__ float act(float g)
 {
-    return g * gate_of<ACT>(g);
+    return g * (1.0f / (1.0f + expf(-exponent_of<ACT>(g))));
 }
 
 // The same with the hardware's exp2 and reciprocal (each within about one
@@ -34,8 +33,7 @@ __device__ __forceinline__ float act(float g)
 template <int ACT>
 __device__ __forceinline__ float act_fast(float g)
 {
-    const float w = ACT == DP_ACT_SILU ? g : kGeluA * (g + kGeluB * g * g * g);
-    return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * w));
+    return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * exponent_of<ACT>(g)));
 }
 
 // for results kept in T
@@ -45,13 +43,16 @@ __device__ __forceinline__ float act_for(float g)
     return sizeof(T) == 4 ? act<ACT>(g) : act_fast<ACT>(g);
 }
 
-// act(g) and act'(g) = p + g p (1 - p) w'(g), p = sigmoid(w(g)).  For large
-// |g| in the GELU form p (1 - p) is 0 while g w'(g) may be infinite: the term is 0.
+// act(g) and act'(g) = p + g p (1 - p) w'(g), p = sigmoid(w(g)).  1 - p is formed
+// as e p with p = 1 / (1 + e): the difference would lose its bits where p comes
+// near 1 (2^-25 times g w'(g) = 34 at g = 5 in the GELU form, 33 half steps of
+// the slope; so 3).  Where e overflows both are 0.  For large |g| in the GELU
+// form p (1 - p) is 0 while g w'(g) may be infinite: the term is 0.
 template <int ACT>
 __device__ __forceinline__ void act_and_slope(float g, float &a, float &s)
 {
-    const float p = gate_of<ACT>(g);
-    const float q = p * (1.0f - p);
+    const float e = expf(-exponent_of<ACT>(g)), p = 1.0f / (1.0f + e);
+    const float q = p == 0.0f ? 0.0f : p * (e * p);
     a = g * p;
     if constexpr (ACT == DP_ACT_SILU) s = p + g * q;
     else s = q == 0.0f ? p : p + q * (g * (kGeluA * (1.0f + 3.0f * kGeluB * g * g)));
