@@ -402,6 +402,34 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
     }
 }
 
+// dX = the splits' partial sums, in split order; rows of ld (a multiple of 4) there, of D here
+__global__ __launch_bounds__(256) void ffn_dx_sum_kernel(const float *__restrict__ part, i64 M, i64 D, i64 ld,
+                                                         int splits, uint16_t *__restrict__ dX)
+{
+    const i64 n = M * ld;
+    for (i64 i = ((i64)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (i64)gridDim.x * 1024) {
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < splits; k += 8) {
+            float4 p[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                p[j] = k + j < splits ? *reinterpret_cast<const float4 *>(part + (i64)(k + j) * n + i)
+                                      : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[0] += p[j].x;
+                v[1] += p[j].y;
+                v[2] += p[j].z;
+                v[3] += p[j].w;
+            }
+        }
+        const i64 m = D == ld ? 0 : i / ld, d = i - m * ld;  // D = ld: one row of all values
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (D == ld || d + j < D) store_elem(dX + m * D + d + j, v[j]);
+    }
+}
+
 typedef DxShape<256, 256, 2, 4, 64, 2> LargeDx;
 typedef DxShape<128, 128, 2, 2, 64, 4> MidDx;
 typedef DxShape<64, 128, 1, 4, 64, 3> Rows64Dx;
@@ -421,7 +449,8 @@ void launch_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, const
     }
     ffn_dx_kernel<S, true><<<grid, S::THREADS, 0, stream>>>(BG, BU, Wg, Wu, M, D, F, lda, ldw, tm, td, splits, dX, part,
                                                             vec);
-    sum_splits(part, M, D, ldw, splits, dX, Whole{}, stream);
+    const i64 blocks = ceil_div(M * ldw, 1024);
+    ffn_dx_sum_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(part, M, D, ldw, splits, dX);
 }
 
 size_t pad_bytes(i64 rows, i64 cols)

@@ -26,8 +26,8 @@ void ffn_bf16_dx(const uint16_t *BG, const uint16_t *BU, const uint16_t *Wg, con
 // The same for fp32 values, each as three bf16 parts and every product as six
 // bf16 products (what is left out is 2^-24 of a product), M > kFfnRowsMax.
 // Rows of any length and alignment (the splitting kernel lays them out anew).
-// Values that have no such parts (infinities, NaN, and magnitudes under 2^-100
-// or from 2^127 on) turn the whole call over to the fp32 units (ffn_any.hpp),
+// Tiles whose sums come out non-finite (infinities, NaN, magnitudes from about
+// 2^104 on, sums from 2^80 on) are formed again on the fp32 units (ffn_any.hpp),
 // inside the same launches.
 size_t ffn_parts_forward_workspace(i64 M, i64 K, i64 F);
 void ffn_parts_forward(const float *X, const float *Wg, const float *Wu, i64 M, i64 K, i64 F, dp_act act, float *H,

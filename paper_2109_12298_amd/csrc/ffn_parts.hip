@@ -1,8 +1,17 @@
 // Gated feed-forward block in fp32 on v_mfma_f32_32x32x16_bf16: every value as
-// three bf16 parts (ffn_split_kernel), every product as six bf16 products
+// three bf16 parts (split_bf16.hpp), every product as six bf16 products
 //   x w = x0 w2 + x2 w0 + x1 w1 + x0 w1 + x1 w0 + x0 w0
 // added in fp32 in this order.  What is left out (x1 w2, x2 w1: 2^-24 of the
-// product at most, and x2 w2) is within the rounding of an fp32 product.
+// product at most, and x2 w2) is within the rounding of an fp32 product.  The
+// parts are those of 2^24 x, so that a value of any size has normal ones and
+// small values beside ordinary ones cost nothing (GELU's slopes end at 2^-100
+// and below); 2^-48 comes out of the sums.
+//
+// Infinities, NaN, values whose parts overflow (from about 2^104 on) and sums
+// that do (from 2^80 on) leave non-finite sums.  A workgroup that finds one
+// among its own forms its tile again on the fp32 units (ffn_any.hpp): the other
+// tiles keep their bits and their time.  Such a tile is slow, single loads and
+// no overlap: with one NaN in dH, 512 x 2752 -> 1024 takes 684 us instead of 61.
 //
 // A stage holds 16 columns of all three parts of each operand, so that a part
 // is staged once and read from LDS once for all the products that take it: 12
@@ -18,6 +27,7 @@
 #include "ffn_any.hpp"
 #include "ffn_bf16.hpp"
 #include "ffn_tiles.hpp"
+#include "split_bf16.hpp"
 
 #include <type_traits>
 
@@ -31,19 +41,24 @@ constexpr int kCols = 128;                // columns of a staged row of Wg and W
 constexpr int kWRpi = 1024 / (2 * kCols); // such rows per load instruction
 constexpr int kWLoads = kBK / kWRpi;      // load instructions per part and stage
 constexpr int kSplitBlocks = 1024;        // workgroups of the splitting kernel, at most
+constexpr int kSumRows = 16;              // rows by kTN columns of a workgroup that adds splits
 constexpr int kProducts = 6;
 constexpr int kXPart[kProducts] = {0, 2, 1, 0, 1, 0}, kWPart[kProducts] = {2, 0, 1, 1, 0, 0};
 
-// whether a value has no parts, from this thread's words
-__device__ __forceinline__ int own_flags(const Whole &w)
+// The operands themselves, for tiles that are formed again: X (b unused), or BG
+// and BU, with K features in a row.
+struct Whole {
+    const float *a, *b, *wg, *wu;
+    i64 K;
+};
+
+// 0, or NaN where a value is not finite
+__device__ __forceinline__ float probe(const f32x16_t &v)
 {
-    int bad = 0;
+    float t = 0.0f;
 #pragma unroll
-    for (int k = 0; k < kSplitBlocks / kThreads; ++k) {      // past the end the first word again
-        const int i = threadIdx.x + k * kThreads;
-        bad |= w.flags[i < w.count ? i : 0];
-    }
-    return bad;
+    for (int r = 0; r < 16; ++r) t = fmaf(v[r], 0.0f, t);
+    return t;
 }
 
 // The parts lie in memory as they do in LDS: a load instruction copies 1 KB of
@@ -72,20 +87,15 @@ __device__ __forceinline__ int piece_of(int row, int q) { return q ^ ((row >> 3)
 // of stage c; read(c, j, f): operand j of stage c; mma(i, f): matrix
 // instruction i.  The loads and reads of what comes next are issued in the
 // shadow of the matrix instructions (32 clocks each), in this order.
-template <typename Issue>
-__device__ __forceinline__ void start_stages(int nst, const Issue &issue)
+template <typename Frag, typename Issue, typename Read, typename Mma>
+__device__ __forceinline__ void run_stages(int nst, const Issue &issue, const Read &read, const Mma &mma)
 {
+    static_assert(kNS == 3, "two stages ahead");
 #pragma unroll
     for (int c = 0; c < kNS; ++c)
         if (c < nst)
 #pragma unroll
             for (int r = 0; r < kLoads; ++r) issue(c, r);
-}
-
-template <typename Frag, typename Issue, typename Read, typename Mma>
-__device__ __forceinline__ void run_stages(int nst, const Issue &issue, const Read &read, const Mma &mma)
-{
-    static_assert(kNS == 3, "two stages ahead");
     wait_later<kLoads>(nst - 1);
     stage_barrier();
     Frag fa, fb;
@@ -160,7 +170,6 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_forward_kernel(Parts X,
     int tm, tf;
     tile_of((int)blockIdx.x, (int)gridDim.x, tiles_m, tiles_f, tm, tf);
     const i64 m0 = (i64)tm * S::BM, f0 = (i64)tf * S::BF;
-    const int bad = own_flags(whole);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / 2 * (FM * 32), wf = wave % 2 * (FF * 32);
@@ -219,19 +228,19 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_forward_kernel(Parts X,
             u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.u[kWPart[n]][y], f.x[kXPart[n]][x], u, 0, 0, 0);
         }
     };
-    const int nst = (int)X.stages;
-    start_stages(nst, issue);
-    if (__syncthreads_or(bad)) {
-        wait_vmcnt<0>();
-        __syncthreads();
+    run_stages<Frag>((int)X.stages, issue, read, mma);
+    float sums = 0.0f;
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+        for (int y = 0; y < FF; ++y) sums += probe(ag[x][y]) + probe(au[x][y]);
+    if (__syncthreads_or(sums != 0.0f)) {                       // the stages are free from here on
         for (int t = 0; t < (S::BM / kTM) * (S::BF / kTN); ++t)
             any_forward_tile<kThreads, ACT>(whole.a, whole.wg, whole.wu, M, whole.K, F, m0 + t / (S::BF / kTN) * kTM,
                                             f0 + t % (S::BF / kTN) * kTN, H, G, U, reinterpret_cast<float *>(smem));
         return;
     }
-    run_stages<Frag>(nst, issue, read, mma);
-    __syncthreads();                                         // the stages become the output transposes
-
+    // the stages become the output transposes
     constexpr int LDT = FF * 128 + 16;
     char *L = smem + wave * 32 * LDT;
     const auto put = [&](int x, auto value, float *O) {
@@ -245,10 +254,12 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_forward_kernel(Parts X,
     };
 #pragma unroll
     for (int x = 0; x < FM; ++x) {
-        put(x, [&](int y, int r) { return act_for<ACT, float>(ag[x][y][r]) * au[x][y][r]; }, H);
+        const auto g = [&](int y, int r) { return ag[x][y][r] * split::kUnscale; };
+        const auto u = [&](int y, int r) { return au[x][y][r] * split::kUnscale; };
+        put(x, [&](int y, int r) { return act_for<ACT, float>(g(y, r)) * u(y, r); }, H);
         if (G != nullptr) {
-            put(x, [&](int y, int r) { return ag[x][y][r]; }, G);
-            put(x, [&](int y, int r) { return au[x][y][r]; }, U);
+            put(x, g, G);
+            put(x, u, U);
         }
     }
 }
@@ -285,7 +296,6 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_dx_kernel(Parts BG, Par
     const int tiles = tiles_m * tiles_d, split = SPLIT ? (int)blockIdx.x / tiles : 0;
     tile_of((int)blockIdx.x - split * tiles, tiles, tiles_m, tiles_d, tm, td);
     const i64 m0 = (i64)tm * S::BM, d0 = (i64)td * S::BD;
-    const int bad = own_flags(whole);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / 2 * (FM * 32), wd = wave % 2 * (FD * 32);
@@ -294,7 +304,8 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_dx_kernel(Parts BG, Par
     const int first = SPLIT ? (int)((i64)split * 2 * half / splits) : 0;
     const int nst = (SPLIT ? (int)((i64)(split + 1) * 2 * half / splits) : 2 * half) - first;
 
-    // groups past the end read the last one (their products are not stored)
+    // groups past the end read the last one (their products are not stored, and what is not finite among them is so in
+    // the tile's own rows)
     const char *baseA[2][S::A_LOADS];
 #pragma unroll
     for (int r = 0; r < S::A_LOADS; ++r) {
@@ -340,16 +351,6 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_dx_kernel(Parts BG, Par
         f32x16_t &a = acc[x][y];
         a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.w[kWPart[n]][y], f.a[kXPart[n]][x], a, 0, 0, 0);
     };
-    start_stages(nst, issue);
-    if (__syncthreads_or(bad)) {
-        wait_vmcnt<0>();
-        __syncthreads();
-        if (split == 0)
-            for (int t = 0; t < (S::BM / kTM) * (S::BD / kTN); ++t)
-                any_dx_tile<kThreads>(whole.a, whole.b, whole.wg, whole.wu, M, D, whole.K, m0 + t / (S::BD / kTN) * kTM,
-                                      d0 + t % (S::BD / kTN) * kTN, dX, reinterpret_cast<float *>(smem));
-        return;
-    }
     run_stages<Frag>(nst, issue, read, mma);
     if constexpr (SPLIT) {
         float *P = part + (i64)split * M * ldw;
@@ -366,7 +367,17 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_dx_kernel(Parts BG, Par
                 }
         return;
     }
-    __syncthreads();
+    float sums = 0.0f;
+#pragma unroll
+    for (int x = 0; x < FM; ++x)
+#pragma unroll
+        for (int y = 0; y < FD; ++y) sums += probe(acc[x][y]);
+    if (__syncthreads_or(sums != 0.0f)) {                       // the stages are free from here on
+        for (int t = 0; t < (S::BM / kTM) * (S::BD / kTN); ++t)
+            any_dx_tile<kThreads>(whole.a, whole.b, whole.wg, whole.wu, M, D, whole.K, m0 + t / (S::BD / kTN) * kTM,
+                                  d0 + t % (S::BD / kTN) * kTN, dX, reinterpret_cast<float *>(smem));
+        return;
+    }
     constexpr int LDT = FD * 128 + 16;
     char *L = smem + wave * 32 * LDT;
 #pragma unroll
@@ -375,36 +386,61 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_dx_kernel(Parts BG, Par
         for (int y = 0; y < FD; ++y)
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb)
-                put4(reinterpret_cast<float *>(L + li * LDT) + 32 * y + 8 * rb + 4 * lk, acc[x][y][4 * rb],
-                     acc[x][y][4 * rb + 1], acc[x][y][4 * rb + 2], acc[x][y][4 * rb + 3]);
+                put4(reinterpret_cast<float *>(L + li * LDT) + 32 * y + 8 * rb + 4 * lk,
+                     acc[x][y][4 * rb] * split::kUnscale, acc[x][y][4 * rb + 1] * split::kUnscale,
+                     acc[x][y][4 * rb + 2] * split::kUnscale, acc[x][y][4 * rb + 3] * split::kUnscale);
         store_rows<float, FD * 32, LDT>(L, dX, M, D, m0 + wm + 32 * x, d0 + wd, vec != 0, lane);
     }
+}
+
+// dX = the splits' partial sums (times 2^48; rows of ld, a multiple of 8) in split order; a workgroup takes kSumRows rows
+// by kTN columns, and forms them again where a sum is not finite
+__global__ __launch_bounds__(kThreads) void ffn_parts_sum_kernel(const float *__restrict__ part, i64 M, i64 D, i64 ld,
+                                                                 int splits, int tiles_d, float *__restrict__ dX,
+                                                                 Whole whole)
+{
+    __shared__ float lds[kAnyFloats];
+    const i64 r0 = (i64)(blockIdx.x / tiles_d) * kSumRows, c0 = (i64)(blockIdx.x % tiles_d) * kTN;
+    const i64 m = r0 + threadIdx.x / (kTN / 4), d = c0 + threadIdx.x % (kTN / 4) * 4;
+    const bool in = m < M && d < ld;
+    const float *p = part + (in ? m * ld + d : 0);
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < splits; k += 8) {
+        float4 q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            q[j] = k + j < splits ? *reinterpret_cast<const float4 *>(p + (i64)(k + j) * M * ld)
+                                  : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[0] += q[j].x;
+            v[1] += q[j].y;
+            v[2] += q[j].z;
+            v[3] += q[j].w;
+        }
+    }
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bad |= in && d + j < D && !split::finite_f32(v[j]);
+    if (__syncthreads_or(bad)) {
+        any_dx_tile<kThreads>(whole.a, whole.b, whole.wg, whole.wu, r0 + kSumRows < M ? r0 + kSumRows : M, D, whole.K, r0,
+                              c0, dX, lds);
+        return;
+    }
+    if (!in) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (d + j < D) dX[m * D + d + j] = v[j] * split::kUnscale;
 }
 
 // ---------------------------------------------------------------------------
 // the parts
 // ---------------------------------------------------------------------------
-// x = p[0] + p[1] + p[2] exactly, each a bf16 value (8 bits each, rounded to
-// nearest, so that what the left-out products hold has no preferred sign).
-// Returns true where that fails: infinities and NaN, values so large that
-// they round to infinity, and values under 2^-100, whose last bits may lie
-// below the smallest normal bf16, which the matrix unit takes as zero.
-__device__ __forceinline__ bool split3(float x, uint32_t (&p)[3])
-{
-    const uint32_t e = (__float_as_uint(x) >> 23) & 255u;
-    p[0] = bf16_bits(x);
-    const float r1 = x - bf16_to_f32((uint16_t)p[0]);
-    p[1] = bf16_bits(r1);
-    p[2] = bf16_bits(r1 - bf16_to_f32((uint16_t)p[1]));
-    return x != 0.0f && (e >= 254u || e < 27u);
-}
-
 // Arrays to split: P [rows][cols] as the kilobytes of its parts at O (Parts,
 // or, by_cols, as W of ffn_parts_dx_kernel), zeros past rows and cols.  One
 // launch for all of a call's, a wave per kilobyte of values' worth (the three
 // parts of 64 pieces of eight), first[k] the first of array k, of at most
-// kSplitBlocks workgroups, each leaving a word that says whether it met a
-// value that cannot be split.
+// kSplitBlocks workgroups.
 struct Splits {
     int count;
     const float *P[4];
@@ -413,11 +449,10 @@ struct Splits {
     int by_cols[4];
 };
 
-__global__ __launch_bounds__(256) void ffn_split_kernel(Splits s, int32_t *__restrict__ flags)
+__global__ __launch_bounds__(256) void ffn_split_kernel(Splits s)
 {
     const int lane = threadIdx.x & 63;
     const i64 wave = (i64)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    bool bad = false;
     for (i64 i = wave; i < s.first[s.count]; i += (i64)gridDim.x * 4) {
         int k = 0;
         while (k + 1 < s.count && i >= s.first[k + 1]) ++k;
@@ -453,23 +488,13 @@ __global__ __launch_bounds__(256) void ffn_split_kernel(Splits s, int32_t *__res
         }
         uint32_t w[3][4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            uint32_t a[3], b[3];
-            bad |= split3(x[2 * q], a);
-            bad |= split3(x[2 * q + 1], b);
-#pragma unroll
-            for (int n = 0; n < 3; ++n) w[n][q] = a[n] | (b[n] << 16);
-        }
+        for (int q = 0; q < 4; ++q) split::split2(x[2 * q], x[2 * q + 1], w[0][q], w[1][q], w[2][q]);
 #pragma unroll
         for (int n = 0; n < 3; ++n)
             *reinterpret_cast<uint4 *>(s.O[k] + (at + n * step) * 1024 + 16 * lane) =
                 make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
     }
-    const int any = __syncthreads_or(bad);
-    if (threadIdx.x == 0) flags[blockIdx.x] = any;
 }
-
-constexpr size_t kFlagBytes = sizeof(int32_t) * kSplitBlocks;
 
 i64 stages_of(i64 features) { return ceil_div(features, kBK); }
 
@@ -499,13 +524,10 @@ Parts add_rows(Splits &s, const float *P, i64 rows, i64 cols, char *&ws)
     return Parts{p, ceil_div(rows, kRpi), stages_of(cols)};
 }
 
-// Splits the arrays; returns how many words were left at flags.
-int split(const Splits &s, int32_t *flags, hipStream_t stream)
+void split_arrays(const Splits &s, hipStream_t stream)
 {
     const i64 blocks = ceil_div(s.first[s.count], 4);
-    const int n = (int)(blocks < kSplitBlocks ? blocks : kSplitBlocks);
-    ffn_split_kernel<<<(unsigned)n, 256, 0, stream>>>(s, flags);
-    return n;
+    ffn_split_kernel<<<(unsigned)(blocks < kSplitBlocks ? blocks : kSplitBlocks), 256, 0, stream>>>(s);
 }
 
 // Splits of the features by the time they take: a stage at 0.55 us while most
@@ -535,17 +557,17 @@ int dx_splits(i64 M, i64 D, i64 F)
 
 size_t ffn_parts_forward_workspace(i64 M, i64 K, i64 F)
 {
-    return kFlagBytes + kPlanes * 1024 * (size_t)(row_parts(M, K) + 2 * row_parts(F, K));
+    return kPlanes * 1024 * (size_t)(row_parts(M, K) + 2 * row_parts(F, K));
 }
 
 void ffn_parts_forward(const float *X, const float *Wg, const float *Wu, i64 M, i64 K, i64 F, dp_act act, float *H,
                        float *G, float *U, void *ws, hipStream_t stream)
 {
-    int32_t *flags = (int32_t *)ws;
-    char *w = (char *)ws + kFlagBytes;
+    char *w = (char *)ws;
     Splits s = {};
     const Parts x = add_rows(s, X, M, K, w), g = add_rows(s, Wg, F, K, w), u = add_rows(s, Wu, F, K, w);
-    const Whole whole = {X, nullptr, Wg, Wu, K, flags, split(s, flags, stream)};
+    split_arrays(s, stream);
+    const Whole whole = {X, nullptr, Wg, Wu, K};
     const int tm = (int)ceil_div(M, Tile::BM), tf = (int)ceil_div(F, Tile::BF);
     const int vec = F % 4 == 0 && aligned(H, 16) && aligned(G, 16) && aligned(U, 16);
     const unsigned grid = (unsigned)((i64)tm * tf);
@@ -561,7 +583,7 @@ size_t ffn_parts_dx_workspace(i64 M, i64 D, i64 F)
 {
     const int splits = dx_splits(M, D, F);
     const size_t part = splits > 1 ? sizeof(float) * (size_t)splits * (size_t)(M * padded(D)) : 0;
-    return kFlagBytes + kPlanes * 1024 * (size_t)(2 * row_parts(M, F) + 2 * col_parts(F, D)) + part;
+    return kPlanes * 1024 * (size_t)(2 * row_parts(M, F) + 2 * col_parts(F, D)) + part;
 }
 
 void ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float *Wu, i64 M, i64 D, i64 F, float *dX,
@@ -569,14 +591,14 @@ void ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float
 {
     const i64 ldw = padded(D);
     const int splits = dx_splits(M, D, F);
-    int32_t *flags = (int32_t *)ws;
-    char *w = (char *)ws + kFlagBytes;
+    char *w = (char *)ws;
     Splits s = {};
     const Parts g = add_rows(s, BG, M, F, w), u = add_rows(s, BU, M, F, w);
     const char *W = add_split(s, Wg, F, D, true, w);
     add_split(s, Wu, F, D, true, w);                         // behind Wg's
     float *part = (float *)w;
-    const Whole whole = {BG, BU, Wg, Wu, F, flags, split(s, flags, stream)};
+    split_arrays(s, stream);
+    const Whole whole = {BG, BU, Wg, Wu, F};
     const int tm = (int)ceil_div(M, DxTile::BM), td = (int)ceil_div(D, DxTile::BD);
     const int vec = D % 4 == 0 && aligned(dX, 16);
     const unsigned grid = (unsigned)((i64)tm * td * splits);
@@ -585,7 +607,10 @@ void ffn_parts_dx(const float *BG, const float *BU, const float *Wg, const float
         return;
     }
     ffn_parts_dx_kernel<true><<<grid, kThreads, 0, stream>>>(g, u, W, M, D, ldw, tm, td, splits, dX, part, vec, whole);
-    sum_splits(part, M, D, ldw, splits, dX, whole, stream);
+    // (several splits only of up to 512 tiles: a grid of at most 8192 workgroups)
+    const i64 cols = ceil_div(D, kTN);
+    ffn_parts_sum_kernel<<<(unsigned)(ceil_div(M, kSumRows) * cols), kThreads, 0, stream>>>(part, M, D, ldw, splits,
+                                                                                           (int)cols, dX, whole);
 }
 
 }  // namespace dpg

@@ -1,6 +1,5 @@
 // What the tile kernels of the gated feed-forward block share (ffn_bf16.hip,
-// ffn_parts.hip): staging loads, tile order, output stores, the sum of split
-// products.
+// ffn_parts.hip): staging loads, tile order, output stores.
 #pragma once
 
 #include "bf16_stage.hpp"
@@ -106,61 +105,6 @@ __device__ __forceinline__ void put4(uint16_t *p, float a, float b, float c, flo
 __device__ __forceinline__ void put4(float *p, float a, float b, float c, float d)
 {
     *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d);
-}
-
-// What the kernels of an fp32 call need besides the parts: the values
-// themselves (K features in a row), and a word per workgroup of the splitting
-// kernel that is not 0 where it met a value without parts.
-struct Whole {
-    const float *a, *b, *wg, *wu;         // X (b unused), or BG and BU
-    i64 K;
-    const int32_t *flags;
-    int count;
-};
-
-// whether any of the words is set, in every thread of the workgroup
-__device__ __forceinline__ bool any_flag(const Whole &w)
-{
-    int bad = 0;
-    for (int i = threadIdx.x; i < w.count; i += blockDim.x) bad |= w.flags[i];
-    return __syncthreads_or(bad) != 0;
-}
-
-// dX = the splits' partial sums, in split order; rows of ld (a multiple of 4) there, of D here
-template <typename T>
-__global__ __launch_bounds__(256) void ffn_dx_sum_kernel(const float *__restrict__ part, i64 M, i64 D, i64 ld,
-                                                         int splits, T *__restrict__ dX, Whole whole)
-{
-    if (sizeof(T) == 4 && any_flag(whole)) return;           // dX is there already
-    const i64 n = M * ld;
-    for (i64 i = ((i64)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (i64)gridDim.x * 1024) {
-        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int k = 0; k < splits; k += 8) {
-            float4 p[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                p[j] = k + j < splits ? *reinterpret_cast<const float4 *>(part + (i64)(k + j) * n + i)
-                                      : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[0] += p[j].x;
-                v[1] += p[j].y;
-                v[2] += p[j].z;
-                v[3] += p[j].w;
-            }
-        }
-        const i64 m = D == ld ? 0 : i / ld, d = i - m * ld;  // D = ld: one row of all values
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (D == ld || d + j < D) store_elem(dX + m * D + d + j, v[j]);
-    }
-}
-
-template <typename T>
-void sum_splits(const float *part, i64 M, i64 D, i64 ld, int splits, T *dX, const Whole &whole, hipStream_t stream)
-{
-    const i64 blocks = ceil_div(M * ld, 1024);
-    ffn_dx_sum_kernel<T><<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(part, M, D, ld, splits, dX, whole);
 }
 
 inline i64 padded(i64 cols) { return (cols + 7) / 8 * 8; }

@@ -63,3 +63,127 @@ def test_slopes_between_the_tails(act):
     R.within(BG, slope, 1.01 * bound, "slope")
     R.within(BU, g * p, 1.01 * np.abs(g) * (p * (ep + u) + tiny) + tiny, "value")
     assert (dX == 0).all()
+
+
+# ------------------------------------------------------------------ fp32 by parts: over 64 rows
+
+SIZES = [(70, 64, 40), (300, 264, 136), (520, 72, 1000), (300, 264, 2048)]
+
+
+def inputs(M, K, F, seed=0):
+    rng = np.random.default_rng(M + K + F + seed)
+    t = lambda *s: torch.from_numpy(rng.standard_normal(s)).float()  # noqa: E731
+    return t(M, K), t(F, K) / math.sqrt(K), t(F, K) / math.sqrt(K), t(M, F), t(M, F), t(M, F)
+
+
+def bits(t):
+    return t.view(torch.int32)
+
+
+def check_forward(X, Wg, Wu, act):
+    out = forward(X.to(DEV), Wg.to(DEV), Wu.to(DEV), act)
+    want, bound = R.ffn_forward(act, R.f64(X), R.f64(Wg), R.f64(Wu), torch.float32)
+    for name, g, w, b in zip("HGU", out, want, bound):
+        R.within(g, w, b, name)
+    return out
+
+
+def check_backward(dH, G, U, Wg, Wu, act):
+    BG, BU, dX = backward(dH.to(DEV), G.to(DEV), U.to(DEV), Wg.to(DEV), Wu.to(DEV), act)
+    want, bound = R.ffn_backprops(act, R.f64(dH), R.f64(G), R.f64(U), torch.float32)
+    for name, g, w, b in zip(("BG", "BU"), (BG, BU), want, bound):
+        R.within(g, w, b, name)
+    R.within(dX, *R.ffn_dx(R.f64(BG), R.f64(BU), R.f64(Wg), R.f64(Wu), torch.float32), "dX")
+    return BG, BU, dX
+
+
+@pytest.mark.parametrize("M,K,F", SIZES)
+@pytest.mark.parametrize("value", [1e-30, 1e-36, 1e-42])
+def test_f32_small_values_change_no_other_row(M, K, F, value):
+    """One small value in a row or a feature: the others keep their bits."""
+    say("ffn small value", M, K, F, value)
+    act = dp.DP_ACT_GELU_TANH
+    X, Wg, Wu, dH, G, U = inputs(M, K, F)
+    out = check_forward(X, Wg, Wu, act)
+    BG, BU, dX = check_backward(dH, G, U, Wg, Wu, act)
+    m, f = M // 2, F // 3
+    x, wg, dh = X.clone(), Wg.clone(), dH.clone()
+    x[m, K // 3] = wg[f, K // 3] = dh[m, f] = value
+    rows, feats = [i for i in range(M) if i != m], [i for i in range(F) if i != f]
+    for a, b in zip(out, check_forward(x, Wg, Wu, act)):
+        assert torch.equal(bits(a[rows]), bits(b[rows]))
+    h, g, u = check_forward(X, wg, Wu, act)
+    assert torch.equal(bits(h[:, feats]), bits(out[0][:, feats])) and torch.equal(bits(u), bits(out[2]))
+    assert torch.equal(bits(g[:, feats]), bits(out[1][:, feats]))
+    bg, bu, dx = check_backward(dh, G, U, Wg, Wu, act)
+    assert torch.equal(bits(dx[rows]), bits(dX[rows]))
+    cols = [i for i in range(K) if i != K // 3]
+    assert torch.equal(bits(check_backward(dH, G, U, wg, Wu, act)[2][:, cols]), bits(dX[:, cols]))
+
+
+@pytest.mark.parametrize("M,K,F", SIZES[1:])
+@pytest.mark.parametrize("value", [math.nan, math.inf, 3e38])
+def test_f32_other_tiles_keep_their_bits(M, K, F, value):
+    """A value without parts turns its own tiles (128 rows, 64 features) over to the fp32 units, no others."""
+    say("ffn tiles", M, K, F, value)
+    act = dp.DP_ACT_SILU
+    X, Wg, Wu, dH, G, U = inputs(M, K, F, 1)
+    out = forward(X.to(DEV), Wg.to(DEV), Wu.to(DEV), act)
+    dX = backward(dH.to(DEV), G.to(DEV), U.to(DEV), Wg.to(DEV), Wu.to(DEV), act)[2]
+    m, f = 140, 70
+    x, wg, dh = X.clone(), Wg.clone(), dH.clone()
+    x[m, 5] = wg[f, 5] = dh[m, 5] = value
+    rows, feats = [i for i in range(M) if i // 128 != m // 128], [i for i in range(F) if i // 64 != f // 64]
+    for a, b in zip(out, forward(x.to(DEV), Wg.to(DEV), Wu.to(DEV), act)):
+        assert torch.equal(bits(a[rows]), bits(b[rows]))
+    for a, b in zip(out, forward(X.to(DEV), wg.to(DEV), Wu.to(DEV), act)):
+        assert torch.equal(bits(a[:, feats]), bits(b[:, feats]))
+    dx = backward(dh.to(DEV), G.to(DEV), U.to(DEV), Wg.to(DEV), Wu.to(DEV), act)[2]
+    assert torch.equal(bits(dx[rows]), bits(dX[rows]))
+    assert not dx[m].isfinite().any() if not math.isfinite(value) else True
+
+
+@pytest.mark.parametrize("M,K,F", SIZES)
+@pytest.mark.parametrize("deviation", [3.0, 12.0])
+def test_f32_gelu_gates_in_the_tails(M, K, F, deviation):
+    """A mean loss's gradient over gates whose slopes go down to nothing."""
+    say("ffn gelu tails", M, K, F, deviation)
+    X, Wg, Wu, dH, G, U = inputs(M, K, F, 2)
+    BG, _, _ = check_backward(dH / 4096, G * deviation, U, Wg, Wu, dp.DP_ACT_GELU_TANH)
+    assert (BG != 0).logical_and(BG.abs() < 2.0 ** -100).any() or M * F < 100000
+
+
+@pytest.mark.parametrize("M,K,F", SIZES)
+@pytest.mark.parametrize("value", [1e30, 1e32, 2e38, float(torch.finfo(torch.float32).max)])
+def test_f32_single_large_values(M, K, F, value):
+    """One large finite value with small partners, so that the sums stay finite: of parts, of parts that overflow, and of
+    a magnitude that bf16 rounds to infinity."""
+    say("ffn large value", M, K, F, value)
+    act = dp.DP_ACT_SILU
+    X, Wg, Wu, dH, G, U = inputs(M, K, F, 3)
+    m, k, f = M - 1, K // 2, F - 1
+    X[m, k] = value
+    Wg[:, k] *= 1e-20
+    Wu[:, k] *= 1e-20
+    out = check_forward(X, Wg, Wu, act)
+    assert all(t.isfinite().all() for t in out) and out[1][m].abs().max() > 1e-22 * value
+    X, Wg, Wu, dH, G, U = inputs(M, K, F, 4)
+    dH[m, f] = value                                         # BG = about -0.3 value, BU = 0.2 value
+    G[m, f], U[m, f] = -1.0, -4.0
+    Wg[f] *= 1e-20
+    Wu[f] *= 1e-20
+    if value > 1e38:
+        U[m, f] = 1.0
+    BG, BU, dX = check_backward(dH, G, U, Wg, Wu, act)
+    assert all(t.isfinite().all() for t in (BG, BU, dX)) and BU[m, f].abs() > 0.2 * value
+
+
+@pytest.mark.parametrize("M,K,F", SIZES)
+def test_f32_large_sums(M, K, F):
+    """Ordinary rows and weights whose products pass what the scaled parts' sums hold (2^80)."""
+    say("ffn large sums", M, K, F)
+    X, Wg, Wu, dH, G, U = inputs(M, K, F, 5)
+    out = check_forward(X * 1e13, Wg * 1e13, Wu * 1e-13, dp.DP_ACT_SILU)
+    assert all(t.isfinite().all() for t in out) and out[1].abs().max() > 2.0 ** 80
+    dX = check_backward(dH * 1e13, G, U, Wg * 1e13, Wu * 1e13, dp.DP_ACT_SILU)[2]
+    assert dX.isfinite().all() and dX.abs().max() > 2.0 ** 80
