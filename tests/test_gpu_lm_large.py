@@ -115,6 +115,42 @@ def test_ffn_of_long_sums(dt):
     assert ((dX.double() - want).abs() <= eps * want.abs() + 12 * n * 2.0 ** -24 * 15 * math.sqrt(n)).all()
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_ffn_of_long_sums_exactly(dt):
+    """The same lengths on whole numbers small enough that every sum is exact in fp32 in any order (|partial sums| under
+    2^24: forward at most 4 n = 2^23, backward 300 standard deviations of sqrt(n (0.9 + 32^2 * 1.4)) = 5.5e4): the
+    outputs are the exact sums, rounded once."""
+    say("long sums exactly", dt)
+    tt, ct = (torch.float32, dp.DP_F32) if dt == "f32" else (torch.bfloat16, dp.DP_BF16)
+    g = torch.Generator(device=DEV).manual_seed(6)
+    n, M, few = 2 ** 21 + 8, 66, 3
+    ints = lambda top, *s: torch.randint(-top, top + 1, s, generator=g, device=DEV).to(tt)  # noqa: E731
+    X, Wg, Wu = ints(2, M, n), ints(2, few, n), ints(2, few, n)
+    H, G, U = [torch.full((M, few), 7.0, dtype=tt, device=DEV) for _ in range(3)]
+    dp.dp_gated_ffn_forward(X, Wg, Wu, ct, M, n, few, dp.DP_ACT_SILU, H, G, U,
+                            ws(dp.dp_gated_ffn_forward_workspace_bytes(M, n, few, ct)))
+    g64, u64 = X.double() @ Wg.double().t(), X.double() @ Wu.double().t()
+    assert g64.abs().mean() > 1000 and u64.abs().mean() > 1000
+    assert torch.equal(G, g64.to(tt)) and torch.equal(U, u64.to(tt))
+    h64 = g64 * torch.sigmoid(g64) * u64
+    # expf, the sum, the quotient and two products in fp32 (8 half steps), and the rounding to bf16; gates under the
+    # smallest normal value may be 0
+    eps = 8 * 2.0 ** -24 if dt == "f32" else 1.01 * 2.0 ** -8
+    assert ((H.double() - h64).abs() <= eps * h64.abs() + 1e-30).all()
+    del X, Wg, Wu
+    dH, U = ints(1, M, n), ints(1, M, n)
+    G = torch.full((M, n), 32.0, dtype=tt, device=DEV)                # act(32) = 32, act'(32) = 1 in fp32
+    Wg, Wu = ints(2, n, few), ints(2, n, few)
+    BG, BU = torch.full_like(G, 7.0), torch.full_like(G, 7.0)
+    dX = torch.full((M, few), 7.0, dtype=tt, device=DEV)
+    dp.dp_gated_ffn_backward(dH, G, U, Wg, Wu, ct, M, few, n, dp.DP_ACT_SILU, BG, BU, dX,
+                             ws(dp.dp_gated_ffn_backward_workspace_bytes(M, few, n, ct)))
+    assert torch.equal(BG, dH * U) and torch.equal(BU, 32 * dH)
+    want = BG.double() @ Wg.double() + BU.double() @ Wu.double()
+    assert want.abs().mean() > 10000
+    assert torch.equal(dX, want.to(tt))
+
+
 def test_norm_of_a_large_tensor():
     say("large norm")
     n = 2 ** 31 + 12345
