@@ -106,13 +106,21 @@ class DPParam(ctypes.Structure):
 DP_PARAM_REDUCE = 1
 
 
+def _item_array(kind, entries):
+    """Items of a grouped call, one per entry.  The array keeps the entries, and with them the tensors whose addresses it
+    holds."""
+    arr = (kind * max(len(entries), 1))()
+    arr.entries = list(entries)
+    return arr
+
+
 def make_params(entries):
     """A dp_param array from (grad_sample, sum, out, numel, param_index[, accum]) tuples.
 
     grad_sample None means the sum is already formed (no DP_PARAM_REDUCE);
     an empty tensor (N = 0) still asks for the reduction.  accum (optional,
     default None) is the running sum of a virtual step."""
-    arr = (DPParam * max(len(entries), 1))()
+    arr = _item_array(DPParam, entries)
     for i, ent in enumerate(entries):
         g, s, o, numel, pidx = ent[:5]
         arr[i].accum = _ptr(ent[5]) if len(ent) > 5 else None
@@ -134,7 +142,7 @@ class DPLinearClip(ctypes.Structure):
 
 def make_linear_clips(entries):
     """A dp_linear_clip array from (A, B, T, d_in, d_out, scale, sumW, sumb) tuples."""
-    arr = (DPLinearClip * max(len(entries), 1))()
+    arr = _item_array(DPLinearClip, entries)
     for i, (A, B, T, d_in, d_out, scale, sumW, sumb) in enumerate(entries):
         arr[i].A = _ptr(A)
         arr[i].B = _ptr(B)
@@ -171,7 +179,7 @@ def conv2d_grad_item(X, GY, Cin, H, W, Cout, Ho, Wo, kh, kw, sh, sw, ph, pw, sca
 
 def make_layer_grads(entries):
     """A dp_layer_grad array from linear_grad_item / conv2d_grad_item dicts."""
-    arr = (DPLayerGrad * max(len(entries), 1))()
+    arr = _item_array(DPLayerGrad, entries)
     for i, e in enumerate(entries):
         for k, v in e.items():
             if k in ("A", "B", "gW", "gb", "sqnorm"):
@@ -192,7 +200,7 @@ class DPGhostLayer(ctypes.Structure):
 
 def make_ghost_layers(entries):
     """A dp_ghost_layer array from (A, B, T, d_in, d_out, scale, bias, sqnorm) tuples."""
-    arr = (DPGhostLayer * max(len(entries), 1))()
+    arr = _item_array(DPGhostLayer, entries)
     for i, (A, B, T, d_in, d_out, scale, bias, sqnorm) in enumerate(entries):
         arr[i].A = _ptr(A)
         arr[i].B = _ptr(B)
@@ -212,7 +220,7 @@ class DPLayerNormLayer(ctypes.Structure):
 
 def make_layernorm_layers(entries):
     """A dp_layernorm_layer array from (xhat, B, T, D, scale, ggamma, gbeta, sqnorm) tuples."""
-    arr = (DPLayerNormLayer * max(len(entries), 1))()
+    arr = _item_array(DPLayerNormLayer, entries)
     for i, (xh, B, T, D, scale, gg, gb, sq) in enumerate(entries):
         arr[i].xhat = _ptr(xh)
         arr[i].B = _ptr(B)
@@ -232,7 +240,7 @@ class DPGradTensor(ctypes.Structure):
 
 def make_grad_tensors(entries):
     """A dp_grad_tensor array from (g, out, numel, dtype) tuples; out None: the tensor counts in the norm only."""
-    arr = (DPGradTensor * max(len(entries), 1))()
+    arr = _item_array(DPGradTensor, entries)
     dev, ptrs = _tensors("make_grad_tensors", *[(n, x, _tdtype(dt), numel) for g, out, numel, dt in entries
                                                 for n, x in (("g", g), ("out", out))])
     for i, (g, out, numel, dt) in enumerate(entries):

@@ -164,3 +164,44 @@ def test_tensors_are_checked_before_the_call():
             with pytest.raises(ValueError, match="tensors of an array of"):
                 call(few, n)
     assert dp.dp_clip_global_norm_many_workspace_bytes(None, 0) == dp.dp_clip_global_norm_many_workspace_bytes(items, 0)
+
+
+def test_item_lists_keep_their_tensors():
+    """A list of items holds addresses: the tensors behind them live as long as the list."""
+    import gc
+    import weakref
+
+    class Fake:                                      # stands for a GPU tensor
+        dtype = torch.float32
+
+        def get_device(self):
+            return 0
+
+        def is_contiguous(self):
+            return True
+
+        def numel(self):
+            return 40
+
+        def data_ptr(self):
+            return FAKE
+
+    def tensors(n):
+        return [Fake() for _ in range(n)]
+
+    for make, entry in ((dp.make_grad_tensors, lambda a, b, c, d: (a, b, 40, dp.DP_F32)),
+                        (dp.make_params, lambda a, b, c, d: (a, b, c, 40, 0, d)),
+                        (dp.make_linear_clips, lambda a, b, c, d: (a, b, 1, 4, 4, 1.0, c, d)),
+                        (dp.make_layer_grads, lambda a, b, c, d: dp.linear_grad_item(a, b, 1, 4, 4, 1.0, c, d)),
+                        (dp.make_ghost_layers, lambda a, b, c, d: (a, b, 1, 4, 4, 1.0, False, c)),
+                        (dp.make_layernorm_layers, lambda a, b, c, d: (a, b, 1, 4, 1.0, c, d, None))):
+        xs = tensors(4)
+        used = {dp.make_grad_tensors: 2, dp.make_ghost_layers: 3}.get(make, 4)
+        refs = [weakref.ref(x) for x in xs[:used]]
+        items = make([entry(*xs)])
+        del xs
+        gc.collect()
+        assert all(r() is not None for r in refs), make.__name__
+        del items
+        gc.collect()
+        assert all(r() is None for r in refs), make.__name__
