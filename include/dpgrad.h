@@ -392,7 +392,7 @@ dp_status dp_gated_ffn_forward(const void *X, const void *Wg, const void *Wu, dp
  * arrays as dH, G or U (they then overwrite them), not the same as each other;
  * otherwise outputs overlap nothing.  Sizes as for the forward.  Workspace:
  * dp_gated_ffn_backward_workspace_bytes(M, d_in, d_ff, dt) bytes, 16-byte
- * aligned. */
+ * aligned; none where dX is NULL. */
 size_t dp_gated_ffn_backward_workspace_bytes(int64_t M, int64_t d_in, int64_t d_ff, dp_dtype dt);
 dp_status dp_gated_ffn_backward(const void *dH, const void *G, const void *U, const void *Wg,
                                 const void *Wu, dp_dtype dt, int64_t M, int64_t d_in, int64_t d_ff,

@@ -202,7 +202,7 @@ extern "C" dp_status dp_gated_ffn_backward(const void *dH, const void *G, const 
     if (M == 0) return DP_OK;
     DPG_REQUIRE(dH != nullptr && G != nullptr && U != nullptr && BG != nullptr && BU != nullptr && BG != BU, DP_EINVAL);
     DPG_REQUIRE(dX == nullptr || (Wg != nullptr && Wu != nullptr), DP_EINVAL);
-    const size_t need = dp_gated_ffn_backward_workspace_bytes(M, d_in, d_ff, dt);
+    const size_t need = dX == nullptr ? 0 : dp_gated_ffn_backward_workspace_bytes(M, d_in, d_ff, dt);
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
     const i64 n = M * d_ff;
     if (dt == DP_F32) {

@@ -243,3 +243,18 @@ def test_empty():
     assert forward(torch.empty((0, 8), device=DEV), W, W, 0)[0].shape == (0, 4)
     e = torch.empty((0, 4), device=DEV)
     assert backward(e, e.clone(), e.clone(), W, W, 0, BG=None)[2].shape == (0, 8)
+
+
+@pytest.mark.parametrize("M,K,F", [(20, 64, 2048), (300, 264, 136)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_backprops_alone_take_no_workspace(M, K, F, dt):
+    """Without dX nothing but the elementwise pass runs: no workspace, no weights."""
+    say("ffn backprops alone", M, K, F, dt)
+    rng = np.random.default_rng(M)
+    tt, ct = DT[dt]
+    dH, G, U = [torch.from_numpy(rng.standard_normal((M, F))).to(tt) for _ in range(3)]
+    BG, BU = [torch.full((M, F), 7.0, dtype=tt, device=DEV) for _ in range(2)]
+    dp.dp_gated_ffn_backward(dH.to(DEV), G.to(DEV), U.to(DEV), None, None, ct, M, K, F, dp.DP_ACT_SILU, BG, BU)
+    (wg, wu), (bg, bu) = R.ffn_backprops(dp.DP_ACT_SILU, R.f64(dH), R.f64(G), R.f64(U), tt)
+    R.within(BG, wg, bg, "BG")
+    R.within(BU, wu, bu, "BU")
