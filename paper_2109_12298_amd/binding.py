@@ -9,7 +9,8 @@ library is not built, loading fails loudly.  The functions of the
 language-model operators (dp_embedding_lookup, dp_clip_accumulate_tokens,
 dp_gated_ffn_*, dp_clip_global_norm_many) also check their tensors: dense, on
 one GPU, of the declared type and at least the declared size, else ValueError
-or TypeError; they are enqueued on the tensors' GPU.
+or TypeError; they are enqueued on the tensors' GPU, and a torch stream of
+another one is refused (ValueError).
 """
 from __future__ import annotations
 
@@ -361,6 +362,8 @@ def _tensors(where, *args):
 def _run(where, dev, fn, *args, stream):
     """The call on GPU `dev` (None: the current one), on its current stream unless the caller names one."""
     import torch
+    if stream is not None and dev is not None and dev != getattr(stream, "device_index", dev):
+        raise ValueError("%s: the stream is on GPU %d, the tensors on GPU %d" % (where, stream.device_index, dev))
     if dev is None or dev == torch.cuda.current_device():
         code = fn(*args, _raw_stream(dev) if stream is None and dev is not None else _stream(stream))
     else:

@@ -205,3 +205,35 @@ def test_item_lists_keep_their_tensors():
         del items
         gc.collect()
         assert all(r() is None for r in refs), make.__name__
+
+
+def test_a_stream_of_another_gpu_is_refused():
+    """The kernels would run there, on addresses of this one."""
+    class Fake:                                      # stands for a GPU tensor
+        def __init__(self, dtype, n):
+            self.dtype, self.n = dtype, n
+
+        def get_device(self):
+            return 0
+
+        def is_contiguous(self):
+            return True
+
+        def numel(self):
+            return self.n
+
+        def data_ptr(self):
+            return FAKE
+
+        def element_size(self):
+            return 4
+
+    class Stream:
+        device_index, cuda_stream = 1, FAKE
+
+    f = lambda n: Fake(torch.float32, n)  # noqa: E731
+    with pytest.raises(ValueError, match="stream is on GPU 1, the tensors on GPU 0"):
+        dp.dp_embedding_lookup(Fake(torch.int64, 6), f(40), dp.DP_F32, 2, 3, 10, 4, 1.0, f(24), dp.DP_F32, stream=Stream())
+    items = dp.make_grad_tensors([(f(40), None, 40, dp.DP_F32)])
+    with pytest.raises(ValueError, match="stream is on GPU 1, the tensors on GPU 0"):
+        dp.dp_clip_global_norm_many(items, 1, 1.0, FAKE, None, Fake(torch.uint8, 400), stream=Stream())
