@@ -65,9 +65,16 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const int64_t *__restr
                 Pack<TY, VEC> out;
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) from_f32(ok ? scale * to_f32(in[k].v[i]) : 0.0f, out.v[i]);
-                if constexpr (STREAM) {
-                    typedef uint32_t u32_t __attribute__((ext_vector_type(sizeof(out) / 4)));
-                    __builtin_nontemporal_store(__builtin_bit_cast(u32_t, out), reinterpret_cast<u32_t *>(y + d));
+                if constexpr (STREAM) {           // pieces of at most 16 bytes, as the rows are aligned
+                    constexpr int W = sizeof(out) < 16 ? sizeof(out) / 4 : 4, PIECES = sizeof(out) / (4 * W);
+                    typedef uint32_t piece_t __attribute__((ext_vector_type(W)));
+                    struct Pieces {
+                        piece_t v[PIECES];
+                    };
+                    const Pieces p = __builtin_bit_cast(Pieces, out);
+#pragma unroll
+                    for (int i = 0; i < PIECES; ++i)
+                        __builtin_nontemporal_store(p.v[i], reinterpret_cast<piece_t *>(y + d) + i);
                 } else {
                     *reinterpret_cast<Pack<TY, VEC> *>(y + d) = out;
                 }

@@ -76,6 +76,25 @@ def test_lookup_large_output(te, ty):
     assert torch.equal(Y, (E.float() * 1.5).to(yt)[ids])               # one product, one rounding: the same bits
 
 
+@pytest.mark.parametrize("te,ty", [("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("D", [2056, 2060])
+def test_lookup_large_output_between_boundaries(te, ty, D):
+    """Outputs stored past the caches, from 16 bytes behind a 32-byte boundary."""
+    say("lookup large between boundaries", te, ty, D)
+    (tt, ct), (yt, cy) = DT[te], DT[ty]
+    N, T, V = 7, 3700, 900
+    g = torch.Generator(device=DEV).manual_seed(3)
+    E = torch.randn((V, D), generator=g, device=DEV).to(tt)
+    ids = torch.randint(0, V, (N, T), generator=g, device=DEV)
+    by = 16 // torch.empty((), dtype=yt).element_size()
+    buf = torch.full((N * T * D + 64,), 7.0, dtype=yt, device=DEV)
+    Y = buf[by:by + N * T * D].view(N, T, D)
+    assert Y.data_ptr() % 32 == 16 and Y.numel() * Y.element_size() > 96 << 20
+    dp.dp_embedding_lookup(ids, E, ct, N, T, V, D, 1.5, Y, cy)
+    assert torch.equal(Y, (E.float() * 1.5).to(yt)[ids])
+    assert (buf[:by] == 7).all() and (buf[by + N * T * D:] == 7).all()
+
+
 def test_lookup_bad_ids_and_empty():
     say("lookup bad ids")
     V, D = 6, 40
