@@ -175,20 +175,22 @@ void launch(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, 
     while (waves < max_waves<MB>() && groups * waves < 2048 && units >= 2 * waves * UNITS) waves *= 2;
     const size_t lds = (size_t)waves * 2 * MB * 64 * sizeof(f32x4_t);
     const bool vec = K % Piece<T>::N == 0 && aligned(X, 16) && aligned(Wg, 16) && aligned(Wu, 16);
-    if (vec)
-        ffn_rows_kernel<T, ACT, MB, UNITS, true><<<(unsigned)groups, 64 * waves, lds, stream>>>(
-            (const T *)X, (const T *)Wg, (const T *)Wu, (int)M, K, F, (T *)H, (T *)G, (T *)U);
-    else
-        ffn_rows_kernel<T, ACT, MB, UNITS, false><<<(unsigned)groups, 64 * waves, lds, stream>>>(
-            (const T *)X, (const T *)Wg, (const T *)Wu, (int)M, K, F, (T *)H, (T *)G, (T *)U);
+    const auto go = [&](auto kernel) {
+        kernel<<<(unsigned)groups, 64 * waves, lds, stream>>>((const T *)X, (const T *)Wg, (const T *)Wu, (int)M, K, F,
+                                                              (T *)H, (T *)G, (T *)U);
+    };
+    // (aligned bf16 rows above kFfnRowsBf16 go to the tiles, but for d_in from 2^21 on: single loads do for those)
+    constexpr bool VEC = sizeof(T) == 4 || MB == 1;
+    if (VEC && vec) go(ffn_rows_kernel<T, ACT, MB, UNITS, VEC>);
+    else go(ffn_rows_kernel<T, ACT, MB, UNITS, false>);
 }
 
 template <typename T, int ACT>
 void by_rows(const void *X, const void *Wg, const void *Wu, i64 M, i64 K, i64 F, void *H, void *G, void *U,
              hipStream_t stream)
 {
-    // units in flight, 4096 -> 11008: one row bf16 37.8 us with 2, 38.0 with 1, 41 with 4; fp32 32 rows 104 us with 1,
-    // 119 with 2; 64 rows 165 with 3, 179 with 1
+    // units in flight, measured at 4096 -> 11008 alone and taken for all sizes: one row bf16 37.8 us with 2, 38.0 with 1,
+    // 41 with 4; fp32 32 rows 104 us with 1, 119 with 2; 64 rows 165 with 3, 179 with 1
     if (M <= 16) launch<T, ACT, 1, 2>(X, Wg, Wu, M, K, F, H, G, U, stream);
     else if (M <= 32) launch<T, ACT, 2, 1>(X, Wg, Wu, M, K, F, H, G, U, stream);
     else launch<T, ACT, 4, 3>(X, Wg, Wu, M, K, F, H, G, U, stream);
@@ -333,7 +335,6 @@ __global__ __launch_bounds__(256) void ffn_dx_rows_sum_kernel(const float *__res
         out[i] = ordered_sum(part + i, n, splits);
 }
 
-// runs of features: 512 workgroups with the column blocks, each wave two groups of features at the least
 // Runs of features by the time they take: 32 features at 0.75 us (1.35 over 32
 // rows) per round of 256 workgroups; more than one run takes one more launch
 // and writes and reads partial sums.  64 x 4096 -> 4096: 182 us in two runs, 59

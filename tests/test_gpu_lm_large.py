@@ -115,15 +115,16 @@ def test_ffn_of_long_sums(dt):
     assert ((dX.double() - want).abs() <= eps * want.abs() + 12 * n * 2.0 ** -24 * 15 * math.sqrt(n)).all()
 
 
+@pytest.mark.parametrize("M", [66, 40, 9])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-def test_ffn_of_long_sums_exactly(dt):
+def test_ffn_of_long_sums_exactly(M, dt):
     """The same lengths on whole numbers small enough that every sum is exact in fp32 in any order (|partial sums| under
     2^24: forward at most 4 n = 2^23, backward 300 standard deviations of sqrt(n (0.9 + 32^2 * 1.4)) = 5.5e4): the
     outputs are the exact sums, rounded once."""
-    say("long sums exactly", dt)
+    say("long sums exactly", M, dt)
     tt, ct = (torch.float32, dp.DP_F32) if dt == "f32" else (torch.bfloat16, dp.DP_BF16)
     g = torch.Generator(device=DEV).manual_seed(6)
-    n, M, few = 2 ** 21 + 8, 66, 3
+    n, few = 2 ** 21 + 8, 3
     ints = lambda top, *s: torch.randint(-top, top + 1, s, generator=g, device=DEV).to(tt)  # noqa: E731
     X, Wg, Wu = ints(2, M, n), ints(2, few, n), ints(2, few, n)
     H, G, U = [torch.full((M, few), 7.0, dtype=tt, device=DEV) for _ in range(3)]
