@@ -21,6 +21,9 @@
 namespace dpg {
 namespace {
 
+// piece q of row r lies at piece q ^ swizzle(r)
+__device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
+
 template <int BM_, int BF_, int WM_, int WF_, int BK_, int NS_>
 struct Shape {
     static constexpr int BM = BM_, BF = BF_, WM = WM_, WF = WF_, BK = BK_, NS = NS_;
@@ -35,7 +38,7 @@ struct Shape {
     static_assert(LOADS * RPI * WAVES == ROWS && BM % RPI == 0 && BF % RPI == 0, "stage split");
     static_assert(WAVES * 32 * (FF * 128 + 16) <= LDS, "the output transpose fits the stages");
     static_assert(NS >= 2 && NS <= 4, "waits");
-    static_assert(BK / 16 % 2 == 0, "two sets of operands in turn");
+    static_assert(BK == 64, "eight pieces in a row; two sets of operands in turn");
 };
 
 template <typename S, int ACT>
@@ -71,7 +74,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16
         const int in = first < S::BM ? row : first < S::BM + S::BF ? row - S::BM : row - S::BM - S::BF;
         const i64 left = first < S::BM ? M - m0 : F - f0;
         base[r] = reinterpret_cast<const char *>(P);
-        q[r] = (lane % (64 / S::RPI)) ^ swizzle<BK>(row);
+        q[r] = (lane % (64 / S::RPI)) ^ swizzle(row);
         off[r] = (uint32_t)(in < left ? in : (int)left - 1) * (uint32_t)(2 * K) + 16u * q[r];
     }
     const auto issue = [&](int c) {
@@ -104,7 +107,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16
         bf16x8_t x[FM], g[FF], u[FF];
     };
     const int li = lane & 31, lk = lane >> 5;
-    const int sw = swizzle<BK>(li);                          // of every row li + 32 n
+    const int sw = swizzle(li);                          // of every row li + 32 n
     const auto load_frag = [&](const char *L, int ks, Frag &f) {
         const int at = 16 * ((2 * ks + lk) ^ sw) + li * ROW;
 #pragma unroll
@@ -142,7 +145,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16
         if (c < nst) issue(c);
     {
         const int later = (nst < NS - 1 ? nst : NS - 1) - 1;
-        wait_later<S::LOADS>(later);
+        wait_stages_after<S::LOADS>(later);
         zero_tail(0);
         wait_lgkmcnt0();
         stage_barrier();
@@ -162,7 +165,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_forward_kernel(const uint16
     for (int c = 0; c + 1 < nst; ++c) {
         inside(smem + (c % NS) * S::STAGE);
         // stage c + 1 has landed, and every wave has read the last of stage c: its buffer takes stage c + NS
-        wait_later<S::LOADS>(nst - 2 - c < NS - 2 ? nst - 2 - c : NS - 2);
+        wait_stages_after<S::LOADS>(nst - 2 - c < NS - 2 ? nst - 2 - c : NS - 2);
         zero_tail(c + 1);
         wait_lgkmcnt0();
         stage_barrier();
@@ -228,6 +231,7 @@ struct DxShape {
     static constexpr int FM = BM / WM / 32, FD = BD / WD / 32;
     static constexpr int LDS = NS * STAGE;
     static_assert(A_LOADS * WAVES * 1024 == A_BYTES && W_LOADS * WAVES * 1024 == W_BYTES, "stage split");
+    static_assert(BK == 64, "eight pieces in a row; two sets of operands in turn");
     static_assert(WAVES * 32 * (FD * 128 + 16) <= LDS, "the output transpose fits the stages");
 };
 
@@ -261,7 +265,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
 #pragma unroll
     for (int r = 0; r < S::A_LOADS; ++r) {
         const int row = (wave + S::WAVES * r) * S::A_RPI + lane / (64 / S::A_RPI);
-        q[r] = (lane % (64 / S::A_RPI)) ^ swizzle<BK>(row);
+        q[r] = (lane % (64 / S::A_RPI)) ^ swizzle(row);
         offA[r] = (uint32_t)(row < M - m0 ? row : (int)(M - m0) - 1) * (uint32_t)(2 * lda) + 16u * q[r];
     }
 #pragma unroll
@@ -313,7 +317,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
         bf16x8_t a[FM], w[FD];
     };
     const int li = lane & 31, lk = lane >> 5;
-    const int sw = swizzle<BK>(li);
+    const int sw = swizzle(li);
     const auto load_frag = [&](const char *L, int ks, Frag &f) {
 #pragma unroll
         for (int x = 0; x < FM; ++x)
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
 #pragma unroll
     for (int c = 0; c < NS - 1; ++c)
         if (c < nst) issue(c);
-    wait_later<S::LOADS>((nst < NS - 1 ? nst : NS - 1) - 1);
+    wait_stages_after<S::LOADS>((nst < NS - 1 ? nst : NS - 1) - 1);
     zero_tail(0);
     wait_lgkmcnt0();
     stage_barrier();
@@ -359,7 +363,7 @@ __global__ __launch_bounds__(S::THREADS, 1) void ffn_dx_kernel(const uint16_t *_
     };
     for (int c = 0; c + 1 < nst; ++c) {
         inside(smem + (c % NS) * S::STAGE);
-        wait_later<S::LOADS>(nst - 2 - c < NS - 2 ? nst - 2 - c : NS - 2);
+        wait_stages_after<S::LOADS>(nst - 2 - c < NS - 2 ? nst - 2 - c : NS - 2);
         zero_tail(c + 1);
         wait_lgkmcnt0();
         stage_barrier();
@@ -514,8 +518,8 @@ struct DxPlan {
 
 // Tile shape and splits by the time they take: rounds of 256 workgroups, each
 // of its stages at what one takes (256 x 256 tiles 1.75 us, 128 x 128 0.59:
-// measured at 8192 x 11008 -> 4096 and 4096 x 2048 -> 768), and the partial
-// tiles written and read.  4096 x 2048 -> 768 (192 tiles of 128): 53 us in one
+// measured at 8192 x 11008 -> 4096 and 4096 x 2048 -> 768 alone, and taken for
+// all sizes), and the partial tiles written and read.  4096 x 2048 -> 768 (192 tiles of 128): 53 us in one
 // split, 65 in two; 128 x 11008 -> 4096 (32 tiles): 206 us in one, 64 in eight.
 DxPlan dx_plan(i64 M, i64 D, i64 F)
 {

@@ -96,7 +96,7 @@ __device__ __forceinline__ void run_stages(int nst, const Issue &issue, const Re
         if (c < nst)
 #pragma unroll
             for (int r = 0; r < kLoads; ++r) issue(c, r);
-    wait_later<kLoads>(nst - 1);
+    wait_stages_after<kLoads>(nst - 1);
     stage_barrier();
     Frag fa, fb;
 #pragma unroll
@@ -105,7 +105,7 @@ __device__ __forceinline__ void run_stages(int nst, const Issue &issue, const Re
     const auto step = [&](auto ISSUE, int c, const Frag &f, Frag &next) {
         // stage c + 1 has landed, and every wave has read stage c: its buffer takes stage c + kNS
         if constexpr (decltype(ISSUE)::value) wait_vmcnt<kLoads>();
-        else wait_later<kLoads>(nst - 2 - c < 1 ? 0 : 1);
+        else wait_stages_after<kLoads>(nst - 2 - c < 1 ? 0 : 1);
         wait_lgkmcnt0();
         stage_barrier();
         if constexpr (!decltype(ISSUE)::value)

@@ -26,21 +26,6 @@ __device__ __forceinline__ void dma16_off(const void *base, uint32_t off, uint32
                      : "memory", "m0");
 }
 
-// wait until all but the last `later` (at most 2) stages' loads have landed, N loads each
-template <int N>
-__device__ __forceinline__ void wait_later(int later)
-{
-    if (later >= 2) wait_vmcnt<2 * N>();
-    else if (later == 1) wait_vmcnt<N>();
-    else wait_vmcnt<0>();
-}
-
-template <int BK>
-__device__ __forceinline__ int swizzle(int row)
-{
-    return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
-}
-
 // Tile order: workgroups go round robin over the XCDs; each XCD takes a run of
 // consecutive tiles, 8 tiles of positions by as many tiles of features as the
 // run holds, so that its L2 serves the operand rows that they share.

@@ -172,7 +172,7 @@ __device__ __forceinline__ int rank_tile(const uint32_t (&digit)[ITEMS], const b
     return run;
 }
 
-// zeros to the 16-byte pieces [lo, hi) of a 16-byte aligned array, by the workgroups first, first + 1, ...
+// zeros to the n 16-byte pieces at p, of which `blocks` workgroups take equal shares (this one is number `block`)
 __device__ __forceinline__ void fill16(uint4 *p, i64 n, i64 block, i64 blocks)
 {
     const uint4 z = make_uint4(0, 0, 0, 0);
