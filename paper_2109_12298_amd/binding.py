@@ -240,7 +240,8 @@ class DPGradTensor(ctypes.Structure):
 
 
 def make_grad_tensors(entries):
-    """A dp_grad_tensor array from (g, out, numel, dtype) tuples; out None: the tensor counts in the norm only."""
+    """A dp_grad_tensor array from (g, out, numel, dtype) tuples; out None: the tensor counts in the norm only.  Takes
+    about 1 us of the host's time per tensor: keep the array while the buffers stay."""
     arr = _item_array(DPGradTensor, entries)
     dev, ptrs = _tensors("make_grad_tensors", *[(n, x, _tdtype(dt), numel) for g, out, numel, dt in entries
                                                 for n, x in (("g", g), ("out", out))])

@@ -533,9 +533,9 @@ void split_arrays(const Splits &s, hipStream_t stream)
 // Splits of the features by the time they take: a stage at 0.55 us while most
 // workgroups have a CU to themselves, at 1.39 us per round of two per CU, the
 // first loads and last stores, and the partial tiles written and read.
-// 512 x 2752 -> 1024 (32 tiles), the whole call: 184 us in one split, 72 in
-// four, 64 in six, 72 in eight, 75 in sixteen; 4096 x 2752 -> 1024 (256 tiles)
-// 307 in one, 310 in two, 338 in eight.
+// 512 x 2752 -> 1024 (32 tiles), the whole call: 183 us in one split, 68 in
+// four, 60 in six and in eight, 71 in sixteen; 4096 x 2752 -> 1024 (256 tiles)
+// 304 in one, 309 in two, 334 in eight.
 int dx_splits(i64 M, i64 D, i64 F)
 {
     const i64 stages = 2 * stages_of(F), tiles = ceil_div(M, DxTile::BM) * ceil_div(D, DxTile::BD);
