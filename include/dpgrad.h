@@ -369,7 +369,7 @@ typedef enum dp_act { DP_ACT_SILU = 0, DP_ACT_GELU_TANH = 1 } dp_act;
  * 64 rows run on the bf16 matrix units as three bf16 parts, which keep every
  * bit; tiles of up to 128 rows and columns that an infinity, a NaN, a value
  * from about 2^104 on or a sum from 2^80 on reaches run again on the fp32
- * units, ten times slower: the results agree to rounding.)  The block's output
+ * units, far slower: the results agree to rounding.)  The block's output
  * projection is a Linear layer that takes H as its A.  Workspace:
  * dp_gated_ffn_forward_workspace_bytes(M, d_in, d_ff, dt) bytes, 16-byte
  * aligned. */

@@ -234,7 +234,7 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_forward_kernel(Parts X,
     for (int x = 0; x < FM; ++x)
 #pragma unroll
         for (int y = 0; y < FF; ++y) sums += probe(ag[x][y]) + probe(au[x][y]);
-    if (__syncthreads_or(sums != 0.0f)) {                       // the stages are free from here on
+    if (__syncthreads_or(sums != 0.0f)) {                    // the stages are free from here on
         for (int t = 0; t < (S::BM / kTM) * (S::BF / kTN); ++t)
             any_forward_tile<kThreads, ACT>(whole.a, whole.wg, whole.wu, M, whole.K, F, m0 + t / (S::BF / kTN) * kTM,
                                             f0 + t % (S::BF / kTN) * kTN, H, G, U, reinterpret_cast<float *>(smem));
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(kThreads, 2) void ffn_parts_dx_kernel(Parts BG, Par
     for (int x = 0; x < FM; ++x)
 #pragma unroll
         for (int y = 0; y < FD; ++y) sums += probe(acc[x][y]);
-    if (__syncthreads_or(sums != 0.0f)) {                       // the stages are free from here on
+    if (__syncthreads_or(sums != 0.0f)) {                    // the stages are free from here on
         for (int t = 0; t < (S::BM / kTM) * (S::BD / kTN); ++t)
             any_dx_tile<kThreads>(whole.a, whole.b, whole.wg, whole.wu, M, D, whole.K, m0 + t / (S::BD / kTN) * kTM,
                                   d0 + t % (S::BD / kTN) * kTN, dX, reinterpret_cast<float *>(smem));
