@@ -400,6 +400,124 @@ dp_status dp_gated_ffn_backward(const void *dH, const void *G, const void *U, co
                                 hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
+ * A token model between its weight layers: positions, attention, loss
+ * ------------------------------------------------------------------------- */
+
+/* Rotary positions over one or several axes (text; or time, height and width
+ * of images and video).  Pair j of a head is turned by the angle
+ *   t = pos[a(j)][n][t] * freq[j]:
+ *   (x, y) -> (x cos t - y sin t, y cos t + x sin t),
+ * a(j) being the axis whose section holds j: axis 0 has the first sections[0]
+ * pairs, axis 1 the next sections[1], and so on; P = the sections' sum.
+ * DP_ROTARY_HALVES pairs value j with value j + P, DP_ROTARY_ADJACENT value
+ * 2j with 2j + 1; values from 2P on are copied.  inverse != 0 turns by -t: the
+ * gradient of the call (it takes the backprops of Y and gives those of X).
+ * X: [N][T] positions of `dt`, ldx values from one to the next, each H heads
+ * of D values; Y: the same with ldy; so both may lie inside a fused
+ * projection's output, and heads of queries and keys that lie side by side
+ * take one call.  Y may be X (with ldy = ldx); otherwise they do not overlap.
+ * pos: int64 [axes][N][T], any values below 2^53 in size; freq: fp64 [P];
+ * sections: a host array of `axes` counts >= 0, read during the call only.
+ * Angles are formed and reduced in 64 bits (their error is 2^-53 of the
+ * angle), sines, cosines and products in fp32, rounded once.
+ * N, T >= 0, H, D >= 1, 1 <= axes <= 4, 2P <= D, ldx, ldy >= H*D; needs
+ * N*T < 2^31, D <= 1024, H < 2^20, ldx, ldy < 2^31 (else DP_EUNSUPPORTED). */
+typedef enum dp_rotary_layout { DP_ROTARY_HALVES = 0, DP_ROTARY_ADJACENT = 1 } dp_rotary_layout;
+dp_status dp_rotary(const void *X, dp_dtype dt, int64_t N, int64_t T, int64_t H, int64_t D, int64_t ldx,
+                    const int64_t *pos, const int64_t *sections, int32_t axes, const double *freq,
+                    dp_rotary_layout layout, int32_t inverse, void *Y, int64_t ldy, hipStream_t stream);
+
+/* What an attention call works on (a host struct, read during the call only).
+ *
+ * Q and O: [N][Tq] positions, ldq (ldo) values from one to the next, each Hq
+ * heads of D values; K and V: [N][Tk] positions with ldk (ldv), each Hk heads;
+ * query heads h with equal h / (Hq / Hk) share a key head.  A sample's
+ * positions follow the previous sample's (sample stride Tq*ldq and so on), so
+ * Q, K and V may be sections of one fused projection's output, and K and V a
+ * cache of Tk places.
+ *
+ * Sample n has L = lens[n] keys (clamped to [0, Tk]; lens NULL: Tk); keys from
+ * L on are not looked at.  Query i stands at position i, or with
+ * DP_ATTENTION_LAST at L - Tq + i (the last ones: new tokens over a cache).
+ * The query at position p sees key j < L if
+ *   - without DP_ATTENTION_CAUSAL, always; with it, j <= p or j < prefix[n]
+ *     (prefix NULL: 0), and
+ *   - docs is NULL, or docs[n][j] == docs[n][p] >= 0.
+ * Queries at positions outside [0, L) are padding and see nothing.
+ * The score of a visible pair is
+ *   s = scale * q.k;  s = softcap * tanh(s / softcap) if softcap > 0;
+ *   s -= slopes[h] * |p - j| if slopes is given,
+ * and o = sum_j softmax(s)_j v_j.  A query that sees nothing has o = 0.
+ * Pairs that are not visible have no part in any result, whatever is in them. */
+typedef struct dp_attention {
+    int32_t dt;             /* a dp_dtype: of Q, K, V, O and their gradients */
+    uint32_t flags;         /* DP_ATTENTION_CAUSAL, DP_ATTENTION_LAST; other bits must be 0 */
+    int64_t N, Tq, Tk, Hq, Hk, D;
+    int64_t ldq, ldk, ldv, ldo;
+    float scale;            /* finite */
+    float softcap;          /* 0: none; finite, >= 0 */
+    const float *slopes;    /* fp32 [Hq], or NULL */
+    const int32_t *lens;    /* int32 [N], or NULL */
+    const int32_t *prefix;  /* int32 [N], or NULL; with DP_ATTENTION_CAUSAL only */
+    const int32_t *docs;    /* int32 [N][Tk], or NULL */
+} dp_attention;
+
+enum { DP_ATTENTION_CAUSAL = 1, DP_ATTENTION_LAST = 2 };
+
+/* O, and lse (fp32 [N][Hq][Tq], or NULL): the logarithm of a query's softmax
+ * sum, -inf where it sees nothing.  Scores, sums and outputs are formed in
+ * fp32; with bf16 inputs the softmax weights are rounded to bf16 before their
+ * product with V.  N, Tq, Tk >= 0; Hq a multiple of Hk >= 1; 1 <= D <= 256;
+ * ldq, ldo >= Hq*D, ldk, ldv >= Hk*D.  Needs Tq, Tk < 2^24, N*Hq*Tq < 2^31,
+ * N*Hk*Tk < 2^31 and ld* < 2^23 (else DP_EUNSUPPORTED).  O overlaps no input.
+ * Workspace: dp_attention_forward_workspace_bytes(a), 16-byte aligned (0 but
+ * for few queries over many keys, whose keys are split over workgroups and
+ * joined in a fixed order). */
+size_t dp_attention_forward_workspace_bytes(const dp_attention *a);
+dp_status dp_attention_forward(const dp_attention *a, const void *Q, const void *K, const void *V, void *O,
+                               float *lse, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* The backprops of Q, K and V from dO, the backprops of O, and from what the
+ * forward call read and wrote (O and lse).  With p = exp(s - lse):
+ *   dV_j = sum p_ij dO_i,  g_ij = p_ij (dO_i.V_j - dO_i.O_i) (1 - tanh^2) scale,
+ *   dQ_i = sum_j g_ij K_j, dK_j = sum_i g_ij Q_i
+ * (tanh^2 as the score's, 0 without softcap; the sums of a key head run over
+ * its query heads).  dO is laid out as O, dQ, dK and dV as Q, K and V.
+ * Padding queries and keys from L on get zeros.  Sums are formed in fp32; with
+ * bf16 inputs p and g are rounded to bf16 before their products.  Outputs
+ * overlap nothing.  Sizes as the forward call; workspace:
+ * dp_attention_backward_workspace_bytes(a), 16-byte aligned. */
+size_t dp_attention_backward_workspace_bytes(const dp_attention *a);
+dp_status dp_attention_backward(const dp_attention *a, const void *Q, const void *K, const void *V, const void *O,
+                                const float *lse, const void *dO, void *dQ, void *dK, void *dV, void *ws,
+                                size_t ws_bytes, hipStream_t stream);
+
+/* The loss at a token model's end and its gradient in one call: distillation
+ * from a teacher's top logits, and cross entropy with a label, at M positions
+ * over V classes.  With P = softmax(logits[m][k] / tau) over the k with
+ * ids[m][k] >= 0, q_t = softmax(Z[m] / t):
+ *   loss[m] = w ( alpha tau^2 sum_k P_k (log P_k - log q_tau[ids[m][k]])
+ *                 + (1 - alpha) (-log q_1[labels[m]]) ),
+ *   dZ[m][v] = w ( alpha tau (q_tau[v] - sum over ids[m][k] = v of P_k)
+ *                  + (1 - alpha) (q_1[v] - [v = labels[m]]) ),  w = weight[m].
+ * The first part is absent where K = 0 or every id of the position is
+ * negative, the second where labels is NULL or labels[m] < 0.  A position with
+ * weight 0 is left out: loss 0, zeros in dZ, nothing of it is looked at.
+ * weight NULL: 1.  An id may occur twice.  A logit of -inf has probability 0.
+ * Z, dZ: [M][V] of `dt`; dZ may be Z itself (in place) or NULL (the loss only);
+ * ids: int64 [M][K]; logits: fp32 [M][K]; labels: int64 [M]; weight, loss: fp32
+ * [M].  An id or label >= V sets DP_FLAG_BAD_INDEX and is left out.  dZ is the
+ * output layer's backprops B of the per-sample losses (divide by nothing: the
+ * clipped step averages).  Softmax sums are formed in fp32, dZ is rounded once.
+ * M, K >= 0, V >= 1, 0 <= alpha <= 1, tau > 0 finite; needs M < 2^31, V < 2^30,
+ * K <= 1024 (else DP_EUNSUPPORTED).  Workspace:
+ * dp_distill_loss_workspace_bytes(M, V, K, dt), 16-byte aligned. */
+size_t dp_distill_loss_workspace_bytes(int64_t M, int64_t V, int64_t K, dp_dtype dt);
+dp_status dp_distill_loss(const void *Z, dp_dtype dt, int64_t M, int64_t V, const int64_t *ids, const float *logits,
+                          int64_t K, const int64_t *labels, float alpha, float tau, const float *weight, float *loss,
+                          void *dZ, int32_t *status, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Norms and clipping
  * ------------------------------------------------------------------------- */
 

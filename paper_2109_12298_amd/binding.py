@@ -7,10 +7,13 @@ workspace tensor; ``stream`` defaults to torch's current HIP stream.  A status
 other than DP_OK raises :class:`DPError`.  There is no fallback: if the
 library is not built, loading fails loudly.  The functions of the
 language-model operators (dp_embedding_lookup, dp_clip_accumulate_tokens,
-dp_gated_ffn_*, dp_clip_global_norm_many) also check their tensors: dense, on
-one GPU, of the declared type and at least the declared size, else ValueError
-or TypeError; they are enqueued on the tensors' GPU, and a torch stream of
-another one is refused (ValueError).
+dp_gated_ffn_*, dp_clip_global_norm_many, dp_rotary, dp_attention_*,
+dp_distill_loss) also check their tensors: dense, on one GPU, of the declared
+type and at least the declared size, else ValueError or TypeError; they are
+enqueued on the tensors' GPU, and a torch stream of another one is refused
+(ValueError).  Where a call takes the values from one position to the next
+(ldx, ldq and the like), a tensor may be a view of [N][T] positions with those
+strides, such as a section of a fused projection's output.
 """
 from __future__ import annotations
 
@@ -57,6 +60,13 @@ SIGNATURES = {
     "dp_gated_ffn_forward": (_ST, [_P, _P, _P, _ST, _I64, _I64, _I64, _ST, _P, _P, _P, _P, _SZ, _P]),
     "dp_gated_ffn_backward_workspace_bytes": (_SZ, [_I64, _I64, _I64, _ST]),
     "dp_gated_ffn_backward": (_ST, [_P, _P, _P, _P, _P, _ST, _I64, _I64, _I64, _ST, _P, _P, _P, _P, _SZ, _P]),
+    "dp_rotary": (_ST, [_P, _ST, _I64, _I64, _I64, _I64, _I64, _P, _P, _I32, _P, _ST, _I32, _P, _I64, _P]),
+    "dp_attention_forward_workspace_bytes": (_SZ, [_P]),
+    "dp_attention_forward": (_ST, [_P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "dp_attention_backward_workspace_bytes": (_SZ, [_P]),
+    "dp_attention_backward": (_ST, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "dp_distill_loss_workspace_bytes": (_SZ, [_I64, _I64, _I64, _ST]),
+    "dp_distill_loss": (_ST, [_P, _ST, _I64, _I64, _P, _P, _I64, _P, _F, _F, _P, _P, _P, _P, _P, _SZ, _P]),
     "dp_grad_sample_layernorm_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
     "dp_grad_sample_layernorm": (_ST, [_P, _P, _ST, _I64, _I64, _I64, _F, _P, _P, _P, _P, _P, _SZ, _P]),
     "dp_grad_sample_groupnorm_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
@@ -253,6 +263,32 @@ def make_grad_tensors(entries):
     return arr
 
 
+DP_ATTENTION_CAUSAL, DP_ATTENTION_LAST = 1, 2
+
+
+class DPAttention(ctypes.Structure):
+    """struct dp_attention of dpgrad.h."""
+    _fields_ = [("dt", ctypes.c_int32), ("flags", ctypes.c_uint32)] + \
+               [(f, ctypes.c_int64) for f in ("N", "Tq", "Tk", "Hq", "Hk", "D", "ldq", "ldk", "ldv", "ldo")] + \
+               [("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + \
+               [(f, ctypes.c_void_p) for f in ("slopes", "lens", "prefix", "docs")]
+
+
+def make_attention(dt, N, Tq, Tk, Hq, Hk, D, scale, flags=0, softcap=0.0, slopes=None, lens=None, prefix=None, docs=None,
+                   ldq=None, ldk=None, ldv=None, ldo=None):
+    """A dp_attention; ld* default to dense positions.  It keeps the tensors whose addresses it holds."""
+    import torch
+    a = DPAttention(dt=dt, flags=flags, N=N, Tq=Tq, Tk=Tk, Hq=Hq, Hk=Hk, D=D, scale=scale, softcap=softcap)
+    a.ldq, a.ldo = [Hq * D if ld is None else ld for ld in (ldq, ldo)]
+    a.ldk, a.ldv = [Hk * D if ld is None else ld for ld in (ldk, ldv)]
+    i32 = torch.int32
+    a.dev, p = _tensors("make_attention", ("slopes", slopes, torch.float32, Hq), ("lens", lens, i32, N),
+                        ("prefix", prefix, i32, N), ("docs", docs, i32, N * Tk))
+    a.slopes, a.lens, a.prefix, a.docs = p
+    a.kept = (slopes, lens, prefix, docs)
+    return a
+
+
 class DPError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -356,6 +392,46 @@ def _tensors(where, *args):
             raise ValueError("%s: %s is not contiguous" % (where, name))
         if x.numel() < numel:
             raise ValueError("%s: %s has %d elements, %d are needed" % (where, name, x.numel(), numel))
+        ptrs.append(x.data_ptr())
+    return dev, ptrs
+
+
+def _rows(where, dev, dtype, *args):
+    """As _tensors for arrays of N samples of T positions with `ld` values from
+    one position to the next, `width` of them used (name, tensor, N, T, ld,
+    width).  A tensor that is not dense has to be a view [N][T][...] with those
+    strides.  `dev`: the GPU of the call's other tensors, or None."""
+    ptrs = []
+    for name, x, N, T, ld, width in args:
+        if x is None or x.__class__ is int:
+            ptrs.append(x)
+            continue
+        d = x.get_device()
+        if d != dev:
+            if d < 0:
+                raise ValueError("%s: %s is not on a GPU" % (where, name))
+            if dev is not None:
+                raise ValueError("%s: %s is on GPU %d, other arguments on GPU %d" % (where, name, d, dev))
+            dev = d
+        if dtype is not None and x.dtype is not dtype:
+            raise TypeError("%s: %s is %s, not %s" % (where, name, x.dtype, dtype))
+        need = (N * T - 1) * ld + width if N > 0 and T > 0 else 0
+        if not x.is_contiguous():
+            st, sh = x.stride(), x.shape
+            inner = 1
+            for k in range(x.dim() - 1, 1, -1):
+                if sh[k] != 1 and st[k] != inner:
+                    break
+                inner *= sh[k]
+            else:
+                if x.dim() >= 3 and sh[0] >= N and sh[1] >= T and inner >= width and (N <= 1 or (st[0] == T * ld and sh[1] == T)) \
+                        and (T <= 1 or st[1] == ld):
+                    ptrs.append(x.data_ptr())
+                    continue
+            raise ValueError("%s: %s is neither contiguous nor [N][T][...] with %d values from one position to the next"
+                             % (where, name, ld))
+        if x.numel() < need:
+            raise ValueError("%s: %s has %d elements, %d are needed" % (where, name, x.numel(), need))
         ptrs.append(x.data_ptr())
     return dev, ptrs
 
@@ -489,6 +565,72 @@ def dp_gated_ffn_backward(dH, G, U, Wg, Wu, dt, M, d_in, d_ff, act, BG, BU, dX=N
                       ("Wu", Wu, t, k), ("BG", BG, t, n), ("BU", BU, t, n), ("dX", dX, t, M * d_in), ("ws", ws, None, 0))
     _run("dp_gated_ffn_backward", dev, lib().dp_gated_ffn_backward, p[0], p[1], p[2], p[3], p[4], dt, M, d_in, d_ff, act,
          p[5], p[6], p[7], p[8], _nbytes(ws), stream=stream)
+
+
+DP_ROTARY_HALVES, DP_ROTARY_ADJACENT = 0, 1
+
+
+def dp_rotary(X, dt, N, T, H, D, ldx, pos, sections, freq, layout, inverse, Y, ldy, stream=None):
+    """sections: a list of pairs per axis."""
+    import torch
+    where, axes = "dp_rotary", len(sections)
+    counts = (ctypes.c_int64 * max(axes, 1))(*sections)
+    dev, p = _tensors(where, ("pos", pos, torch.int64, axes * N * T), ("freq", freq, torch.float64, sum(sections)))
+    dev, r = _rows(where, dev, _tdtype(dt), ("X", X, N, T, ldx, H * D), ("Y", Y, N, T, ldy, H * D))
+    _run(where, dev, lib().dp_rotary, r[0], dt, N, T, H, D, ldx, p[0], ctypes.addressof(counts), axes, p[1], layout,
+         1 if inverse else 0, r[1], ldy, stream=stream)
+
+
+def dp_attention_forward_workspace_bytes(a) -> int:
+    return lib().dp_attention_forward_workspace_bytes(ctypes.addressof(a))
+
+
+def _attention_tensors(where, a, lse, ws, rows):
+    """rows: (name, tensor, positions, ld, heads)."""
+    import torch
+    dev, p = _tensors(where, ("lse", lse, torch.float32, a.N * a.Hq * a.Tq), ("ws", ws, None, 0))
+    on = getattr(a, "dev", None)
+    if dev is not None and on is not None and dev != on:
+        raise ValueError("%s: lse or ws is on GPU %d, the masks on GPU %d" % (where, dev, on))
+    dev, r = _rows(where, on if dev is None else dev, _tdtype(a.dt), *[(n, x, a.N, T, ld, H * a.D) for n, x, T, ld, H in rows])
+    return dev, p, r
+
+
+def dp_attention_forward(a, Q, K, V, O, lse=None, ws=None, stream=None):
+    dev, p, r = _attention_tensors("dp_attention_forward", a, lse, ws,
+                                   (("Q", Q, a.Tq, a.ldq, a.Hq), ("K", K, a.Tk, a.ldk, a.Hk), ("V", V, a.Tk, a.ldv, a.Hk),
+                                    ("O", O, a.Tq, a.ldo, a.Hq)))
+    _run("dp_attention_forward", dev, lib().dp_attention_forward, ctypes.addressof(a), r[0], r[1], r[2], r[3], p[0], p[1],
+         _nbytes(ws), stream=stream)
+
+
+def dp_attention_backward_workspace_bytes(a) -> int:
+    return lib().dp_attention_backward_workspace_bytes(ctypes.addressof(a))
+
+
+def dp_attention_backward(a, Q, K, V, O, lse, dO, dQ, dK, dV, ws=None, stream=None):
+    dev, p, r = _attention_tensors("dp_attention_backward", a, lse, ws,
+                                   (("Q", Q, a.Tq, a.ldq, a.Hq), ("K", K, a.Tk, a.ldk, a.Hk), ("V", V, a.Tk, a.ldv, a.Hk),
+                                    ("O", O, a.Tq, a.ldo, a.Hq), ("dO", dO, a.Tq, a.ldo, a.Hq),
+                                    ("dQ", dQ, a.Tq, a.ldq, a.Hq), ("dK", dK, a.Tk, a.ldk, a.Hk),
+                                    ("dV", dV, a.Tk, a.ldv, a.Hk)))
+    _run("dp_attention_backward", dev, lib().dp_attention_backward, ctypes.addressof(a), r[0], r[1], r[2], r[3], p[0], r[4],
+         r[5], r[6], r[7], p[1], _nbytes(ws), stream=stream)
+
+
+def dp_distill_loss_workspace_bytes(M, V, K, dt) -> int:
+    return lib().dp_distill_loss_workspace_bytes(M, V, K, dt)
+
+
+def dp_distill_loss(Z, dt, M, V, ids, logits, K, labels, alpha, tau, weight, loss, dZ=None, status=None, ws=None,
+                    stream=None):
+    import torch
+    t, f = _tdtype(dt), torch.float32
+    dev, p = _tensors("dp_distill_loss", ("Z", Z, t, M * V), ("ids", ids, torch.int64, M * K), ("logits", logits, f, M * K),
+                      ("labels", labels, torch.int64, M), ("weight", weight, f, M), ("loss", loss, f, M), ("dZ", dZ, t, M * V),
+                      ("status", status, torch.int32, 1), ("ws", ws, None, 0))
+    _run("dp_distill_loss", dev, lib().dp_distill_loss, p[0], dt, M, V, p[1], p[2], K, p[3], alpha, tau, p[4], p[5], p[6],
+         p[7], p[8], _nbytes(ws), stream=stream)
 
 
 def dp_lstm_backward(gates, c, W_hh, dh_out, dh_last, N, T, H, delta, status=None, stream=None):

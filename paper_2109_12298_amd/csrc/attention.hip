@@ -1,0 +1,75 @@
+// Attention's entry points: argument checks and the choice of kernels.
+#include "attention.hpp"
+
+#include <math.h>
+
+using namespace dpg;
+using namespace dpg::attn;
+
+namespace {
+
+constexpr i64 kMaxT = i64(1) << 24, kMaxRows = i64(1) << 31, kMaxLd = i64(1) << 23;
+
+dp_status check(const dp_attention *a)
+{
+    DPG_REQUIRE(a != nullptr, DP_EINVAL);
+    DPG_REQUIRE(a->dt == DP_F32 || a->dt == DP_BF16, DP_EDTYPE);
+    DPG_REQUIRE((a->flags & ~(uint32_t)(DP_ATTENTION_CAUSAL | DP_ATTENTION_LAST)) == 0, DP_EINVAL);
+    DPG_REQUIRE(a->N >= 0 && a->Tq >= 0 && a->Tk >= 0 && a->Hk >= 1 && a->Hq >= 1 && a->Hq % a->Hk == 0 && a->D >= 1,
+                DP_EINVAL);
+    DPG_REQUIRE(isfinite(a->scale) && isfinite(a->softcap) && a->softcap >= 0.0f, DP_EINVAL);
+    DPG_REQUIRE(a->prefix == nullptr || (a->flags & DP_ATTENTION_CAUSAL) != 0, DP_EINVAL);
+    DPG_REQUIRE(aligned(a->slopes, 4) && aligned(a->lens, 4) && aligned(a->prefix, 4) && aligned(a->docs, 4), DP_EINVAL);
+    DPG_REQUIRE(a->D <= kMaxD && a->Tq < kMaxT && a->Tk < kMaxT && a->N < kMaxRows && a->Hq < kMaxLd, DP_EUNSUPPORTED);
+    DPG_REQUIRE(a->N * a->Hq < kMaxRows && a->N * a->Hq * a->Tq < kMaxRows && a->N * a->Hk * a->Tk < kMaxRows,
+                DP_EUNSUPPORTED);
+    DPG_REQUIRE(a->ldq >= a->Hq * a->D && a->ldo >= a->Hq * a->D && a->ldk >= a->Hk * a->D && a->ldv >= a->Hk * a->D, DP_EINVAL);
+    DPG_REQUIRE(a->ldq < kMaxLd && a->ldo < kMaxLd && a->ldk < kMaxLd && a->ldv < kMaxLd, DP_EUNSUPPORTED);
+    return DP_OK;
+}
+
+Call call_of(const dp_attention &a, const void *Q, const void *K, const void *V)
+{
+    return {Q,     K,     V,     (int)a.N, (int)a.Tq, (int)a.Tk, (int)a.Hq,  (int)a.Hk, (int)a.D, (int)(a.Hq / a.Hk),
+            a.ldq, a.ldk, a.ldv, a.ldo,    a.scale,   a.softcap, a.slopes,   a.lens,    a.prefix, a.docs,
+            (a.flags & DP_ATTENTION_CAUSAL) != 0, (a.flags & DP_ATTENTION_LAST) != 0};
+}
+
+}  // namespace
+
+extern "C" size_t dp_attention_forward_workspace_bytes(const dp_attention *) { return 0; }
+
+extern "C" dp_status dp_attention_forward(const dp_attention *a, const void *Q, const void *K, const void *V, void *O,
+                                          float *lse, void *ws, size_t ws_bytes, hipStream_t stream)
+{
+    const dp_status s = check(a);
+    if (s != DP_OK) return s;
+    if (a->N == 0 || a->Tq == 0) return DP_OK;
+    const size_t e = dtype_bytes((dp_dtype)a->dt);
+    DPG_REQUIRE(Q != nullptr && O != nullptr && (a->Tk == 0 || (K != nullptr && V != nullptr)), DP_EINVAL);
+    DPG_REQUIRE(aligned(Q, e) && aligned(K, e) && aligned(V, e) && aligned(O, e) && aligned(lse, 4), DP_EINVAL);
+    const size_t need = dp_attention_forward_workspace_bytes(a);
+    DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
+    return rows_forward(call_of(*a, Q, K, V), (dp_dtype)a->dt, O, lse, stream);
+}
+
+extern "C" size_t dp_attention_backward_workspace_bytes(const dp_attention *) { return 0; }
+
+extern "C" dp_status dp_attention_backward(const dp_attention *a, const void *Q, const void *K, const void *V,
+                                           const void *O, const float *lse, const void *dO, void *dQ, void *dK, void *dV,
+                                           void *ws, size_t ws_bytes, hipStream_t stream)
+{
+    const dp_status s = check(a);
+    if (s != DP_OK) return s;
+    if (a->N == 0 || (a->Tq == 0 && a->Tk == 0)) return DP_OK;
+    const size_t e = dtype_bytes((dp_dtype)a->dt);
+    DPG_REQUIRE(a->Tq == 0 || (Q != nullptr && O != nullptr && lse != nullptr && dO != nullptr && dQ != nullptr), DP_EINVAL);
+    DPG_REQUIRE(a->Tk == 0 || (K != nullptr && V != nullptr && dK != nullptr && dV != nullptr), DP_EINVAL);
+    DPG_REQUIRE(a->Tk == 0 || dK != dV, DP_EINVAL);
+    DPG_REQUIRE(aligned(Q, e) && aligned(K, e) && aligned(V, e) && aligned(O, e) && aligned(lse, 4) && aligned(dO, e) &&
+                    aligned(dQ, e) && aligned(dK, e) && aligned(dV, e),
+                DP_EINVAL);
+    const size_t need = dp_attention_backward_workspace_bytes(a);
+    DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
+    return rows_backward(call_of(*a, Q, K, V), (dp_dtype)a->dt, O, lse, dO, dQ, dK, dV, stream);
+}

@@ -1,0 +1,361 @@
+// Distillation from a teacher's top logits, and cross entropy, with the gradient.
+//
+// With q_t = softmax(z / t) and P the teacher's softmax over its K logits,
+//   loss = w (a tau^2 sum P (log P - log q_tau) + (1 - a) (-log q_1[label]))
+//   dz   = w (a tau (q_tau - P) + (1 - a) (q_1 - onehot)).
+// Bound by its bytes: the logits are read once and the gradient written once.
+// One workgroup takes a position.  Rows that fit its registers stay there
+// between the three steps (maximum; sums of exponentials; gradient), so that
+// they are read once; longer rows are read again, by the same threads.  The
+// gradient leaves for the whole row as if no class had a target; after a
+// barrier (which waits for the stores) the at most K + 1 target classes are
+// written anew, each formed in fp32 from its own logit and rounded once.  Those
+// logits are read before the first store, so dZ may be Z.
+//
+// Rows start at any element: up to 16 / sizeof(T) - 1 elements before the first
+// 16-byte piece and behind the last one are single loads and stores.
+#include "common.hpp"
+
+namespace dpg {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxK = 1024;
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint16_t bf16_bits(float x)
+{
+    const __bf16 b = (__bf16)x;
+    return __builtin_bit_cast(uint16_t, b);
+}
+__device__ __forceinline__ void put(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put(uint16_t *p, float v) { *p = bf16_bits(v); }
+
+// element e of a 16-byte piece
+template <typename T>
+__device__ __forceinline__ float elem(u32x4_t v, int e)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(v[e]);
+    else return __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
+}
+
+// piece of f(0) .. f(N - 1)
+template <typename T, typename F>
+__device__ __forceinline__ u32x4_t piece(F &&f)
+{
+    u32x4_t v;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(f(e));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (uint32_t)bf16_bits(f(2 * e)) | ((uint32_t)bf16_bits(f(2 * e + 1)) << 16);
+    }
+    return v;
+}
+
+struct Args {
+    i64 V;
+    const int64_t *ids;
+    const float *logits;
+    int K;
+    const int64_t *labels;
+    float alpha, tau;
+    const float *weight;
+    float *loss;
+    int32_t *status;
+};
+
+// maximum (a NaN is passed over here and turns the sums to NaN) and sum over the
+// workgroup; `red` is __shared__ float[16], every thread gets the result
+__device__ __forceinline__ float wave_max(float v)
+{
+    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, kWave));
+    return v;
+}
+template <int THREADS>
+__device__ __forceinline__ float block_max(float v, float *red)
+{
+    v = wave_max(v);
+    if constexpr (THREADS > kWave) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = red[0];
+#pragma unroll
+        for (int w = 1; w < THREADS / kWave; ++w) v = fmaxf(v, red[w]);
+    }
+    return v;
+}
+template <int THREADS>
+__device__ __forceinline__ float sum_of_block(float v, float *red)
+{
+    if constexpr (THREADS == kWave) return wave_sum(v);
+    return block_sum(v, red);
+}
+
+// NV pieces of a row per thread are held; RESIDENT: they are the whole row.
+// SOFT, HARD: which parts of the loss the call has (a position may lack its own).
+template <typename T, int THREADS, int NV, bool RESIDENT, bool HARD>
+__global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, Args a, T *dZ)
+{
+    constexpr int N = 16 / sizeof(T);
+    __shared__ float red[16];
+    __shared__ float target[kMaxK];                        // P_k
+    __shared__ int32_t target_id[kMaxK];                   // -1: unused
+    const i64 m = blockIdx.x, V = a.V;
+    const int tid = threadIdx.x;
+    const T *z = Z + m * V;
+    T *dz = dZ != nullptr ? dZ + m * V : nullptr;
+    const float w = a.weight != nullptr ? a.weight[m] : 1.0f;
+
+    const int head = (int)(((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / sizeof(T));
+    const int first = head < V ? head : (int)V;
+    const int pieces = (int)((V - first) / N);
+    const int rest = first + pieces * N;                   // first element behind the pieces
+    const bool vec = dz != nullptr && ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+    // the single element of this thread, if any
+    const int single = tid < first ? tid : tid < first + (int)V - rest ? rest + tid - first : -1;
+
+    const auto leave_out = [&]() {
+        if (dz != nullptr) {
+            for (int p = tid; p < pieces; p += THREADS)
+                if (vec) *reinterpret_cast<u32x4_t *>(dz + first + (i64)p * N) = u32x4_t{0, 0, 0, 0};
+                else
+                    for (int e = 0; e < N; ++e) put(dz + first + (i64)p * N + e, 0.0f);
+            if (single >= 0) put(dz + single, 0.0f);
+        }
+        if (tid == 0) a.loss[m] = 0.0f;
+    };
+    if (w == 0.0f) {
+        leave_out();
+        return;
+    }
+
+    // the row's loads leave first
+    u32x4_t v[NV];
+    const auto load = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int p = base + i * THREADS + tid;
+            if (p < pieces) {
+                const u32x4_t *at = reinterpret_cast<const u32x4_t *>(z + first + (i64)p * N);
+                v[i] = RESIDENT ? __builtin_nontemporal_load(at) : *at;
+            }
+        }
+    };
+    float one = -INFINITY;
+    if (single >= 0) one = load_elem<T>(z, single);
+    if constexpr (RESIDENT) load(0);
+
+    // the teacher's softmax, and the target classes' own logits (before any store)
+    const float inv_tau = 1.0f / a.tau, c_tau = kLog2e * inv_tau;
+    float tmax = -INFINITY;
+    for (int k = tid; k < a.K; k += THREADS) {
+        const int64_t id = a.ids[m * a.K + k];
+        const bool ok = id >= 0 && id < V;
+        if (id >= V) raise_flag(a.status, DP_FLAG_BAD_INDEX);
+        target_id[k] = ok ? (int32_t)id : -1;
+        target[k] = ok ? a.logits[m * a.K + k] : -INFINITY;
+        tmax = fmaxf(tmax, target[k]);
+    }
+    tmax = block_max<THREADS>(tmax, red);
+    const float tbase = tmax == -INFINITY ? 0.0f : tmax;
+    float tsum = 0.0f;
+    for (int k = tid; k < a.K; k += THREADS)
+        if (target_id[k] >= 0) tsum += expf((target[k] - tbase) * inv_tau);
+    tsum = sum_of_block<THREADS>(tsum, red);
+    const bool soft = a.alpha > 0.0f && tsum != 0.0f;
+    const float ltsum = logf(tsum);
+    int label = -1;
+    if constexpr (HARD) {
+        const int64_t l = a.labels[m];
+        if (l >= V && tid == 0) raise_flag(a.status, DP_FLAG_BAD_INDEX);
+        if (l >= 0 && l < V) label = (int)l;
+    }
+    const bool hard = HARD && label >= 0 && a.alpha < 1.0f;
+    if (!soft && !hard) {                                  // no part of the loss
+        leave_out();
+        return;
+    }
+    const float z_label = hard ? load_elem<T>(z, label) : 0.0f;
+
+    // maximum, then the sums of exponentials
+    float zmax = one, s_tau = 0.0f, s_1 = 0.0f;
+    const auto add = [&](float x, float top) {
+        s_tau += __builtin_amdgcn_exp2f((x - top) * c_tau);
+        if constexpr (HARD) s_1 += __builtin_amdgcn_exp2f((x - top) * kLog2e);
+    };
+    if constexpr (RESIDENT) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * THREADS + tid < pieces)
+#pragma unroll
+                for (int e = 0; e < N; ++e) zmax = fmaxf(zmax, elem<T>(v[i], e));
+        zmax = block_max<THREADS>(zmax, red);
+    } else {
+        // one reading: a thread's sums follow its own maximum
+        float top = -INFINITY;
+        for (int base = 0; base < pieces; base += NV * THREADS) {
+            load(base);
+            float t = top;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (base + i * THREADS + tid < pieces)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) t = fmaxf(t, elem<T>(v[i], e));
+            if (t > top) {
+                s_tau *= __builtin_amdgcn_exp2f((top - t) * c_tau);
+                if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f((top - t) * kLog2e);
+                top = t;
+            }
+            const float b = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (base + i * THREADS + tid < pieces)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), b);
+        }
+        zmax = block_max<THREADS>(fmaxf(zmax, top), red);
+        if (top != -INFINITY) {
+            s_tau *= __builtin_amdgcn_exp2f((top - zmax) * c_tau);
+            if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f((top - zmax) * kLog2e);
+        }
+    }
+    const float zbase = zmax == -INFINITY ? 0.0f : zmax;
+    if (single >= 0) add(one, zbase);
+    if constexpr (RESIDENT)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i * THREADS + tid < pieces)
+#pragma unroll
+                for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), zbase);
+    s_tau = sum_of_block<THREADS>(s_tau, red);
+    if constexpr (HARD) s_1 = sum_of_block<THREADS>(s_1, red);
+
+    // P in place of the teacher's logits; the loss
+    float part = 0.0f;
+    const float lq = logf(s_tau);
+    for (int k = tid; k < a.K; k += THREADS) {
+        const int32_t id = target_id[k];
+        float P = 0.0f;
+        if (soft && id >= 0) {
+            const float lp = (target[k] - tbase) * inv_tau - ltsum;
+            P = expf(lp);
+            const float zk = load_elem<T>(z, id);
+            if (P != 0.0f) part += P * (lp - ((zk - zbase) * inv_tau - lq));
+        }
+        target[k] = P;
+    }
+    part = sum_of_block<THREADS>(part, red);
+    const float g_soft = soft ? a.alpha : 0.0f, g_hard = hard ? 1.0f - a.alpha : 0.0f;
+    if (tid == 0) {
+        float l = g_soft * a.tau * a.tau * part;
+        if (hard) l += g_hard * (logf(s_1) - (z_label - zbase));
+        a.loss[m] = w * l;
+    }
+    if (dz == nullptr) return;
+
+    // gradient of a class without a target: w a tau q_tau + w (1 - a) q_1
+    const float k_tau = soft ? w * g_soft * a.tau / s_tau : 0.0f, k_1 = hard ? w * g_hard / s_1 : 0.0f;
+    const auto grad = [&](float x) {
+        float g = k_tau * __builtin_amdgcn_exp2f((x - zbase) * c_tau);
+        if constexpr (HARD) g += k_1 * __builtin_amdgcn_exp2f((x - zbase) * kLog2e);
+        return g;
+    };
+    // the target classes' logits, before the stores (dZ may be Z)
+    float mine[(kMaxK + THREADS - 1) / THREADS];
+    for (int k = tid, i = 0; k < a.K; k += THREADS, ++i)
+        if (target_id[k] >= 0) mine[i] = load_elem<T>(z, target_id[k]);
+    __syncthreads();
+    for (int base = 0; base < (RESIDENT ? 1 : pieces); base += NV * THREADS) {
+        if constexpr (!RESIDENT) load(base);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int p = base + i * THREADS + tid;
+            if (p < pieces) {
+                const u32x4_t o = piece<T>([&](int e) { return grad(elem<T>(v[i], e)); });
+                T *at = dz + first + (i64)p * N;
+                if (vec) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t *>(at));
+                else
+#pragma unroll
+                    for (int e = 0; e < N; ++e) put(at + e, elem<T>(o, e));
+            }
+        }
+    }
+    if (single >= 0) put(dz + single, grad(one));
+    __syncthreads();                                       // waits for the stores above
+
+    // target classes: an id that occurs twice is written by its first place, with both
+    for (int k = tid, i = 0; k < a.K; k += THREADS, ++i) {
+        const int32_t id = target_id[k];
+        if (id < 0) continue;
+        float P = 0.0f;
+        bool mine_first = true;
+        for (int j = 0; j < a.K; ++j)
+            if (target_id[j] == id) {
+                P += target[j];
+                mine_first = mine_first && j >= k;
+            }
+        if (!mine_first) continue;
+        float g = grad(mine[i]) - w * g_soft * a.tau * P;
+        if (id == label) g -= w * g_hard;
+        put(dz + id, g);
+    }
+    if (tid == 0 && hard) {
+        bool alone = true;
+        for (int j = 0; j < a.K; ++j) alone = alone && target_id[j] != label;
+        if (alone) put(dz + label, grad(z_label) - w * g_hard);
+    }
+}
+
+template <typename T, int THREADS, int NV, bool RESIDENT>
+void launch(const T *Z, i64 M, const Args &a, T *dZ, hipStream_t stream)
+{
+    if (a.labels != nullptr && a.alpha < 1.0f)
+        distill_kernel<T, THREADS, NV, RESIDENT, true><<<(unsigned)M, THREADS, 0, stream>>>(Z, a, dZ);
+    else
+        distill_kernel<T, THREADS, NV, RESIDENT, false><<<(unsigned)M, THREADS, 0, stream>>>(Z, a, dZ);
+}
+
+template <typename T>
+dp_status run(const void *Zp, i64 M, const Args &a, void *dZp, hipStream_t stream)
+{
+    const T *Z = (const T *)Zp;
+    T *dZ = (T *)dZp;
+    const i64 pieces = a.V / (16 / (i64)sizeof(T));
+    if (pieces <= 64 * 4) launch<T, 64, 4, true>(Z, M, a, dZ, stream);
+    else if (pieces <= 256 * 4) launch<T, 256, 4, true>(Z, M, a, dZ, stream);
+    else if (pieces <= 1024 * 4) launch<T, 1024, 4, true>(Z, M, a, dZ, stream);
+    else if (pieces <= 1024 * 8) launch<T, 1024, 8, true>(Z, M, a, dZ, stream);
+    else if (pieces <= 1024 * 13) launch<T, 1024, 13, true>(Z, M, a, dZ, stream);
+    else if (pieces <= 1024 * 20) launch<T, 1024, 20, true>(Z, M, a, dZ, stream);
+    else launch<T, 1024, 8, false>(Z, M, a, dZ, stream);
+    return launch_status();
+}
+
+}  // namespace
+}  // namespace dpg
+
+using namespace dpg;
+
+extern "C" size_t dp_distill_loss_workspace_bytes(int64_t, int64_t, int64_t, dp_dtype) { return 0; }
+
+extern "C" dp_status dp_distill_loss(const void *Z, dp_dtype dt, int64_t M, int64_t V, const int64_t *ids,
+                                     const float *logits, int64_t K, const int64_t *labels, float alpha, float tau,
+                                     const float *weight, float *loss, void *dZ, int32_t *status, void *, size_t,
+                                     hipStream_t stream)
+{
+    DPG_REQUIRE(dtype_ok(dt), DP_EDTYPE);
+    DPG_REQUIRE(M >= 0 && K >= 0 && V >= 1, DP_EINVAL);
+    DPG_REQUIRE(alpha >= 0.0f && alpha <= 1.0f && tau > 0.0f && tau < INFINITY, DP_EINVAL);
+    DPG_REQUIRE(M < (i64(1) << 31) && V < (i64(1) << 30) && K <= kMaxK, DP_EUNSUPPORTED);
+    if (M == 0) return DP_OK;
+    DPG_REQUIRE(Z != nullptr && loss != nullptr && (K == 0 || (ids != nullptr && logits != nullptr)), DP_EINVAL);
+    DPG_REQUIRE(aligned(Z, dtype_bytes(dt)) && aligned(dZ, dtype_bytes(dt)) && aligned(loss, 4) && aligned(weight, 4) &&
+                    aligned(logits, 4) && aligned(ids, 8) && aligned(labels, 8) && aligned(status, 4),
+                DP_EINVAL);
+    const Args a = {V, ids, logits, (int)K, labels, alpha, tau, weight, loss, status};
+    return dt == DP_F32 ? run<float>(Z, M, a, dZ, stream) : run<uint16_t>(Z, M, a, dZ, stream);
+}
