@@ -32,7 +32,11 @@ HIPFLAGS = ["-O3", "-std=c++17", "--offload-arch=" + ARCH, "-fPIC", "-Wall",
 # Per-file extra flags.  clipsum_many.hip keeps its MFMA accumulators in
 # VGPRs (it rescales them with VALU multiplies once per sample) and clobbers
 # M0 in inline assembly on purpose.
-EXTRA = {"clipsum_many.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
+EXTRA = {"attention_backward.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
+         "attention_backward_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
+         "attention_forward.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
+         "attention_forward_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
+         "clipsum_many.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],
          "conv2d_split.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "conv2d_small.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
          "ffn_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Wno-inline-asm"],

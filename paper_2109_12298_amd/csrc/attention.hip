@@ -1,5 +1,7 @@
 // Attention's entry points: argument checks and the choice of kernels.
 #include "attention.hpp"
+#include "attention_backward.hpp"
+#include "attention_forward.hpp"
 
 #include <math.h>
 
@@ -8,7 +10,8 @@ using namespace dpg::attn;
 
 namespace {
 
-constexpr i64 kMaxT = i64(1) << 24, kMaxRows = i64(1) << 31, kMaxLd = i64(1) << 23;
+constexpr i64 kMaxT = i64(1) << 24, kMaxRows = i64(1) << 31, kMaxLd = i64(1) << 22,
+              kMaxBlocks = i64(1) << 24;
 
 dp_status check(const dp_attention *a)
 {
@@ -21,7 +24,9 @@ dp_status check(const dp_attention *a)
     DPG_REQUIRE(a->prefix == nullptr || (a->flags & DP_ATTENTION_CAUSAL) != 0, DP_EINVAL);
     DPG_REQUIRE(aligned(a->slopes, 4) && aligned(a->lens, 4) && aligned(a->prefix, 4) && aligned(a->docs, 4), DP_EINVAL);
     DPG_REQUIRE(a->D <= kMaxD && a->Tq < kMaxT && a->Tk < kMaxT && a->N < kMaxRows && a->Hq < kMaxLd, DP_EUNSUPPORTED);
-    DPG_REQUIRE(a->N * a->Hq < kMaxRows && a->N * a->Hq * a->Tq < kMaxRows && a->N * a->Hk * a->Tk < kMaxRows,
+    DPG_REQUIRE(a->N * a->Hq < kMaxRows, DP_EUNSUPPORTED);
+    // a dimension of a grid holds fewer than 2^32 threads, and 32 queries or keys of a head are a workgroup at the least
+    DPG_REQUIRE(a->N * a->Hq * ceil_div(a->Tq, 32) < kMaxBlocks && a->N * a->Hk * ceil_div(a->Tk, 32) < kMaxBlocks,
                 DP_EUNSUPPORTED);
     DPG_REQUIRE(a->ldq >= a->Hq * a->D && a->ldo >= a->Hq * a->D && a->ldk >= a->Hk * a->D && a->ldv >= a->Hk * a->D, DP_EINVAL);
     DPG_REQUIRE(a->ldq < kMaxLd && a->ldo < kMaxLd && a->ldk < kMaxLd && a->ldv < kMaxLd, DP_EUNSUPPORTED);
@@ -37,7 +42,11 @@ Call call_of(const dp_attention &a, const void *Q, const void *K, const void *V)
 
 }  // namespace
 
-extern "C" size_t dp_attention_forward_workspace_bytes(const dp_attention *) { return 0; }
+extern "C" size_t dp_attention_forward_workspace_bytes(const dp_attention *a)
+{
+    if (check(a) != DP_OK || a->D > kTileD) return 0;
+    return tiles_forward_workspace(*a);
+}
 
 extern "C" dp_status dp_attention_forward(const dp_attention *a, const void *Q, const void *K, const void *V, void *O,
                                           float *lse, void *ws, size_t ws_bytes, hipStream_t stream)
@@ -50,10 +59,16 @@ extern "C" dp_status dp_attention_forward(const dp_attention *a, const void *Q, 
     DPG_REQUIRE(aligned(Q, e) && aligned(K, e) && aligned(V, e) && aligned(O, e) && aligned(lse, 4), DP_EINVAL);
     const size_t need = dp_attention_forward_workspace_bytes(a);
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
-    return rows_forward(call_of(*a, Q, K, V), (dp_dtype)a->dt, O, lse, stream);
+    const Call c = call_of(*a, Q, K, V);
+    if (a->D > kTileD) return rows_forward(c, (dp_dtype)a->dt, O, lse, stream);
+    return tiles_forward(c, (dp_dtype)a->dt, forward_splits(*a), O, lse, ws, stream);
 }
 
-extern "C" size_t dp_attention_backward_workspace_bytes(const dp_attention *) { return 0; }
+extern "C" size_t dp_attention_backward_workspace_bytes(const dp_attention *a)
+{
+    if (check(a) != DP_OK || a->D > kTileD) return 0;
+    return tiles_backward_workspace(*a);
+}
 
 extern "C" dp_status dp_attention_backward(const dp_attention *a, const void *Q, const void *K, const void *V,
                                            const void *O, const float *lse, const void *dO, void *dQ, void *dK, void *dV,
@@ -71,5 +86,7 @@ extern "C" dp_status dp_attention_backward(const dp_attention *a, const void *Q,
                 DP_EINVAL);
     const size_t need = dp_attention_backward_workspace_bytes(a);
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
-    return rows_backward(call_of(*a, Q, K, V), (dp_dtype)a->dt, O, lse, dO, dQ, dK, dV, stream);
+    const Call c = call_of(*a, Q, K, V);
+    if (a->D > kTileD) return rows_backward(c, (dp_dtype)a->dt, O, lse, dO, dQ, dK, dV, stream);
+    return tiles_backward(c, (dp_dtype)a->dt, {O, dO, lse, dQ, dK, dV, nullptr, nullptr, 0, false, false}, ws, stream);
 }

@@ -7,7 +7,7 @@
 namespace dpg {
 namespace attn {
 
-constexpr int kMaxD = 256;
+constexpr int kMaxD = 256, kTileD = 128;      // values of a head, at the most: at all, and in the tiles
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Call {

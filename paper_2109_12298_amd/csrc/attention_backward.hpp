@@ -1,0 +1,25 @@
+// Attention backward on tiles: see attention_backward_kernel.hpp.
+#pragma once
+
+#include "attention.hpp"
+
+namespace dpg {
+namespace attn {
+
+struct Grads {
+    const void *O, *dO;
+    const float *lse;
+    void *dQ, *dK, *dV;
+    float *row_lse, *row_delta;      // [N][Hq][pad]: lse in units of ln 2 (+inf: the query sees nothing), dO.O
+    int pad;                         // queries, rounded up to 64
+    bool small_q, small_k;           // 32 rows (keys) a workgroup instead of 128
+};
+
+size_t tiles_backward_workspace(const dp_attention &a);
+dp_status tiles_backward(const Call &c, dp_dtype dt, Grads g, void *ws, hipStream_t stream);
+
+dp_status backward_bf16(const Call &c, const Grads &g, hipStream_t stream);
+dp_status backward_f32(const Call &c, const Grads &g, hipStream_t stream);
+
+}  // namespace attn
+}  // namespace dpg

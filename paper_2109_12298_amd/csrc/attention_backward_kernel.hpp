@@ -1,0 +1,597 @@
+// Attention backward: with s the scores, p = exp(s - lse) and delta = dO.O,
+//   dV_j = sum_i p_ij dO_i,  e_ij = p_ij (dO_i.V_j - delta_i) (1 - tanh^2),
+//   dQ_i = scale sum_j e_ij K_j,  dK_j = scale sum_i e_ij Q_i.
+//
+// Three launches: lse and delta of every query; dQ, by blocks of rows over
+// tiles of keys, as the forward pass; dK and dV, by blocks of keys over tiles
+// of queries.  Scores and dO.V are formed in both (seven products where five
+// would do), so that every sum belongs to one workgroup: no atomics, no partial
+// sums in memory, the same bits every run, and a key head's sum over its query
+// heads is one more loop.
+//
+// dQ forms scores as keys x rows and dK, dV as rows x keys, so that p and e are
+// in either the second operand of the product that sums over them, in the
+// registers they were formed in (attention_tile.hpp).  Blocks of 128 rows or
+// keys share tiles, two stages deep, where there are blocks enough to fill the
+// card; else 32 are one workgroup whose waves take different tiles and whose
+// sums are added in wave order.
+//
+// As in the forward pass, a block whose sums are not finite is formed again row
+// by row, over visible pairs only.
+#pragma once
+
+#include "attention_backward.hpp"
+
+#include "attention_tile.hpp"
+
+#include <type_traits>
+
+namespace dpg {
+namespace attn {
+namespace {
+
+constexpr int kGroup = 1024;             // tiles in a list
+constexpr i64 kMaxGrid = i64(1) << 22;   // a dimension of a grid holds fewer than 2^32 threads
+
+template <typename T, int DP, bool SMALL>
+struct Shape {
+    typedef Tile<T, DP> TL;
+    static constexpr int NW = SMALL && TL::RB >= 384 ? 2 : 4;
+    static constexpr int BN = SMALL || sizeof(T) == 4 ? 32 : 64;         // rows of a staged tile
+    static constexpr int BR = SMALL ? 32 : 32 * NW;                      // rows (or keys) of a workgroup
+    static constexpr int FN = BN / 32, THREADS = 64 * NW;
+    static constexpr int HALF = BN * TL::RB, INFO = 2 * 256, STAGE = 2 * HALF + INFO;
+    static constexpr int OUT_ROW = SMALL ? DP * 4 + 16 : TL::RB + 16;    // bytes of an output row in LDS
+    static constexpr int STAGES = (SMALL ? NW : 1) * 2 * STAGE, OUTPUT = NW * 32 * OUT_ROW;
+    static constexpr int LDS = STAGES > OUTPUT ? STAGES : OUTPUT;
+};
+
+// ---------------------------------------------------------------------------
+// lse and delta of every query: 16 lanes a query
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void row_info_kernel(Call c, Grads gr, bool vec)
+{
+    constexpr int N = 16 / sizeof(T);
+    const i64 per = (i64)c.Hq * gr.pad;
+    const int sub = threadIdx.x & 15;
+    for (i64 q = (i64)blockIdx.x * 16 + threadIdx.x / 16; q < (i64)c.N * per; q += (i64)gridDim.x * 16) {
+        const int n = (int)(q / per);
+        const i64 at = q - n * per;
+        // heads fastest, so that neighbours in memory are read together
+        const int i = (int)(at / c.Hq), h = (int)(at - (i64)i * c.Hq);
+        const i64 to = ((i64)n * c.Hq + h) * gr.pad + i;
+        float lse = INFINITY, delta = 0.0f;
+        const Sample s(c, n);
+        const int p = s.first + i;
+        if (i < c.Tq && p >= 0 && p < s.L) {
+            const i64 from = ((i64)n * c.Tq + i) * c.ldo + (i64)h * c.D;
+            const T *o = (const T *)gr.O + from, *d = (const T *)gr.dO + from;
+            const float l = gr.lse[((i64)n * c.Hq + h) * c.Tq + i];
+            lse = l == -INFINITY ? INFINITY : l * kLog2e;
+            for (int k = sub * N; k < c.D; k += 16 * N) {
+                if (vec) {
+                    const u32x4_t a = *reinterpret_cast<const u32x4_t *>(o + k), b = *reinterpret_cast<const u32x4_t *>(d + k);
+                    const T *x = reinterpret_cast<const T *>(&a), *y = reinterpret_cast<const T *>(&b);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) delta += load_elem<T>(x, e) * load_elem<T>(y, e);
+                } else {
+                    for (int e = 0; e < N && k + e < c.D; ++e) delta += load_elem<T>(o, k + e) * load_elem<T>(d, k + e);
+                }
+            }
+        }
+        for (int off = 8; off >= 1; off >>= 1) delta += __shfl_xor(delta, off, 16);
+        if (sub == 0) {
+            gr.row_lse[to] = lse;
+            gr.row_delta[to] = lse == INFINITY ? 0.0f : delta;
+        }
+    }
+}
+
+// Ordered list of the tiles [t0, t1) that classify() does not skip: entries (tile - t0) << 2 | class; returns their number.
+// Every thread of the workgroup takes part.
+template <int THREADS, typename F>
+__device__ __forceinline__ int tile_list(int t0, int t1, uint16_t *list, uint8_t *cls_of, int *counts, F &&classify)
+{
+    const int lane = threadIdx.x & 63;
+    __syncthreads();
+    for (int k = threadIdx.x; k < kGroup; k += THREADS) {
+        const int cls = k < t1 - t0 ? classify(t0 + k) : kSkip;
+        cls_of[k] = (uint8_t)cls;
+        const unsigned long long some = __ballot(cls != kSkip);
+        if (lane == 0) counts[k >> 6] = __popcll(some);
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < kGroup; k += THREADS) {
+        const int cls = cls_of[k];
+        const unsigned long long some = __ballot(cls != kSkip);
+        int at = __popcll(some & ((1ull << lane) - 1));
+        for (int w = 0; w < k >> 6; ++w) at += counts[w];
+        if (cls != kSkip) list[at] = (uint16_t)(k << 2 | cls);
+    }
+    int count = 0;
+    for (int w = 0; w < kGroup / 64; ++w) count += counts[w];
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(count);
+}
+
+// range of docs[p0 .. p1], by one wave
+__device__ __forceinline__ void wave_docs_range(const int32_t *docs, int p0, int p1, int lane, int &lo, int &hi)
+{
+    lo = 0x7fffffff;
+    hi = -0x7fffffff - 1;
+    for (int p = p0 + lane; p <= p1; p += 64) {
+        const int d = docs[p];
+        lo = d < lo ? d : lo;
+        hi = d > hi ? d : hi;
+    }
+    for (int off = 32; off >= 1; off >>= 1) {
+        const int l2 = __shfl_xor(lo, off, kWave), h2 = __shfl_xor(hi, off, kWave);
+        lo = l2 < lo ? l2 : lo;
+        hi = h2 > hi ? h2 : hi;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+}
+
+// 32 output rows from LDS rows of LDT bytes (values of T); to(row): where the row lies, or NULL
+template <typename T, int DP, int LDT, typename F>
+__device__ __forceinline__ void store_rows(const char *L, int D, bool vec, int lane, F &&to)
+{
+    typedef Tile<T, DP> TL;
+#pragma unroll 4
+    for (int at = lane; at < 32 * TL::PIECES; at += kWave) {
+        const int row = at / TL::PIECES, d = (at - row * TL::PIECES) * TL::N;
+        T *o = d < D ? to(row) : nullptr;
+        if (o == nullptr) continue;
+        const T *x = reinterpret_cast<const T *>(L + row * LDT) + d;
+        if (vec) *reinterpret_cast<u32x4_t *>(o + d) = *reinterpret_cast<const u32x4_t *>(x);
+        else
+#pragma unroll
+            for (int e = 0; e < TL::N; ++e)
+                if (d + e < D) o[d + e] = x[e];
+    }
+}
+
+// The sums of a block of 32 columns, f * acc, to memory: a wave's own (LARGE), or the waves' sums added in wave order (SMALL,
+// all waves take part).  Returns whether a value is not finite.
+template <typename T, int DP, typename S, bool SMALL, typename F>
+__device__ __forceinline__ bool put_block(char *smem, f32x16_t (&acc)[Tile<T, DP>::DB], float f, int D, bool vec, int lane, int wave,
+                                          F &&to)
+{
+    constexpr int DB = Tile<T, DP>::DB;
+    const int li = lane & 31, h = lane >> 5;
+    char *L = smem + wave * 32 * S::OUT_ROW + li * S::OUT_ROW;
+    bool bad = false;
+    if constexpr (!SMALL) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float v = f * acc[d][e];
+                bad = bad || not_finite(v);
+                store_elem(reinterpret_cast<T *>(L) + 32 * d + 8 * (e >> 2) + 4 * h + (e & 3), v);
+            }
+        store_rows<T, DP, S::OUT_ROW>(smem + wave * 32 * S::OUT_ROW, D, vec, lane, to);
+        return bad;
+    } else {
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<float4 *>(L + 4 * (32 * d + 2 * e + 4 * h)) =
+                    make_float4(acc[d][e], acc[d][e + 1], acc[d][e + 2], acc[d][e + 3]);
+        __syncthreads();
+        for (int at = threadIdx.x; at < 32 * (DP / 4); at += S::THREADS) {
+            const int row = at / (DP / 4), d = 4 * (at - row * (DP / 4));
+            T *o = d < D ? to(row) : nullptr;
+            if (o == nullptr) continue;
+            float v[4] = {};
+#pragma unroll
+            for (int w = 0; w < S::NW; ++w) {
+                const float4 x = *reinterpret_cast<const float4 *>(smem + (w * 32 + row) * S::OUT_ROW + 4 * d);
+                v[0] += x.x;
+                v[1] += x.y;
+                v[2] += x.z;
+                v[3] += x.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] *= f;
+                bad = bad || not_finite(v[e]);
+                if (d + e < D) store_elem(o + d + e, v[e]);
+            }
+        }
+        return bad;
+    }
+}
+
+template <int DB>
+__device__ __forceinline__ void zero(f32x16_t (&acc)[DB])
+{
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] = 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// dQ
+// ---------------------------------------------------------------------------
+template <typename T, int DP, bool VEC, int MOD, bool SMALL>
+__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, DP>::RB >= 384 ? 1 : 2)) void query_kernel(
+    Call c, Grads gr, int tiles_m, bool vec_out)
+{
+    typedef Shape<T, DP, SMALL> S;
+    typedef Tile<T, DP> TL;
+    constexpr int BN = S::BN, FN = S::FN, DB = TL::DB, KS = TL::KS, NW = S::NW;
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    __shared__ uint16_t list[kGroup];
+    __shared__ uint8_t cls_of[kGroup];
+    __shared__ int counts[kGroup / 64];
+
+    const int lane = threadIdx.x & 63, li = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int heads = c.N * c.Hk;
+    const int nk = (int)blockIdx.x % heads, tm = tiles_m - 1 - (int)blockIdx.x / heads;
+    const int n = nk / c.Hk, kv = nk - n * c.Hk;
+    const Sample smp(c, n);
+    const int M = c.Tq * c.G, r0 = tm * S::BR, rw = SMALL ? r0 : r0 + 32 * wave;
+    const T *K = (const T *)c.K + (i64)n * c.Tk * c.ldk + (i64)kv * c.D;
+    const T *V = (const T *)c.V + (i64)n * c.Tk * c.ldv + (i64)kv * c.D;
+
+    const int r = rw + li, i = r / c.G, g = r - i * c.G;
+    const bool row_ok = r < M;
+    const int pos = smp.first + i;
+    const bool seeing = row_ok && pos >= 0 && pos < smp.L;
+    const int lim = seeing ? smp.end_for(pos) : 0;
+    const int doc = seeing && smp.docs != nullptr ? smp.docs[pos] : -1;
+    const int head = kv * c.G + (row_ok ? g : 0);
+    const i64 row = (i64)n * c.Tq + (row_ok ? i : 0), info = ((i64)n * c.Hq + head) * gr.pad + (row_ok ? i : 0);
+    u32x4_t qf[KS], df[KS];
+    TL::load_row((const T *)c.Q + row * c.ldq + (i64)head * c.D, c.D, row_ok, VEC, lane, qf);
+    TL::load_row((const T *)gr.dO + row * c.ldo + (i64)head * c.D, c.D, row_ok, VEC, lane, df);
+    const float lse2 = row_ok ? gr.row_lse[info] : INFINITY, delta = row_ok ? gr.row_delta[info] : 0.0f;
+    const Mod mod(c);
+    const float slope2 = MOD == 1 && c.slopes != nullptr ? c.slopes[head] * kLog2e : 0.0f;
+
+    RowSpan span = span_of(smp, c.G, M, r0, S::BR);
+    const int end = smp.end_for(span.pmax < span.pmin ? -1 : span.pmax), t1 = (end + BN - 1) / BN;
+    if (smp.docs != nullptr) wave_docs_range(smp.docs, span.pmin, span.pmax, lane, span.dmin, span.dmax);
+
+    f32x16_t acc[DB];
+    zero(acc);
+    const Stager<TL, T, BN, SMALL ? 1 : NW, VEC> stk(c.ldk, c.D, SMALL ? 0 : wave, lane), stv(c.ldv, c.D, SMALL ? 0 : wave, lane);
+    char *mine = smem + (SMALL ? wave * 2 * S::STAGE : 0);
+    const uint32_t lds0 = lds_addr(mine);
+    const auto issue = [&](int t, int buf) {
+        const i64 k0 = (i64)t * BN;
+        const int left = (int)(end - k0);
+        stk.issue(K + k0 * c.ldk, left, lds0 + buf * S::STAGE, mine + buf * S::STAGE);
+        stv.issue(V + k0 * c.ldv, left, lds0 + buf * S::STAGE + S::HALF, mine + buf * S::STAGE + S::HALF);
+    };
+    const auto step = [&](const char *LK, const char *LV, int k0, int cls) {
+#pragma unroll
+        for (int x = 0; x < FN; ++x) {
+            f32x16_t s, e;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) s[k] = e[k] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                TL::mma(TL::rows(LK, 32 * x, ks, lane), qf[ks], s);
+                TL::mma(TL::rows(LV, 32 * x, ks, lane), df[ks], e);
+            }
+            const auto key = [&](int k) { return k0 + 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                float bend = 1.0f;
+                float p;
+                if constexpr (MOD == 0) p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k], mod.scale2, -lse2));
+                else
+                    p = __builtin_amdgcn_exp2f(
+                        modded<T>(mod, s[k], slope2, __builtin_fabsf((float)(pos - key(k))), bend) - lse2);
+                e[k] = p * (e[k] - delta);
+                if constexpr (MOD == 1) e[k] *= bend;
+            }
+            if (cls != kFull) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) e[k] = key(k) < lim ? e[k] : 0.0f;
+                if (smp.docs != nullptr) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const int j = key(k), d = smp.docs[j < end ? j : end - 1];
+                        e[k] = d == doc && d >= 0 ? e[k] : 0.0f;
+                    }
+                }
+            }
+            TL::mma_columns(LK, 32 * x, e, acc, lane);
+        }
+    };
+
+    int base = 0;
+    while (base < t1) {
+        const bool docs = smp.docs != nullptr;
+        const int stop = !docs || t1 - base <= kGroup ? t1 : base + kGroup;
+        int count = stop - base;
+        if (docs)
+            count = tile_list<S::THREADS>(base, stop, list, cls_of, counts, [&](int t) {
+                const int j0 = t * BN, j1 = j0 + BN < end ? j0 + BN : end;
+                int lo, hi;
+                docs_range(smp.docs, j0, j1, lo, hi);
+                return meet(smp, span, j0, j0 + BN, lo, hi);
+            });
+        const auto entry = [&](int k, int &t, int &cls) {
+            if (docs) {
+                const int e = __builtin_amdgcn_readfirstlane(list[k]);
+                t = base + (e >> 2);
+                cls = e & 3;
+            } else {
+                t = base + k;
+                cls = meet(smp, span, t * BN, t * BN + BN, 0, 0);
+            }
+        };
+        int t, cls;
+        constexpr int STEP = SMALL ? NW : 1;
+        const int k0 = SMALL ? wave : 0;
+        if (k0 < count) {
+            entry(k0, t, cls);
+            issue(t, 0);
+            int buf = 0;
+            for (int k = k0; k < count; k += STEP, buf ^= 1) {
+                const int at = t * BN, now = cls;
+                wait_loads();
+                if constexpr (SMALL) bf16s::wait_lgkmcnt0();
+                else lds_barrier();                     // this tile has landed, the one before is read
+                if (k + STEP < count) {
+                    entry(k + STEP, t, cls);
+                    issue(t, buf ^ 1);
+                }
+                step(mine + buf * S::STAGE, mine + buf * S::STAGE + S::HALF, at, now);
+            }
+        }
+        if constexpr (!SMALL) lds_barrier();
+        base = stop;
+    }
+
+    const auto to = [&](int k) -> T * {
+        const int rr = rw + k, ik = rr / c.G;
+        return rr < M ? (T *)gr.dQ + ((i64)n * c.Tq + ik) * c.ldq + (i64)(kv * c.G + rr - ik * c.G) * c.D : nullptr;
+    };
+    const bool bad = put_block<T, DP, S, SMALL>(smem, acc, c.scale, c.D, vec_out, lane, wave, to);
+    wait_loads();                                        // the stores above come before those below
+    if (SMALL ? __syncthreads_or(bad) : __any(bad))
+        for (int k = SMALL ? wave : 0; k < 32 && rw + k < M; k += SMALL ? NW : 1) {
+            const int ik = (rw + k) / c.G;
+            backward_query_row<T>(c, n, kv * c.G + rw + k - ik * c.G, ik, (const T *)gr.O, gr.lse, (const T *)gr.dO, (T *)gr.dQ);
+        }
+}
+
+// ---------------------------------------------------------------------------
+// dK and dV
+// ---------------------------------------------------------------------------
+template <typename T, int DP, bool VEC, int MOD, bool SMALL>
+__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), 1) void key_kernel(Call c, Grads gr, bool vec_k, bool vec_v)
+{
+    typedef Shape<T, DP, SMALL> S;
+    typedef Tile<T, DP> TL;
+    constexpr int BN = S::BN, FN = S::FN, DB = TL::DB, KS = TL::KS, NW = S::NW;
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    __shared__ uint16_t list[kGroup];
+    __shared__ uint8_t cls_of[kGroup];
+    __shared__ int counts[kGroup / 64];
+
+    const int lane = threadIdx.x & 63, li = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int heads = c.N * c.Hk;
+    // first keys first: with a causal mask they have most queries
+    const int nk = (int)blockIdx.x % heads, tk = (int)blockIdx.x / heads;
+    const int n = nk / c.Hk, kv = nk - n * c.Hk;
+    const Sample smp(c, n);
+    const int j0 = tk * S::BR, jw = SMALL ? j0 : j0 + 32 * wave;
+    const T *Q = (const T *)c.Q + (i64)n * c.Tq * c.ldq + (i64)kv * c.G * c.D;
+    const T *dO = (const T *)gr.dO + (i64)n * c.Tq * c.ldo + (i64)kv * c.G * c.D;
+    const float *row_lse = gr.row_lse + ((i64)n * c.Hq + kv * c.G) * gr.pad;
+    const float *row_delta = gr.row_delta + ((i64)n * c.Hq + kv * c.G) * gr.pad;
+
+    const int j = jw + li;                               // this lane's key
+    const bool key_ok = j < smp.L;
+    const i64 krow = (i64)n * c.Tk + (key_ok ? j : 0);
+    u32x4_t kf[KS], vf[KS];
+    TL::load_row((const T *)c.K + krow * c.ldk + (i64)kv * c.D, c.D, key_ok, VEC, lane, kf);
+    TL::load_row((const T *)c.V + krow * c.ldv + (i64)kv * c.D, c.D, key_ok, VEC, lane, vf);
+    // queries at positions from .. L - 1 see it
+    const int from = !key_ok ? 0x7fffffff : !smp.causal || j < smp.prefix ? 0 : j;
+    const int doc = key_ok && smp.docs != nullptr ? smp.docs[j] : -1;
+    const Mod mod(c);
+
+    // the block's keys, and the queries that may see one of them: [i0, i1)
+    const int end = j0 + S::BR < smp.L ? j0 + S::BR : smp.L;
+    int i0 = -smp.first, i1 = smp.L - smp.first;
+    if (smp.causal && j0 >= smp.prefix) i0 = j0 - smp.first;
+    i0 = i0 > 0 ? i0 : 0;
+    i1 = i1 < c.Tq ? i1 : c.Tq;
+    int kd0 = 0, kd1 = 0;
+    if (j0 < smp.L && smp.docs != nullptr) wave_docs_range(smp.docs, j0, end - 1, lane, kd0, kd1);
+    const int t0 = i0 / BN, t1 = j0 < smp.L && i0 < i1 ? (i1 + BN - 1) / BN : t0;
+
+    f32x16_t ak[DB], av[DB];
+    zero(ak);
+    zero(av);
+    const Stager<TL, T, BN, SMALL ? 1 : NW, VEC> stq(c.ldq, c.D, SMALL ? 0 : wave, lane), std(c.ldo, c.D, SMALL ? 0 : wave, lane);
+    char *mine = smem + (SMALL ? wave * 2 * S::STAGE : 0);
+    const uint32_t lds0 = lds_addr(mine);
+    const auto issue = [&](int t, int g, int buf) {
+        const int q0 = t * BN;
+        const uint32_t L = lds0 + buf * S::STAGE;
+        stq.issue(Q + (i64)q0 * c.ldq + (i64)g * c.D, c.Tq - q0, L, mine + buf * S::STAGE);
+        std.issue(dO + (i64)q0 * c.ldo + (i64)g * c.D, c.Tq - q0, L + S::HALF, mine + buf * S::STAGE + S::HALF);
+        // 64 floats each, inside the padded rows: q0 is a multiple of BN, a short tile's are read twice
+        if (SMALL || wave == 0) {
+            const uint32_t off = 4u * (uint32_t)(lane & (BN - 1));
+            dma4_off(row_lse + (i64)g * gr.pad + q0, off, L + 2 * S::HALF);
+            dma4_off(row_delta + (i64)g * gr.pad + q0, off, L + 2 * S::HALF + 256);
+        }
+    };
+    const auto step = [&](const char *L, int q0, int g, int cls) {
+        const char *LQ = L, *LD = L + S::HALF;
+        const float slope2 = MOD == 1 && c.slopes != nullptr ? c.slopes[kv * c.G + g] * kLog2e : 0.0f;
+#pragma unroll
+        for (int x = 0; x < FN; ++x) {
+            f32x16_t s, e;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) s[k] = e[k] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                TL::mma(TL::rows(LQ, 32 * x, ks, lane), kf[ks], s);
+                TL::mma(TL::rows(LD, 32 * x, ks, lane), vf[ks], e);
+            }
+            const auto place = [&](int k) { return 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const float4 l4 = *reinterpret_cast<const float4 *>(L + 2 * S::HALF + 4 * (32 * x + 8 * b + 4 * h));
+                const float4 d4 = *reinterpret_cast<const float4 *>(L + 2 * S::HALF + 256 + 4 * (32 * x + 8 * b + 4 * h));
+                const float lse2[4] = {l4.x, l4.y, l4.z, l4.w}, delta[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int k = 4 * b + w;
+                    float bend = 1.0f;
+                    if constexpr (MOD == 0) s[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k], mod.scale2, -lse2[w]));
+                    else
+                        s[k] = __builtin_amdgcn_exp2f(
+                            modded<T>(mod, s[k], slope2, __builtin_fabsf((float)(smp.first + q0 + place(k) - j)), bend) - lse2[w]);
+                    e[k] = s[k] * (e[k] - delta[w]);
+                    if constexpr (MOD == 1) e[k] *= bend;
+                }
+            }
+            if (cls != kFull) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const int p = smp.first + q0 + place(k);
+                    bool see = p >= from && p < smp.L && q0 + place(k) < c.Tq;
+                    if (smp.docs != nullptr) {
+                        const int d = smp.docs[p < 0 ? 0 : p < smp.L ? p : smp.L - 1];
+                        see = see && d == doc && d >= 0;
+                    }
+                    s[k] = see ? s[k] : 0.0f;
+                    e[k] = see ? e[k] : 0.0f;
+                }
+            }
+            TL::mma_columns(LD, 32 * x, s, av, lane);
+            TL::mma_columns(LQ, 32 * x, e, ak, lane);
+        }
+    };
+
+    int base = t0;
+    while (base < t1) {
+        const bool docs = smp.docs != nullptr;
+        const int stop = !docs || t1 - base <= kGroup ? t1 : base + kGroup;
+        const auto class_of = [&](int t, bool with_docs) {
+            RowSpan span = span_of(smp, 1, c.Tq, t * BN, BN);
+            if (with_docs) docs_range(smp.docs, span.pmin, span.pmax + 1, span.dmin, span.dmax);
+            return meet(smp, span, j0, j0 + S::BR, kd0, kd1);
+        };
+        int count = stop - base;
+        if (docs)
+            count = tile_list<S::THREADS>(base, stop, list, cls_of, counts, [&](int t) { return class_of(t, true); });
+        // the heads one after another, each over the tiles
+        const int all = count * c.G;
+        const auto entry = [&](int k, int &t, int &g, int &cls) {
+            g = k / count;
+            if (docs) {
+                const int e = __builtin_amdgcn_readfirstlane(list[k - g * count]);
+                t = base + (e >> 2);
+                cls = e & 3;
+            } else {
+                t = base + k - g * count;
+                cls = class_of(t, false);
+            }
+        };
+        int t, g, cls;
+        constexpr int STEP = SMALL ? NW : 1;
+        const int k0 = SMALL ? wave : 0;
+        if (k0 < all) {
+            entry(k0, t, g, cls);
+            issue(t, g, 0);
+            int buf = 0;
+            for (int k = k0; k < all; k += STEP, buf ^= 1) {
+                const int at = t * BN, head = g, now = cls;
+                wait_loads();
+                if constexpr (SMALL) bf16s::wait_lgkmcnt0();
+                else lds_barrier();                     // this tile has landed, the one before is read
+                if (k + STEP < all) {
+                    entry(k + STEP, t, g, cls);
+                    issue(t, g, buf ^ 1);
+                }
+                step(mine + buf * S::STAGE, at, head, now);
+            }
+        }
+        if constexpr (!SMALL) lds_barrier();
+        base = stop;
+    }
+
+    const auto row_of = [&](void *p, i64 ld, int k) -> T * {
+        return jw + k < c.Tk ? (T *)p + ((i64)n * c.Tk + jw + k) * ld + (i64)kv * c.D : nullptr;
+    };
+    bool bad = put_block<T, DP, S, SMALL>(smem, ak, c.scale, c.D, vec_k, lane, wave, [&](int k) { return row_of(gr.dK, c.ldk, k); });
+    bad |= put_block<T, DP, S, SMALL>(smem, av, 1.0f, c.D, vec_v, lane, wave, [&](int k) { return row_of(gr.dV, c.ldv, k); });
+    wait_loads();                                        // the stores above come before those below
+    if (SMALL ? __syncthreads_or(bad) : __any(bad))
+        for (int k = SMALL ? wave : 0; k < 32 && jw + k < c.Tk; k += SMALL ? NW : 1)
+            backward_key_row<T>(c, n, kv, jw + k, (const T *)gr.O, gr.lse, (const T *)gr.dO, (T *)gr.dK, (T *)gr.dV);
+}
+
+template <typename T, int DP, bool VEC, int MOD>
+void launch(const Call &c, const Grads &g, hipStream_t stream)
+{
+    constexpr int N = 16 / sizeof(T);
+    const i64 heads = (i64)c.N * c.Hk, M = (i64)c.Tq * c.G;
+    const auto wide = [&](const void *p, i64 ld) { return c.D % N == 0 && ld % N == 0 && aligned(p, 16); };
+    if (M > 0) {
+        const int tiles = (int)ceil_div(M, g.small_q ? 32 : 128);
+        if (g.small_q)
+            query_kernel<T, DP, VEC, MOD, true><<<(unsigned)(heads * tiles), Shape<T, DP, true>::THREADS, 0, stream>>>(
+                c, g, tiles, wide(g.dQ, c.ldq));
+        else
+            query_kernel<T, DP, VEC, MOD, false><<<(unsigned)(heads * tiles), Shape<T, DP, false>::THREADS, 0, stream>>>(
+                c, g, tiles, wide(g.dQ, c.ldq));
+    }
+    if (c.Tk > 0) {
+        const i64 tiles = ceil_div(c.Tk, g.small_k ? 32 : 128);
+        if (g.small_k)
+            key_kernel<T, DP, VEC, MOD, true><<<(unsigned)(heads * tiles), Shape<T, DP, true>::THREADS, 0, stream>>>(
+                c, g, wide(g.dK, c.ldk), wide(g.dV, c.ldv));
+        else
+            key_kernel<T, DP, VEC, MOD, false><<<(unsigned)(heads * tiles), Shape<T, DP, false>::THREADS, 0, stream>>>(
+                c, g, wide(g.dK, c.ldk), wide(g.dV, c.ldv));
+    }
+}
+
+template <typename T, int DP>
+void by_kind(const Call &c, const Grads &g, hipStream_t stream)
+{
+    constexpr int N = 16 / sizeof(T);
+    const bool vec = c.D % N == 0 && c.ldq % N == 0 && c.ldk % N == 0 && c.ldv % N == 0 && c.ldo % N == 0 && aligned(c.Q, 16) &&
+                     aligned(c.K, 16) && aligned(c.V, 16) && aligned(g.dO, 16);
+    const bool mod = c.cap > 0.0f || c.slopes != nullptr;
+    if (vec) mod ? launch<T, DP, true, 1>(c, g, stream) : launch<T, DP, true, 0>(c, g, stream);
+    else mod ? launch<T, DP, false, 1>(c, g, stream) : launch<T, DP, false, 0>(c, g, stream);
+}
+
+template <typename T>
+dp_status tiles_of(const Call &c, const Grads &g, hipStream_t stream)
+{
+    constexpr int N = 16 / sizeof(T);
+    const i64 queries = (i64)c.N * c.Hq * g.pad;
+    const bool vec = c.D % N == 0 && c.ldo % N == 0 && aligned(g.O, 16) && aligned(g.dO, 16);
+    if (queries > 0) row_info_kernel<T><<<(unsigned)(ceil_div(queries, 16) < kMaxGrid ? ceil_div(queries, 16) : kMaxGrid), 256, 0, stream>>>(c, g, vec);
+    if (c.D <= 32) by_kind<T, 32>(c, g, stream);
+    else if (c.D <= 64) by_kind<T, 64>(c, g, stream);
+    else if (c.D <= 96) by_kind<T, 96>(c, g, stream);
+    else by_kind<T, 128>(c, g, stream);
+    return launch_status();
+}
+
+}  // namespace
+}  // namespace attn
+}  // namespace dpg

@@ -11,32 +11,34 @@ constexpr int kThreads = 256, kRows = kThreads / kWave;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void rows_forward_kernel(Call c, T *O, float *lse)
 {
-    const i64 r = (i64)blockIdx.x * kRows + threadIdx.x / kWave;
-    if (r >= (i64)c.N * c.Hq * c.Tq) return;
-    const i64 nh = r / c.Tq;
-    forward_row<T>(c, (int)(nh / c.Hq), (int)(nh % c.Hq), (int)(r % c.Tq), O, lse);
+    for (i64 r = (i64)blockIdx.x * kRows + threadIdx.x / kWave; r < (i64)c.N * c.Hq * c.Tq; r += (i64)gridDim.x * kRows) {
+        const i64 nh = r / c.Tq;
+        forward_row<T>(c, (int)(nh / c.Hq), (int)(nh % c.Hq), (int)(r % c.Tq), O, lse);
+    }
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void rows_backward_query_kernel(Call c, const T *O, const float *lse, const T *dO, T *dQ)
 {
-    const i64 r = (i64)blockIdx.x * kRows + threadIdx.x / kWave;
-    if (r >= (i64)c.N * c.Hq * c.Tq) return;
-    const i64 nh = r / c.Tq;
-    backward_query_row<T>(c, (int)(nh / c.Hq), (int)(nh % c.Hq), (int)(r % c.Tq), O, lse, dO, dQ);
+    for (i64 r = (i64)blockIdx.x * kRows + threadIdx.x / kWave; r < (i64)c.N * c.Hq * c.Tq; r += (i64)gridDim.x * kRows) {
+        const i64 nh = r / c.Tq;
+        backward_query_row<T>(c, (int)(nh / c.Hq), (int)(nh % c.Hq), (int)(r % c.Tq), O, lse, dO, dQ);
+    }
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void rows_backward_key_kernel(Call c, const T *O, const float *lse, const T *dO, T *dK,
                                                                      T *dV)
 {
-    const i64 r = (i64)blockIdx.x * kRows + threadIdx.x / kWave;
-    if (r >= (i64)c.N * c.Hk * c.Tk) return;
-    const i64 nh = r / c.Tk;
-    backward_key_row<T>(c, (int)(nh / c.Hk), (int)(nh % c.Hk), (int)(r % c.Tk), O, lse, dO, dK, dV);
+    for (i64 r = (i64)blockIdx.x * kRows + threadIdx.x / kWave; r < (i64)c.N * c.Hk * c.Tk; r += (i64)gridDim.x * kRows) {
+        const i64 nh = r / c.Tk;
+        backward_key_row<T>(c, (int)(nh / c.Hk), (int)(nh % c.Hk), (int)(r % c.Tk), O, lse, dO, dK, dV);
+    }
 }
 
-unsigned blocks(i64 rows) { return (unsigned)ceil_div(rows, kRows); }
+// a dimension of a grid holds fewer than 2^32 threads: past kMaxGrid workgroups a wave takes several rows
+constexpr i64 kMaxGrid = i64(1) << 22;
+unsigned blocks(i64 rows) { return (unsigned)(ceil_div(rows, kRows) < kMaxGrid ? ceil_div(rows, kRows) : kMaxGrid); }
 
 template <typename T>
 dp_status backward(const Call &c, const void *O, const float *lse, const void *dO, void *dQ, void *dK, void *dV,

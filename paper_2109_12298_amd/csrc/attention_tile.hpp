@@ -1,0 +1,317 @@
+// What the attention tile kernels share: operand tiles in LDS, matrix products
+// over them, scores, and which tiles of keys a block of rows meets.
+//
+// Rows.  The query heads that share a key head run over the same keys, so a
+// key head's rows are its (query, head) pairs, r = i * G + g: one product
+// serves prompts, shared heads and single tokens alike, and a key head's
+// gradients add over its query heads inside a workgroup.
+//
+// Operands.  A 32 x 32 product of a wave has its two operands' values in pieces
+// of 16 bytes: lane l has row l % 32 and the piece l / 32 of a 32-byte k-step
+// (bf16: one v_mfma_f32_32x32x16; fp32: four v_mfma_f32_32x32x2, whose two k are
+// the two halves' same element: the order of a sum's terms is free as long as
+// both operands have the same).  Register r of the result is row
+// 8 * (r / 4) + 4 * (l / 32) + r % 4, column l % 32.  With scores formed as
+// keys x rows (or rows x keys), a lane has 16 scores of one column, and they
+// are, as they lie, the second operand of the product that sums over them:
+// bf16 takes registers 8 c .. 8 c + 7 as k = 16 c + {4 h .. 4 h + 3, 8 + 4 h ..
+// 8 + 4 h + 3} (h = l / 32), fp32 register r alone.  The first operand is then
+// the other tile read by columns: transposing LDS reads in bf16 (four rows
+// each), plain ones in fp32.
+//
+// Tiles.  Rows of DP values (D rounded up to 32; what is behind D repeats the
+// row's first piece and meets zeros in the other operand), 16-byte piece q of
+// row r at place q ^ swz(r): 16 rows' same pieces lie in 16 different places of
+// the 256-byte bank window, and 4 rows' same 64 bytes in 4.
+#pragma once
+
+#include "attention_rows.hpp"
+#include "bf16_stage.hpp"
+
+namespace dpg {
+namespace attn {
+
+using bf16s::bf16x8_t;
+using bf16s::f32x16_t;
+using bf16s::i16x4_t;
+using bf16s::i16x8_t;
+using bf16s::lds_addr;
+using bf16s::lds_i16x4_t;
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+// a pointer that is the same in all lanes, in scalar registers
+template <typename P>
+__device__ __forceinline__ P *uniform(P *p)
+{
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return reinterpret_cast<P *>((uint64_t)hi << 32 | lo);
+}
+
+// lane l's 16 (4) bytes at base + off go to LDS byte lds + 16 l (4 l); see bf16s::dma16
+__device__ __forceinline__ void dma16_off(const void *base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(uniform(base)),
+                 "s"(__builtin_amdgcn_readfirstlane(lds))
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void dma4_off(const void *base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(uniform(base)),
+                 "s"(__builtin_amdgcn_readfirstlane(lds))
+                 : "memory", "m0");
+}
+
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// the value of lane ^ 32
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, kWave); }
+
+template <typename T, int DP_>
+struct Tile {
+    static constexpr int DP = DP_, RB = DP * (int)sizeof(T), PIECES = RB / 16, KS = RB / 32, DB = DP / 32;
+    static constexpr int N = 16 / (int)sizeof(T);                // values in a piece
+    static constexpr bool BF16 = sizeof(T) == 2;
+
+    static __device__ __forceinline__ int swz(int r)
+    {
+        if constexpr (BF16) {
+            if constexpr (RB % 256 == 0) return ((r & 3) << 2) | ((r >> 2) & 3);
+            else if constexpr (RB % 256 == 128) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+            else return (r >> 2) & 3;
+        } else {
+            // rows four apart, which the two halves of a wave read together, in different halves of the window
+            if constexpr (RB % 256 == 0) return (((r >> 2) & 1) << 3) | ((r & 3) << 1) | ((r >> 3) & 1);
+            else return (r >> 1) & 7;
+        }
+    }
+
+    // operand of the rows r0 .. r0 + 31 at k-step ks
+    static __device__ __forceinline__ u32x4_t rows(const char *L, int r0, int ks, int lane)
+    {
+        const int r = r0 + (lane & 31);
+        return *reinterpret_cast<const u32x4_t *>(L + r * RB + 16 * ((2 * ks + (lane >> 5)) ^ swz(r)));
+    }
+    static __device__ __forceinline__ void mma(const u32x4_t &a, const u32x4_t &b, f32x16_t &acc)
+    {
+        if constexpr (BF16) {
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc,
+                                                          0, 0, 0);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), acc, 0, 0, 0);
+        }
+    }
+    // acc[block of 32 values][.] += sum over the 32 rows from r0 on of tile[row][value] * w[row]
+    static __device__ __forceinline__ void mma_columns(const char *L, int r0, const f32x16_t &w, f32x16_t (&acc)[DB], int lane)
+    {
+        const int h = lane >> 5;
+        if constexpr (BF16) {
+            const int s = lane & 15, g = (lane >> 4) & 1;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                bf16x8_t b;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) b[e] = (__bf16)w[8 * c + e];
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const int t = r0 + 16 * c + 4 * h + (s >> 2);
+                    const int q = 4 * d + 2 * g + ((s & 3) >> 1), in = 8 * (s & 1);
+                    const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(L + t * RB + 16 * (q ^ swz(t)) + in));
+                    const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds_i16x4_t *)(L + (t + 8) * RB + 16 * (q ^ swz(t + 8)) + in));
+                    const i16x8_t a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), b, acc[d], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int t = r0 + 8 * (r >> 2) + 4 * h + (r & 3);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const int v = 32 * d + (lane & 31);
+                    const float a = *reinterpret_cast<const float *>(L + t * RB + 16 * ((v >> 2) ^ swz(t)) + 4 * (v & 3));
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], acc[d], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+    // A row's operands for all k-steps, from memory; zeros behind D and where !ok
+    static __device__ __forceinline__ void load_row(const T *p, int D, bool ok, bool vec, int lane, u32x4_t (&f)[KS])
+    {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int d = (2 * ks + (lane >> 5)) * N;
+            u32x4_t v = {0, 0, 0, 0};
+            if (vec) {
+                if (ok && d < D) v = *reinterpret_cast<const u32x4_t *>(p + d);
+            } else if (ok) {
+                v = piece(p, d, D);
+            }
+            f[ks] = v;
+        }
+    }
+    // values d .. of a row of any alignment, zeros from D on
+    static __device__ __forceinline__ u32x4_t piece(const T *p, int d, int D)
+    {
+        u32x4_t v = {0, 0, 0, 0};
+        if constexpr (BF16) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (d + e < D) v[e >> 1] |= (uint32_t)p[d + e] << (16 * (e & 1));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (d + e < D) v[e] = __float_as_uint(p[d + e]);
+        }
+        return v;
+    }
+};
+
+// Brings R rows of a tile to LDS with NW waves.
+template <typename TL, typename T, int R, int NW, bool VEC>
+struct Stager {
+    static constexpr int LOADS = R * TL::RB / 1024 / NW;
+    static_assert(LOADS * NW * 1024 == R * TL::RB, "stage split");
+
+    uint32_t ld_bytes;
+    int D, wave, lane;
+
+    __device__ __forceinline__ Stager(i64 ld, int D_, int wave_, int lane_)
+        : ld_bytes((uint32_t)(ld * sizeof(T))), D(D_), wave(wave_), lane(lane_)
+    {
+    }
+    __device__ __forceinline__ void place(int k, int &row, int &piece) const
+    {
+        const int at = 64 * (wave + NW * k) + lane;
+        row = at / TL::PIECES;
+        piece = (at - row * TL::PIECES) ^ TL::swz(row);
+    }
+    // rows behind `left` read the last of them (their weights are zeros)
+    __device__ __forceinline__ void issue(const T *base, int left, uint32_t lds, char *generic) const
+    {
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            int row, q;
+            place(k, row, q);
+            const int r = row < left ? row : left - 1;
+            if constexpr (VEC) {
+                const int c = q * TL::N < D ? q : 0;
+                dma16_off(base, (uint32_t)r * ld_bytes + 16u * (uint32_t)c, lds + 1024u * (uint32_t)(wave + NW * k));
+            } else {
+                const T *p = reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + (i64)r * ld_bytes);
+                *reinterpret_cast<u32x4_t *>(generic + 1024 * (wave + NW * k) + 16 * lane) = TL::piece(p, q * TL::N, D);
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------
+// scores in units of ln 2
+// ---------------------------------------------------------------------------
+// MOD 0: scale alone (scale > 0); 1: a cap and/or a bias by distance, or any scale
+struct Mod {
+    float scale2;            // scale * log2 e
+    float y_scale, cap2;     // scale / cap, cap * log2 e; cap2 = 0: no cap
+    __device__ __forceinline__ explicit Mod(const Call &c)
+    {
+        scale2 = c.scale * kLog2e;
+        cap2 = c.cap * kLog2e;
+        y_scale = c.cap > 0.0f ? c.scale / c.cap : 0.0f;
+    }
+};
+
+// tanh, for scores of bf16 inputs by exp2 and reciprocal (off by some 2^-22, where
+// the inputs' rounding is 2^-9 of a score), for fp32 ones to fp32's last bits
+template <typename T>
+__device__ __forceinline__ float tanh_for(float y)
+{
+    if constexpr (sizeof(T) == 2)
+        return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * y));
+    else
+        return tanhf(y);
+}
+
+template <typename T>
+__device__ __forceinline__ float modded(const Mod &m, float x, float slope2, float far, float &bend)
+{
+    float s;
+    if (m.cap2 != 0.0f) {
+        const float t = tanh_for<T>(m.y_scale * x);
+        s = m.cap2 * t;
+        bend = 1.0f - t * t;
+    } else {
+        s = m.scale2 * x;
+        bend = 1.0f;
+    }
+    return s - slope2 * far;
+}
+
+// ---------------------------------------------------------------------------
+// which tiles two blocks meet in
+// ---------------------------------------------------------------------------
+// A block of rows: the positions of its valid rows and their documents
+struct RowSpan {
+    int pmin, pmax;          // pmax < pmin: none is valid
+    bool all;                // every row of the block is valid
+    int dmin, dmax;          // their documents' range (with docs; -1 .. : one may be negative)
+};
+
+// r0 .. r0 + count - 1 of M rows
+__device__ __forceinline__ RowSpan span_of(const Sample &s, int G, int M, int r0, int count)
+{
+    RowSpan b;
+    const int last = r0 + count < M ? r0 + count : M;
+    const int p0 = s.first + r0 / G, p1 = s.first + (last - 1) / G;
+    b.pmin = p0 > 0 ? p0 : 0;
+    b.pmax = p1 < s.L ? p1 : s.L - 1;
+    if (last <= r0) b.pmax = b.pmin - 1;
+    b.all = r0 + count <= M && p0 >= 0 && p1 < s.L;
+    b.dmin = b.dmax = 0;
+    return b;
+}
+
+enum { kSkip = 0, kPartial = 1, kFull = 2 };
+
+// keys [k0, k1) against the span; kd0, kd1: the documents' range of those below L
+__device__ __forceinline__ int meet(const Sample &s, const RowSpan &b, int k0, int k1, int kd0, int kd1)
+{
+    if (b.pmax < b.pmin || k0 >= s.end_for(b.pmax)) return kSkip;
+    bool full = b.all && k1 <= s.L && (!s.causal || k1 - 1 <= b.pmin || k1 <= s.prefix);
+    if (s.docs != nullptr) {
+        if (kd1 < 0 || b.dmax < 0 || kd1 < b.dmin || kd0 > b.dmax) return kSkip;
+        full = full && kd0 == kd1 && b.dmin == b.dmax && kd0 == b.dmin;
+    }
+    return full ? kFull : kPartial;
+}
+
+// range of docs[j0 .. j1)
+__device__ __forceinline__ void docs_range(const int32_t *docs, int j0, int j1, int &lo, int &hi)
+{
+    lo = 0x7fffffff;
+    hi = -0x7fffffff - 1;
+    int j = j0;
+    for (; j + 8 <= j1; j += 8) {
+        int v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = docs[j + k];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            lo = v[k] < lo ? v[k] : lo;
+            hi = v[k] > hi ? v[k] : hi;
+        }
+    }
+    for (; j < j1; ++j) {
+        lo = docs[j] < lo ? docs[j] : lo;
+        hi = docs[j] > hi ? docs[j] : hi;
+    }
+}
+
+__device__ __forceinline__ bool not_finite(float v) { return !(__builtin_fabsf(v) < INFINITY); }
+
+}  // namespace attn
+}  // namespace dpg

@@ -98,14 +98,16 @@ __device__ __forceinline__ float sum_of_block(float v, float *red)
 // NV pieces of a row per thread are held; RESIDENT: they are the whole row.
 // SOFT, HARD: which parts of the loss the call has (a position may lack its own).
 template <typename T, int THREADS, int NV, bool RESIDENT, bool HARD>
-__global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, Args a, T *dZ)
+__global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Args a, T *dZ)
 {
     constexpr int N = 16 / sizeof(T);
     __shared__ float red[16];
     __shared__ float target[kMaxK];                        // P_k
     __shared__ int32_t target_id[kMaxK];                   // -1: unused
-    const i64 m = blockIdx.x, V = a.V;
+    const i64 V = a.V;
     const int tid = threadIdx.x;
+    const i64 m = (i64)blockIdx.y * gridDim.x + blockIdx.x;
+    if (m >= M) return;
     const T *z = Z + m * V;
     T *dz = dZ != nullptr ? dZ + m * V : nullptr;
     const float w = a.weight != nullptr ? a.weight[m] : 1.0f;
@@ -313,10 +315,13 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, Args a, T 
 template <typename T, int THREADS, int NV, bool RESIDENT>
 void launch(const T *Z, i64 M, const Args &a, T *dZ, hipStream_t stream)
 {
+    // a dimension of a grid holds fewer than 2^32 threads
+    const i64 gx = M < (i64(1) << 20) ? M : i64(1) << 20;
+    const dim3 grid((unsigned)gx, (unsigned)ceil_div(M, gx));
     if (a.labels != nullptr && a.alpha < 1.0f)
-        distill_kernel<T, THREADS, NV, RESIDENT, true><<<(unsigned)M, THREADS, 0, stream>>>(Z, a, dZ);
+        distill_kernel<T, THREADS, NV, RESIDENT, true><<<grid, THREADS, 0, stream>>>(Z, M, a, dZ);
     else
-        distill_kernel<T, THREADS, NV, RESIDENT, false><<<(unsigned)M, THREADS, 0, stream>>>(Z, a, dZ);
+        distill_kernel<T, THREADS, NV, RESIDENT, false><<<grid, THREADS, 0, stream>>>(Z, M, a, dZ);
 }
 
 template <typename T>

@@ -61,8 +61,8 @@ def test_attention_refusals():
                     dict(ldv=15), dict(ldo=31), dict(slopes=FAKE + 2), dict(lens=FAKE + 1), dict(docs=FAKE + 2), dict(Q=None), dict(K=None),
                     dict(V=None), dict(O=None), dict(Q=FAKE + 2), dict(V=FAKE + 1), dict(lse=FAKE + 2)):
             assert call(**bad) == dp.DP_EINVAL, bad
-        for much in (dict(D=257), dict(Tq=2 ** 24), dict(Tk=2 ** 24), dict(N=2 ** 31), dict(N=2 ** 20, Tk=2 ** 11), dict(N=2 ** 20, Tq=2 ** 10),
-                     dict(Hq=2 ** 23, ldq=2 ** 40, ldo=2 ** 40), dict(ldq=2 ** 23), dict(ldk=2 ** 23), dict(ldv=2 ** 23), dict(ldo=2 ** 23)):
+        for much in (dict(D=257), dict(Tq=2 ** 24), dict(Tk=2 ** 24), dict(N=2 ** 31), dict(N=2 ** 23, Tk=33), dict(N=2 ** 22, Tq=1),
+                     dict(Hq=2 ** 23, ldq=2 ** 40, ldo=2 ** 40), dict(ldq=2 ** 22), dict(ldk=2 ** 22), dict(ldv=2 ** 22), dict(ldo=2 ** 22)):
             assert call(**much) == dp.DP_EUNSUPPORTED, much
         assert call(N=0, Q=None, K=None, V=None, O=None, lse=None, ws=None, n=0) == dp.DP_OK
     for k in ("lse", "dO", "dQ", "dK", "dV"):

@@ -5,7 +5,9 @@ import numpy as np
 
 from lm_ref import SUM, U32, half_step
 
-LOG2E = 1.4426950408889634
+# Below 2^-126 a weight, or its product, may be taken as 0 (the units flush subnormal numbers): each is off by at most TINY
+# then, and so is every sum by TINY times what multiplies the weight, and by TINY for every term.
+TINY = 2.0 ** -126
 
 
 # ---------------------------------------------------------------------------
@@ -107,7 +109,8 @@ def attention(Q, K, V, mask, scale, cap=0.0, slopes=None, dt=None):
             n_keys = w.shape[1]
             rel = 2 * (2 * e + 4 * U32) + 2 * SUM(n_keys) + hp
             O[n, rows, hq] = o
-            eO[n, rows, hq] = rel * mag + h * (np.abs(o) + rel * mag) + float(1e-37)
+            flushed = TINY * (n_keys + 1 + np.abs(vz).sum(1))
+            eO[n, rows, hq] = rel * mag + h * (np.abs(o) + rel * mag) + flushed
             lse[n, hq, rows] = (top + np.log(tot))[:, 0]
             el[n, hq, rows] = (2 * e + SUM(n_keys) + 8 * U32 * (1 + np.abs(top) + np.abs(np.log(tot))))[:, 0]
     return (O, lse), (eO, el)
@@ -146,6 +149,7 @@ def attention_grads(Q, K, V, dO, mask, scale, cap=0.0, slopes=None, dt=None):
                 eg = np.where(sub, np.abs(g) * (ep + hp + 8 * U32) + abs(scale) * p * (
                     (edp + edelta) * bend + (np.abs(dp - delta) + edp + edelta) * (16 * U32 + 2 * es / max(cap, 1e-30)) * (cap > 0)),
                     0.0)
+                eg = eg + np.where(sub, TINY * (1 + abs(scale) * (np.abs(dp - delta) + edp + edelta)), 0.0)
                 dz = np.where(sub[:, :, None], d[:, None, :], 0.0)
                 qz = np.where(sub[:, :, None], q[:, None, :], 0.0)
                 kz = np.where(sub[:, :, None], k[None], 0.0)
@@ -155,8 +159,8 @@ def attention_grads(Q, K, V, dO, mask, scale, cap=0.0, slopes=None, dt=None):
                 out[1][n, used, g_] += (g[:, :, None] * qz).sum(0)
                 err[1][n, used, g_] += ((eg + SUM(nq) * (np.abs(g) + eg))[:, :, None] * np.abs(qz)).sum(0)
                 out[2][n, used, g_] += (p[:, :, None] * dz).sum(0)
-                err[2][n, used, g_] += (np.where(sub, p * (ep + hp + SUM(nq) * (1 + ep)), 0.0)[:, :, None] * np.abs(dz)).sum(0)
-    return out, [e + h * (np.abs(o) + e) + 1e-37 for o, e in zip(out, err)]
+                err[2][n, used, g_] += (np.where(sub, p * (ep + hp + SUM(nq) * (1 + ep)) + TINY, 0.0)[:, :, None] * np.abs(dz)).sum(0)
+    return out, [e + h * (np.abs(o) + e) + TINY * (2 + Tk + Tq * G) for o, e in zip(out, err)]
 
 
 # ---------------------------------------------------------------------------
