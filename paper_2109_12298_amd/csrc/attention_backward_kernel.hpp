@@ -253,8 +253,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     TL::load_row((const T *)c.Q + row * c.ldq + (i64)head * c.D, c.D, row_ok, VEC, lane, qf);
     TL::load_row((const T *)gr.dO + row * c.ldo + (i64)head * c.D, c.D, row_ok, VEC, lane, df);
     const float lse2 = row_ok ? gr.row_lse[info] : INFINITY, delta = row_ok ? gr.row_delta[info] : 0.0f;
-    const Mod mod(c);
-    const float slope2 = MOD == 1 && c.slopes != nullptr ? c.slopes[head] * kLog2e : 0.0f;
+    const Scores<T, MOD> score(c);
+    const float slope2 = (MOD & kSlope) != 0 && c.slopes != nullptr ? c.slopes[head] * kLog2e : 0.0f;
 
     RowSpan span = span_of(smp, c.G, M, r0, S::BR);
     const int end = smp.end_for(span.pmax < span.pmin ? -1 : span.pmax), t1 = (end + BN - 1) / BN;
@@ -283,17 +283,18 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 TL::mma(TL::rows(LV, 32 * x, ks, lane), df[ks], e);
             }
             const auto key = [&](int k) { return k0 + 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
+            const auto weigh = [&](auto is_near) {
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                float bend = 1.0f;
-                float p;
-                if constexpr (MOD == 0) p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k], mod.scale2, -lse2));
-                else
-                    p = __builtin_amdgcn_exp2f(
-                        modded<T>(mod, s[k], slope2, __builtin_fabsf((float)(pos - key(k))), bend) - lse2);
-                e[k] = p * (e[k] - delta);
-                if constexpr (MOD == 1) e[k] *= bend;
-            }
+                for (int k = 0; k < 16; ++k) {
+                    float bend;
+                    const float p = __builtin_amdgcn_exp2f(score.template of<decltype(is_near)::value>(
+                        s[k], lse2, slope2, __builtin_fabsf((float)(pos - key(k))), bend));
+                    e[k] = p * (e[k] - delta);
+                    if constexpr ((MOD & kCap) != 0) e[k] *= bend;
+                }
+            };
+            if (score.near(s)) weigh(std::true_type{});
+            else weigh(std::false_type{});
             if (cls != kFull) {
 #pragma unroll
                 for (int k = 0; k < 16; ++k) e[k] = key(k) < lim ? e[k] : 0.0f;
@@ -301,7 +302,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
                         const int j = key(k), d = smp.docs[j < end ? j : end - 1];
-                        e[k] = d == doc && d >= 0 ? e[k] : 0.0f;
+                        e[k] = ((d == doc) & (d >= 0)) ? e[k] : 0.0f;
                     }
                 }
             }
@@ -347,6 +348,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                     entry(k + STEP, t, cls);
                     issue(t, buf ^ 1);
                 }
+                wave_together();
                 step(mine + buf * S::STAGE, mine + buf * S::STAGE + S::HALF, at, now);
             }
         }
@@ -371,7 +373,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
 // dK and dV
 // ---------------------------------------------------------------------------
 template <typename T, int DP, bool VEC, int MOD, bool SMALL>
-__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), 1) void key_kernel(Call c, Grads gr, bool vec_k, bool vec_v)
+__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, DP>::RB > 128 ? 1 : 2)) void key_kernel(Call c, Grads gr, bool vec_k, bool vec_v)
 {
     typedef Shape<T, DP, SMALL> S;
     typedef Tile<T, DP> TL;
@@ -403,7 +405,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), 1) void key_kernel(
     // queries at positions from .. L - 1 see it
     const int from = !key_ok ? 0x7fffffff : !smp.causal || j < smp.prefix ? 0 : j;
     const int doc = key_ok && smp.docs != nullptr ? smp.docs[j] : -1;
-    const Mod mod(c);
+    const Scores<T, MOD> score(c);
 
     // the block's keys, and the queries that may see one of them: [i0, i1)
     const int end = j0 + S::BR < smp.L ? j0 + S::BR : smp.L;
@@ -435,7 +437,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), 1) void key_kernel(
     };
     const auto step = [&](const char *L, int q0, int g, int cls) {
         const char *LQ = L, *LD = L + S::HALF;
-        const float slope2 = MOD == 1 && c.slopes != nullptr ? c.slopes[kv * c.G + g] * kLog2e : 0.0f;
+        const float slope2 = (MOD & kSlope) != 0 && c.slopes != nullptr ? c.slopes[kv * c.G + g] * kLog2e : 0.0f;
 #pragma unroll
         for (int x = 0; x < FN; ++x) {
             f32x16_t s, e;
@@ -447,31 +449,33 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), 1) void key_kernel(
                 TL::mma(TL::rows(LD, 32 * x, ks, lane), vf[ks], e);
             }
             const auto place = [&](int k) { return 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
+            const auto weigh = [&](auto is_near) {
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const float4 l4 = *reinterpret_cast<const float4 *>(L + 2 * S::HALF + 4 * (32 * x + 8 * b + 4 * h));
-                const float4 d4 = *reinterpret_cast<const float4 *>(L + 2 * S::HALF + 256 + 4 * (32 * x + 8 * b + 4 * h));
-                const float lse2[4] = {l4.x, l4.y, l4.z, l4.w}, delta[4] = {d4.x, d4.y, d4.z, d4.w};
+                for (int b = 0; b < 4; ++b) {
+                    const float4 l4 = *reinterpret_cast<const float4 *>(L + 2 * S::HALF + 4 * (32 * x + 8 * b + 4 * h));
+                    const float4 d4 = *reinterpret_cast<const float4 *>(L + 2 * S::HALF + 256 + 4 * (32 * x + 8 * b + 4 * h));
+                    const float lse2[4] = {l4.x, l4.y, l4.z, l4.w}, delta[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int k = 4 * b + w;
-                    float bend = 1.0f;
-                    if constexpr (MOD == 0) s[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k], mod.scale2, -lse2[w]));
-                    else
-                        s[k] = __builtin_amdgcn_exp2f(
-                            modded<T>(mod, s[k], slope2, __builtin_fabsf((float)(smp.first + q0 + place(k) - j)), bend) - lse2[w]);
-                    e[k] = s[k] * (e[k] - delta[w]);
-                    if constexpr (MOD == 1) e[k] *= bend;
+                    for (int w = 0; w < 4; ++w) {
+                        const int k = 4 * b + w;
+                        float bend;
+                        s[k] = __builtin_amdgcn_exp2f(score.template of<decltype(is_near)::value>(
+                            s[k], lse2[w], slope2, __builtin_fabsf((float)(smp.first + q0 + place(k) - j)), bend));
+                        e[k] = s[k] * (e[k] - delta[w]);
+                        if constexpr ((MOD & kCap) != 0) e[k] *= bend;
+                    }
                 }
-            }
+            };
+            if (score.near(s)) weigh(std::true_type{});
+            else weigh(std::false_type{});
             if (cls != kFull) {
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
                     const int p = smp.first + q0 + place(k);
-                    bool see = p >= from && p < smp.L && q0 + place(k) < c.Tq;
+                    bool see = (p >= from) & (p < smp.L) & (q0 + place(k) < c.Tq);
                     if (smp.docs != nullptr) {
                         const int d = smp.docs[p < 0 ? 0 : p < smp.L ? p : smp.L - 1];
-                        see = see && d == doc && d >= 0;
+                        see = see & (d == doc) & (d >= 0);
                     }
                     s[k] = see ? s[k] : 0.0f;
                     e[k] = see ? e[k] : 0.0f;
@@ -523,6 +527,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), 1) void key_kernel(
                     entry(k + STEP, t, g, cls);
                     issue(t, g, buf ^ 1);
                 }
+                wave_together();
                 step(mine + buf * S::STAGE, at, head, now);
             }
         }
@@ -573,9 +578,12 @@ void by_kind(const Call &c, const Grads &g, hipStream_t stream)
     constexpr int N = 16 / sizeof(T);
     const bool vec = c.D % N == 0 && c.ldq % N == 0 && c.ldk % N == 0 && c.ldv % N == 0 && c.ldo % N == 0 && aligned(c.Q, 16) &&
                      aligned(c.K, 16) && aligned(c.V, 16) && aligned(g.dO, 16);
-    const bool mod = c.cap > 0.0f || c.slopes != nullptr;
-    if (vec) mod ? launch<T, DP, true, 1>(c, g, stream) : launch<T, DP, true, 0>(c, g, stream);
-    else mod ? launch<T, DP, false, 1>(c, g, stream) : launch<T, DP, false, 0>(c, g, stream);
+    const int mod = c.scale <= 0.0f ? kBoth : (c.cap > 0.0f ? kCap : kPlain) | (c.slopes != nullptr ? kSlope : kPlain);
+    if (!vec) launch<T, DP, false, kBoth>(c, g, stream);
+    else if (mod == kPlain) launch<T, DP, true, kPlain>(c, g, stream);
+    else if (mod == kCap) launch<T, DP, true, kCap>(c, g, stream);
+    else if (mod == kSlope) launch<T, DP, true, kSlope>(c, g, stream);
+    else launch<T, DP, true, kBoth>(c, g, stream);
 }
 
 template <typename T>

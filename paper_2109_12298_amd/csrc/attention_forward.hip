@@ -13,10 +13,13 @@ int forward_splits(const dp_attention &a)
 {
     const i64 M = a.Tq * (a.Hq / a.Hk), heads = a.N * a.Hk;
     if (M == 0 || heads == 0 || a.Tk == 0) return 1;
-    if (heads * ceil_div(M, 128) >= 256) return 0;
+    if (M > 64 && heads * ceil_div(M, 128) >= 256) return 0;
     const i64 blocks = heads * ceil_div(M, 32);
-    // workgroups for every CU, each at least four tiles of keys (one a wave)
-    i64 splits = ceil_div(256, blocks);
+    // workgroups for every CU, each at least a tile of keys for every wave; where there are many keys more of them, as samples may
+    // differ in length
+    i64 splits = ceil_div(256, blocks), more = ceil_div(1024, blocks);
+    if (more > a.Tk / 512) more = a.Tk / 512;
+    if (splits < more) splits = more;
     const i64 most = ceil_div(a.Tk, 4 * 32);
     if (splits > most) splits = most;
     return (int)(splits < 1 ? 1 : splits);

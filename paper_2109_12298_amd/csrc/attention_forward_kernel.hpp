@@ -34,13 +34,13 @@ constexpr int kGroup = 1024;             // tiles in a list
 template <typename T, int DP, bool SMALL>
 struct Shape {
     typedef Tile<T, DP> TL;
-    static constexpr int NW = SMALL && TL::RB >= 384 ? 2 : 4;
+    static constexpr int NW = 4;
     static constexpr int BN = SMALL || sizeof(T) == 4 ? 32 : 64;         // keys in a tile
     static constexpr int BR = SMALL ? 32 : 32 * NW;                      // rows of a workgroup
     static constexpr int FN = BN / 32, THREADS = 64 * NW;
     static constexpr int HALF = BN * TL::RB, STAGE = 2 * HALF;           // K, then V
     static constexpr int OUT_ROW = SMALL ? DP * 4 + 16 : TL::RB + 16;    // bytes of an output row in LDS
-    static constexpr int STAGES = (SMALL ? NW : 1) * 2 * STAGE, OUTPUT = NW * 32 * OUT_ROW;
+    static constexpr int STAGES = (SMALL ? NW : 2) * STAGE, OUTPUT = NW * 32 * OUT_ROW;
     static constexpr int LDS = STAGES > OUTPUT ? STAGES : OUTPUT;
 };
 
@@ -105,8 +105,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const int head = kv * c.G + (row_ok ? g : 0);
     u32x4_t qf[KS];
     TL::load_row((const T *)c.Q + ((i64)n * c.Tq + (row_ok ? i : 0)) * c.ldq + (i64)head * c.D, c.D, row_ok, VEC, lane, qf);
-    const Mod mod(c);
-    const float slope2 = MOD == 1 && c.slopes != nullptr ? c.slopes[head] * kLog2e : 0.0f;
+    const Scores<T, MOD> score(c);
+    const float slope2 = (MOD & kSlope) != 0 && c.slopes != nullptr ? c.slopes[head] * kLog2e : 0.0f;
 
     RowSpan span = span_of(smp, c.G, M, r0, S::BR);
     // keys of this workgroup
@@ -151,16 +151,18 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     float top = -INFINITY, sum = 0.0f;
 
     const Stager<TL, T, BN, SMALL ? 1 : NW, VEC> stk(c.ldk, c.D, SMALL ? 0 : wave, lane), stv(c.ldv, c.D, SMALL ? 0 : wave, lane);
-    char *mine = smem + (SMALL ? wave * 2 * S::STAGE : 0);
+    char *mine = smem + (SMALL ? wave * S::STAGE : 0);
     const uint32_t lds0 = lds_addr(mine);
-    const auto issue = [&](int t, int buf) {
+    const auto issue_k = [&](int t, int buf) {
         const i64 k0 = (i64)t * BN;
-        const int left = (int)(end - k0);
-        stk.issue(K + k0 * c.ldk, left, lds0 + buf * S::STAGE, mine + buf * S::STAGE);
-        stv.issue(V + k0 * c.ldv, left, lds0 + buf * S::STAGE + S::HALF, mine + buf * S::STAGE + S::HALF);
+        stk.issue(K + k0 * c.ldk, (int)(end - k0), lds0 + buf * S::STAGE, mine + buf * S::STAGE);
     };
-    const auto step = [&](const char *LK, const char *LV, int k0, int cls) {
-        f32x16_t s[FN];
+    const auto issue_v = [&](int t, int buf) {
+        const i64 k0 = (i64)t * BN;
+        stv.issue(V + k0 * c.ldv, (int)(end - k0), lds0 + buf * S::STAGE + S::HALF, mine + buf * S::STAGE + S::HALF);
+    };
+    f32x16_t s[FN];
+    const auto scores = [&](const char *LK) {
 #pragma unroll
         for (int x = 0; x < FN; ++x)
 #pragma unroll
@@ -169,39 +171,40 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int x = 0; x < FN; ++x) TL::mma(TL::rows(LK, 32 * x, ks, lane), qf[ks], s[x]);
+    };
+    // scores to weights, running maximum and sum
+    const auto soften = [&](int k0, int cls) {
         const auto key = [&](int x, int e) { return k0 + 32 * x + 8 * (e >> 2) + 4 * h + (e & 3); };
-        if constexpr (MOD == 1) {
+        const auto far = [&](int x, int e) { return __builtin_fabsf((float)(pos - key(x, e))); };
+        const auto each = [&](auto &&f) {
 #pragma unroll
             for (int x = 0; x < FN; ++x)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float unused;
-                    s[x][e] = modded<T>(mod, s[x][e], slope2, __builtin_fabsf((float)(pos - key(x, e))), unused);
-                }
-        }
-        if (cls != kFull) {
+                for (int e = 0; e < 16; ++e) s[x][e] = f(x, e, s[x][e]);
+        };
+        const auto hide = [&](float with) {
+            each([&](int x, int e, float v) { return key(x, e) < lim ? v : with; });
+            if (smp.docs != nullptr)
+                each([&](int x, int e, float v) {
+                    const int j = key(x, e), d = smp.docs[j < end ? j : end - 1];
+                    return ((d == doc) & (d >= 0)) ? v : with;
+                });
+        };
+        float unused;
+        bool near = MOD == kCap;
+        if constexpr (MOD == kCap)
 #pragma unroll
-            for (int x = 0; x < FN; ++x)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[x][e] = key(x, e) < lim ? s[x][e] : -INFINITY;
-            if (smp.docs != nullptr) {
-#pragma unroll
-                for (int x = 0; x < FN; ++x)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int j = key(x, e);
-                        const int d = smp.docs[j < end ? j : end - 1];
-                        s[x][e] = d == doc && d >= 0 ? s[x][e] : -INFINITY;
-                    }
-            }
-        }
+            for (int x = 0; x < FN; ++x) near = near && score.near(s[x]);
+        if constexpr (MOD >= kSlope) each([&](int x, int e, float v) { return score.template of<false>(v, 0.0f, slope2, far(x, e), unused); });
+        if (cls != kFull) hide(-INFINITY);
         float t = s[0][0];
 #pragma unroll
         for (int x = 0; x < FN; ++x)
 #pragma unroll
             for (int e = 0; e < 16; ++e) t = fmaxf(t, s[x][e]);
-        if constexpr (MOD == 0) t *= mod.scale2;
         t = fmaxf(t, other_half(t));
+        if constexpr (MOD == kPlain) t *= score.scale2;
+        if constexpr (MOD == kCap) t = t == -INFINITY ? t : score.cap2 * tanh_for<T>(score.y_scale * t);
         if (__any(t > top + 8.0f)) {
             const float was = top;
             top = fmaxf(top, t);
@@ -213,15 +216,30 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 for (int e = 0; e < 16; ++e) acc[d][e] *= f;
         }
         const float base = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-        for (int x = 0; x < FN; ++x) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[x][e] = __builtin_amdgcn_exp2f(MOD == 0 ? __builtin_fmaf(s[x][e], mod.scale2, -base) : s[x][e] - base);
-                sum += s[x][e];
+        const auto weigh = [&](auto is_near) {
+            each([&](int, int, float v) {
+                return __builtin_amdgcn_exp2f(
+                    MOD >= kSlope ? v - base : score.template of<decltype(is_near)::value>(v, base, 0.0f, 0.0f, unused));
+            });
+        };
+        if constexpr (MOD == kCap) {
+            // (a hidden score, -inf, has weight 0 by the polynomial, but tanh = -1 has not)
+            if (near) weigh(std::true_type{});
+            else {
+                weigh(std::false_type{});
+                if (cls != kFull) hide(0.0f);
             }
-            TL::mma_columns(LV, 32 * x, s[x], acc, lane);
+        } else {
+            weigh(std::false_type{});
         }
+#pragma unroll
+        for (int x = 0; x < FN; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum += s[x][e];
+    };
+    const auto values = [&](const char *LV) {
+#pragma unroll
+        for (int x = 0; x < FN; ++x) TL::mma_columns(LV, 32 * x, s[x], acc, lane);
     };
 
     for (int base = t0; base < t1; base += kGroup) {
@@ -269,35 +287,54 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         };
         int t, cls;
         if constexpr (SMALL) {
-            // a wave's own tiles, in its own buffers
+            // a wave's own tiles, in its own buffers: K's takes the next tile once the scores are formed, V's once the sums are
             if (wave < count) {
                 entry(wave, t, cls);
-                issue(t, 0);
-                int buf = 0;
-                for (int k = wave; k < count; k += NW, buf ^= 1) {
+                issue_k(t, 0);
+                issue_v(t, 0);
+                for (int k = wave; k < count; k += NW) {
                     const int k0 = t * BN, now = cls;
-                    wait_loads();                       // and for the reads of the buffer that the next tile goes to
+                    const bool more = k + NW < count;
+                    if constexpr (VEC) bf16s::wait_vmcnt<decltype(stv)::LOADS>();
                     bf16s::wait_lgkmcnt0();
-                    if (k + NW < count) {
+                    wave_together();
+                    scores(mine);
+                    bf16s::wait_lgkmcnt0();
+                    if (more) {
                         entry(k + NW, t, cls);
-                        issue(t, buf ^ 1);
+                        issue_k(t, 0);
                     }
-                    step(mine + buf * S::STAGE, mine + buf * S::STAGE + S::HALF, k0, now);
+                    soften(k0, now);
+                    if constexpr (VEC) {
+                        if (more) bf16s::wait_vmcnt<decltype(stk)::LOADS>();
+                        else wait_loads();
+                    }
+                    bf16s::wait_lgkmcnt0();
+                    wave_together();
+                    values(mine + S::HALF);
+                    bf16s::wait_lgkmcnt0();
+                    if (more) issue_v(t, 0);
                 }
             }
         } else {
             if (count > 0) {
                 entry(0, t, cls);
-                issue(t, 0);
+                issue_k(t, 0);
+                issue_v(t, 0);
                 for (int k = 0; k < count; ++k) {
                     const int k0 = t * BN, now = cls;
                     wait_loads();
                     lds_barrier();                      // this tile has landed, the one before is read
                     if (k + 1 < count) {
                         entry(k + 1, t, cls);
-                        issue(t, (k + 1) & 1);
+                        issue_k(t, (k + 1) & 1);
+                        issue_v(t, (k + 1) & 1);
                     }
-                    step(smem + (k & 1) * S::STAGE, smem + (k & 1) * S::STAGE + S::HALF, k0, now);
+                    const char *L = smem + (k & 1) * S::STAGE;
+                    wave_together();
+                    scores(L);
+                    soften(k0, now);
+                    values(L + S::HALF);
                 }
             }
             lds_barrier();
@@ -410,38 +447,65 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     }
 }
 
-// A wave joins a row's sums over the splits.
+// A workgroup joins a row's sums over the splits: its waves take every fourth, eight loads in flight (a loop of single loads over
+// 32 splits took 30 us), and are added in wave order.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(Call c, ForwardOut out)
 {
-    const i64 rr = (i64)blockIdx.x * 4 + threadIdx.x / kWave;
-    if (rr >= out.rows) return;
-    const int lane = threadIdx.x & (kWave - 1), M = c.Tq * c.G, nk = (int)(rr / M), r = (int)(rr - (i64)nk * M);
+    constexpr int NW = 4, PER = kTileD / kWave, AHEAD = 8;
+    __shared__ float part[NW][kTileD];
+    const i64 rr = blockIdx.x;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int M = c.Tq * c.G, nk = (int)(rr / M), r = (int)(rr - (i64)nk * M);
     const int n = nk / c.Hk, kv = nk - n * c.Hk, i = r / c.G, head = kv * c.G + r - i * c.G;
     const float *ml = out.part + (i64)out.splits * out.rows * c.D + 2 * rr;
+    const i64 step = 2 * out.rows;
     float all = -INFINITY;
-    for (int s = 0; s < out.splits; ++s) all = fmaxf(all, ml[2 * s * out.rows]);
+    for (int s = lane; s < out.splits; s += kWave) all = fmaxf(all, ml[s * step]);
+    all = wave_max(all);
     const float base = all == -INFINITY ? 0.0f : all;
-    float total = 0.0f, v[kMaxD / kWave] = {};
-    for (int s = 0; s < out.splits; ++s) {
-        const float f = __builtin_amdgcn_exp2f(ml[2 * s * out.rows] - base);
-        total += f * ml[2 * s * out.rows + 1];
-        const float *p = out.part + ((i64)s * out.rows + rr) * c.D;
+    float total = 0.0f;
+    for (int s = lane; s < out.splits; s += kWave) total += __builtin_amdgcn_exp2f(ml[s * step] - base) * ml[s * step + 1];
+    total = wave_sum(total);
+    float v[PER] = {};
+    for (int s0 = wave; s0 < out.splits; s0 += NW * AHEAD) {
+        float f[AHEAD], x[AHEAD][PER];
 #pragma unroll
-        for (int k = 0; k < kMaxD / kWave; ++k)
-            if (lane + kWave * k < c.D) v[k] += f * p[lane + kWave * k];
+        for (int a = 0; a < AHEAD; ++a) {
+            const int s = s0 + NW * a;
+            const bool ok = s < out.splits;
+            f[a] = ok ? ml[s * step] : -INFINITY;
+            const float *p = out.part + ((i64)(ok ? s : s0) * out.rows + rr) * c.D;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) x[a][k] = lane + kWave * k < c.D ? p[lane + kWave * k] : 0.0f;
+        }
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const float g = __builtin_amdgcn_exp2f(f[a] - base);
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (s0 + NW * a < out.splits) v[k] += g * x[a][k];
+        }
     }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) part[wave][lane + kWave * k] = v[k];
+    __syncthreads();
+    if (wave != 0) return;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     T *o = (T *)out.O + ((i64)n * c.Tq + i) * c.ldo + (i64)head * c.D;
-    bool bad = not_finite(inv);
+    bool bad = not_finite(inv) || not_finite(total);
 #pragma unroll
-    for (int k = 0; k < kMaxD / kWave; ++k) bad = bad || not_finite(v[k] *= inv);
+    for (int k = 0; k < PER; ++k) {
+        const int d = lane + kWave * k;
+        v[k] = (((part[0][d] + part[1][d]) + part[2][d]) + part[3][d]) * inv;
+        bad = bad || not_finite(v[k]);
+    }
     if (__any(bad)) {
         forward_row<T>(c, n, head, i, (T *)out.O, out.lse);
         return;
     }
 #pragma unroll
-    for (int k = 0; k < kMaxD / kWave; ++k)
+    for (int k = 0; k < PER; ++k)
         if (lane + kWave * k < c.D) store_elem(o + lane + kWave * k, v[k]);
     if (out.lse != nullptr && lane == 0)
         out.lse[((i64)n * c.Hq + head) * c.Tq + i] = total == 0.0f ? -INFINITY : all * kLn2 + logf(total);
@@ -463,17 +527,16 @@ void by_kind(const Call &c, const ForwardOut &out, bool small, hipStream_t strea
     const bool vec = c.D % N == 0 && c.ldq % N == 0 && c.ldk % N == 0 && c.ldv % N == 0 && aligned(c.Q, 16) && aligned(c.K, 16) &&
                      aligned(c.V, 16);
     const bool vec_out = c.D % N == 0 && c.ldo % N == 0 && aligned(out.O, 16);
-    const bool mod = c.cap > 0.0f || c.slopes != nullptr || c.scale <= 0.0f;
+    const int mod = c.scale <= 0.0f ? kBoth : (c.cap > 0.0f ? kCap : kPlain) | (c.slopes != nullptr ? kSlope : kPlain);
     const auto go = [&](auto v, auto m) {
         if (small) launch<T, DP, decltype(v)::value, decltype(m)::value, true>(c, out, vec_out, stream);
         else launch<T, DP, decltype(v)::value, decltype(m)::value, false>(c, out, vec_out, stream);
     };
-    typedef std::integral_constant<bool, true> yes;
-    typedef std::integral_constant<bool, false> no;
-    typedef std::integral_constant<int, 0> plain;
-    typedef std::integral_constant<int, 1> bent;
-    if (vec) mod ? go(yes{}, bent{}) : go(yes{}, plain{});
-    else mod ? go(no{}, bent{}) : go(no{}, plain{});
+    if (!vec) go(std::false_type{}, std::integral_constant<int, kBoth>{});
+    else if (mod == kPlain) go(std::true_type{}, std::integral_constant<int, kPlain>{});
+    else if (mod == kCap) go(std::true_type{}, std::integral_constant<int, kCap>{});
+    else if (mod == kSlope) go(std::true_type{}, std::integral_constant<int, kSlope>{});
+    else go(std::true_type{}, std::integral_constant<int, kBoth>{});
 }
 
 template <typename T>
@@ -483,7 +546,7 @@ dp_status tiles_of(const Call &c, const ForwardOut &out, bool small, hipStream_t
     else if (c.D <= 64) by_kind<T, 64>(c, out, small, stream);
     else if (c.D <= 96) by_kind<T, 96>(c, out, small, stream);
     else by_kind<T, 128>(c, out, small, stream);
-    if (out.splits > 1) join_kernel<T><<<(unsigned)ceil_div(out.rows, 4), 256, 0, stream>>>(c, out);
+    if (out.splits > 1) join_kernel<T><<<(unsigned)out.rows, 256, 0, stream>>>(c, out);
     return launch_status();
 }
 

@@ -65,6 +65,11 @@ __device__ __forceinline__ void dma4_off(const void *base, uint32_t off, uint32_
 
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// All lanes of the wave go on from here together.  The matrix instructions and LDS reads are not marked as ones that a wave runs
+// as a whole: a lane-dependent branch right before a loop of them was once drawn into the loop, whose trips then ran with some
+// lanes switched off.
+__device__ __forceinline__ void wave_together() { __builtin_amdgcn_wave_barrier(); }
+
 // the value of lane ^ 32
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, kWave); }
 
@@ -140,33 +145,35 @@ struct Tile {
         }
     }
 
-    // A row's operands for all k-steps, from memory; zeros behind D and where !ok
+    // A row's operands for all k-steps, from memory; zeros behind D and where !ok (the row is one that may be read all the same).
+    // No branches: the values are lanes' own, and what follows has to be run by all lanes together.
     static __device__ __forceinline__ void load_row(const T *p, int D, bool ok, bool vec, int lane, u32x4_t (&f)[KS])
     {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const int d = (2 * ks + (lane >> 5)) * N;
-            u32x4_t v = {0, 0, 0, 0};
-            if (vec) {
-                if (ok && d < D) v = *reinterpret_cast<const u32x4_t *>(p + d);
-            } else if (ok) {
-                v = piece(p, d, D);
-            }
+            u32x4_t v = vec ? *reinterpret_cast<const u32x4_t *>(p + (d < D ? d : 0)) : piece(p, d, D);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = ok && d < D ? v[e] : 0;
             f[ks] = v;
         }
     }
-    // values d .. of a row of any alignment, zeros from D on
+    // values d .. of a row of any alignment, zeros from D on (a value behind the end is loaded from the row's first place)
     static __device__ __forceinline__ u32x4_t piece(const T *p, int d, int D)
     {
         u32x4_t v = {0, 0, 0, 0};
         if constexpr (BF16) {
+            uint32_t x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (d + e < D) v[e >> 1] |= (uint32_t)p[d + e] << (16 * (e & 1));
+            for (int e = 0; e < 8; ++e) x[e] = p[d + e < D ? d + e : 0];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e >> 1] |= (d + e < D ? x[e] : 0) << (16 * (e & 1));
         } else {
+            float x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (d + e < D) v[e] = __float_as_uint(p[d + e]);
+            for (int e = 0; e < 4; ++e) x[e] = p[d + e < D ? d + e : 0];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = d + e < D ? __float_as_uint(x[e]) : 0;
         }
         return v;
     }
@@ -213,43 +220,98 @@ struct Stager {
 // ---------------------------------------------------------------------------
 // scores in units of ln 2
 // ---------------------------------------------------------------------------
-// MOD 0: scale alone (scale > 0); 1: a cap and/or a bias by distance, or any scale
-struct Mod {
-    float scale2;            // scale * log2 e
-    float y_scale, cap2;     // scale / cap, cap * log2 e; cap2 = 0: no cap
-    __device__ __forceinline__ explicit Mod(const Call &c)
-    {
-        scale2 = c.scale * kLog2e;
-        cap2 = c.cap * kLog2e;
-        y_scale = c.cap > 0.0f ? c.scale / c.cap : 0.0f;
-    }
-};
+// What a score has besides its scale (> 0): kBoth looks at run time, and takes any scale
+enum { kPlain = 0, kCap = 1, kSlope = 2, kBoth = 3 };
 
-// tanh, for scores of bf16 inputs by exp2 and reciprocal (off by some 2^-22, where
-// the inputs' rounding is 2^-9 of a score), for fp32 ones to fp32's last bits
+// For scores of bf16 inputs, whose rounding is 2^-9 of a score: tanh y = y P(y^2),
+// within 6e-7 of itself for |y| <= 3/4 (a least-maximum fit of five terms), where
+// no score of a wave's block goes further, which a cap is chosen for; else by
+// exp2 and reciprocal (off by some 2^-22).  The polynomial with the scales in its
+// coefficients takes five instructions a score, of which the last forms the
+// exponent; the other way three and two quarter-rate ones.
+constexpr float kNear = 0.75f;
+constexpr float kTanh[5] = {0.999999435f, -0.333282516f, 0.132589834f, -0.0500563036f, 0.0129296314f};
+
+// For fp32 inputs without branches: seven terms up to |y| = 3/4 (1.5e-9 of itself, before rounding), from there 1 - 2 / (1 +
+// exp 2|y|), whose subtrahend is at most 0.37 and off by some 2^-23 of it.
+constexpr float kTanh7[7] = {0.999999999f, -0.333333072f, 0.133325791f, -0.0538856315f, 0.0214308735f, -0.00762702948f, 0.00172035412f};
+
 template <typename T>
 __device__ __forceinline__ float tanh_for(float y)
 {
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2) {
         return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * y));
-    else
-        return tanhf(y);
+    } else {
+        const float a = __builtin_fabsf(y), u = y * y;
+        float p = kTanh7[6];
+#pragma unroll
+        for (int k = 5; k >= 0; --k) p = __builtin_fmaf(u, p, kTanh7[k]);
+        const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * a));
+        return a < kNear ? y * p : __builtin_copysignf(far, y);
+    }
 }
 
-template <typename T>
-__device__ __forceinline__ float modded(const Mod &m, float x, float slope2, float far, float &bend)
-{
-    float s;
-    if (m.cap2 != 0.0f) {
-        const float t = tanh_for<T>(m.y_scale * x);
-        s = m.cap2 * t;
-        bend = 1.0f - t * t;
-    } else {
-        s = m.scale2 * x;
-        bend = 1.0f;
+template <typename T, int MOD>
+struct Scores {
+    float scale2;            // scale * log2 e
+    float y_scale, cap2;     // scale / cap, cap * log2 e; cap2 = 0: no cap
+    float inv_cap2;          // 1 / cap2
+    float c[5];              // the polynomial's, of the raw score
+
+    __device__ __forceinline__ explicit Scores(const Call &a)
+    {
+        scale2 = a.scale * kLog2e;
+        cap2 = a.cap * kLog2e;
+        y_scale = a.cap > 0.0f ? a.scale / a.cap : 0.0f;
+        inv_cap2 = a.cap > 0.0f ? 1.0f / cap2 : 0.0f;
+        float f = cap2 * y_scale;
+#pragma unroll
+        for (int k = 0; k < 5; ++k, f *= y_scale * y_scale) c[k] = f * kTanh[k];
     }
-    return s - slope2 * far;
-}
+    // whether the polynomial may be taken for all raw scores of the wave's block
+    __device__ __forceinline__ bool near(const f32x16_t &x) const
+    {
+        if constexpr (MOD != kCap || sizeof(T) != 2) return false;
+        float m = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, __builtin_fabsf(x[e]));
+        return !__any(!(m * __builtin_fabsf(y_scale) <= kNear));
+    }
+    __device__ __forceinline__ float poly(float x) const
+    {
+        const float u = x * x;
+        return __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, c[4], c[3]), c[2]), c[1]), c[0]);
+    }
+    // a raw score less `base`; bend: the capped score's derivative by the uncapped one
+    template <bool NEAR>
+    __device__ __forceinline__ float of(float x, float base, float slope2, float far, float &bend) const
+    {
+        bend = 1.0f;
+        if constexpr (MOD == kPlain) {
+            return __builtin_fmaf(x, scale2, -base);
+        } else if constexpr (MOD == kSlope) {
+            return __builtin_fmaf(-slope2, far, __builtin_fmaf(x, scale2, -base));
+        } else if constexpr (MOD == kCap) {
+            if constexpr (NEAR) {
+                const float p = poly(x), t = x * p * inv_cap2;
+                bend = __builtin_fmaf(-t, t, 1.0f);
+                return __builtin_fmaf(x, p, -base);
+            } else {
+                const float t = tanh_for<T>(y_scale * x);
+                bend = __builtin_fmaf(-t, t, 1.0f);
+                return __builtin_fmaf(cap2, t, -base);
+            }
+        } else {
+            float v = scale2 * x;
+            if (cap2 != 0.0f) {
+                const float t = tanh_for<T>(y_scale * x);
+                bend = __builtin_fmaf(-t, t, 1.0f);
+                v = cap2 * t;
+            }
+            return v - slope2 * far - base;
+        }
+    }
+};
 
 // ---------------------------------------------------------------------------
 // which tiles two blocks meet in
