@@ -260,7 +260,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const int end = smp.end_for(span.pmax < span.pmin ? -1 : span.pmax), t1 = (end + BN - 1) / BN;
     if (smp.docs != nullptr) wave_docs_range(smp.docs, span.pmin, span.pmax, lane, span.dmin, span.dmax);
 
-    f32x16_t acc[DB];
+    typedef f32x16_t Sums[DB];
+    Sums acc;
     zero(acc);
     const Stager<TL, T, BN, SMALL ? 1 : NW, VEC> stk(c.ldk, c.D, SMALL ? 0 : wave, lane), stv(c.ldv, c.D, SMALL ? 0 : wave, lane);
     char *mine = smem + (SMALL ? wave * 2 * S::STAGE : 0);
@@ -277,11 +278,9 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             f32x16_t s, e;
 #pragma unroll
             for (int k = 0; k < 16; ++k) s[k] = e[k] = 0.0f;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                TL::mma(TL::rows(LK, 32 * x, ks, lane), qf[ks], s);
-                TL::mma(TL::rows(LV, 32 * x, ks, lane), df[ks], e);
-            }
+            TL::template products<2>([&](int i, int ks) { return TL::rows(i == 0 ? LK : LV, 32 * x, ks, lane); },
+                                     [&](int i, int ks) -> const u32x4_t & { return i == 0 ? qf[ks] : df[ks]; },
+                                     [&](int i) -> f32x16_t & { return i == 0 ? s : e; });
             const auto key = [&](int k) { return k0 + 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
             const auto weigh = [&](auto is_near) {
 #pragma unroll
@@ -298,15 +297,17 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             if (cls != kFull) {
 #pragma unroll
                 for (int k = 0; k < 16; ++k) e[k] = key(k) < lim ? e[k] : 0.0f;
-                if (smp.docs != nullptr) {
+                if (cls == kDocs) {
+                    // (all loads before the first comparison)
+                    int d[16];
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const int j = key(k), d = smp.docs[j < end ? j : end - 1];
-                        e[k] = ((d == doc) & (d >= 0)) ? e[k] : 0.0f;
-                    }
+                    for (int k = 0; k < 16; ++k) d[k] = smp.docs[key(k) < end ? key(k) : end - 1];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) e[k] = d[k] == doc && doc >= 0 ? e[k] : 0.0f;
                 }
             }
-            TL::mma_columns(LK, 32 * x, e, acc, lane);
+            TL::template columns<1>([&](int) { return LK + 32 * x * TL::RB; }, [&](int) -> const f32x16_t & { return e; },
+                                    [&](int) -> Sums & { return acc; }, lane);
         }
     };
 
@@ -372,9 +373,15 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
 // ---------------------------------------------------------------------------
 // dK and dV
 // ---------------------------------------------------------------------------
-template <typename T, int DP, bool VEC, int MOD, bool SMALL>
-__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, DP>::RB > 128 ? 1 : 2)) void key_kernel(Call c, Grads gr, bool vec_k, bool vec_v)
+// SUMS: which of the two a launch forms.  Both in one take sums and operands of 260 and more registers a lane where rows are 192
+// bytes or longer, so one wave per SIMD, which waits half of its time (8192 causal queries in documents, 32 and 8 heads of 128,
+// capped scores: 2515 us); each in a launch of its own has two, for one product more.
+enum { kSumV = 1, kSumK = 2 };
+
+template <typename T, int DP, bool VEC, int MOD, bool SMALL, int SUMS>
+__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, DP>::RB > (SUMS == 3 ? 128 : 256) ? 1 : 2)) void key_kernel(Call c, Grads gr, bool vec_k, bool vec_v)
 {
+    constexpr bool SUM_K = (SUMS & kSumK) != 0, SUM_V = (SUMS & kSumV) != 0;
     typedef Shape<T, DP, SMALL> S;
     typedef Tile<T, DP> TL;
     constexpr int BN = S::BN, FN = S::FN, DB = TL::DB, KS = TL::KS, NW = S::NW;
@@ -401,9 +408,9 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const i64 krow = (i64)n * c.Tk + (key_ok ? j : 0);
     u32x4_t kf[KS], vf[KS];
     TL::load_row((const T *)c.K + krow * c.ldk + (i64)kv * c.D, c.D, key_ok, VEC, lane, kf);
-    TL::load_row((const T *)c.V + krow * c.ldv + (i64)kv * c.D, c.D, key_ok, VEC, lane, vf);
+    if constexpr (SUM_K) TL::load_row((const T *)c.V + krow * c.ldv + (i64)kv * c.D, c.D, key_ok, VEC, lane, vf);
     // queries at positions from .. L - 1 see it
-    const int from = !key_ok ? 0x7fffffff : !smp.causal || j < smp.prefix ? 0 : j;
+    const int from = !key_ok ? 1 << 30 : !smp.causal || j < smp.prefix ? 0 : j;
     const int doc = key_ok && smp.docs != nullptr ? smp.docs[j] : -1;
     const Scores<T, MOD> score(c);
 
@@ -417,7 +424,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     if (j0 < smp.L && smp.docs != nullptr) wave_docs_range(smp.docs, j0, end - 1, lane, kd0, kd1);
     const int t0 = i0 / BN, t1 = j0 < smp.L && i0 < i1 ? (i1 + BN - 1) / BN : t0;
 
-    f32x16_t ak[DB], av[DB];
+    typedef f32x16_t Sums[DB];
+    Sums ak, av;
     zero(ak);
     zero(av);
     const Stager<TL, T, BN, SMALL ? 1 : NW, VEC> stq(c.ldq, c.D, SMALL ? 0 : wave, lane), std(c.ldo, c.D, SMALL ? 0 : wave, lane);
@@ -443,11 +451,9 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             f32x16_t s, e;
 #pragma unroll
             for (int k = 0; k < 16; ++k) s[k] = e[k] = 0.0f;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                TL::mma(TL::rows(LQ, 32 * x, ks, lane), kf[ks], s);
-                TL::mma(TL::rows(LD, 32 * x, ks, lane), vf[ks], e);
-            }
+            TL::template products<SUM_K ? 2 : 1>([&](int i, int ks) { return TL::rows(i == 0 ? LQ : LD, 32 * x, ks, lane); },
+                                                 [&](int i, int ks) -> const u32x4_t & { return i == 0 ? kf[ks] : vf[ks]; },
+                                                 [&](int i) -> f32x16_t & { return i == 0 ? s : e; });
             const auto place = [&](int k) { return 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
             const auto weigh = [&](auto is_near) {
 #pragma unroll
@@ -461,28 +467,43 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                         float bend;
                         s[k] = __builtin_amdgcn_exp2f(score.template of<decltype(is_near)::value>(
                             s[k], lse2[w], slope2, __builtin_fabsf((float)(smp.first + q0 + place(k) - j)), bend));
-                        e[k] = s[k] * (e[k] - delta[w]);
-                        if constexpr ((MOD & kCap) != 0) e[k] *= bend;
+                        if constexpr (SUM_K) {
+                            e[k] = s[k] * (e[k] - delta[w]);
+                            if constexpr ((MOD & kCap) != 0) e[k] *= bend;
+                        }
                     }
                 }
             };
             if (score.near(s)) weigh(std::true_type{});
             else weigh(std::false_type{});
             if (cls != kFull) {
+                const int lo = from - smp.first - q0, hi = (smp.L - smp.first < c.Tq ? smp.L - smp.first : c.Tq) - q0;
+                const auto hide = [&](auto &&seen) {
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const int p = smp.first + q0 + place(k);
-                    bool see = (p >= from) & (p < smp.L) & (q0 + place(k) < c.Tq);
-                    if (smp.docs != nullptr) {
-                        const int d = smp.docs[p < 0 ? 0 : p < smp.L ? p : smp.L - 1];
-                        see = see & (d == doc) & (d >= 0);
+                    for (int k = 0; k < 16; ++k) {
+                        const bool see = seen(k);
+                        s[k] = see ? s[k] : 0.0f;
+                        e[k] = see ? e[k] : 0.0f;
                     }
-                    s[k] = see ? s[k] : 0.0f;
-                    e[k] = see ? e[k] : 0.0f;
+                };
+                hide([&](int k) { return place(k) >= lo && place(k) < hi; });
+                if (cls == kDocs) {
+                    // (all loads before the first comparison)
+                    int d[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        int p = smp.first + q0 + place(k);
+                        p = p > 0 ? p : 0;
+                        d[k] = smp.docs[p < smp.L ? p : smp.L - 1];
+                    }
+                    hide([&](int k) { return d[k] == doc && doc >= 0; });
                 }
             }
-            TL::mma_columns(LD, 32 * x, s, av, lane);
-            TL::mma_columns(LQ, 32 * x, e, ak, lane);
+            const char *LX = L + 32 * x * TL::RB;
+            TL::template columns<SUM_K && SUM_V ? 2 : 1>(
+                [&](int i) { return SUM_V && i == 0 ? LX + S::HALF : LX; },
+                [&](int i) -> const f32x16_t & { return SUM_V && i == 0 ? s : e; },
+                [&](int i) -> Sums & { return SUM_V && i == 0 ? av : ak; }, lane);
         }
     };
 
@@ -538,12 +559,16 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const auto row_of = [&](void *p, i64 ld, int k) -> T * {
         return jw + k < c.Tk ? (T *)p + ((i64)n * c.Tk + jw + k) * ld + (i64)kv * c.D : nullptr;
     };
-    bool bad = put_block<T, DP, S, SMALL>(smem, ak, c.scale, c.D, vec_k, lane, wave, [&](int k) { return row_of(gr.dK, c.ldk, k); });
-    bad |= put_block<T, DP, S, SMALL>(smem, av, 1.0f, c.D, vec_v, lane, wave, [&](int k) { return row_of(gr.dV, c.ldv, k); });
+    bool bad = false;
+    if constexpr (SUM_K)
+        bad |= put_block<T, DP, S, SMALL>(smem, ak, c.scale, c.D, vec_k, lane, wave, [&](int k) { return row_of(gr.dK, c.ldk, k); });
+    if constexpr (SUM_V)
+        bad |= put_block<T, DP, S, SMALL>(smem, av, 1.0f, c.D, vec_v, lane, wave, [&](int k) { return row_of(gr.dV, c.ldv, k); });
     wait_loads();                                        // the stores above come before those below
     if (SMALL ? __syncthreads_or(bad) : __any(bad))
         for (int k = SMALL ? wave : 0; k < 32 && jw + k < c.Tk; k += SMALL ? NW : 1)
-            backward_key_row<T>(c, n, kv, jw + k, (const T *)gr.O, gr.lse, (const T *)gr.dO, (T *)gr.dK, (T *)gr.dV);
+            backward_key_row<T>(c, n, kv, jw + k, (const T *)gr.O, gr.lse, (const T *)gr.dO, SUM_K ? (T *)gr.dK : nullptr,
+                                SUM_V ? (T *)gr.dV : nullptr);
 }
 
 template <typename T, int DP, bool VEC, int MOD>
@@ -562,13 +587,16 @@ void launch(const Call &c, const Grads &g, hipStream_t stream)
                 c, g, tiles, wide(g.dQ, c.ldq));
     }
     if (c.Tk > 0) {
-        const i64 tiles = ceil_div(c.Tk, g.small_k ? 32 : 128);
-        if (g.small_k)
-            key_kernel<T, DP, VEC, MOD, true><<<(unsigned)(heads * tiles), Shape<T, DP, true>::THREADS, 0, stream>>>(
-                c, g, wide(g.dK, c.ldk), wide(g.dV, c.ldv));
-        else
-            key_kernel<T, DP, VEC, MOD, false><<<(unsigned)(heads * tiles), Shape<T, DP, false>::THREADS, 0, stream>>>(
-                c, g, wide(g.dK, c.ldk), wide(g.dV, c.ldv));
+        const unsigned blocks = (unsigned)(heads * ceil_div(c.Tk, g.small_k ? 32 : 128));
+        const bool vk = wide(g.dK, c.ldk), vv = wide(g.dV, c.ldv);
+        if (g.small_k) {
+            key_kernel<T, DP, VEC, MOD, true, kSumK | kSumV><<<blocks, Shape<T, DP, true>::THREADS, 0, stream>>>(c, g, vk, vv);
+        } else if constexpr (sizeof(T) == 2 && Tile<T, DP>::RB > 1280) {
+            key_kernel<T, DP, VEC, MOD, false, kSumV><<<blocks, Shape<T, DP, false>::THREADS, 0, stream>>>(c, g, vk, vv);
+            key_kernel<T, DP, VEC, MOD, false, kSumK><<<blocks, Shape<T, DP, false>::THREADS, 0, stream>>>(c, g, vk, vv);
+        } else {
+            key_kernel<T, DP, VEC, MOD, false, kSumK | kSumV><<<blocks, Shape<T, DP, false>::THREADS, 0, stream>>>(c, g, vk, vv);
+        }
     }
 }
 

@@ -167,10 +167,9 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         for (int x = 0; x < FN; ++x)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-            for (int x = 0; x < FN; ++x) TL::mma(TL::rows(LK, 32 * x, ks, lane), qf[ks], s[x]);
+        TL::template products<FN>([&](int x, int ks) { return TL::rows(LK, 32 * x, ks, lane); },
+                                  [&](int, int ks) -> const u32x4_t & { return qf[ks]; },
+                                  [&](int x) -> f32x16_t & { return s[x]; });
     };
     // scores to weights, running maximum and sum
     const auto soften = [&](int k0, int cls) {
@@ -184,11 +183,15 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         };
         const auto hide = [&](float with) {
             each([&](int x, int e, float v) { return key(x, e) < lim ? v : with; });
-            if (smp.docs != nullptr)
-                each([&](int x, int e, float v) {
-                    const int j = key(x, e), d = smp.docs[j < end ? j : end - 1];
-                    return ((d == doc) & (d >= 0)) ? v : with;
-                });
+            if (cls == kDocs) {
+                // (all loads before the first comparison)
+                int d[FN][16];
+#pragma unroll
+                for (int x = 0; x < FN; ++x)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) d[x][e] = smp.docs[key(x, e) < end ? key(x, e) : end - 1];
+                each([&](int x, int e, float v) { return d[x][e] == doc && doc >= 0 ? v : with; });
+            }
         };
         float unused;
         bool near = MOD == kCap;
@@ -238,8 +241,9 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             for (int e = 0; e < 16; ++e) sum += s[x][e];
     };
     const auto values = [&](const char *LV) {
-#pragma unroll
-        for (int x = 0; x < FN; ++x) TL::mma_columns(LV, 32 * x, s[x], acc, lane);
+        typedef f32x16_t Sums[DB];
+        TL::template columns<FN>([&](int x) { return LV + 32 * x * TL::RB; }, [&](int x) -> const f32x16_t & { return s[x]; },
+                                 [&](int) -> Sums & { return acc; }, lane);
     };
 
     for (int base = t0; base < t1; base += kGroup) {

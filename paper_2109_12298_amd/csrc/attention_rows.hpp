@@ -108,6 +108,7 @@ __device__ void backward_query_row(const Call &c, int n, int h, int i, const T *
         if (lane + kWave * k < c.D) store_elem(dQ + at + lane + kWave * k, acc[k]);
 }
 
+// dK, dV: either may be NULL
 template <typename T>
 __device__ void backward_key_row(const Call &c, int n, int kv, int j, const T *O, const float *lse, const T *dO, T *dK, T *dV)
 {
@@ -138,8 +139,8 @@ __device__ void backward_key_row(const Call &c, int n, int kv, int j, const T *O
 #pragma unroll
     for (int e = 0; e < kPerLane; ++e)
         if (lane + kWave * e < c.D) {
-            store_elem(dK + ((i64)n * c.Tk + j) * c.ldk + (i64)kv * c.D + lane + kWave * e, ak[e]);
-            store_elem(dV + ((i64)n * c.Tk + j) * c.ldv + (i64)kv * c.D + lane + kWave * e, av[e]);
+            if (dK != nullptr) store_elem(dK + ((i64)n * c.Tk + j) * c.ldk + (i64)kv * c.D + lane + kWave * e, ak[e]);
+            if (dV != nullptr) store_elem(dV + ((i64)n * c.Tk + j) * c.ldv + (i64)kv * c.D + lane + kWave * e, av[e]);
         }
 }
 

@@ -109,38 +109,89 @@ struct Tile {
                 acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), acc, 0, 0, 0);
         }
     }
-    // acc[block of 32 values][.] += sum over the 32 rows from r0 on of tile[row][value] * w[row]
-    static __device__ __forceinline__ void mma_columns(const char *L, int r0, const f32x16_t &w, f32x16_t (&acc)[DB], int lane)
+    // The products below are given by what their steps read, take and add to.  LDS reads run ahead of the matrix instructions that
+    // take them, kept there by scheduling barriers that neither may cross: left to itself the compiler keeps registers low by a
+    // read right before each, whose latency the wave then waits for (two prompts of 4096, 32 and 8 heads of 128: 325 us).
+    static __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }
+
+    // acc(i) += read(i, ks) x operand(i, ks) over all k-steps, for COUNT products side by side
+    template <int COUNT, typename Read, typename Operand, typename Acc>
+    static __device__ __forceinline__ void products(Read &&read, Operand &&operand, Acc &&acc)
+    {
+        constexpr int AHEAD = KS < 2 ? KS : 2, BUFS = AHEAD + 1;
+        u32x4_t f[BUFS][COUNT];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) f[k][i] = read(i, k);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            if (ks + AHEAD < KS)
+#pragma unroll
+                for (int i = 0; i < COUNT; ++i) f[(ks + AHEAD) % BUFS][i] = read(i, ks + AHEAD);
+            keep_order();
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) mma(f[ks % BUFS][i], operand(i, ks), acc(i));
+            keep_order();
+        }
+    }
+
+    // acc(i)[block of 32 values][.] += sum over 32 rows r of tile(i)[r][value] * w(i)[r], for COUNT blocks of rows one after
+    // another; tile(i): where the block starts (a multiple of 32 rows of a tile)
+    template <int COUNT, typename At, typename W, typename Acc>
+    static __device__ __forceinline__ void columns(At &&tile, W &&w, Acc &&acc, int lane)
     {
         const int h = lane >> 5;
         if constexpr (BF16) {
             const int s = lane & 15, g = (lane >> 4) & 1;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                bf16x8_t b;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) b[e] = (__bf16)w[8 * c + e];
+            const auto load = [&](int step, bf16x8_t (&a)[DB]) {
+                const char *L = tile(step >> 1);
+                const int t = 16 * (step & 1) + 4 * h + (s >> 2);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
-                    const int t = r0 + 16 * c + 4 * h + (s >> 2);
                     const int q = 4 * d + 2 * g + ((s & 3) >> 1), in = 8 * (s & 1);
                     const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(L + t * RB + 16 * (q ^ swz(t)) + in));
                     const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                         (lds_i16x4_t *)(L + (t + 8) * RB + 16 * (q ^ swz(t + 8)) + in));
-                    const i16x8_t a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), b, acc[d], 0, 0, 0);
+                    a[d] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                 }
+            };
+            bf16x8_t a[2][DB];
+            load(0, a[0]);
+#pragma unroll
+            for (int step = 0; step < 2 * COUNT; ++step) {
+                if (step + 1 < 2 * COUNT) load(step + 1, a[(step + 1) & 1]);
+                bf16x8_t b;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) b[e] = (__bf16)w(step >> 1)[8 * (step & 1) + e];
+                keep_order();
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    acc(step >> 1)[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[step & 1][d], b, acc(step >> 1)[d], 0, 0, 0);
+                keep_order();
             }
         } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int t = r0 + 8 * (r >> 2) + 4 * h + (r & 3);
+            const auto load = [&](int step, float (&a)[DB]) {
+                const char *L = tile(step >> 4);
+                const int r = step & 15, t = 8 * (r >> 2) + 4 * h + (r & 3);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     const int v = 32 * d + (lane & 31);
-                    const float a = *reinterpret_cast<const float *>(L + t * RB + 16 * ((v >> 2) ^ swz(t)) + 4 * (v & 3));
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], acc[d], 0, 0, 0);
+                    a[d] = *reinterpret_cast<const float *>(L + t * RB + 16 * ((v >> 2) ^ swz(t)) + 4 * (v & 3));
                 }
+            };
+            float a[3][DB];
+            load(0, a[0]);
+            load(1, a[1]);
+#pragma unroll
+            for (int step = 0; step < 16 * COUNT; ++step) {
+                if (step + 2 < 16 * COUNT) load(step + 2, a[(step + 2) % 3]);
+                keep_order();
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    acc(step >> 4)[d] =
+                        __builtin_amdgcn_mfma_f32_32x32x2f32(a[step % 3][d], w(step >> 4)[step & 15], acc(step >> 4)[d], 0, 0, 0);
+                keep_order();
             }
         }
     }
@@ -179,18 +230,30 @@ struct Tile {
     }
 };
 
-// Brings R rows of a tile to LDS with NW waves.
+// Brings R rows of a tile to LDS with NW waves: places are formed once, and again only for a tile that ends early.
 template <typename TL, typename T, int R, int NW, bool VEC>
 struct Stager {
     static constexpr int LOADS = R * TL::RB / 1024 / NW;
     static_assert(LOADS * NW * 1024 == R * TL::RB, "stage split");
+    // 16 rows on, a place is the same but for the rows: PERIOD places, the others by the base
+    static constexpr bool WHOLE = 64 * NW % TL::PIECES == 0;
+    static constexpr int STEP = WHOLE ? 64 * NW / TL::PIECES : 1;        // rows from one load to the next
+    static constexpr int EVERY = !WHOLE ? LOADS : STEP % 16 == 0 ? 1 : 16 % STEP == 0 ? 16 / STEP : LOADS;
+    static constexpr int PERIOD = EVERY < LOADS ? EVERY : LOADS;
 
-    uint32_t ld_bytes;
+    uint32_t ld_bytes, off[VEC ? PERIOD : 1];
     int D, wave, lane;
 
     __device__ __forceinline__ Stager(i64 ld, int D_, int wave_, int lane_)
         : ld_bytes((uint32_t)(ld * sizeof(T))), D(D_), wave(wave_), lane(lane_)
     {
+        if constexpr (VEC)
+#pragma unroll
+            for (int k = 0; k < PERIOD; ++k) {
+                int row, q;
+                place(k, row, q);
+                off[k] = (uint32_t)row * ld_bytes + byte(q);
+            }
     }
     __device__ __forceinline__ void place(int k, int &row, int &piece) const
     {
@@ -198,17 +261,26 @@ struct Stager {
         row = at / TL::PIECES;
         piece = (at - row * TL::PIECES) ^ TL::swz(row);
     }
+    __device__ __forceinline__ uint32_t byte(int q) const { return 16u * (uint32_t)(q * TL::N < D ? q : 0); }
     // rows behind `left` read the last of them (their weights are zeros)
     __device__ __forceinline__ void issue(const T *base, int left, uint32_t lds, char *generic) const
     {
+        if constexpr (VEC) {
+            if (left >= R) {
+#pragma unroll
+                for (int k = 0; k < LOADS; ++k)
+                    dma16_off(reinterpret_cast<const char *>(base) + (i64)(k / PERIOD * PERIOD * STEP) * ld_bytes, off[k % PERIOD],
+                              lds + 1024u * (uint32_t)(wave + NW * k));
+                return;
+            }
+        }
 #pragma unroll
         for (int k = 0; k < LOADS; ++k) {
             int row, q;
             place(k, row, q);
             const int r = row < left ? row : left - 1;
             if constexpr (VEC) {
-                const int c = q * TL::N < D ? q : 0;
-                dma16_off(base, (uint32_t)r * ld_bytes + 16u * (uint32_t)c, lds + 1024u * (uint32_t)(wave + NW * k));
+                dma16_off(base, (uint32_t)r * ld_bytes + byte(q), lds + 1024u * (uint32_t)(wave + NW * k));
             } else {
                 const T *p = reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + (i64)r * ld_bytes);
                 *reinterpret_cast<u32x4_t *>(generic + 1024 * (wave + NW * k) + 16 * lane) = TL::piece(p, q * TL::N, D);
@@ -337,7 +409,8 @@ __device__ __forceinline__ RowSpan span_of(const Sample &s, int G, int M, int r0
     return b;
 }
 
-enum { kSkip = 0, kPartial = 1, kFull = 2 };
+// kDocs: partial, and documents have to be compared
+enum { kSkip = 0, kPartial = 1, kFull = 2, kDocs = 3 };
 
 // keys [k0, k1) against the span; kd0, kd1: the documents' range of those below L
 __device__ __forceinline__ int meet(const Sample &s, const RowSpan &b, int k0, int k1, int kd0, int kd1)
@@ -346,7 +419,7 @@ __device__ __forceinline__ int meet(const Sample &s, const RowSpan &b, int k0, i
     bool full = b.all && k1 <= s.L && (!s.causal || k1 - 1 <= b.pmin || k1 <= s.prefix);
     if (s.docs != nullptr) {
         if (kd1 < 0 || b.dmax < 0 || kd1 < b.dmin || kd0 > b.dmax) return kSkip;
-        full = full && kd0 == kd1 && b.dmin == b.dmax && kd0 == b.dmin;
+        if (kd0 != kd1 || b.dmin != b.dmax) return kDocs;
     }
     return full ? kFull : kPartial;
 }
