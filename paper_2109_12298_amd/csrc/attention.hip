@@ -88,5 +88,5 @@ extern "C" dp_status dp_attention_backward(const dp_attention *a, const void *Q,
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
     const Call c = call_of(*a, Q, K, V);
     if (a->D > kTileD) return rows_backward(c, (dp_dtype)a->dt, O, lse, dO, dQ, dK, dV, stream);
-    return tiles_backward(c, (dp_dtype)a->dt, {O, dO, lse, dQ, dK, dV, nullptr, nullptr, 0, false, false}, ws, stream);
+    return tiles_backward(c, (dp_dtype)a->dt, {O, dO, lse, dQ, dK, dV}, ws, stream);
 }

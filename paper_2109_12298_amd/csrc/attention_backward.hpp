@@ -12,7 +12,9 @@ struct Grads {
     void *dQ, *dK, *dV;
     float *row_lse, *row_delta;      // [N][Hq][pad]: lse in units of ln 2 (+inf: the query sees nothing), dO.O
     int pad;                         // queries, rounded up to 64
+    float *part;                     // [splits][N][Hk][Tk][2][D]: sums for dK and dV
     bool small_q, small_k;           // 32 rows (keys) a workgroup instead of 128
+    int splits;                      // workgroups over which a block of keys' queries are split (small_k)
 };
 
 size_t tiles_backward_workspace(const dp_attention &a);

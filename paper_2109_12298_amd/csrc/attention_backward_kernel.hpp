@@ -2,11 +2,11 @@
 //   dV_j = sum_i p_ij dO_i,  e_ij = p_ij (dO_i.V_j - delta_i) (1 - tanh^2),
 //   dQ_i = scale sum_j e_ij K_j,  dK_j = scale sum_i e_ij Q_i.
 //
-// Three launches: lse and delta of every query; dQ, by blocks of rows over
-// tiles of keys, as the forward pass; dK and dV, by blocks of keys over tiles
-// of queries.  Scores and dO.V are formed in both (seven products where five
-// would do), so that every sum belongs to one workgroup: no atomics, no partial
-// sums in memory, the same bits every run, and a key head's sum over its query
+// Two launches: dQ (with lse and delta of every query, which the other reads), by
+// blocks of rows over tiles of keys, as the forward pass; dK and dV, by blocks of
+// keys over tiles of queries.  Scores and dO.V are formed in both (seven products
+// where five would do), so that every sum belongs to one workgroup: no atomics, no
+// partial sums in memory, the same bits every run, and a key head's sum over its query
 // heads is one more loop.
 //
 // dQ forms scores as keys x rows and dK, dV as rows x keys, so that p and e are
@@ -14,7 +14,9 @@
 // registers they were formed in (attention_tile.hpp).  Blocks of 128 rows or
 // keys share tiles, two stages deep, where there are blocks enough to fill the
 // card; else 32 are one workgroup whose waves take different tiles and whose
-// sums are added in wave order.
+// sums are added in wave order; few blocks of keys have their queries split over
+// workgroups as well, and the splits' sums are added by a launch of their own (500
+// queries, 6 and 2 heads of 48, fp32: 96 blocks 70 us).
 //
 // As in the forward pass, a block whose sums are not finite is formed again row
 // by row, over visible pairs only.
@@ -31,7 +33,6 @@ namespace attn {
 namespace {
 
 constexpr int kGroup = 1024;             // tiles in a list
-constexpr i64 kMaxGrid = i64(1) << 22;   // a dimension of a grid holds fewer than 2^32 threads
 
 template <typename T, int DP, bool SMALL>
 struct Shape {
@@ -45,48 +46,6 @@ struct Shape {
     static constexpr int STAGES = (SMALL ? NW : 1) * 2 * STAGE, OUTPUT = NW * 32 * OUT_ROW;
     static constexpr int LDS = STAGES > OUTPUT ? STAGES : OUTPUT;
 };
-
-// ---------------------------------------------------------------------------
-// lse and delta of every query: 16 lanes a query
-// ---------------------------------------------------------------------------
-template <typename T>
-__global__ __launch_bounds__(256) void row_info_kernel(Call c, Grads gr, bool vec)
-{
-    constexpr int N = 16 / sizeof(T);
-    const i64 per = (i64)c.Hq * gr.pad;
-    const int sub = threadIdx.x & 15;
-    for (i64 q = (i64)blockIdx.x * 16 + threadIdx.x / 16; q < (i64)c.N * per; q += (i64)gridDim.x * 16) {
-        const int n = (int)(q / per);
-        const i64 at = q - n * per;
-        // heads fastest, so that neighbours in memory are read together
-        const int i = (int)(at / c.Hq), h = (int)(at - (i64)i * c.Hq);
-        const i64 to = ((i64)n * c.Hq + h) * gr.pad + i;
-        float lse = INFINITY, delta = 0.0f;
-        const Sample s(c, n);
-        const int p = s.first + i;
-        if (i < c.Tq && p >= 0 && p < s.L) {
-            const i64 from = ((i64)n * c.Tq + i) * c.ldo + (i64)h * c.D;
-            const T *o = (const T *)gr.O + from, *d = (const T *)gr.dO + from;
-            const float l = gr.lse[((i64)n * c.Hq + h) * c.Tq + i];
-            lse = l == -INFINITY ? INFINITY : l * kLog2e;
-            for (int k = sub * N; k < c.D; k += 16 * N) {
-                if (vec) {
-                    const u32x4_t a = *reinterpret_cast<const u32x4_t *>(o + k), b = *reinterpret_cast<const u32x4_t *>(d + k);
-                    const T *x = reinterpret_cast<const T *>(&a), *y = reinterpret_cast<const T *>(&b);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) delta += load_elem<T>(x, e) * load_elem<T>(y, e);
-                } else {
-                    for (int e = 0; e < N && k + e < c.D; ++e) delta += load_elem<T>(o, k + e) * load_elem<T>(d, k + e);
-                }
-            }
-        }
-        for (int off = 8; off >= 1; off >>= 1) delta += __shfl_xor(delta, off, 16);
-        if (sub == 0) {
-            gr.row_lse[to] = lse;
-            gr.row_delta[to] = lse == INFINITY ? 0.0f : delta;
-        }
-    }
-}
 
 // Ordered list of the tiles [t0, t1) that classify() does not skip: entries (tile - t0) << 2 | class; returns their number.
 // Every thread of the workgroup takes part.
@@ -185,7 +144,7 @@ __device__ __forceinline__ bool put_block(char *smem, f32x16_t (&acc)[Tile<T, DP
         __syncthreads();
         for (int at = threadIdx.x; at < 32 * (DP / 4); at += S::THREADS) {
             const int row = at / (DP / 4), d = 4 * (at - row * (DP / 4));
-            T *o = d < D ? to(row) : nullptr;
+            auto *o = d < D ? to(row) : nullptr;
             if (o == nullptr) continue;
             float v[4] = {};
 #pragma unroll
@@ -252,7 +211,22 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     u32x4_t qf[KS], df[KS];
     TL::load_row((const T *)c.Q + row * c.ldq + (i64)head * c.D, c.D, row_ok, VEC, lane, qf);
     TL::load_row((const T *)gr.dO + row * c.ldo + (i64)head * c.D, c.D, row_ok, VEC, lane, df);
-    const float lse2 = row_ok ? gr.row_lse[info] : INFINITY, delta = row_ok ? gr.row_delta[info] : 0.0f;
+    // lse in units of ln 2 (+inf where the query sees nothing: its weights are then 0) and delta, which dK and dV's launch reads
+    float lse2 = INFINITY, delta = 0.0f;
+    {
+        u32x4_t of[KS];
+        TL::load_row((const T *)gr.O + row * c.ldo + (i64)head * c.D, c.D, row_ok, VEC, lane, of);
+        const float l = gr.lse[((i64)n * c.Hq + head) * c.Tq + (row_ok ? i : 0)];
+        if (seeing && l != -INFINITY) lse2 = l * kLog2e;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) delta += TL::dot(of[ks], df[ks]);
+        delta += other_half(delta);
+        if (lse2 == INFINITY) delta = 0.0f;
+        if (row_ok && h == 0 && (!SMALL || wave == 0)) {
+            gr.row_lse[info] = lse2;
+            gr.row_delta[info] = delta;
+        }
+    }
     const Scores<T, MOD> score(c);
     const float slope2 = (MOD & kSlope) != 0 && c.slopes != nullptr ? c.slopes[head] * kLog2e : 0.0f;
 
@@ -373,15 +347,13 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
 // ---------------------------------------------------------------------------
 // dK and dV
 // ---------------------------------------------------------------------------
-// SUMS: which of the two a launch forms.  Both in one take sums and operands of 260 and more registers a lane where rows are 192
-// bytes or longer, so one wave per SIMD, which waits half of its time (8192 causal queries in documents, 32 and 8 heads of 128,
-// capped scores: 2515 us); each in a launch of its own has two, for one product more.
-enum { kSumV = 1, kSumK = 2 };
-
-template <typename T, int DP, bool VEC, int MOD, bool SMALL, int SUMS>
-__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, DP>::RB > (SUMS == 3 ? 128 : 256) ? 1 : 2)) void key_kernel(Call c, Grads gr, bool vec_k, bool vec_v)
+// (Rows of 192 bytes or longer leave one wave per SIMD, by sums and operands of 260 registers and more.  8192 causal queries in
+// documents, 32 and 8 heads of 128, capped scores: 1717 us; dV and dK in launches of their own, two waves per SIMD and one product
+// more, 813 + 1033; V's operands in LDS, two waves and some of K's in scratch memory, 2297.)
+template <typename T, int DP, bool VEC, int MOD, bool SMALL>
+__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, DP>::RB > 128 ? 1 : 2)) void key_kernel(
+    Call c, Grads gr, bool vec_k, bool vec_v)
 {
-    constexpr bool SUM_K = (SUMS & kSumK) != 0, SUM_V = (SUMS & kSumV) != 0;
     typedef Shape<T, DP, SMALL> S;
     typedef Tile<T, DP> TL;
     constexpr int BN = S::BN, FN = S::FN, DB = TL::DB, KS = TL::KS, NW = S::NW;
@@ -394,7 +366,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int heads = c.N * c.Hk;
     // first keys first: with a causal mask they have most queries
-    const int nk = (int)blockIdx.x % heads, tk = (int)blockIdx.x / heads;
+    const int split = SMALL ? (int)blockIdx.x % gr.splits : 0, at_block = SMALL ? (int)blockIdx.x / gr.splits : (int)blockIdx.x;
+    const int nk = at_block % heads, tk = at_block / heads;
     const int n = nk / c.Hk, kv = nk - n * c.Hk;
     const Sample smp(c, n);
     const int j0 = tk * S::BR, jw = SMALL ? j0 : j0 + 32 * wave;
@@ -408,7 +381,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const i64 krow = (i64)n * c.Tk + (key_ok ? j : 0);
     u32x4_t kf[KS], vf[KS];
     TL::load_row((const T *)c.K + krow * c.ldk + (i64)kv * c.D, c.D, key_ok, VEC, lane, kf);
-    if constexpr (SUM_K) TL::load_row((const T *)c.V + krow * c.ldv + (i64)kv * c.D, c.D, key_ok, VEC, lane, vf);
+    TL::load_row((const T *)c.V + krow * c.ldv + (i64)kv * c.D, c.D, key_ok, VEC, lane, vf);
     // queries at positions from .. L - 1 see it
     const int from = !key_ok ? 1 << 30 : !smp.causal || j < smp.prefix ? 0 : j;
     const int doc = key_ok && smp.docs != nullptr ? smp.docs[j] : -1;
@@ -451,7 +424,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             f32x16_t s, e;
 #pragma unroll
             for (int k = 0; k < 16; ++k) s[k] = e[k] = 0.0f;
-            TL::template products<SUM_K ? 2 : 1>([&](int i, int ks) { return TL::rows(i == 0 ? LQ : LD, 32 * x, ks, lane); },
+            TL::template products<2>([&](int i, int ks) { return TL::rows(i == 0 ? LQ : LD, 32 * x, ks, lane); },
                                                  [&](int i, int ks) -> const u32x4_t & { return i == 0 ? kf[ks] : vf[ks]; },
                                                  [&](int i) -> f32x16_t & { return i == 0 ? s : e; });
             const auto place = [&](int k) { return 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
@@ -467,10 +440,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                         float bend;
                         s[k] = __builtin_amdgcn_exp2f(score.template of<decltype(is_near)::value>(
                             s[k], lse2[w], slope2, __builtin_fabsf((float)(smp.first + q0 + place(k) - j)), bend));
-                        if constexpr (SUM_K) {
-                            e[k] = s[k] * (e[k] - delta[w]);
-                            if constexpr ((MOD & kCap) != 0) e[k] *= bend;
-                        }
+                        e[k] = s[k] * (e[k] - delta[w]);
+                        if constexpr ((MOD & kCap) != 0) e[k] *= bend;
                     }
                 }
             };
@@ -500,10 +471,9 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 }
             }
             const char *LX = L + 32 * x * TL::RB;
-            TL::template columns<SUM_K && SUM_V ? 2 : 1>(
-                [&](int i) { return SUM_V && i == 0 ? LX + S::HALF : LX; },
-                [&](int i) -> const f32x16_t & { return SUM_V && i == 0 ? s : e; },
-                [&](int i) -> Sums & { return SUM_V && i == 0 ? av : ak; }, lane);
+            TL::template columns<2>([&](int i) { return i == 0 ? LX + S::HALF : LX; },
+                                    [&](int i) -> const f32x16_t & { return i == 0 ? s : e; },
+                                    [&](int i) -> Sums & { return i == 0 ? av : ak; }, lane);
         }
     };
 
@@ -519,8 +489,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         int count = stop - base;
         if (docs)
             count = tile_list<S::THREADS>(base, stop, list, cls_of, counts, [&](int t) { return class_of(t, true); });
-        // the heads one after another, each over the tiles
-        const int all = count * c.G;
+        // the heads one after another, each over the tiles; this split's part of them
+        const int whole = count * c.G, all = SMALL ? (int)((i64)whole * (split + 1) / gr.splits) : whole;
         const auto entry = [&](int k, int &t, int &g, int &cls) {
             g = k / count;
             if (docs) {
@@ -534,7 +504,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         };
         int t, g, cls;
         constexpr int STEP = SMALL ? NW : 1;
-        const int k0 = SMALL ? wave : 0;
+        const int k0 = SMALL ? (int)((i64)whole * split / gr.splits) + wave : 0;
         if (k0 < all) {
             entry(k0, t, g, cls);
             issue(t, g, 0);
@@ -556,19 +526,57 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         base = stop;
     }
 
+    if constexpr (SMALL)
+        if (gr.splits > 1) {
+            const auto part_of = [&](int which, int k) -> float * {
+                return jw + k < c.Tk ? gr.part + (((i64)split * heads + nk) * c.Tk + jw + k) * 2 * c.D + which * c.D : nullptr;
+            };
+            put_block<T, DP, S, SMALL>(smem, ak, c.scale, c.D, false, lane, wave, [&](int k) { return part_of(0, k); });
+            put_block<T, DP, S, SMALL>(smem, av, 1.0f, c.D, false, lane, wave, [&](int k) { return part_of(1, k); });
+            return;
+        }
     const auto row_of = [&](void *p, i64 ld, int k) -> T * {
         return jw + k < c.Tk ? (T *)p + ((i64)n * c.Tk + jw + k) * ld + (i64)kv * c.D : nullptr;
     };
-    bool bad = false;
-    if constexpr (SUM_K)
-        bad |= put_block<T, DP, S, SMALL>(smem, ak, c.scale, c.D, vec_k, lane, wave, [&](int k) { return row_of(gr.dK, c.ldk, k); });
-    if constexpr (SUM_V)
-        bad |= put_block<T, DP, S, SMALL>(smem, av, 1.0f, c.D, vec_v, lane, wave, [&](int k) { return row_of(gr.dV, c.ldv, k); });
+    bool bad = put_block<T, DP, S, SMALL>(smem, ak, c.scale, c.D, vec_k, lane, wave, [&](int k) { return row_of(gr.dK, c.ldk, k); });
+    bad |= put_block<T, DP, S, SMALL>(smem, av, 1.0f, c.D, vec_v, lane, wave, [&](int k) { return row_of(gr.dV, c.ldv, k); });
     wait_loads();                                        // the stores above come before those below
     if (SMALL ? __syncthreads_or(bad) : __any(bad))
         for (int k = SMALL ? wave : 0; k < 32 && jw + k < c.Tk; k += SMALL ? NW : 1)
-            backward_key_row<T>(c, n, kv, jw + k, (const T *)gr.O, gr.lse, (const T *)gr.dO, SUM_K ? (T *)gr.dK : nullptr,
-                                SUM_V ? (T *)gr.dV : nullptr);
+            backward_key_row<T>(c, n, kv, jw + k, (const T *)gr.O, gr.lse, (const T *)gr.dO, (T *)gr.dK, (T *)gr.dV);
+}
+
+// A wave adds a key's sums over the splits, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void key_join_kernel(Call c, Grads gr)
+{
+    constexpr int PER = kTileD / kWave;
+    const i64 rows = (i64)c.N * c.Hk * c.Tk, r = (i64)blockIdx.x * 4 + threadIdx.x / kWave;
+    if (r >= rows) return;
+    const int lane = threadIdx.x & (kWave - 1), nk = (int)(r / c.Tk), j = (int)(r - (i64)nk * c.Tk), n = nk / c.Hk, kv = nk - n * c.Hk;
+    float v[2][PER] = {};
+    bool bad = false;
+#pragma unroll 4
+    for (int s = 0; s < gr.splits; ++s)
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (lane + kWave * k < c.D) v[w][k] += gr.part[((s * rows + r) * 2 + w) * c.D + lane + kWave * k];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int k = 0; k < PER; ++k) bad = bad || not_finite(v[w][k]);
+    if (__any(bad)) {
+        backward_key_row<T>(c, n, kv, j, (const T *)gr.O, gr.lse, (const T *)gr.dO, (T *)gr.dK, (T *)gr.dV);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+        if (lane + kWave * k < c.D) {
+            store_elem((T *)gr.dK + ((i64)n * c.Tk + j) * c.ldk + (i64)kv * c.D + lane + kWave * k, v[0][k]);
+            store_elem((T *)gr.dV + ((i64)n * c.Tk + j) * c.ldv + (i64)kv * c.D + lane + kWave * k, v[1][k]);
+        }
 }
 
 template <typename T, int DP, bool VEC, int MOD>
@@ -587,16 +595,12 @@ void launch(const Call &c, const Grads &g, hipStream_t stream)
                 c, g, tiles, wide(g.dQ, c.ldq));
     }
     if (c.Tk > 0) {
-        const unsigned blocks = (unsigned)(heads * ceil_div(c.Tk, g.small_k ? 32 : 128));
+        const unsigned blocks = (unsigned)(heads * ceil_div(c.Tk, g.small_k ? 32 : 128) * (g.small_k ? g.splits : 1));
         const bool vk = wide(g.dK, c.ldk), vv = wide(g.dV, c.ldv);
-        if (g.small_k) {
-            key_kernel<T, DP, VEC, MOD, true, kSumK | kSumV><<<blocks, Shape<T, DP, true>::THREADS, 0, stream>>>(c, g, vk, vv);
-        } else if constexpr (sizeof(T) == 2 && Tile<T, DP>::RB > 1280) {
-            key_kernel<T, DP, VEC, MOD, false, kSumV><<<blocks, Shape<T, DP, false>::THREADS, 0, stream>>>(c, g, vk, vv);
-            key_kernel<T, DP, VEC, MOD, false, kSumK><<<blocks, Shape<T, DP, false>::THREADS, 0, stream>>>(c, g, vk, vv);
-        } else {
-            key_kernel<T, DP, VEC, MOD, false, kSumK | kSumV><<<blocks, Shape<T, DP, false>::THREADS, 0, stream>>>(c, g, vk, vv);
-        }
+        if (g.small_k) key_kernel<T, DP, VEC, MOD, true><<<blocks, Shape<T, DP, true>::THREADS, 0, stream>>>(c, g, vk, vv);
+        else key_kernel<T, DP, VEC, MOD, false><<<blocks, Shape<T, DP, false>::THREADS, 0, stream>>>(c, g, vk, vv);
+        if (g.small_k && g.splits > 1)
+            key_join_kernel<T><<<(unsigned)ceil_div(heads * c.Tk, 4), 256, 0, stream>>>(c, g);
     }
 }
 
@@ -605,7 +609,7 @@ void by_kind(const Call &c, const Grads &g, hipStream_t stream)
 {
     constexpr int N = 16 / sizeof(T);
     const bool vec = c.D % N == 0 && c.ldq % N == 0 && c.ldk % N == 0 && c.ldv % N == 0 && c.ldo % N == 0 && aligned(c.Q, 16) &&
-                     aligned(c.K, 16) && aligned(c.V, 16) && aligned(g.dO, 16);
+                     aligned(c.K, 16) && aligned(c.V, 16) && aligned(g.O, 16) && aligned(g.dO, 16);
     const int mod = c.scale <= 0.0f ? kBoth : (c.cap > 0.0f ? kCap : kPlain) | (c.slopes != nullptr ? kSlope : kPlain);
     if (!vec) launch<T, DP, false, kBoth>(c, g, stream);
     else if (mod == kPlain) launch<T, DP, true, kPlain>(c, g, stream);
@@ -617,10 +621,6 @@ void by_kind(const Call &c, const Grads &g, hipStream_t stream)
 template <typename T>
 dp_status tiles_of(const Call &c, const Grads &g, hipStream_t stream)
 {
-    constexpr int N = 16 / sizeof(T);
-    const i64 queries = (i64)c.N * c.Hq * g.pad;
-    const bool vec = c.D % N == 0 && c.ldo % N == 0 && aligned(g.O, 16) && aligned(g.dO, 16);
-    if (queries > 0) row_info_kernel<T><<<(unsigned)(ceil_div(queries, 16) < kMaxGrid ? ceil_div(queries, 16) : kMaxGrid), 256, 0, stream>>>(c, g, vec);
     if (c.D <= 32) by_kind<T, 32>(c, g, stream);
     else if (c.D <= 64) by_kind<T, 64>(c, g, stream);
     else if (c.D <= 96) by_kind<T, 96>(c, g, stream);

@@ -98,6 +98,21 @@ struct Tile {
         const int r = r0 + (lane & 31);
         return *reinterpret_cast<const u32x4_t *>(L + r * RB + 16 * ((2 * ks + (lane >> 5)) ^ swz(r)));
     }
+    // sum of the products of two pieces' values
+    static __device__ __forceinline__ float dot(const u32x4_t &a, const u32x4_t &b)
+    {
+        float v = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (BF16) {
+                v = __builtin_fmaf(__uint_as_float(a[e] << 16), __uint_as_float(b[e] << 16), v);
+                v = __builtin_fmaf(__uint_as_float(a[e] & 0xffff0000u), __uint_as_float(b[e] & 0xffff0000u), v);
+            } else {
+                v = __builtin_fmaf(__uint_as_float(a[e]), __uint_as_float(b[e]), v);
+            }
+        }
+        return v;
+    }
     static __device__ __forceinline__ void mma(const u32x4_t &a, const u32x4_t &b, f32x16_t &acc)
     {
         if constexpr (BF16) {
@@ -115,10 +130,10 @@ struct Tile {
     static __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }
 
     // acc(i) += read(i, ks) x operand(i, ks) over all k-steps, for COUNT products side by side
-    template <int COUNT, typename Read, typename Operand, typename Acc>
+    template <int COUNT, int STEPS_AHEAD = 2, typename Read, typename Operand, typename Acc>
     static __device__ __forceinline__ void products(Read &&read, Operand &&operand, Acc &&acc)
     {
-        constexpr int AHEAD = KS < 2 ? KS : 2, BUFS = AHEAD + 1;
+        constexpr int AHEAD = KS < STEPS_AHEAD ? KS : STEPS_AHEAD, BUFS = AHEAD + 1;
         u32x4_t f[BUFS][COUNT];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k)
@@ -138,7 +153,7 @@ struct Tile {
 
     // acc(i)[block of 32 values][.] += sum over 32 rows r of tile(i)[r][value] * w(i)[r], for COUNT blocks of rows one after
     // another; tile(i): where the block starts (a multiple of 32 rows of a tile)
-    template <int COUNT, typename At, typename W, typename Acc>
+    template <int COUNT, bool PACK_FIRST = false, typename At, typename W, typename Acc>
     static __device__ __forceinline__ void columns(At &&tile, W &&w, Acc &&acc, int lane)
     {
         const int h = lane >> 5;
@@ -156,18 +171,20 @@ struct Tile {
                     a[d] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                 }
             };
-            bf16x8_t a[2][DB];
+            bf16x8_t a[2][DB], b[2 * COUNT];
+#pragma unroll
+            for (int step = 0; step < 2 * COUNT; ++step)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) b[step][e] = (__bf16)w(step >> 1)[8 * (step & 1) + e];
+            if constexpr (PACK_FIRST) __builtin_amdgcn_sched_barrier(0);
             load(0, a[0]);
 #pragma unroll
             for (int step = 0; step < 2 * COUNT; ++step) {
                 if (step + 1 < 2 * COUNT) load(step + 1, a[(step + 1) & 1]);
-                bf16x8_t b;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) b[e] = (__bf16)w(step >> 1)[8 * (step & 1) + e];
                 keep_order();
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
-                    acc(step >> 1)[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[step & 1][d], b, acc(step >> 1)[d], 0, 0, 0);
+                    acc(step >> 1)[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[step & 1][d], b[step], acc(step >> 1)[d], 0, 0, 0);
                 keep_order();
             }
         } else {

@@ -67,32 +67,49 @@ struct Args {
     int32_t *status;
 };
 
-// maximum (a NaN is passed over here and turns the sums to NaN) and sum over the
-// workgroup; `red` is __shared__ float[16], every thread gets the result
+// Maxima (a NaN is passed over here and turns the sums to NaN) and sums over the
+// workgroup, several at once, as each costs a barrier; every thread gets the results.
 __device__ __forceinline__ float wave_max(float v)
 {
     for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, kWave));
     return v;
 }
-template <int THREADS>
-__device__ __forceinline__ float block_max(float v, float *red)
+// `red` (N values a wave) is not used again before a barrier
+template <int THREADS, int N>
+__device__ __forceinline__ void block_max(float (&v)[N], float (*red)[16])
 {
-    v = wave_max(v);
-    if constexpr (THREADS > kWave) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = red[0];
 #pragma unroll
-        for (int w = 1; w < THREADS / kWave; ++w) v = fmaxf(v, red[w]);
+    for (int i = 0; i < N; ++i) v[i] = wave_max(v[i]);
+    if constexpr (THREADS > kWave) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[i][threadIdx.x >> 6] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = red[i][0];
+#pragma unroll
+            for (int w = 1; w < THREADS / kWave; ++w) v[i] = fmaxf(v[i], red[i][w]);
+        }
     }
-    return v;
 }
-template <int THREADS>
-__device__ __forceinline__ float sum_of_block(float v, float *red)
+template <int THREADS, int N>
+__device__ __forceinline__ void block_add(float (&v)[N], float (*red)[16])
 {
-    if constexpr (THREADS == kWave) return wave_sum(v);
-    return block_sum(v, red);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (THREADS > kWave) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[i][threadIdx.x >> 6] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < THREADS / kWave; ++w) v[i] += red[i][w];
+        }
+    }
 }
 
 // NV pieces of a row per thread are held; RESIDENT: they are the whole row.
@@ -101,7 +118,7 @@ template <typename T, int THREADS, int NV, bool RESIDENT, bool HARD>
 __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Args a, T *dZ)
 {
     constexpr int N = 16 / sizeof(T);
-    __shared__ float red[16];
+    __shared__ float red[6][16];                           // two maxima, three sums, the loss
     __shared__ float target[kMaxK];                        // P_k
     __shared__ int32_t target_id[kMaxK];                   // -1: unused
     const i64 V = a.V;
@@ -162,43 +179,20 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
         target[k] = ok ? a.logits[m * a.K + k] : -INFINITY;
         tmax = fmaxf(tmax, target[k]);
     }
-    tmax = block_max<THREADS>(tmax, red);
-    const float tbase = tmax == -INFINITY ? 0.0f : tmax;
-    float tsum = 0.0f;
-    for (int k = tid; k < a.K; k += THREADS)
-        if (target_id[k] >= 0) tsum += expf((target[k] - tbase) * inv_tau);
-    tsum = sum_of_block<THREADS>(tsum, red);
-    const bool soft = a.alpha > 0.0f && tsum != 0.0f;
-    const float ltsum = logf(tsum);
-    int label = -1;
-    if constexpr (HARD) {
-        const int64_t l = a.labels[m];
-        if (l >= V && tid == 0) raise_flag(a.status, DP_FLAG_BAD_INDEX);
-        if (l >= 0 && l < V) label = (int)l;
-    }
-    const bool hard = HARD && label >= 0 && a.alpha < 1.0f;
-    if (!soft && !hard) {                                  // no part of the loss
-        leave_out();
-        return;
-    }
-    const float z_label = hard ? load_elem<T>(z, label) : 0.0f;
-
-    // maximum, then the sums of exponentials
+    // the teacher's and the row's maxima, then the sums of exponentials
     float zmax = one, s_tau = 0.0f, s_1 = 0.0f;
     const auto add = [&](float x, float top) {
         s_tau += __builtin_amdgcn_exp2f((x - top) * c_tau);
         if constexpr (HARD) s_1 += __builtin_amdgcn_exp2f((x - top) * kLog2e);
     };
+    float top = -INFINITY;                                 // !RESIDENT: the maximum that this thread's sums are taken from
     if constexpr (RESIDENT) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (i * THREADS + tid < pieces)
 #pragma unroll
                 for (int e = 0; e < N; ++e) zmax = fmaxf(zmax, elem<T>(v[i], e));
-        zmax = block_max<THREADS>(zmax, red);
     } else {
-        // one reading: a thread's sums follow its own maximum
-        float top = -INFINITY;
         for (int base = 0; base < pieces; base += NV * THREADS) {
             load(base);
             float t = top;
@@ -219,13 +213,18 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
 #pragma unroll
                     for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), b);
         }
-        zmax = block_max<THREADS>(fmaxf(zmax, top), red);
-        if (top != -INFINITY) {
-            s_tau *= __builtin_amdgcn_exp2f((top - zmax) * c_tau);
-            if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f((top - zmax) * kLog2e);
-        }
+        zmax = fmaxf(zmax, top);
     }
-    const float zbase = zmax == -INFINITY ? 0.0f : zmax;
+    float maxima[2] = {tmax, zmax};
+    block_max<THREADS>(maxima, red);
+    const float tbase = maxima[0] == -INFINITY ? 0.0f : maxima[0], zbase = maxima[1] == -INFINITY ? 0.0f : maxima[1];
+    float tsum = 0.0f;
+    for (int k = tid; k < a.K; k += THREADS)
+        if (target_id[k] >= 0) tsum += expf((target[k] - tbase) * inv_tau);
+    if (!RESIDENT && top != -INFINITY) {
+        s_tau *= __builtin_amdgcn_exp2f((top - zbase) * c_tau);
+        if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f((top - zbase) * kLog2e);
+    }
     if (single >= 0) add(one, zbase);
     if constexpr (RESIDENT)
 #pragma unroll
@@ -233,8 +232,27 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
             if (i * THREADS + tid < pieces)
 #pragma unroll
                 for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), zbase);
-    s_tau = sum_of_block<THREADS>(s_tau, red);
-    if constexpr (HARD) s_1 = sum_of_block<THREADS>(s_1, red);
+    float sums[HARD ? 3 : 2] = {tsum, s_tau};
+    if constexpr (HARD) sums[2] = s_1;
+    block_add<THREADS>(sums, red + 2);
+    tsum = sums[0];
+    s_tau = sums[1];
+    if constexpr (HARD) s_1 = sums[2];
+
+    const bool soft = a.alpha > 0.0f && tsum != 0.0f;
+    const float ltsum = logf(tsum);
+    int label = -1;
+    if constexpr (HARD) {
+        const int64_t l = a.labels[m];
+        if (l >= V && tid == 0) raise_flag(a.status, DP_FLAG_BAD_INDEX);
+        if (l >= 0 && l < V) label = (int)l;
+    }
+    const bool hard = HARD && label >= 0 && a.alpha < 1.0f;
+    if (!soft && !hard) {                                  // no part of the loss
+        leave_out();
+        return;
+    }
+    const float z_label = hard ? load_elem<T>(z, label) : 0.0f;
 
     // P in place of the teacher's logits; the loss
     float part = 0.0f;
@@ -250,10 +268,12 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
         }
         target[k] = P;
     }
-    part = sum_of_block<THREADS>(part, red);
+    float parts[1] = {part};
+    if (a.K > kWave) block_add<THREADS>(parts, red + 5);
+    else parts[0] = wave_sum(part);                        // the first wave has all of them
     const float g_soft = soft ? a.alpha : 0.0f, g_hard = hard ? 1.0f - a.alpha : 0.0f;
     if (tid == 0) {
-        float l = g_soft * a.tau * a.tau * part;
+        float l = g_soft * a.tau * a.tau * parts[0];
         if (hard) l += g_hard * (logf(s_1) - (z_label - zbase));
         a.loss[m] = w * l;
     }
