@@ -34,7 +34,7 @@ constexpr int kGroup = 1024;             // tiles in a list
 template <typename T, int DP, bool SMALL>
 struct Shape {
     typedef Tile<T, DP> TL;
-    static constexpr int NW = 4;
+    static constexpr int NW = SMALL && TL::RB >= 384 ? 2 : 4;
     static constexpr int BN = SMALL || sizeof(T) == 4 ? 32 : 64;         // keys in a tile
     static constexpr int BR = SMALL ? 32 : 32 * NW;                      // rows of a workgroup
     static constexpr int FN = BN / 32, THREADS = 64 * NW;

@@ -19,7 +19,7 @@
 namespace dpg {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxK = 1024;
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -147,12 +147,8 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
         }
         if (tid == 0) a.loss[m] = 0.0f;
     };
-    if (w == 0.0f) {
-        leave_out();
-        return;
-    }
-
-    // the row's loads leave first
+    // All loads leave before the first is waited for: the row's, the label's, the teacher's and, behind its ids, the target classes'
+    // own logits (which are read before any store).
     u32x4_t v[NV];
     const auto load = [&](int base) {
 #pragma unroll
@@ -164,26 +160,52 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
             }
         }
     };
+    int64_t wanted = -1;
+    if constexpr (HARD) wanted = a.labels[m];
+    constexpr int PER = (kMaxK + THREADS - 1) / THREADS;
+    int64_t id_of[PER];
+    float logit_of[PER], mine[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = tid + i * THREADS;
+        id_of[i] = k < a.K ? a.ids[m * a.K + k] : -1;
+        logit_of[i] = k < a.K ? a.logits[m * a.K + k] : -INFINITY;
+    }
+    if constexpr (RESIDENT) load(0);
     float one = -INFINITY;
     if (single >= 0) one = load_elem<T>(z, single);
-    if constexpr (RESIDENT) load(0);
-
-    // the teacher's softmax, and the target classes' own logits (before any store)
+    const int label = HARD && wanted >= 0 && wanted < V ? (int)wanted : -1;
+    const bool hard = HARD && label >= 0 && a.alpha < 1.0f;
+    const float z_label = hard ? load_elem<T>(z, label) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mine[i] = id_of[i] >= 0 && id_of[i] < V ? load_elem<T>(z, id_of[i]) : 0.0f;
+    if (w == 0.0f) {
+        leave_out();
+        return;
+    }
     const float inv_tau = 1.0f / a.tau, c_tau = kLog2e * inv_tau;
     float tmax = -INFINITY;
-    for (int k = tid; k < a.K; k += THREADS) {
-        const int64_t id = a.ids[m * a.K + k];
-        const bool ok = id >= 0 && id < V;
-        if (id >= V) raise_flag(a.status, DP_FLAG_BAD_INDEX);
-        target_id[k] = ok ? (int32_t)id : -1;
-        target[k] = ok ? a.logits[m * a.K + k] : -INFINITY;
+    bool bad_id = HARD && tid == 0 && wanted >= V;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = tid + i * THREADS;
+        if (k >= a.K) break;
+        const bool ok = id_of[i] >= 0 && id_of[i] < V;
+        bad_id = bad_id || id_of[i] >= V;
+        target_id[k] = ok ? (int32_t)id_of[i] : -1;
+        target[k] = ok ? logit_of[i] : -INFINITY;
         tmax = fmaxf(tmax, target[k]);
     }
+    if (bad_id) raise_flag(a.status, DP_FLAG_BAD_INDEX);
     // the teacher's and the row's maxima, then the sums of exponentials
     float zmax = one, s_tau = 0.0f, s_1 = 0.0f;
-    const auto add = [&](float x, float top) {
-        s_tau += __builtin_amdgcn_exp2f((x - top) * c_tau);
-        if constexpr (HARD) s_1 += __builtin_amdgcn_exp2f((x - top) * kLog2e);
+    // exp((x - top) / t) as exp2 of one fused product, less a rounded top / t log2 e: its rounding is one factor of all of a row's
+    // exponentials, and so none of a softmax
+    const bool same = a.tau == 1.0f;                       // one exponential serves both
+    const auto add = [&](float x, float base_tau, float base_1) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x, c_tau, -base_tau));
+        s_tau += e;
+        if constexpr (HARD) s_1 += same ? e : __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -base_1));
     };
     float top = -INFINITY;                                 // !RESIDENT: the maximum that this thread's sums are taken from
     if constexpr (RESIDENT) {
@@ -202,16 +224,16 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
 #pragma unroll
                     for (int e = 0; e < N; ++e) t = fmaxf(t, elem<T>(v[i], e));
             if (t > top) {
-                s_tau *= __builtin_amdgcn_exp2f((top - t) * c_tau);
-                if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f((top - t) * kLog2e);
+                s_tau *= __builtin_amdgcn_exp2f(top * c_tau - t * c_tau);
+                if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f(top * kLog2e - t * kLog2e);
                 top = t;
             }
-            const float b = top == -INFINITY ? 0.0f : top;
+            const float b_tau = top == -INFINITY ? 0.0f : top * c_tau, b_1 = top == -INFINITY ? 0.0f : top * kLog2e;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (base + i * THREADS + tid < pieces)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), b);
+                    for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), b_tau, b_1);
         }
         zmax = fmaxf(zmax, top);
     }
@@ -221,17 +243,18 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
     float tsum = 0.0f;
     for (int k = tid; k < a.K; k += THREADS)
         if (target_id[k] >= 0) tsum += expf((target[k] - tbase) * inv_tau);
+    const float b_tau = zbase * c_tau, b_1 = zbase * kLog2e;
     if (!RESIDENT && top != -INFINITY) {
-        s_tau *= __builtin_amdgcn_exp2f((top - zbase) * c_tau);
-        if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f((top - zbase) * kLog2e);
+        s_tau *= __builtin_amdgcn_exp2f(top * c_tau - b_tau);
+        if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f(top * kLog2e - b_1);
     }
-    if (single >= 0) add(one, zbase);
+    if (single >= 0) add(one, b_tau, b_1);
     if constexpr (RESIDENT)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (i * THREADS + tid < pieces)
 #pragma unroll
-                for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), zbase);
+                for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), b_tau, b_1);
     float sums[HARD ? 3 : 2] = {tsum, s_tau};
     if constexpr (HARD) sums[2] = s_1;
     block_add<THREADS>(sums, red + 2);
@@ -241,30 +264,23 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
 
     const bool soft = a.alpha > 0.0f && tsum != 0.0f;
     const float ltsum = logf(tsum);
-    int label = -1;
-    if constexpr (HARD) {
-        const int64_t l = a.labels[m];
-        if (l >= V && tid == 0) raise_flag(a.status, DP_FLAG_BAD_INDEX);
-        if (l >= 0 && l < V) label = (int)l;
-    }
-    const bool hard = HARD && label >= 0 && a.alpha < 1.0f;
     if (!soft && !hard) {                                  // no part of the loss
         leave_out();
         return;
     }
-    const float z_label = hard ? load_elem<T>(z, label) : 0.0f;
 
     // P in place of the teacher's logits; the loss
     float part = 0.0f;
     const float lq = logf(s_tau);
-    for (int k = tid; k < a.K; k += THREADS) {
-        const int32_t id = target_id[k];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = tid + i * THREADS;
+        if (k >= a.K) break;
         float P = 0.0f;
-        if (soft && id >= 0) {
+        if (soft && target_id[k] >= 0) {
             const float lp = (target[k] - tbase) * inv_tau - ltsum;
             P = expf(lp);
-            const float zk = load_elem<T>(z, id);
-            if (P != 0.0f) part += P * (lp - ((zk - zbase) * inv_tau - lq));
+            if (P != 0.0f) part += P * (lp - (kLn2 * __builtin_fmaf(mine[i], c_tau, -b_tau) - lq));
         }
         target[k] = P;
     }
@@ -274,7 +290,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
     const float g_soft = soft ? a.alpha : 0.0f, g_hard = hard ? 1.0f - a.alpha : 0.0f;
     if (tid == 0) {
         float l = g_soft * a.tau * a.tau * parts[0];
-        if (hard) l += g_hard * (logf(s_1) - (z_label - zbase));
+        if (hard) l += g_hard * (logf(s_1) - kLn2 * __builtin_fmaf(z_label, kLog2e, -b_1));
         a.loss[m] = w * l;
     }
     if (dz == nullptr) return;
@@ -282,14 +298,11 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
     // gradient of a class without a target: w a tau q_tau + w (1 - a) q_1
     const float k_tau = soft ? w * g_soft * a.tau / s_tau : 0.0f, k_1 = hard ? w * g_hard / s_1 : 0.0f;
     const auto grad = [&](float x) {
-        float g = k_tau * __builtin_amdgcn_exp2f((x - zbase) * c_tau);
-        if constexpr (HARD) g += k_1 * __builtin_amdgcn_exp2f((x - zbase) * kLog2e);
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x, c_tau, -b_tau));
+        float g = k_tau * e;
+        if constexpr (HARD) g += k_1 * (same ? e : __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -b_1)));
         return g;
     };
-    // the target classes' logits, before the stores (dZ may be Z)
-    float mine[(kMaxK + THREADS - 1) / THREADS];
-    for (int k = tid, i = 0; k < a.K; k += THREADS, ++i)
-        if (target_id[k] >= 0) mine[i] = load_elem<T>(z, target_id[k]);
     __syncthreads();
     for (int base = 0; base < (RESIDENT ? 1 : pieces); base += NV * THREADS) {
         if constexpr (!RESIDENT) load(base);
@@ -310,7 +323,10 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
     __syncthreads();                                       // waits for the stores above
 
     // target classes: an id that occurs twice is written by its first place, with both
-    for (int k = tid, i = 0; k < a.K; k += THREADS, ++i) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = tid + i * THREADS;
+        if (k >= a.K) break;
         const int32_t id = target_id[k];
         if (id < 0) continue;
         float P = 0.0f;
