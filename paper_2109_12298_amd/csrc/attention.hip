@@ -61,7 +61,7 @@ extern "C" dp_status dp_attention_forward(const dp_attention *a, const void *Q, 
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
     const Call c = call_of(*a, Q, K, V);
     if (a->D > kTileD) return rows_forward(c, (dp_dtype)a->dt, O, lse, stream);
-    return tiles_forward(c, (dp_dtype)a->dt, forward_splits(*a), O, lse, ws, stream);
+    return tiles_forward(*a, c, (dp_dtype)a->dt, O, lse, ws, stream);
 }
 
 extern "C" size_t dp_attention_backward_workspace_bytes(const dp_attention *a)
@@ -88,5 +88,5 @@ extern "C" dp_status dp_attention_backward(const dp_attention *a, const void *Q,
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
     const Call c = call_of(*a, Q, K, V);
     if (a->D > kTileD) return rows_backward(c, (dp_dtype)a->dt, O, lse, dO, dQ, dK, dV, stream);
-    return tiles_backward(c, (dp_dtype)a->dt, {O, dO, lse, dQ, dK, dV}, ws, stream);
+    return tiles_backward(*a, c, (dp_dtype)a->dt, {O, dO, lse, dQ, dK, dV}, ws, stream);
 }

@@ -193,7 +193,13 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const int lane = threadIdx.x & 63, li = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int heads = c.N * c.Hk;
-    const int nk = (int)blockIdx.x % heads, tm = tiles_m - 1 - (int)blockIdx.x / heads;
+    int nk = (int)blockIdx.x % heads, tm = tiles_m - 1 - (int)blockIdx.x / heads;
+    if constexpr (!SMALL)
+        if (gr.row_order != nullptr) {
+            const int e = gr.row_order[(int)blockIdx.x / c.Hk], of = e / tiles_m;
+            nk = of * c.Hk + (int)blockIdx.x % c.Hk;
+            tm = e - of * tiles_m;
+        }
     const int n = nk / c.Hk, kv = nk - n * c.Hk;
     const Sample smp(c, n);
     const int M = c.Tq * c.G, r0 = tm * S::BR, rw = SMALL ? r0 : r0 + 32 * wave;
@@ -367,7 +373,13 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const int heads = c.N * c.Hk;
     // first keys first: with a causal mask they have most queries
     const int split = SMALL ? (int)blockIdx.x % gr.splits : 0, at_block = SMALL ? (int)blockIdx.x / gr.splits : (int)blockIdx.x;
-    const int nk = at_block % heads, tk = at_block / heads;
+    int nk = at_block % heads, tk = at_block / heads;
+    if constexpr (!SMALL)
+        if (gr.key_order != nullptr) {
+            const int blocks = (c.Tk + S::BR - 1) / S::BR, e = gr.key_order[at_block / c.Hk], of = e / blocks;
+            nk = of * c.Hk + at_block % c.Hk;
+            tk = e - of * blocks;
+        }
     const int n = nk / c.Hk, kv = nk - n * c.Hk;
     const Sample smp(c, n);
     const int j0 = tk * S::BR, jw = SMALL ? j0 : j0 + 32 * wave;

@@ -1,5 +1,6 @@
 // Attention forward: the choice of shape, and the kernels for bf16.
 #include "attention_forward_kernel.hpp"
+#include "attention_order.hpp"
 
 namespace dpg {
 namespace attn {
@@ -9,6 +10,9 @@ dp_status forward_bf16(const Call &c, const ForwardOut &out, bool small, hipStre
     return tiles_of<uint16_t>(c, out, small, stream);
 }
 
+namespace {
+
+// Workgroups over which a sample's keys are split (1: none; 0: rows are blocks of 128).
 int forward_splits(const dp_attention &a)
 {
     const i64 M = a.Tq * (a.Hq / a.Hk), heads = a.N * a.Hk;
@@ -25,16 +29,23 @@ int forward_splits(const dp_attention &a)
     return (int)(splits < 1 ? 1 : splits);
 }
 
+}  // namespace
+
 size_t tiles_forward_workspace(const dp_attention &a)
 {
     const i64 splits = forward_splits(a);
-    if (splits <= 1) return 0;
-    return sizeof(float) * (size_t)(splits * a.N * a.Hq * a.Tq * (a.D + 2));
+    if (splits == 0) return sizeof(int32_t) * (size_t)row_order_entries(a);
+    return splits == 1 ? 0 : sizeof(float) * (size_t)(splits * a.N * a.Hq * a.Tq * (a.D + 2));
 }
 
-dp_status tiles_forward(const Call &c, dp_dtype dt, int splits, void *O, float *lse, void *ws, hipStream_t stream)
+dp_status tiles_forward(const dp_attention &a, const Call &c, dp_dtype dt, void *O, float *lse, void *ws, hipStream_t stream)
 {
-    const ForwardOut out = {O, lse, (float *)ws, (i64)c.N * c.Hq * c.Tq, splits > 1 ? splits : 1};
+    const int splits = forward_splits(a);
+    ForwardOut out = {O, lse, (float *)ws, (i64)c.N * c.Hq * c.Tq, splits > 1 ? splits : 1, nullptr};
+    if (splits == 0 && row_order_entries(a) > 0) {
+        out.order = (const int32_t *)ws;
+        order_blocks(c, (int32_t *)ws, nullptr, stream);
+    }
     return dt == DP_F32 ? forward_f32(c, out, splits > 0, stream) : forward_bf16(c, out, splits > 0, stream);
 }
 

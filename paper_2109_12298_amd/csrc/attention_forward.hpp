@@ -12,12 +12,11 @@ struct ForwardOut {
     float *part;             // [splits][rows][D], and behind it [splits][rows][2]: maximum and sum
     i64 rows;                // N * Hk * M
     int splits;
+    const int32_t *order;    // [N * blocks of rows]: when they run, or NULL (attention_order.hip)
 };
 
-// Workgroups over which a sample's keys are split (1: none; 0: rows are blocks of 128).
-int forward_splits(const dp_attention &a);
 size_t tiles_forward_workspace(const dp_attention &a);
-dp_status tiles_forward(const Call &c, dp_dtype dt, int splits, void *O, float *lse, void *ws, hipStream_t stream);
+dp_status tiles_forward(const dp_attention &a, const Call &c, dp_dtype dt, void *O, float *lse, void *ws, hipStream_t stream);
 
 dp_status forward_bf16(const Call &c, const ForwardOut &out, bool small, hipStream_t stream);
 dp_status forward_f32(const Call &c, const ForwardOut &out, bool small, hipStream_t stream);

@@ -88,7 +88,13 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         split = b % out.splits;
         b /= out.splits;
     }
-    const int nk = b % heads, tm = tiles_m - 1 - b / heads;
+    int nk = b % heads, tm = tiles_m - 1 - b / heads;
+    if constexpr (!SMALL)
+        if (out.order != nullptr) {
+            const int e = out.order[b / c.Hk], of = e / tiles_m;
+            nk = of * c.Hk + b % c.Hk;
+            tm = e - of * tiles_m;
+        }
     const int n = nk / c.Hk, kv = nk - n * c.Hk;
     const Sample smp(c, n);
     const int M = c.Tq * c.G, r0 = tm * S::BR, rw = SMALL ? r0 : r0 + 32 * wave;

@@ -196,6 +196,17 @@ def test_large_and_small_scores(scale, size, dt):
     Case(1, 100, 140, 2, 1, 64, dt=dt, scale=scale, size=size, seed=4).check()
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("G,causal", [(1, True), (2, False)])
+def test_many_blocks_of_documents(G, causal, dt):
+    """Blocks enough to be run in the order of their work: documents of different lengths, in runs and mixed, padded samples."""
+    say("blocks", G, causal, dt)
+    N, T, Hk = 2, 1100, 16
+    docs = np.repeat(np.arange(5), [100, 500, 30, 300, 170])[None].repeat(N, 0)
+    docs[1] = np.repeat([3, -1, 3, 9, 0], [50, 20, 400, 600, 30])
+    Case(N, T, T, Hk * G, Hk, 16, dt=dt, causal=causal, docs=docs, lens=[1100, 1071], prefix=[200, 0] if causal else None, seed=12).check()
+
+
 def test_gradients_against_differences():
     """The fp32 kernels' gradients against central differences of the forward definition in 64 bits."""
     c = Case(1, 9, 9, 4, 2, 12, causal=True, cap=2.0, slopes=True, docs=np.array([[0] * 4 + [1] * 5]), seed=8)

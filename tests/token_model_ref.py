@@ -75,6 +75,13 @@ def _scores(q, k, scale, cap, slope, far, see):
     return np.where(see, s, -np.inf), bend, np.where(see, es, 0.0)
 
 
+def _over_visible(w, x, see):
+    """sum_j w[i][j] x[j] over the visible j (a hidden x is not looked at, whatever it is)."""
+    if np.isfinite(x).all():
+        return w @ x
+    return (w[:, :, None] * np.where(see[:, :, None], x[None], 0.0)).sum(1)
+
+
 def attention(Q, K, V, mask, scale, cap=0.0, slopes=None, dt=None):
     """Q [N][Tq][Hq][D], K, V [N][Tk][Hk][D] -> O, lse and the bounds of their errors."""
     N, Tq, Hq, D = Q.shape
@@ -100,16 +107,16 @@ def attention(Q, K, V, mask, scale, cap=0.0, slopes=None, dt=None):
             tot = w.sum(1, keepdims=True)
             p = w / tot
             with np.errstate(invalid="ignore"):
-                vz = np.where(see[rows][:, used][:, :, None], v[None], 0.0)       # weights of hidden keys take nothing
-                o = (p[:, :, None] * vz).sum(1)
-                mag = (p[:, :, None] * np.abs(vz)).sum(1)
+                sub = see[rows][:, used]
+                o = _over_visible(p, v, sub)
+                mag = _over_visible(p, np.abs(v), sub)
             # a weight is off by its score's error, the maximum's that it is taken from and 4 half steps (exp2, rescaling
             # counted with the sum); the sum by as much
             e = es.max(1, keepdims=True)
             n_keys = w.shape[1]
             rel = 2 * (2 * e + 4 * U32) + 2 * SUM(n_keys) + hp
             O[n, rows, hq] = o
-            flushed = TINY * (n_keys + 1 + np.abs(vz).sum(1))
+            flushed = TINY * (n_keys + 1 + _over_visible(sub.astype(float), np.abs(v), sub))
             eO[n, rows, hq] = rel * mag + h * (np.abs(o) + rel * mag) + flushed
             lse[n, hq, rows] = (top + np.log(tot))[:, 0]
             el[n, hq, rows] = (2 * e + SUM(n_keys) + 8 * U32 * (1 + np.abs(top) + np.abs(np.log(tot))))[:, 0]
@@ -150,16 +157,14 @@ def attention_grads(Q, K, V, dO, mask, scale, cap=0.0, slopes=None, dt=None):
                     (edp + edelta) * bend + (np.abs(dp - delta) + edp + edelta) * (16 * U32 + 2 * es / max(cap, 1e-30)) * (cap > 0)),
                     0.0)
                 eg = eg + np.where(sub, TINY * (1 + abs(scale) * (np.abs(dp - delta) + edp + edelta)), 0.0)
-                dz = np.where(sub[:, :, None], d[:, None, :], 0.0)
-                qz = np.where(sub[:, :, None], q[:, None, :], 0.0)
-                kz = np.where(sub[:, :, None], k[None], 0.0)
                 nq, nk = int(rows.sum()) * G, int(used.sum())
-                out[0][n, rows, hq] = (g[:, :, None] * kz).sum(1)
-                err[0][n, rows, hq] = ((eg + SUM(nk) * (np.abs(g) + eg))[:, :, None] * np.abs(kz)).sum(1)
-                out[1][n, used, g_] += (g[:, :, None] * qz).sum(0)
-                err[1][n, used, g_] += ((eg + SUM(nq) * (np.abs(g) + eg))[:, :, None] * np.abs(qz)).sum(0)
-                out[2][n, used, g_] += (p[:, :, None] * dz).sum(0)
-                err[2][n, used, g_] += (np.where(sub, p * (ep + hp + SUM(nq) * (1 + ep)) + TINY, 0.0)[:, :, None] * np.abs(dz)).sum(0)
+                out[0][n, rows, hq] = _over_visible(g, k, sub)
+                err[0][n, rows, hq] = _over_visible(eg + SUM(nk) * (np.abs(g) + eg), np.abs(k), sub)
+                out[1][n, used, g_] += _over_visible(g.T, q, sub.T)
+                err[1][n, used, g_] += _over_visible((eg + SUM(nq) * (np.abs(g) + eg)).T, np.abs(q), sub.T)
+                out[2][n, used, g_] += _over_visible(p.T, d, sub.T)
+                ev = np.where(sub, p * (ep + hp + SUM(nq) * (1 + ep)) + TINY, 0.0)
+                err[2][n, used, g_] += _over_visible(ev.T, np.abs(d), sub.T)
     return out, [e + h * (np.abs(o) + e) + TINY * (2 + Tk + Tq * G) for o, e in zip(out, err)]
 
 
