@@ -246,13 +246,13 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const Stager<TL, T, BN, SMALL ? 1 : NW, VEC> stk(c.ldk, c.D, SMALL ? 0 : wave, lane), stv(c.ldv, c.D, SMALL ? 0 : wave, lane);
     char *mine = smem + (SMALL ? wave * 2 * S::STAGE : 0);
     const uint32_t lds0 = lds_addr(mine);
-    const auto issue = [&](int t, int buf) {
+    const auto issue = [&](int t, int buf) __attribute__((always_inline)) {
         const i64 k0 = (i64)t * BN;
         const int left = (int)(end - k0);
         stk.issue(K + k0 * c.ldk, left, lds0 + buf * S::STAGE, mine + buf * S::STAGE);
         stv.issue(V + k0 * c.ldv, left, lds0 + buf * S::STAGE + S::HALF, mine + buf * S::STAGE + S::HALF);
     };
-    const auto step = [&](const char *LK, const char *LV, int k0, int cls) {
+    const auto step = [&](const char *LK, const char *LV, int k0, int cls) __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < FN; ++x) {
             f32x16_t s, e;
@@ -261,8 +261,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             TL::template products<2>([&](int i, int ks) { return TL::rows(i == 0 ? LK : LV, 32 * x, ks, lane); },
                                      [&](int i, int ks) -> const u32x4_t & { return i == 0 ? qf[ks] : df[ks]; },
                                      [&](int i) -> f32x16_t & { return i == 0 ? s : e; });
-            const auto key = [&](int k) { return k0 + 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
-            const auto weigh = [&](auto is_near) {
+            const auto key = [&](int k) __attribute__((always_inline)) { return k0 + 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
+            const auto weigh = [&](auto is_near) __attribute__((always_inline)) {
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
                     float bend;
@@ -303,7 +303,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 docs_range(smp.docs, j0, j1, lo, hi);
                 return meet(smp, span, j0, j0 + BN, lo, hi);
             });
-        const auto entry = [&](int k, int &t, int &cls) {
+        const auto entry = [&](int k, int &t, int &cls) __attribute__((always_inline)) {
             if (docs) {
                 const int e = __builtin_amdgcn_readfirstlane(list[k]);
                 t = base + (e >> 2);
@@ -319,8 +319,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         if (k0 < count) {
             entry(k0, t, cls);
             issue(t, 0);
-            int buf = 0;
-            for (int k = k0; k < count; k += STEP, buf ^= 1) {
+            // (in blocks of 128 each buffer has code of its own, so that its places are constants of the LDS reads)
+            const auto turn = [&](int k, int buf) __attribute__((always_inline)) {
                 const int at = t * BN, now = cls;
                 wait_loads();
                 if constexpr (SMALL) bf16s::wait_lgkmcnt0();
@@ -331,13 +331,21 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 }
                 wave_together();
                 step(mine + buf * S::STAGE, mine + buf * S::STAGE + S::HALF, at, now);
+            };
+            if constexpr (SMALL) {
+                for (int k = k0, buf = 0; k < count; k += STEP, buf ^= 1) turn(k, buf);
+            } else {
+                for (int k = k0; k < count; k += 2) {
+                    turn(k, 0);
+                    if (k + 1 < count) turn(k + 1, 1);
+                }
             }
         }
         if constexpr (!SMALL) lds_barrier();
         base = stop;
     }
 
-    const auto to = [&](int k) -> T * {
+    const auto to = [&](int k) __attribute__((always_inline)) -> T * {
         const int rr = rw + k, ik = rr / c.G;
         return rr < M ? (T *)gr.dQ + ((i64)n * c.Tq + ik) * c.ldq + (i64)(kv * c.G + rr - ik * c.G) * c.D : nullptr;
     };
@@ -416,7 +424,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const Stager<TL, T, BN, SMALL ? 1 : NW, VEC> stq(c.ldq, c.D, SMALL ? 0 : wave, lane), std(c.ldo, c.D, SMALL ? 0 : wave, lane);
     char *mine = smem + (SMALL ? wave * 2 * S::STAGE : 0);
     const uint32_t lds0 = lds_addr(mine);
-    const auto issue = [&](int t, int g, int buf) {
+    const auto issue = [&](int t, int g, int buf) __attribute__((always_inline)) {
         const int q0 = t * BN;
         const uint32_t L = lds0 + buf * S::STAGE;
         stq.issue(Q + (i64)q0 * c.ldq + (i64)g * c.D, c.Tq - q0, L, mine + buf * S::STAGE);
@@ -428,7 +436,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             dma4_off(row_delta + (i64)g * gr.pad + q0, off, L + 2 * S::HALF + 256);
         }
     };
-    const auto step = [&](const char *L, int q0, int g, int cls) {
+    const auto step = [&](const char *L, int q0, int g, int cls) __attribute__((always_inline)) {
         const char *LQ = L, *LD = L + S::HALF;
         const float slope2 = (MOD & kSlope) != 0 && c.slopes != nullptr ? c.slopes[kv * c.G + g] * kLog2e : 0.0f;
 #pragma unroll
@@ -439,8 +447,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             TL::template products<2>([&](int i, int ks) { return TL::rows(i == 0 ? LQ : LD, 32 * x, ks, lane); },
                                                  [&](int i, int ks) -> const u32x4_t & { return i == 0 ? kf[ks] : vf[ks]; },
                                                  [&](int i) -> f32x16_t & { return i == 0 ? s : e; });
-            const auto place = [&](int k) { return 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
-            const auto weigh = [&](auto is_near) {
+            const auto place = [&](int k) __attribute__((always_inline)) { return 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
+            const auto weigh = [&](auto is_near) __attribute__((always_inline)) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     const float4 l4 = *reinterpret_cast<const float4 *>(L + 2 * S::HALF + 4 * (32 * x + 8 * b + 4 * h));
@@ -461,7 +469,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             else weigh(std::false_type{});
             if (cls != kFull) {
                 const int lo = from - smp.first - q0, hi = (smp.L - smp.first < c.Tq ? smp.L - smp.first : c.Tq) - q0;
-                const auto hide = [&](auto &&seen) {
+                const auto hide = [&](auto &&seen) __attribute__((always_inline)) {
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
                         const bool see = seen(k);
@@ -493,7 +501,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     while (base < t1) {
         const bool docs = smp.docs != nullptr;
         const int stop = !docs || t1 - base <= kGroup ? t1 : base + kGroup;
-        const auto class_of = [&](int t, bool with_docs) {
+        const auto class_of = [&](int t, bool with_docs) __attribute__((always_inline)) {
             RowSpan span = span_of(smp, 1, c.Tq, t * BN, BN);
             if (with_docs) docs_range(smp.docs, span.pmin, span.pmax + 1, span.dmin, span.dmax);
             return meet(smp, span, j0, j0 + S::BR, kd0, kd1);
@@ -503,7 +511,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             count = tile_list<S::THREADS>(base, stop, list, cls_of, counts, [&](int t) { return class_of(t, true); });
         // the heads one after another, each over the tiles; this split's part of them
         const int whole = count * c.G, all = SMALL ? (int)((i64)whole * (split + 1) / gr.splits) : whole;
-        const auto entry = [&](int k, int &t, int &g, int &cls) {
+        const auto entry = [&](int k, int &t, int &g, int &cls) __attribute__((always_inline)) {
             g = k / count;
             if (docs) {
                 const int e = __builtin_amdgcn_readfirstlane(list[k - g * count]);
@@ -520,8 +528,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         if (k0 < all) {
             entry(k0, t, g, cls);
             issue(t, g, 0);
-            int buf = 0;
-            for (int k = k0; k < all; k += STEP, buf ^= 1) {
+            const auto turn = [&](int k, int buf) __attribute__((always_inline)) {
                 const int at = t * BN, head = g, now = cls;
                 wait_loads();
                 if constexpr (SMALL) bf16s::wait_lgkmcnt0();
@@ -532,6 +539,14 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 }
                 wave_together();
                 step(mine + buf * S::STAGE, at, head, now);
+            };
+            if constexpr (SMALL) {
+                for (int k = k0, buf = 0; k < all; k += STEP, buf ^= 1) turn(k, buf);
+            } else {
+                for (int k = k0; k < all; k += 2) {
+                    turn(k, 0);
+                    if (k + 1 < all) turn(k + 1, 1);
+                }
             }
         }
         if constexpr (!SMALL) lds_barrier();
@@ -540,14 +555,14 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
 
     if constexpr (SMALL)
         if (gr.splits > 1) {
-            const auto part_of = [&](int which, int k) -> float * {
+            const auto part_of = [&](int which, int k) __attribute__((always_inline)) -> float * {
                 return jw + k < c.Tk ? gr.part + (((i64)split * heads + nk) * c.Tk + jw + k) * 2 * c.D + which * c.D : nullptr;
             };
             put_block<T, DP, S, SMALL>(smem, ak, c.scale, c.D, false, lane, wave, [&](int k) { return part_of(0, k); });
             put_block<T, DP, S, SMALL>(smem, av, 1.0f, c.D, false, lane, wave, [&](int k) { return part_of(1, k); });
             return;
         }
-    const auto row_of = [&](void *p, i64 ld, int k) -> T * {
+    const auto row_of = [&](void *p, i64 ld, int k) __attribute__((always_inline)) -> T * {
         return jw + k < c.Tk ? (T *)p + ((i64)n * c.Tk + jw + k) * ld + (i64)kv * c.D : nullptr;
     };
     bool bad = put_block<T, DP, S, SMALL>(smem, ak, c.scale, c.D, vec_k, lane, wave, [&](int k) { return row_of(gr.dK, c.ldk, k); });
@@ -596,7 +611,7 @@ void launch(const Call &c, const Grads &g, hipStream_t stream)
 {
     constexpr int N = 16 / sizeof(T);
     const i64 heads = (i64)c.N * c.Hk, M = (i64)c.Tq * c.G;
-    const auto wide = [&](const void *p, i64 ld) { return c.D % N == 0 && ld % N == 0 && aligned(p, 16); };
+    const auto wide = [&](const void *p, i64 ld) __attribute__((always_inline)) { return c.D % N == 0 && ld % N == 0 && aligned(p, 16); };
     if (M > 0) {
         const int tiles = (int)ceil_div(M, g.small_q ? 32 : 128);
         if (g.small_q)

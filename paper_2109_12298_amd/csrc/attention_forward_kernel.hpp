@@ -159,16 +159,16 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const Stager<TL, T, BN, SMALL ? 1 : NW, VEC> stk(c.ldk, c.D, SMALL ? 0 : wave, lane), stv(c.ldv, c.D, SMALL ? 0 : wave, lane);
     char *mine = smem + (SMALL ? wave * S::STAGE : 0);
     const uint32_t lds0 = lds_addr(mine);
-    const auto issue_k = [&](int t, int buf) {
+    const auto issue_k = [&](int t, int buf) __attribute__((always_inline)) {
         const i64 k0 = (i64)t * BN;
         stk.issue(K + k0 * c.ldk, (int)(end - k0), lds0 + buf * S::STAGE, mine + buf * S::STAGE);
     };
-    const auto issue_v = [&](int t, int buf) {
+    const auto issue_v = [&](int t, int buf) __attribute__((always_inline)) {
         const i64 k0 = (i64)t * BN;
         stv.issue(V + k0 * c.ldv, (int)(end - k0), lds0 + buf * S::STAGE + S::HALF, mine + buf * S::STAGE + S::HALF);
     };
     f32x16_t s[FN];
-    const auto scores = [&](const char *LK) {
+    const auto scores = [&](const char *LK) __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < FN; ++x)
 #pragma unroll
@@ -178,16 +178,16 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                                   [&](int x) -> f32x16_t & { return s[x]; });
     };
     // scores to weights, running maximum and sum
-    const auto soften = [&](int k0, int cls) {
-        const auto key = [&](int x, int e) { return k0 + 32 * x + 8 * (e >> 2) + 4 * h + (e & 3); };
-        const auto far = [&](int x, int e) { return __builtin_fabsf((float)(pos - key(x, e))); };
-        const auto each = [&](auto &&f) {
+    const auto soften = [&](int k0, int cls) __attribute__((always_inline)) {
+        const auto key = [&](int x, int e) __attribute__((always_inline)) { return k0 + 32 * x + 8 * (e >> 2) + 4 * h + (e & 3); };
+        const auto far = [&](int x, int e) __attribute__((always_inline)) { return __builtin_fabsf((float)(pos - key(x, e))); };
+        const auto each = [&](auto &&f) __attribute__((always_inline)) {
 #pragma unroll
             for (int x = 0; x < FN; ++x)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[x][e] = f(x, e, s[x][e]);
         };
-        const auto hide = [&](float with) {
+        const auto hide = [&](float with) __attribute__((always_inline)) {
             each([&](int x, int e, float v) { return key(x, e) < lim ? v : with; });
             if (cls == kDocs) {
                 // (all loads before the first comparison)
@@ -225,7 +225,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 for (int e = 0; e < 16; ++e) acc[d][e] *= f;
         }
         const float base = top == -INFINITY ? 0.0f : top;
-        const auto weigh = [&](auto is_near) {
+        const auto weigh = [&](auto is_near) __attribute__((always_inline)) {
             each([&](int, int, float v) {
                 return __builtin_amdgcn_exp2f(
                     MOD >= kSlope ? v - base : score.template of<decltype(is_near)::value>(v, base, 0.0f, 0.0f, unused));
@@ -246,7 +246,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
 #pragma unroll
             for (int e = 0; e < 16; ++e) sum += s[x][e];
     };
-    const auto values = [&](const char *LV) {
+    const auto values = [&](const char *LV) __attribute__((always_inline)) {
         typedef f32x16_t Sums[DB];
         TL::template columns<FN>([&](int x) { return LV + 32 * x * TL::RB; }, [&](int x) -> const f32x16_t & { return s[x]; },
                                  [&](int) -> Sums & { return acc; }, lane);
@@ -285,7 +285,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             base = t1;                                  // one group
         }
         const int first = smp.docs != nullptr ? base : t0;
-        const auto entry = [&](int k, int &t, int &cls) {
+        const auto entry = [&](int k, int &t, int &cls) __attribute__((always_inline)) {
             if (smp.docs != nullptr) {
                 const int e = __builtin_amdgcn_readfirstlane(list[k]);
                 t = first + (e >> 2);
@@ -331,20 +331,25 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 entry(0, t, cls);
                 issue_k(t, 0);
                 issue_v(t, 0);
-                for (int k = 0; k < count; ++k) {
+                // (each buffer has code of its own, so that its places are constants of the LDS reads)
+                const auto turn = [&](int k, int buf) __attribute__((always_inline)) {
                     const int k0 = t * BN, now = cls;
                     wait_loads();
                     lds_barrier();                      // this tile has landed, the one before is read
                     if (k + 1 < count) {
                         entry(k + 1, t, cls);
-                        issue_k(t, (k + 1) & 1);
-                        issue_v(t, (k + 1) & 1);
+                        issue_k(t, buf ^ 1);
+                        issue_v(t, buf ^ 1);
                     }
-                    const char *L = smem + (k & 1) * S::STAGE;
+                    const char *L = smem + buf * S::STAGE;
                     wave_together();
                     scores(L);
                     soften(k0, now);
                     values(L + S::HALF);
+                };
+                for (int k = 0; k < count; k += 2) {
+                    turn(k, 0);
+                    if (k + 1 < count) turn(k + 1, 1);
                 }
             }
             lds_barrier();
@@ -538,7 +543,7 @@ void by_kind(const Call &c, const ForwardOut &out, bool small, hipStream_t strea
                      aligned(c.V, 16);
     const bool vec_out = c.D % N == 0 && c.ldo % N == 0 && aligned(out.O, 16);
     const int mod = c.scale <= 0.0f ? kBoth : (c.cap > 0.0f ? kCap : kPlain) | (c.slopes != nullptr ? kSlope : kPlain);
-    const auto go = [&](auto v, auto m) {
+    const auto go = [&](auto v, auto m) __attribute__((always_inline)) {
         if (small) launch<T, DP, decltype(v)::value, decltype(m)::value, true>(c, out, vec_out, stream);
         else launch<T, DP, decltype(v)::value, decltype(m)::value, false>(c, out, vec_out, stream);
     };
