@@ -454,8 +454,8 @@ typedef struct dp_attention {
     uint32_t flags;         /* DP_ATTENTION_CAUSAL, DP_ATTENTION_LAST; other bits must be 0 */
     int64_t N, Tq, Tk, Hq, Hk, D;
     int64_t ldq, ldk, ldv, ldo;
-    float scale;            /* finite */
-    float softcap;          /* 0: none; finite, >= 0 */
+    float scale;            /* at most 2^60 in size */
+    float softcap;          /* 0: none; else 2^-60 to 2^60 */
     const float *slopes;    /* fp32 [Hq], or NULL */
     const int32_t *lens;    /* int32 [N], or NULL */
     const int32_t *prefix;  /* int32 [N], or NULL; with DP_ATTENTION_CAUSAL only */
@@ -466,8 +466,8 @@ enum { DP_ATTENTION_CAUSAL = 1, DP_ATTENTION_LAST = 2 };
 
 /* O, and lse (fp32 [N][Hq][Tq], or NULL): the logarithm of a query's softmax
  * sum, -inf where it sees nothing.  Scores, sums and outputs are formed in
- * fp32; with bf16 inputs the softmax weights are rounded to bf16 before their
- * product with V.  N, Tq, Tk >= 0; Hq a multiple of Hk >= 1; 1 <= D <= 256;
+ * fp32; with bf16 inputs the softmax weights are rounded to bf16 (or to the sum
+ * of two bf16 values) before their product with V.  N, Tq, Tk >= 0; Hq a multiple of Hk >= 1; 1 <= D <= 256;
  * ldq, ldo >= Hq*D, ldk, ldv >= Hk*D.  Needs Tq, Tk < 2^24,
  * N*Hq*ceil(Tq/32) and N*Hk*ceil(Tk/32) < 2^24, N*Hq < 2^31 and ld* < 2^22
  * (else DP_EUNSUPPORTED).  O overlaps no input.
@@ -485,7 +485,8 @@ dp_status dp_attention_forward(const dp_attention *a, const void *Q, const void 
  * (tanh^2 as the score's, 0 without softcap; the sums of a key head run over
  * its query heads).  dO is laid out as O, dQ, dK and dV as Q, K and V.
  * Padding queries and keys from L on get zeros.  Sums are formed in fp32; with
- * bf16 inputs p and g are rounded to bf16 before their products.  Outputs
+ * bf16 inputs p and g are rounded to bf16 (or to the sum of two bf16 values)
+ * before their products.  Outputs
  * overlap nothing.  Sizes as the forward call; workspace:
  * dp_attention_backward_workspace_bytes(a), 16-byte aligned. */
 size_t dp_attention_backward_workspace_bytes(const dp_attention *a);
@@ -510,7 +511,7 @@ dp_status dp_attention_backward(const dp_attention *a, const void *Q, const void
  * [M].  An id or label >= V sets DP_FLAG_BAD_INDEX and is left out.  dZ is the
  * output layer's backprops B of the per-sample losses (divide by nothing: the
  * clipped step averages).  Softmax sums are formed in fp32, dZ is rounded once.
- * M, K >= 0, V >= 1, 0 <= alpha <= 1, tau > 0 finite; needs M < 2^31, V < 2^30,
+ * M, K >= 0, V >= 1, 0 <= alpha <= 1, 2^-20 <= tau <= 2^20; needs M < 2^31, V < 2^30,
  * K <= 1024 (else DP_EUNSUPPORTED).  Workspace:
  * dp_distill_loss_workspace_bytes(M, V, K, dt), 16-byte aligned. */
 size_t dp_distill_loss_workspace_bytes(int64_t M, int64_t V, int64_t K, dp_dtype dt);

@@ -20,7 +20,8 @@ dp_status check(const dp_attention *a)
     DPG_REQUIRE((a->flags & ~(uint32_t)(DP_ATTENTION_CAUSAL | DP_ATTENTION_LAST)) == 0, DP_EINVAL);
     DPG_REQUIRE(a->N >= 0 && a->Tq >= 0 && a->Tk >= 0 && a->Hk >= 1 && a->Hq >= 1 && a->Hq % a->Hk == 0 && a->D >= 1,
                 DP_EINVAL);
-    DPG_REQUIRE(isfinite(a->scale) && isfinite(a->softcap) && a->softcap >= 0.0f, DP_EINVAL);
+    // within these bounds scale / softcap and the scales in units of ln 2 are finite
+    DPG_REQUIRE(fabsf(a->scale) <= 0x1p60f && (a->softcap == 0.0f || (a->softcap >= 0x1p-60f && a->softcap <= 0x1p60f)), DP_EINVAL);
     DPG_REQUIRE(a->prefix == nullptr || (a->flags & DP_ATTENTION_CAUSAL) != 0, DP_EINVAL);
     DPG_REQUIRE(aligned(a->slopes, 4) && aligned(a->lens, 4) && aligned(a->prefix, 4) && aligned(a->docs, 4), DP_EINVAL);
     DPG_REQUIRE(a->D <= kMaxD && a->Tq < kMaxT && a->Tk < kMaxT && a->N < kMaxRows && a->Hq < kMaxLd, DP_EUNSUPPORTED);

@@ -18,6 +18,11 @@
 // workgroups as well, and the splits' sums are added by a launch of their own (500
 // queries, 6 and 2 heads of 48, fp32: 96 blocks 70 us).
 //
+// With bf16 values O is rounded, and dO.O with it; dQ's launch adds up what p and
+// dO.V say it lacks, for dK.  e, which is small where it cancels, is taken as the
+// sum of two bf16 values in its products, p where workgroups are small: with one
+// each, errors were 1.5 times the outputs' own rounding.
+//
 // As in the forward pass, a block whose sums are not finite is formed again row
 // by row, over visible pairs only.
 #pragma once
@@ -228,11 +233,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         for (int ks = 0; ks < KS; ++ks) delta += TL::dot(of[ks], df[ks]);
         delta += other_half(delta);
         if (lse2 == INFINITY) delta = 0.0f;
-        if (row_ok && h == 0 && (!SMALL || wave == 0)) {
-            gr.row_lse[info] = lse2;
-            gr.row_delta[info] = delta;
-        }
     }
+    float excess = 0.0f;                                 // sum of p (dO.V - delta): what delta lacks, as O is rounded
     const Scores<T, MOD> score(c);
     const float slope2 = (MOD & kSlope) != 0 && c.slopes != nullptr ? c.slopes[head] * kLog2e : 0.0f;
 
@@ -262,31 +264,43 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                                      [&](int i, int ks) -> const u32x4_t & { return i == 0 ? qf[ks] : df[ks]; },
                                      [&](int i) -> f32x16_t & { return i == 0 ? s : e; });
             const auto key = [&](int k) __attribute__((always_inline)) { return k0 + 32 * x + 8 * (k >> 2) + 4 * h + (k & 3); };
-            const auto weigh = [&](auto is_near) __attribute__((always_inline)) {
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    float bend;
-                    const float p = __builtin_amdgcn_exp2f(score.template of<decltype(is_near)::value>(
-                        s[k], lse2, slope2, __builtin_fabsf((float)(pos - key(k))), bend));
-                    e[k] = p * (e[k] - delta);
-                    if constexpr ((MOD & kCap) != 0) e[k] *= bend;
-                }
-            };
-            if (score.near(s)) weigh(std::true_type{});
-            else weigh(std::false_type{});
+            unsigned seen = 0;                           // bit k: the pair of row li and key(k) is visible
             if (cls != kFull) {
 #pragma unroll
-                for (int k = 0; k < 16; ++k) e[k] = key(k) < lim ? e[k] : 0.0f;
+                for (int k = 0; k < 16; ++k) seen |= key(k) < lim ? 1u << k : 0u;
                 if (cls == kDocs) {
                     // (all loads before the first comparison)
                     int d[16];
 #pragma unroll
                     for (int k = 0; k < 16; ++k) d[k] = smp.docs[key(k) < end ? key(k) : end - 1];
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) e[k] = d[k] == doc && doc >= 0 ? e[k] : 0.0f;
+                    for (int k = 0; k < 16; ++k) seen &= d[k] == doc && doc >= 0 ? ~0u : ~(1u << k);
                 }
             }
-            TL::template columns<1>([&](int) { return LK + 32 * x * TL::RB; }, [&](int) -> const f32x16_t & { return e; },
+            const auto weigh = [&](auto is_near, auto all) __attribute__((always_inline)) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    float bend;
+                    const float p = __builtin_amdgcn_exp2f(score.template of<decltype(is_near)::value>(
+                        s[k], lse2, slope2, __builtin_fabsf((float)(pos - key(k))), bend));
+                    float g = p * (e[k] - delta);
+                    if constexpr (!decltype(all)::value) g = (seen >> k & 1u) != 0 ? g : 0.0f;
+                    excess += g;
+                    if constexpr ((MOD & kCap) != 0) {
+                        if constexpr (!decltype(all)::value) bend = (seen >> k & 1u) != 0 ? bend : 0.0f;
+                        g *= bend;
+                    }
+                    e[k] = g;
+                }
+            };
+            if (cls == kFull) {
+                if (score.near(s)) weigh(std::true_type{}, std::true_type{});
+                else weigh(std::false_type{}, std::true_type{});
+            } else {
+                if (score.near(s)) weigh(std::true_type{}, std::false_type{});
+                else weigh(std::false_type{}, std::false_type{});
+            }
+            TL::template columns<1, 1>([&](int) { return LK + 32 * x * TL::RB; }, [&](int) -> const f32x16_t & { return e; },
                                     [&](int) -> Sums & { return acc; }, lane);
         }
     };
@@ -349,6 +363,20 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         const int rr = rw + k, ik = rr / c.G;
         return rr < M ? (T *)gr.dQ + ((i64)n * c.Tq + ik) * c.ldq + (i64)(kv * c.G + rr - ik * c.G) * c.D : nullptr;
     };
+    excess += other_half(excess);
+    if constexpr (SMALL) {
+        __syncthreads();                                 // all have read their tiles
+        float *sums = reinterpret_cast<float *>(smem);
+        if (h == 0) sums[wave * 32 + li] = excess;
+        __syncthreads();
+        excess = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) excess += sums[w * 32 + li];
+    }
+    if (row_ok && h == 0 && (!SMALL || wave == 0)) {
+        gr.row_lse[info] = lse2;
+        gr.row_delta[info] = delta + excess;
+    }
     const bool bad = put_block<T, DP, S, SMALL>(smem, acc, c.scale, c.D, vec_out, lane, wave, to);
     wait_loads();                                        // the stores above come before those below
     if (SMALL ? __syncthreads_or(bad) : __any(bad))
@@ -491,7 +519,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 }
             }
             const char *LX = L + 32 * x * TL::RB;
-            TL::template columns<2>([&](int i) { return i == 0 ? LX + S::HALF : LX; },
+            TL::template columns<2, SMALL ? 3 : 2>([&](int i) { return i == 0 ? LX + S::HALF : LX; },
                                     [&](int i) -> const f32x16_t & { return i == 0 ? s : e; },
                                     [&](int i) -> Sums & { return i == 0 ? av : ak; }, lane);
         }

@@ -152,8 +152,10 @@ struct Tile {
     }
 
     // acc(i)[block of 32 values][.] += sum over 32 rows r of tile(i)[r][value] * w(i)[r], for COUNT blocks of rows one after
-    // another; tile(i): where the block starts (a multiple of 32 rows of a tile)
-    template <int COUNT, bool PACK_FIRST = false, typename At, typename W, typename Acc>
+    // another; tile(i): where the block starts (a multiple of 32 rows of a tile).
+    // bf16 products take w rounded to bf16; where bit i of SPLIT is set, as the sum of two bf16 values, whose second product reads
+    // nothing anew.
+    template <int COUNT, unsigned SPLIT = 0, typename At, typename W, typename Acc>
     static __device__ __forceinline__ void columns(At &&tile, W &&w, Acc &&acc, int lane)
     {
         const int h = lane >> 5;
@@ -171,20 +173,26 @@ struct Tile {
                     a[d] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
                 }
             };
-            bf16x8_t a[2][DB], b[2 * COUNT];
-#pragma unroll
-            for (int step = 0; step < 2 * COUNT; ++step)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) b[step][e] = (__bf16)w(step >> 1)[8 * (step & 1) + e];
-            if constexpr (PACK_FIRST) __builtin_amdgcn_sched_barrier(0);
+            bf16x8_t a[2][DB];
             load(0, a[0]);
 #pragma unroll
             for (int step = 0; step < 2 * COUNT; ++step) {
                 if (step + 1 < 2 * COUNT) load(step + 1, a[(step + 1) & 1]);
+                const bool split = (SPLIT >> (step >> 1) & 1) != 0;
+                bf16x8_t b, rest;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = w(step >> 1)[8 * (step & 1) + e];
+                    b[e] = (__bf16)x;
+                    if (split) rest[e] = (__bf16)(x - (float)b[e]);
+                }
                 keep_order();
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    acc(step >> 1)[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[step & 1][d], b[step], acc(step >> 1)[d], 0, 0, 0);
+                for (int d = 0; d < DB; ++d) {
+                    acc(step >> 1)[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[step & 1][d], b, acc(step >> 1)[d], 0, 0, 0);
+                    if (split)
+                        acc(step >> 1)[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[step & 1][d], rest, acc(step >> 1)[d], 0, 0, 0);
+                }
                 keep_order();
             }
         } else {
@@ -312,32 +320,28 @@ struct Stager {
 // What a score has besides its scale (> 0): kBoth looks at run time, and takes any scale
 enum { kPlain = 0, kCap = 1, kSlope = 2, kBoth = 3 };
 
-// For scores of bf16 inputs, whose rounding is 2^-9 of a score: tanh y = y P(y^2),
-// within 6e-7 of itself for |y| <= 3/4 (a least-maximum fit of five terms), where
-// no score of a wave's block goes further, which a cap is chosen for; else by
-// exp2 and reciprocal (off by some 2^-22).  The polynomial with the scales in its
-// coefficients takes five instructions a score, of which the last forms the
-// exponent; the other way three and two quarter-rate ones.
+// tanh y = y P(y^2) up to |y| = 3/4 (least-maximum fits: five terms within 6e-7
+// of it for scores of bf16 inputs, whose rounding is 2^-9 of a score, seven within
+// 1.5e-9 for fp32 ones), from there 1 - 2 / (1 + exp 2|y|), whose subtrahend is at
+// most 0.37 and off by some 2^-23 of it.  Where no score of a bf16 wave's block
+// goes past 3/4, which a cap is chosen for, the polynomial alone is taken, with
+// the scales in its coefficients: five instructions a score, of which the last
+// forms the exponent.  No branches by lane: see wave_together.
 constexpr float kNear = 0.75f;
 constexpr float kTanh[5] = {0.999999435f, -0.333282516f, 0.132589834f, -0.0500563036f, 0.0129296314f};
 
-// For fp32 inputs without branches: seven terms up to |y| = 3/4 (1.5e-9 of itself, before rounding), from there 1 - 2 / (1 +
-// exp 2|y|), whose subtrahend is at most 0.37 and off by some 2^-23 of it.
 constexpr float kTanh7[7] = {0.999999999f, -0.333333072f, 0.133325791f, -0.0538856315f, 0.0214308735f, -0.00762702948f, 0.00172035412f};
 
 template <typename T>
 __device__ __forceinline__ float tanh_for(float y)
 {
-    if constexpr (sizeof(T) == 2) {
-        return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * y));
-    } else {
-        const float a = __builtin_fabsf(y), u = y * y;
-        float p = kTanh7[6];
+    constexpr int TERMS = sizeof(T) == 2 ? 5 : 7;
+    const float a = __builtin_fabsf(y), u = y * y;
+    float p = sizeof(T) == 2 ? kTanh[4] : kTanh7[6];
 #pragma unroll
-        for (int k = 5; k >= 0; --k) p = __builtin_fmaf(u, p, kTanh7[k]);
-        const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * a));
-        return a < kNear ? y * p : __builtin_copysignf(far, y);
-    }
+    for (int k = TERMS - 2; k >= 0; --k) p = __builtin_fmaf(u, p, sizeof(T) == 2 ? kTanh[k] : kTanh7[k]);
+    const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * a));
+    return a < kNear ? y * p : __builtin_copysignf(far, y);
 }
 
 template <typename T, int MOD>
@@ -346,6 +350,7 @@ struct Scores {
     float y_scale, cap2;     // scale / cap, cap * log2 e; cap2 = 0: no cap
     float inv_cap2;          // 1 / cap2
     float c[5];              // the polynomial's, of the raw score
+    float near_to;           // |y| up to which it holds; -1 where its coefficients might overflow
 
     __device__ __forceinline__ explicit Scores(const Call &a)
     {
@@ -356,6 +361,7 @@ struct Scores {
         float f = cap2 * y_scale;
 #pragma unroll
         for (int k = 0; k < 5; ++k, f *= y_scale * y_scale) c[k] = f * kTanh[k];
+        near_to = __builtin_fabsf(y_scale) <= 1024.0f && __builtin_fabsf(scale2) <= 0x1p40f ? kNear : -1.0f;
     }
     // whether the polynomial may be taken for all raw scores of the wave's block
     __device__ __forceinline__ bool near(const f32x16_t &x) const
@@ -364,7 +370,7 @@ struct Scores {
         float m = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) m = fmaxf(m, __builtin_fabsf(x[e]));
-        return !__any(!(m * __builtin_fabsf(y_scale) <= kNear));
+        return !__any(!(m * __builtin_fabsf(y_scale) <= near_to));
     }
     __device__ __forceinline__ float poly(float x) const
     {

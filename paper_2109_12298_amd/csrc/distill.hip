@@ -390,7 +390,7 @@ extern "C" dp_status dp_distill_loss(const void *Z, dp_dtype dt, int64_t M, int6
 {
     DPG_REQUIRE(dtype_ok(dt), DP_EDTYPE);
     DPG_REQUIRE(M >= 0 && K >= 0 && V >= 1, DP_EINVAL);
-    DPG_REQUIRE(alpha >= 0.0f && alpha <= 1.0f && tau > 0.0f && tau < INFINITY, DP_EINVAL);
+    DPG_REQUIRE(alpha >= 0.0f && alpha <= 1.0f && tau >= 0x1p-20f && tau <= 0x1p20f, DP_EINVAL);
     DPG_REQUIRE(M < (i64(1) << 31) && V < (i64(1) << 30) && K <= kMaxK, DP_EUNSUPPORTED);
     if (M == 0) return DP_OK;
     DPG_REQUIRE(Z != nullptr && loss != nullptr && (K == 0 || (ids != nullptr && logits != nullptr)), DP_EINVAL);

@@ -175,6 +175,16 @@ def test_values_in_hidden_places_have_no_part(D, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cap", [1e-5, 0.3, 2e4, 1e9])
+def test_caps_of_all_sizes(cap, dt):
+    """A cap far below the scores, about them, and so far above that its polynomial's coefficients vanish; hidden pairs in all."""
+    say("cap", cap, dt)
+    docs = np.repeat(np.array([[0, 1]]), 2, 0).repeat(45, 1)
+    Case(2, 90, 90, 2, 1, 64, dt=dt, causal=True, cap=float(np.float32(cap)), lens=[90, 75], docs=docs, seed=13).check()
+    Case(1, 1, 500, 4, 2, 64, dt=dt, causal=True, last=True, lens=[333], cap=float(np.float32(cap)), seed=13).check(backward=False)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_rows_that_see_nothing(dt):
     c = Case(2, 50, 50, 2, 1, 64, dt=dt, docs=np.full((2, 50), -1), seed=1)
     out, lse = c.check()

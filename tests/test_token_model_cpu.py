@@ -57,7 +57,7 @@ def test_attention_refusals():
     for call in (fwd, bwd):
         assert call(dt=7) == dp.DP_EDTYPE
         for bad in (dict(N=-1), dict(Tq=-1), dict(Tk=-1), dict(Hk=0), dict(Hq=0), dict(Hq=3), dict(D=0), dict(flags=4), dict(scale=math.nan),
-                    dict(scale=math.inf), dict(softcap=-1.0), dict(softcap=math.inf), dict(prefix=FAKE), dict(ldq=31), dict(ldk=15),
+                    dict(scale=math.inf), dict(softcap=-1.0), dict(softcap=math.inf), dict(softcap=1e-19), dict(softcap=math.nan), dict(scale=1e19), dict(prefix=FAKE), dict(ldq=31), dict(ldk=15),
                     dict(ldv=15), dict(ldo=31), dict(slopes=FAKE + 2), dict(lens=FAKE + 1), dict(docs=FAKE + 2), dict(Q=None), dict(K=None),
                     dict(V=None), dict(O=None), dict(Q=FAKE + 2), dict(V=FAKE + 1), dict(lse=FAKE + 2)):
             assert call(**bad) == dp.DP_EINVAL, bad
@@ -85,7 +85,7 @@ def test_distill_refusals():
 
     assert call(dt=2) == dp.DP_EDTYPE
     for bad in (dict(M=-1), dict(K=-1), dict(V=0), dict(alpha=-0.1), dict(alpha=1.1), dict(alpha=math.nan), dict(tau=0.0), dict(tau=-1.0),
-                dict(tau=math.nan), dict(tau=math.inf), dict(Z=None), dict(loss=None), dict(ids=None), dict(logits=None), dict(Z=FAKE + 2),
+                dict(tau=math.nan), dict(tau=math.inf), dict(tau=1e-7), dict(tau=2e6), dict(Z=None), dict(loss=None), dict(ids=None), dict(logits=None), dict(Z=FAKE + 2),
                 dict(dZ=FAKE + 1), dict(ids=FAKE + 4), dict(labels=FAKE + 4), dict(weight=FAKE + 2), dict(loss=FAKE + 1)):
         assert call(**bad) == dp.DP_EINVAL, bad
     for much in (dict(M=2 ** 31), dict(V=2 ** 30), dict(K=1025)):

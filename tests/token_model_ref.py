@@ -65,9 +65,10 @@ def _scores(q, k, scale, cap, slope, far, see):
         bend, s = np.ones_like(x), x
         if cap > 0:
             t = np.tanh(x / cap)
-            # tanh of an fp32 quotient: 8 half steps of 1 (the exponential form loses the bits below 1's); it has slope <= 1
+            # tanh has slope <= 1; its own form is off by 10 half steps of itself (the shorter polynomial), its coefficients' and
+            # steps' roundings 10 more, the products with the cap 4
             s, bend = cap * t, 1 - t * t
-            ex = ex + 8 * U32 * cap
+            ex = ex + 24 * U32 * np.abs(s)
         bias = slope * far
         s = s - bias
         # the bias, its difference, the factor log2 e, the maximum's or lse's difference: half a step each, of what is largest
