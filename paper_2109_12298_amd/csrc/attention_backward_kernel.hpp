@@ -15,13 +15,19 @@
 // keys share tiles, two stages deep, where there are blocks enough to fill the
 // card; else 32 are one workgroup whose waves take different tiles and whose
 // sums are added in wave order; few blocks of keys have their queries split over
-// workgroups as well, and the splits' sums are added by a launch of their own (500
-// queries, 6 and 2 heads of 48, fp32: 96 blocks 70 us).
+// workgroups as well, and the splits' sums are added by a launch of their own (3
+// samples of 500, 6 and 2 heads of 48, fp32: 96 blocks 70 us, split 31 + 5).
 //
 // With bf16 values O is rounded, and dO.O with it; dQ's launch adds up what p and
 // dO.V say it lacks, for dK.  e, which is small where it cancels, is taken as the
 // sum of two bf16 values in its products, p where workgroups are small: with one
-// each, errors were 1.5 times the outputs' own rounding.
+// each, errors were 1.5 times the outputs' own rounding, with two 1.25 (two samples
+// of 8192 in documents, 32 and 8 heads of 128: dQ 707 -> 833 us, dK and dV 1260 ->
+// 1364).
+//
+// Bound by the vector unit's work on the scores (exponent, cap, e, its rounding)
+// and the matrix instructions, which take turns: 32 samples of 128, 12 heads of 64:
+// dQ 15, dK and dV 13 us.
 //
 // As in the forward pass, a block whose sums are not finite is formed again row
 // by row, over visible pairs only.
@@ -389,8 +395,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
 // ---------------------------------------------------------------------------
 // dK and dV
 // ---------------------------------------------------------------------------
-// (Rows of 192 bytes or longer leave one wave per SIMD, by sums and operands of 260 registers and more.  8192 causal queries in
-// documents, 32 and 8 heads of 128, capped scores: 1717 us; dV and dK in launches of their own, two waves per SIMD and one product
+// (Rows of 192 bytes or longer leave one wave per SIMD, by sums and operands of 260 registers and more.  Two samples of 8192 causal
+// queries in documents, 32 and 8 heads of 128, capped scores, blocks in the order of positions, weights rounded once: 1717 us; dV and dK in launches of their own, two waves per SIMD and one product
 // more, 813 + 1033; V's operands in LDS, two waves and some of K's in scratch memory, 2297.)
 template <typename T, int DP, bool VEC, int MOD, bool SMALL>
 __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, DP>::RB > 128 ? 1 : 2)) void key_kernel(

@@ -19,6 +19,11 @@
 // 2.4e-3; where workgroups are small, which memory or latency bounds, they are the
 // sum of two bf16 values instead.
 //
+// Two prompts of 4096, 32 and 8 heads of 128, bf16: 276 to 290 us, 950 TFLOP/s (209
+// at a large product's rate): softmax on the vector unit and matrix instructions of
+// one SIMD's two waves overlap in part.  One query over 4096 keys: 6 us and the join's
+// 4; 32 queries over up to 8192 keys each: 117 us, 5.2 TB/s of K and V.
+//
 // Hidden pairs have weight 0 by selection; an infinity or NaN in their values
 // would still turn 0 into NaN in the product, so a block whose sums are not
 // finite is formed again row by row, over visible pairs only.

@@ -12,6 +12,11 @@
 // written anew, each formed in fp32 from its own logit and rounded once.  Those
 // logits are read before the first store, so dZ may be Z.
 //
+// 1001 rows of 32001, bf16, labels mixed in: 39 us (26 at a copy's rate: four
+// workgroups a CU at most, each waiting for its own row).  8192 rows of 100000: 790
+// us, 4.2 TB/s; a row fills a CU's registers, so that its loads, exponentials and
+// stores do not overlap with another row's.  256 rows of 10000, fp32: 8 us.
+//
 // Rows start at any element: up to 16 / sizeof(T) - 1 elements before the first
 // 16-byte piece and behind the last one are single loads and stores.
 #include "common.hpp"
@@ -113,7 +118,7 @@ __device__ __forceinline__ void block_add(float (&v)[N], float (*red)[16])
 }
 
 // NV pieces of a row per thread are held; RESIDENT: they are the whole row.
-// SOFT, HARD: which parts of the loss the call has (a position may lack its own).
+// HARD: the call has labels (a position may lack its own).
 template <typename T, int THREADS, int NV, bool RESIDENT, bool HARD>
 __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Args a, T *dZ)
 {
