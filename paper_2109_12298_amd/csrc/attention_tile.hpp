@@ -330,7 +330,7 @@ enum { kPlain = 0, kCap = 1, kSlope = 2, kBoth = 3 };
 constexpr float kNear = 0.75f;
 constexpr float kTanh[5] = {0.999999435f, -0.333282516f, 0.132589834f, -0.0500563036f, 0.0129296314f};
 
-constexpr float kTanh7[7] = {0.999999999f, -0.333333072f, 0.133325791f, -0.0538856315f, 0.0214308735f, -0.00762702948f, 0.00172035412f};
+constexpr float kTanh7[7] = {0.999999999f, -0.33333307f, 0.133325791f, -0.0538856315f, 0.0214308735f, -0.00762702948f, 0.00172035412f};
 
 template <typename T>
 __device__ __forceinline__ float tanh_for(float y)
