@@ -274,3 +274,33 @@ def test_graph_replays_match_eager():
                 torch.cuda.synchronize()
                 for n, t in o.items():
                     assert torch.equal(t, want[n]), (n, k)
+
+
+@pytest.mark.parametrize("N", [3, 300])
+def test_key_gradients_where_dS_cancels(N):
+    """Values that differ little: dO.V - dO.O is a small difference, and O is rounded to bf16 before the call."""
+    T, D = 8, 32
+    say("test_key_gradients_where_dS_cancels", N)
+    case = Case(N, T, T, 1, 1, D, "bf16", scale=2.0 ** -5, seed=11)
+    common = torch.from_numpy(np.random.default_rng(12).standard_normal((N, 1, 1, D)))
+    case.V = (common + case.V.double() / 16).to(torch.bfloat16)
+    Q, K, V, dO = (f64(getattr(case, k))[:, :, 0] for k in ("Q", "K", "V", "dO"))
+    s = case.scale * (Q @ K.transpose(0, 2, 1))
+    p = np.exp(s - s.max(-1, keepdims=True))
+    p /= p.sum(-1, keepdims=True)
+    dP = dO @ V.transpose(0, 2, 1)
+    e = p * (dP - (p * dP).sum(-1, keepdims=True))
+    want = case.scale * (e.transpose(0, 2, 1) @ Q)
+    # dK is rounded once (2^-8); e goes into its product as two bf16 values (2^-16) and has p's error (2^-18: scores of size 1 at
+    # most some units, fp32 sums of 32 products; 2^-14 in all covers both); dO.V and the corrected dO.O are fp32 sums of D and of
+    # D + T products in any order, the latter off by what sum p lacks of 1 as well (2^-18 = 64 * 2^-24)
+    size = (np.abs(dO) @ np.abs(V).transpose(0, 2, 1)).max(-1, keepdims=True)
+    near = p * (2 * (D + T + 8) + 64) * 2.0 ** -24 * size + np.abs(e) * 2.0 ** -14
+    bound = 2.0 ** -8 * np.abs(want) + case.scale * (near.transpose(0, 2, 1) @ np.abs(Q)) + 2.0 ** -126
+    # (with dO.O from the rounded O alone the bound would not hold)
+    rounded = (p @ V).astype(np.float32)
+    O = f64(torch.from_numpy(rounded).to(torch.bfloat16))
+    off = case.scale * ((p * (dP - (dO * O).sum(-1, keepdims=True))).transpose(0, 2, 1) @ Q)
+    assert (np.abs(off - want) > bound).any()
+    got = f64(case.run()[0]["dK"]).reshape(N, T, D)
+    assert (np.abs(got - want) <= bound).all(), float((np.abs(got - want) / bound).max())
