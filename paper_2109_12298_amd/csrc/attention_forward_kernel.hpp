@@ -26,7 +26,8 @@
 //
 // Hidden pairs have weight 0 by selection; an infinity or NaN in their values
 // would still turn 0 into NaN in the product, so a block whose sums are not
-// finite is formed again row by row, over visible pairs only.
+// finite is formed again row by row, over visible pairs only; so is one whose sums
+// vanish, as they may for scores past 2^29 (inverse_sum).
 #pragma once
 
 #include "attention_forward.hpp"
@@ -365,8 +366,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
 
     sum += other_half(sum);
     if constexpr (!SMALL) {
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        bool bad = not_finite(sum);
+        const float inv = inverse_sum(sum, top);
+        bool bad = not_finite(sum) || not_finite(inv);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -427,7 +428,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         }
         // (lane li of every wave has row li's total)
         __syncthreads();
-        if (wave == 0 && h == 0) join[0][0][li] = total == 0.0f ? 0.0f : 1.0f / total;
+        if (wave == 0 && h == 0) join[0][0][li] = inverse_sum(total, all);
         __syncthreads();
         bool bad = false;
         for (int at = threadIdx.x; at < 32 * (DP / 4); at += S::THREADS) {
@@ -513,7 +514,7 @@ __global__ __launch_bounds__(256) void join_kernel(Call c, ForwardOut out)
     for (int k = 0; k < PER; ++k) part[wave][lane + kWave * k] = v[k];
     __syncthreads();
     if (wave != 0) return;
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const float inv = inverse_sum(total, all);
     T *o = (T *)out.O + ((i64)n * c.Tq + i) * c.ldo + (i64)head * c.D;
     bool bad = not_finite(inv) || not_finite(total);
 #pragma unroll

@@ -471,5 +471,14 @@ __device__ __forceinline__ void docs_range(const int32_t *docs, int j0, int j1, 
 
 __device__ __forceinline__ bool not_finite(float v) { return !(__builtin_fabsf(v) < INFINITY); }
 
+// 1 / sum of a row's weights, taken from the maximum `top`: 0 for a row that sees nothing, NaN for one that has to be formed again.
+// A weight's exponent is a fused product less the rounded one of the maximum, so that the largest weight is 2^(rounding of top), not
+// 1: from scores of 2^29 on (in units of ln 2) the roundings reach 2^5, from 2^31 on all weights may vanish, or overflow.
+__device__ __forceinline__ float inverse_sum(float sum, float top)
+{
+    if (sum == 0.0f && top == -INFINITY) return 0.0f;
+    return sum < 0x1p-32f ? NAN : 1.0f / sum;
+}
+
 }  // namespace attn
 }  // namespace dpg
