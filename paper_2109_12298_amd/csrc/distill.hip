@@ -21,6 +21,8 @@
 // 16-byte piece and behind the last one are single loads and stores.
 #include "common.hpp"
 
+#include <type_traits>
+
 namespace dpg {
 namespace {
 
@@ -204,13 +206,22 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
     if (bad_id) raise_flag(a.status, DP_FLAG_BAD_INDEX);
     // the teacher's and the row's maxima, then the sums of exponentials
     float zmax = one, s_tau = 0.0f, s_1 = 0.0f;
-    // exp((x - top) / t) as exp2 of one fused product, less a rounded top / t log2 e: its rounding is one factor of all of a row's
-    // exponentials, and so none of a softmax
+    // exp((x - top) / t) as a power of 2.  In general the difference comes first, which is exact where it is small.  A row in registers
+    // whose top / t is below 2^24 takes one fused product instead, x / t less the rounded top / t, whose rounding is one factor of all
+    // of the row's exponentials, within 2^0.5, and so none of a softmax (8192 rows of 100000, bf16: 787 us, 823 by differences).  From
+    // 2^31 on that factor would vanish or overflow, and sums taken from several maxima would each have their own.
     const bool same = a.tau == 1.0f;                       // one exponential serves both
-    const auto add = [&](float x, float base_tau, float base_1) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x, c_tau, -base_tau));
+    const auto power = [&](auto fused, float x, float base, float c) {
+        return decltype(fused)::value ? __builtin_fmaf(x, c, -(base * c)) : (x - base) * c;
+    };
+    const auto add = [&](auto fused, float x, float base) {
+        const float e = __builtin_amdgcn_exp2f(power(fused, x, base, c_tau));
         s_tau += e;
-        if constexpr (HARD) s_1 += same ? e : __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -base_1));
+        if constexpr (HARD) s_1 += same ? e : __builtin_amdgcn_exp2f(power(fused, x, base, kLog2e));
+    };
+    const auto by = [&](bool fused, auto &&f) {
+        if (fused) f(std::true_type{});
+        else f(std::false_type{});
     };
     float top = -INFINITY;                                 // !RESIDENT: the maximum that this thread's sums are taken from
     if constexpr (RESIDENT) {
@@ -229,16 +240,16 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
 #pragma unroll
                     for (int e = 0; e < N; ++e) t = fmaxf(t, elem<T>(v[i], e));
             if (t > top) {
-                s_tau *= __builtin_amdgcn_exp2f(top * c_tau - t * c_tau);
-                if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f(top * kLog2e - t * kLog2e);
+                s_tau *= __builtin_amdgcn_exp2f((top - t) * c_tau);
+                if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f((top - t) * kLog2e);
                 top = t;
             }
-            const float b_tau = top == -INFINITY ? 0.0f : top * c_tau, b_1 = top == -INFINITY ? 0.0f : top * kLog2e;
+            const float base_t = top == -INFINITY ? 0.0f : top;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (base + i * THREADS + tid < pieces)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), b_tau, b_1);
+                    for (int e = 0; e < N; ++e) add(std::false_type{}, elem<T>(v[i], e), base_t);
         }
         zmax = fmaxf(zmax, top);
     }
@@ -248,18 +259,20 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
     float tsum = 0.0f;
     for (int k = tid; k < a.K; k += THREADS)
         if (target_id[k] >= 0) tsum += expf((target[k] - tbase) * inv_tau);
-    const float b_tau = zbase * c_tau, b_1 = zbase * kLog2e;
     if (!RESIDENT && top != -INFINITY) {
-        s_tau *= __builtin_amdgcn_exp2f(top * c_tau - b_tau);
-        if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f(top * kLog2e - b_1);
+        s_tau *= __builtin_amdgcn_exp2f((top - zbase) * c_tau);
+        if constexpr (HARD) s_1 *= __builtin_amdgcn_exp2f((top - zbase) * kLog2e);
     }
-    if (single >= 0) add(one, b_tau, b_1);
-    if constexpr (RESIDENT)
+    const bool is_fused = RESIDENT && __builtin_fabsf(zbase) * fmaxf(c_tau, kLog2e) < 0x1p24f;
+    by(is_fused, [&](auto fused) {
+        if (single >= 0) add(fused, one, zbase);
+        if constexpr (RESIDENT)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i * THREADS + tid < pieces)
+            for (int i = 0; i < NV; ++i)
+                if (i * THREADS + tid < pieces)
 #pragma unroll
-                for (int e = 0; e < N; ++e) add(elem<T>(v[i], e), b_tau, b_1);
+                    for (int e = 0; e < N; ++e) add(fused, elem<T>(v[i], e), zbase);
+    });
     float sums[HARD ? 3 : 2] = {tsum, s_tau};
     if constexpr (HARD) sums[2] = s_1;
     block_add<THREADS>(sums, red + 2);
@@ -285,7 +298,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
         if (soft && target_id[k] >= 0) {
             const float lp = (target[k] - tbase) * inv_tau - ltsum;
             P = expf(lp);
-            if (P != 0.0f) part += P * (lp - (kLn2 * __builtin_fmaf(mine[i], c_tau, -b_tau) - lq));
+            if (P != 0.0f) by(is_fused, [&](auto fused) { part += P * (lp - (kLn2 * power(fused, mine[i], zbase, c_tau) - lq)); });
         }
         target[k] = P;
     }
@@ -295,36 +308,38 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
     const float g_soft = soft ? a.alpha : 0.0f, g_hard = hard ? 1.0f - a.alpha : 0.0f;
     if (tid == 0) {
         float l = g_soft * a.tau * a.tau * parts[0];
-        if (hard) l += g_hard * (logf(s_1) - kLn2 * __builtin_fmaf(z_label, kLog2e, -b_1));
+        if (hard) by(is_fused, [&](auto fused) { l += g_hard * (logf(s_1) - kLn2 * power(fused, z_label, zbase, kLog2e)); });
         a.loss[m] = w * l;
     }
     if (dz == nullptr) return;
 
     // gradient of a class without a target: w a tau q_tau + w (1 - a) q_1
     const float k_tau = soft ? w * g_soft * a.tau / s_tau : 0.0f, k_1 = hard ? w * g_hard / s_1 : 0.0f;
-    const auto grad = [&](float x) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x, c_tau, -b_tau));
+    const auto grad = [&](auto fused, float x) {
+        const float e = __builtin_amdgcn_exp2f(power(fused, x, zbase, c_tau));
         float g = k_tau * e;
-        if constexpr (HARD) g += k_1 * (same ? e : __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -b_1)));
+        if constexpr (HARD) g += k_1 * (same ? e : __builtin_amdgcn_exp2f(power(fused, x, zbase, kLog2e)));
         return g;
     };
     __syncthreads();
-    for (int base = 0; base < (RESIDENT ? 1 : pieces); base += NV * THREADS) {
-        if constexpr (!RESIDENT) load(base);
+    by(is_fused, [&](auto fused) {
+        for (int base = 0; base < (RESIDENT ? 1 : pieces); base += NV * THREADS) {
+            if constexpr (!RESIDENT) load(base);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int p = base + i * THREADS + tid;
-            if (p < pieces) {
-                const u32x4_t o = piece<T>([&](int e) { return grad(elem<T>(v[i], e)); });
-                T *at = dz + first + (i64)p * N;
-                if (vec) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t *>(at));
-                else
+            for (int i = 0; i < NV; ++i) {
+                const int p = base + i * THREADS + tid;
+                if (p < pieces) {
+                    const u32x4_t o = piece<T>([&](int e) { return grad(fused, elem<T>(v[i], e)); });
+                    T *at = dz + first + (i64)p * N;
+                    if (vec) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t *>(at));
+                    else
 #pragma unroll
-                    for (int e = 0; e < N; ++e) put(at + e, elem<T>(o, e));
+                        for (int e = 0; e < N; ++e) put(at + e, elem<T>(o, e));
+                }
             }
         }
-    }
-    if (single >= 0) put(dz + single, grad(one));
+        if (single >= 0) put(dz + single, grad(fused, one));
+    });
     __syncthreads();                                       // waits for the stores above
 
     // target classes: an id that occurs twice is written by its first place, with both
@@ -342,14 +357,15 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
                 mine_first = mine_first && j >= k;
             }
         if (!mine_first) continue;
-        float g = grad(mine[i]) - w * g_soft * a.tau * P;
+        float g = 0.0f;
+        by(is_fused, [&](auto fused) { g = grad(fused, mine[i]) - w * g_soft * a.tau * P; });
         if (id == label) g -= w * g_hard;
         put(dz + id, g);
     }
     if (tid == 0 && hard) {
         bool alone = true;
         for (int j = 0; j < a.K; ++j) alone = alone && target_id[j] != label;
-        if (alone) put(dz + label, grad(z_label) - w * g_hard);
+        if (alone) by(is_fused, [&](auto fused) { put(dz + label, grad(fused, z_label) - w * g_hard); });
     }
 }
 
