@@ -120,7 +120,7 @@ __device__ __forceinline__ void block_add(float (&v)[N], float (*red)[16])
 }
 
 // NV pieces of a row per thread are held; RESIDENT: they are the whole row.
-// HARD: the call has labels (a position may lack its own).
+// HARD: labels have a share of the loss (a position may lack its own).
 template <typename T, int THREADS, int NV, bool RESIDENT, bool HARD>
 __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Args a, T *dZ)
 {
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
         }
     };
     int64_t wanted = -1;
-    if constexpr (HARD) wanted = a.labels[m];
+    if (HARD || a.labels != nullptr) wanted = a.labels[m];
     constexpr int PER = (kMaxK + THREADS - 1) / THREADS;
     int64_t id_of[PER];
     float logit_of[PER], mine[PER];
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
     }
     const float inv_tau = 1.0f / a.tau, c_tau = kLog2e * inv_tau;
     float tmax = -INFINITY;
-    bool bad_id = HARD && tid == 0 && wanted >= V;
+    bool bad_id = tid == 0 && wanted >= V;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int k = tid + i * THREADS;

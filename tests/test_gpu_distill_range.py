@@ -122,3 +122,16 @@ def test_long_rows_keep_their_bits(spread, tau, offset, V, dt):
     Z += offset
     labels = np.abs(labels)
     check(Z, ids, logits, labels, 0.4, tau, weight, dt)
+
+
+@pytest.mark.parametrize("V", [50, 9000, 100001])
+def test_labels_that_have_no_share_are_looked_at(V):
+    """alpha = 1: a label adds nothing to the loss, and one past the classes is flagged all the same (but not at weight 0)."""
+    Z, ids, logits, labels, weight = draw(3, V, 5, "f32", ragged=False)
+    labels[:] = [1, V, 2]
+    loss, dz, status = run(Z, ids, logits, labels, 1.0, 2.0, weight, "f32")
+    assert status == dp.DP_FLAG_BAD_INDEX
+    want, dwant, none = run(Z, ids, logits, None, 1.0, 2.0, weight, "f32")
+    assert none == 0 and torch.equal(loss, want) and torch.equal(dz, dwant)
+    weight[1] = 0.0
+    assert run(Z, ids, logits, labels, 1.0, 2.0, weight, "f32")[2] == 0
