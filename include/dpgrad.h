@@ -486,7 +486,9 @@ dp_status dp_attention_forward(const dp_attention *a, const void *Q, const void 
  * its query heads).  dO is laid out as O, dQ, dK and dV as Q, K and V.
  * Padding queries and keys from L on get zeros.  Sums are formed in fp32; with
  * bf16 inputs p and g are rounded to bf16 (or to the sum of two bf16 values)
- * before their products.  Outputs
+ * before their products.
+ * dO_i.O_i stands for sum_j p_ij dO_i.V_j: what the O given lacks of it, as it
+ * is rounded to bf16, is made up for in dQ and dK.  Outputs
  * overlap nothing.  Sizes as the forward call; workspace:
  * dp_attention_backward_workspace_bytes(a), 16-byte aligned. */
 size_t dp_attention_backward_workspace_bytes(const dp_attention *a);

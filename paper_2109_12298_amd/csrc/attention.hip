@@ -67,8 +67,8 @@ extern "C" dp_status dp_attention_forward(const dp_attention *a, const void *Q, 
 
 extern "C" size_t dp_attention_backward_workspace_bytes(const dp_attention *a)
 {
-    if (check(a) != DP_OK || a->D > kTileD) return 0;
-    return tiles_backward_workspace(*a);
+    if (check(a) != DP_OK) return 0;
+    return a->D > kTileD ? sizeof(float) * (size_t)(a->N * a->Hq * a->Tq) : tiles_backward_workspace(*a);
 }
 
 extern "C" dp_status dp_attention_backward(const dp_attention *a, const void *Q, const void *K, const void *V,
@@ -88,6 +88,6 @@ extern "C" dp_status dp_attention_backward(const dp_attention *a, const void *Q,
     const size_t need = dp_attention_backward_workspace_bytes(a);
     DPG_REQUIRE(need == 0 || (ws != nullptr && aligned(ws, 16) && ws_bytes >= need), DP_EINVAL);
     const Call c = call_of(*a, Q, K, V);
-    if (a->D > kTileD) return rows_backward(c, (dp_dtype)a->dt, O, lse, dO, dQ, dK, dV, stream);
+    if (a->D > kTileD) return rows_backward(c, (dp_dtype)a->dt, O, lse, dO, dQ, dK, dV, ws, stream);
     return tiles_backward(*a, c, (dp_dtype)a->dt, {O, dO, lse, dQ, dK, dV}, ws, stream);
 }

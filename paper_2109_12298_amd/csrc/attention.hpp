@@ -80,10 +80,10 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
-// host side: the kernels of attention_rows.hip
+// host side: the kernels of attention_rows.hip (the backward ones' workspace: a float for each of N * Hq * Tq rows)
 dp_status rows_forward(const Call &c, dp_dtype dt, void *O, float *lse, hipStream_t stream);
 dp_status rows_backward(const Call &c, dp_dtype dt, const void *O, const float *lse, const void *dO, void *dQ, void *dK,
-                        void *dV, hipStream_t stream);
+                        void *dV, void *ws, hipStream_t stream);
 
 }  // namespace attn
 }  // namespace dpg

@@ -18,12 +18,20 @@
 // workgroups as well, and the splits' sums are added by a launch of their own (3
 // samples of 500, 6 and 2 heads of 48, fp32: 96 blocks 70 us, split 31 + 5).
 //
-// With bf16 values O is rounded, and dO.O with it; dQ's launch adds up what p and
-// dO.V say it lacks, for dK.  e, which is small where it cancels, is taken as the
-// sum of two bf16 values in its products, p where workgroups are small: with one
-// each, errors were 1.5 times the outputs' own rounding, with two 1.25 (two samples
-// of 8192 in documents, 32 and 8 heads of 128: dQ 707 -> 833 us, dK and dV 1260 ->
-// 1364).
+// With bf16 values O is rounded, and delta with it.  What it lacks, x_i = sum_j p_ij
+// (dO_i.V_j - delta_i), is known once dQ's launch has been over all keys: dK's takes
+// the whole delta, and dQ less scale x_i sum_j p_ij (1 - tanh^2) K_j, a second sum
+// beside its own (p rounded to bf16 there, as x is some 2^-9 of dO.O).  A part that
+// all keys share drops out of dQ, as e adds up to 0, but not while delta lacks x:
+// dQ was then off by up to several times itself.  The second sum is a quarter more
+// matrix instructions, and for heads wider than 64 its registers leave one wave per
+// SIMD (two samples of 8192 in documents, 32 and 8 heads of 128: dQ 833 -> 1220 us;
+// going over the keys twice, x first, with two waves: 1290; 4 samples of 2048, 16
+// heads of 64, the whole step: 248 -> 261, going twice 297).
+//
+// e, which is small where it cancels, is taken as the sum of two bf16 values in its
+// products, p where workgroups are small: with one each, errors were 1.5 times the
+// outputs' own rounding, with two 1.25 (dQ 707 -> 833 us, dK and dV 1260 -> 1364).
 //
 // Bound by the vector unit's work on the scores (exponent, cap, e, its rounding)
 // and the matrix instructions, which take turns: 32 samples of 128, 12 heads of 64:
@@ -190,7 +198,7 @@ __device__ __forceinline__ void zero(f32x16_t (&acc)[DB])
 // dQ
 // ---------------------------------------------------------------------------
 template <typename T, int DP, bool VEC, int MOD, bool SMALL>
-__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, DP>::RB >= 384 ? 1 : 2)) void query_kernel(
+__global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, DP>::RB >= 192 ? 1 : 2)) void query_kernel(
     Call c, Grads gr, int tiles_m, bool vec_out)
 {
     typedef Shape<T, DP, SMALL> S;
@@ -240,7 +248,9 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
         delta += other_half(delta);
         if (lse2 == INFINITY) delta = 0.0f;
     }
-    float excess = 0.0f;                                 // sum of p (dO.V - delta): what delta lacks, as O is rounded
+    // sum of p (dO.V - delta): what delta lacks, as O is rounded (fp32: no more than the sums' own roundings, and left in dQ)
+    float excess = 0.0f;
+    constexpr bool BESIDE = TL::BF16;
     const Scores<T, MOD> score(c);
     const float slope2 = (MOD & kSlope) != 0 && c.slopes != nullptr ? c.slopes[head] * kLog2e : 0.0f;
 
@@ -249,8 +259,9 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     if (smp.docs != nullptr) wave_docs_range(smp.docs, span.pmin, span.pmax, lane, span.dmin, span.dmax);
 
     typedef f32x16_t Sums[DB];
-    Sums acc;
+    Sums acc, beside;                                    // sums of e K and of p (1 - tanh^2) K
     zero(acc);
+    if constexpr (BESIDE) zero(beside);
     const Stager<TL, T, BN, SMALL ? 1 : NW, VEC> stk(c.ldk, c.D, SMALL ? 0 : wave, lane), stv(c.ldv, c.D, SMALL ? 0 : wave, lane);
     char *mine = smem + (SMALL ? wave * 2 * S::STAGE : 0);
     const uint32_t lds0 = lds_addr(mine);
@@ -297,6 +308,10 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                         g *= bend;
                     }
                     e[k] = g;
+                    if constexpr (BESIDE) {
+                        s[k] = (MOD & kCap) != 0 ? p * bend : p;
+                        if constexpr (!decltype(all)::value) s[k] = (seen >> k & 1u) != 0 ? s[k] : 0.0f;
+                    }
                 }
             };
             if (cls == kFull) {
@@ -307,7 +322,12 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
                 else weigh(std::false_type{}, std::false_type{});
             }
             TL::template columns<1, 1>([&](int) { return LK + 32 * x * TL::RB; }, [&](int) -> const f32x16_t & { return e; },
-                                    [&](int) -> Sums & { return acc; }, lane);
+                                       [&](int) -> Sums & { return acc; }, lane, [&](int step, int d, const bf16x8_t &a) __attribute__((always_inline)) {
+                bf16x8_t b;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) b[k] = (__bf16)s[8 * step + k];
+                beside[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, beside[d], 0, 0, 0);
+            });
         }
     };
 
@@ -379,6 +399,11 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
 #pragma unroll
         for (int w = 0; w < NW; ++w) excess += sums[w * 32 + li];
     }
+    if constexpr (BESIDE)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[d][k] = __builtin_fmaf(-excess, beside[d][k], acc[d][k]);
     if (row_ok && h == 0 && (!SMALL || wave == 0)) {
         gr.row_lse[info] = lse2;
         gr.row_delta[info] = delta + excess;
@@ -388,7 +413,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     if (SMALL ? __syncthreads_or(bad) : __any(bad))
         for (int k = SMALL ? wave : 0; k < 32 && rw + k < M; k += SMALL ? NW : 1) {
             const int ik = (rw + k) / c.G;
-            backward_query_row<T>(c, n, kv * c.G + rw + k - ik * c.G, ik, (const T *)gr.O, gr.lse, (const T *)gr.dO, (T *)gr.dQ);
+            backward_query_row<T>(c, n, kv * c.G + rw + k - ik * c.G, ik, (const T *)gr.O, gr.lse, (const T *)gr.dO, (T *)gr.dQ, nullptr);
         }
 }
 
@@ -604,7 +629,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     wait_loads();                                        // the stores above come before those below
     if (SMALL ? __syncthreads_or(bad) : __any(bad))
         for (int k = SMALL ? wave : 0; k < 32 && jw + k < c.Tk; k += SMALL ? NW : 1)
-            backward_key_row<T>(c, n, kv, jw + k, (const T *)gr.O, gr.lse, (const T *)gr.dO, (T *)gr.dK, (T *)gr.dV);
+            backward_key_row<T>(c, n, kv, jw + k, gr.lse, gr.row_delta, gr.pad, (const T *)gr.dO, (T *)gr.dK, (T *)gr.dV);
 }
 
 // A wave adds a key's sums over the splits, in their order.
@@ -629,7 +654,7 @@ __global__ __launch_bounds__(256) void key_join_kernel(Call c, Grads gr)
 #pragma unroll
         for (int k = 0; k < PER; ++k) bad = bad || not_finite(v[w][k]);
     if (__any(bad)) {
-        backward_key_row<T>(c, n, kv, j, (const T *)gr.O, gr.lse, (const T *)gr.dO, (T *)gr.dK, (T *)gr.dV);
+        backward_key_row<T>(c, n, kv, j, gr.lse, gr.row_delta, gr.pad, (const T *)gr.dO, (T *)gr.dK, (T *)gr.dV);
         return;
     }
 #pragma unroll

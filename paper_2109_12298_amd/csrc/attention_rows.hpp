@@ -70,19 +70,23 @@ __device__ void forward_row(const Call &c, int n, int h, int i, T *O, float *lse
         lse[((i64)n * c.Hq + h) * c.Tq + i] = sum == 0.0f ? -INFINITY : top * kLn2 + logf(sum);
 }
 
-// p and g of a visible pair of query i (head h) and key j; delta = dO.O of the query
+// p, e = p (dO.V - delta) and g of a visible pair of query i (head h) and key j; delta = dO.O of the query
 template <typename T>
 __device__ __forceinline__ void pair_grads(const Call &c, const T *q, const T *k, const T *v, const T *dO, float slope, int far,
-                                           float lse, float delta, float &p, float &g)
+                                           float lse, float delta, float &p, float &e, float &g)
 {
     float bend;
     const float x = score2(c, dot<T>(q, k, c.D), slope, far, bend);
     p = lse == -INFINITY ? 0.0f : exp2f(x - lse * kLog2e);
-    g = p * (dot<T>(dO, v, c.D) - delta) * bend * c.scale;
+    e = p * (dot<T>(dO, v, c.D) - delta);
+    g = e * bend * c.scale;
 }
 
+// Two passes over the keys: O is rounded, and dO.O with it, so the first one adds up what p and dO.V say it lacks.  row_delta: where
+// the sum goes, which backward_key_row takes, or NULL
 template <typename T>
-__device__ void backward_query_row(const Call &c, int n, int h, int i, const T *O, const float *lse, const T *dO, T *dQ)
+__device__ void backward_query_row(const Call &c, int n, int h, int i, const T *O, const float *lse, const T *dO, T *dQ,
+                                   float *row_delta)
 {
     const int lane = threadIdx.x & (kWave - 1), kv = h / c.G;
     const Sample s(c, n);
@@ -93,14 +97,24 @@ __device__ void backward_query_row(const Call &c, int n, int h, int i, const T *
     const T *V = (const T *)c.V + (i64)n * c.Tk * c.ldv + (i64)kv * c.D;
     const float slope = c.slopes != nullptr ? c.slopes[h] : 0.0f;
     const float l = lse[((i64)n * c.Hq + h) * c.Tq + i];
-    const float delta = end > 0 ? dot<T>(dO + ato, O + ato, c.D) : 0.0f;
+    float delta = end > 0 && l != -INFINITY ? dot<T>(dO + ato, O + ato, c.D) : 0.0f, excess = 0.0f;
     float acc[kPerLane] = {};
+    const auto pair = [&](int j, bool see, float &pr, float &e, float &g) {
+        pr = e = g = 0.0f;
+        if (see)
+            pair_grads<T>(c, q, K + (i64)j * c.ldk, V + (i64)j * c.ldv, dO + ato, slope, p < j ? j - p : p - j, l, delta, pr, e, g);
+    };
+    float pr, e, g;
+    for (int j = lane; j < end; j += kWave) {
+        pair(j, s.sees(p, j), pr, e, g);
+        excess += e;
+    }
+    delta += wave_sum(excess);
+    if (row_delta != nullptr && lane == 0) *row_delta = delta;
     for (int j0 = 0; j0 < end; j0 += kWave) {
         const int j = j0 + lane;
         const bool see = j < end && s.sees(p, j);
-        float pr, g = 0.0f;
-        if (see)
-            pair_grads<T>(c, q, K + (i64)j * c.ldk, V + (i64)j * c.ldv, dO + ato, slope, p < j ? j - p : p - j, l, delta, pr, g);
+        pair(j, see, pr, e, g);
         add_rows<T>(acc, see, g, K, c.ldk, j0, 1, c.D);
     }
 #pragma unroll
@@ -108,9 +122,10 @@ __device__ void backward_query_row(const Call &c, int n, int h, int i, const T *
         if (lane + kWave * k < c.D) store_elem(dQ + at + lane + kWave * k, acc[k]);
 }
 
-// dK, dV: either may be NULL
+// dK, dV: either may be NULL; row_delta: [N][Hq][pad]
 template <typename T>
-__device__ void backward_key_row(const Call &c, int n, int kv, int j, const T *O, const float *lse, const T *dO, T *dK, T *dV)
+__device__ void backward_key_row(const Call &c, int n, int kv, int j, const float *lse, const float *row_delta, int pad, const T *dO,
+                                 T *dK, T *dV)
 {
     const int lane = threadIdx.x & (kWave - 1);
     const Sample s(c, n);
@@ -122,16 +137,14 @@ __device__ void backward_key_row(const Call &c, int n, int kv, int j, const T *O
             const int h = kv * c.G + g;
             const float slope = c.slopes != nullptr ? c.slopes[h] : 0.0f;
             const T *Q = (const T *)c.Q + (i64)n * c.Tq * c.ldq + (i64)h * c.D;
-            const T *On = O + (i64)n * c.Tq * c.ldo + (i64)h * c.D, *dOn = dO + (i64)n * c.Tq * c.ldo + (i64)h * c.D;
+            const T *dOn = dO + (i64)n * c.Tq * c.ldo + (i64)h * c.D;
             for (int i0 = 0; i0 < c.Tq; i0 += kWave) {
                 const int i = i0 + lane, p = s.first + i;
                 const bool see = i < c.Tq && s.sees(p, j);
-                float pr = 0.0f, gr = 0.0f;
-                if (see) {
-                    const T *d = dOn + (i64)i * c.ldo;
-                    pair_grads<T>(c, Q + (i64)i * c.ldq, k, v, d, slope, p < j ? j - p : p - j,
-                                  lse[((i64)n * c.Hq + h) * c.Tq + i], dot<T>(d, On + (i64)i * c.ldo, c.D), pr, gr);
-                }
+                float pr = 0.0f, e, gr = 0.0f;
+                if (see)
+                    pair_grads<T>(c, Q + (i64)i * c.ldq, k, v, dOn + (i64)i * c.ldo, slope, p < j ? j - p : p - j,
+                                  lse[((i64)n * c.Hq + h) * c.Tq + i], row_delta[((i64)n * c.Hq + h) * pad + i], pr, e, gr);
                 add_rows<T>(ak, see, gr, Q, c.ldq, i0, 1, c.D);
                 add_rows<T>(av, see, pr, dOn, c.ldo, i0, 1, c.D);
             }

@@ -154,9 +154,12 @@ struct Tile {
     // acc(i)[block of 32 values][.] += sum over 32 rows r of tile(i)[r][value] * w(i)[r], for COUNT blocks of rows one after
     // another; tile(i): where the block starts (a multiple of 32 rows of a tile).
     // bf16 products take w rounded to bf16; where bit i of SPLIT is set, as the sum of two bf16 values, whose second product reads
-    // nothing anew.
-    template <int COUNT, unsigned SPLIT = 0, typename At, typename W, typename Acc>
-    static __device__ __forceinline__ void columns(At &&tile, W &&w, Acc &&acc, int lane)
+    // nothing anew.  also(step, d, operand): further products of what was read (bf16).
+    struct Nothing {
+        __device__ __forceinline__ void operator()(int, int, const bf16x8_t &) const {}
+    };
+    template <int COUNT, unsigned SPLIT = 0, typename At, typename W, typename Acc, typename Also = Nothing>
+    static __device__ __forceinline__ void columns(At &&tile, W &&w, Acc &&acc, int lane, Also &&also = Also())
     {
         const int h = lane >> 5;
         if constexpr (BF16) {
@@ -192,6 +195,7 @@ struct Tile {
                     acc(step >> 1)[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[step & 1][d], b, acc(step >> 1)[d], 0, 0, 0);
                     if (split)
                         acc(step >> 1)[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[step & 1][d], rest, acc(step >> 1)[d], 0, 0, 0);
+                    also(step, d, a[step & 1][d]);
                 }
                 keep_order();
             }

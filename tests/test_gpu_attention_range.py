@@ -70,3 +70,62 @@ def test_scores_past_the_resolution_of_their_differences(shape, kind, dt):
             l = top[:, 0] + np.log((s == top).sum(1))
             # the score's steps, factors log2 e and ln 2: 16 half steps; the capped score's polynomial 10 more
             assert (np.abs(f64(lse[n, h]) - l) <= 32 * 2.0 ** -24 * (np.abs(l) + far.max())).all(), (n, h)
+
+
+# ---------------------------------------------------------------------------
+# gradients that cancel
+# ---------------------------------------------------------------------------
+
+CANCEL = {  # N, Tq, Tk, Hq, Hk, D: few rows, a workgroup's waves, keys with their queries split, blocks of 128 rows, row by row
+    "few": (3, 8, 8, 1, 1, 32), "small": (2, 200, 200, 2, 1, 64), "split": (1, 300, 40, 8, 2, 80), "small128": (1, 257, 257, 2, 2, 128),
+    "blocks": (16, 150, 150, 16, 16, 128), "blocks64": (8, 260, 260, 32, 16, 64), "blocks96": (16, 97, 97, 16, 16, 96),
+    "rows": (2, 70, 70, 2, 1, 160)}
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", list(CANCEL))
+def test_gradients_where_keys_and_values_differ_little(shape, causal):
+    """Keys and values with a common part: dS sums to 0 over a row and what is left of dQ is small, so that dO.O has to be that of
+    O before it was rounded to bf16."""
+    say("cancel", shape, causal)
+    N, Tq, Tk, Hq, Hk, D = CANCEL[shape]
+    c = Case(*CANCEL[shape], "bf16", causal=causal, scale=2.0 ** -5, seed=31)
+    rng = np.random.default_rng(32)
+    for name, part in (("K", 0.25), ("V", 1 / 16)):
+        common = torch.from_numpy(rng.standard_normal((N, 1, Hk, D)))
+        setattr(c, name, (common + part * getattr(c, name).double()).to(torch.bfloat16))
+    out, _ = c.run()
+    Q, K, V, dO = [f64(getattr(c, k)) for k in ("Q", "K", "V", "dO")]
+    G, U = Hq // Hk, 2.0 ** -24
+    want = {k: np.zeros(x.shape) for k, x in (("dQ", Q), ("dK", K))}
+    off, bound = ({k: np.zeros(x.shape) for k, x in want.items()} for _ in range(2))
+    for n in range(N):
+        see = c.mask.see[n]
+        rows = see.any(1)
+        for h in range(Hq):
+            q, k, v, d = Q[n, :, h], K[n, :, h // G], V[n, :, h // G], dO[n, :, h]
+            s = np.where(see, c.scale * (q @ k.T), -np.inf)
+            top = np.where(rows, s.max(1), 0.0)[:, None]
+            w = np.exp(s - top)
+            tot = np.where(rows, w.sum(1), 1.0)[:, None]
+            p, lse = w / tot, top + np.log(tot)
+            dP = d @ v.T
+            e = p * (dP - (p * dP).sum(1, keepdims=True))
+            # a weight: its score's sum of D products, the scale, lse and their difference; a weight is off by some of itself
+            ep = 2 * U * ((D + 4) * c.scale * (np.abs(q) @ np.abs(k).T) + 8 * (1 + np.abs(lse)))
+            size = np.where(see, np.abs(d) @ np.abs(v).T, 0.0).max(1, keepdims=True)
+            # dO.V and dO.O are fp32 sums of D and of D + Tk products, the latter corrected by what it lacks (the sum of p (dO.V - dO.O),
+            # 2^-8 of the size at the most, off by p's error); dS goes into its products as two bf16 values (2^-16)
+            ee = np.abs(e) * (ep + 2.0 ** -16 + 4 * U) + p * size * (2 * U * (2 * D + Tk + 8) + 2.0 ** -8 * ep.max(1, keepdims=True))
+            rounded = f64(torch.from_numpy((p @ v).astype(np.float32)).to(torch.bfloat16))
+            eo = p * (dP - (d * rounded).sum(1, keepdims=True))
+            for x, y, z in ((want, e, False), (off, eo, False), (bound, ee + 2 * U * (Tk + Tq * G) * np.abs(e), True)):
+                a, b = (np.abs(k), np.abs(q)) if z else (k, q)
+                x["dQ"][n, :, h] = c.scale * (y @ a)
+                x["dK"][n, :, h // G] += c.scale * (y.T @ b)
+    for k in ("dQ", "dK"):
+        b = bound[k] + 2.0 ** -8 * (np.abs(want[k]) + bound[k]) + 2.0 ** -126
+        # (with dO.O from the rounded O dQ's bound would not hold; dK's sum over many queries may hide it)
+        assert k == "dK" or (np.abs(off[k] - want[k]) > 4 * b).any()
+        wrong = np.abs(f64(out[k]) - want[k]) / b
+        assert (wrong <= 1).all(), (k, float(wrong.max()), float((wrong > 1).mean()))
