@@ -234,13 +234,13 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const int head = kv * c.G + (row_ok ? g : 0);
     const i64 row = (i64)n * c.Tq + (row_ok ? i : 0), info = ((i64)n * c.Hq + head) * gr.pad + (row_ok ? i : 0);
     u32x4_t qf[KS], df[KS];
-    TL::load_row((const T *)c.Q + row * c.ldq + (i64)head * c.D, c.D, row_ok, VEC, lane, qf);
-    TL::load_row((const T *)gr.dO + row * c.ldo + (i64)head * c.D, c.D, row_ok, VEC, lane, df);
+    TL::load_row((const T *)c.Q + row * c.ldq + (i64)head * c.D, c.D, seeing, VEC, lane, qf);
+    TL::load_row((const T *)gr.dO + row * c.ldo + (i64)head * c.D, c.D, seeing, VEC, lane, df);
     // lse in units of ln 2 (+inf where the query sees nothing: its weights are then 0) and delta, which dK and dV's launch reads
     float lse2 = INFINITY, delta = 0.0f;
     {
         u32x4_t of[KS];
-        TL::load_row((const T *)gr.O + row * c.ldo + (i64)head * c.D, c.D, row_ok, VEC, lane, of);
+        TL::load_row((const T *)gr.O + row * c.ldo + (i64)head * c.D, c.D, seeing, VEC, lane, of);
         const float l = gr.lse[((i64)n * c.Hq + head) * c.Tq + (row_ok ? i : 0)];
         if (seeing && l != -INFINITY) lse2 = l * kLog2e;
 #pragma unroll
@@ -486,8 +486,8 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const auto issue = [&](int t, int g, int buf) __attribute__((always_inline)) {
         const int q0 = t * BN;
         const uint32_t L = lds0 + buf * S::STAGE;
-        stq.issue(Q + (i64)q0 * c.ldq + (i64)g * c.D, c.Tq - q0, L, mine + buf * S::STAGE);
-        std.issue(dO + (i64)q0 * c.ldo + (i64)g * c.D, c.Tq - q0, L + S::HALF, mine + buf * S::STAGE + S::HALF);
+        stq.issue(Q + (i64)q0 * c.ldq + (i64)g * c.D, i1 - q0, L, mine + buf * S::STAGE, i0 - q0);
+        std.issue(dO + (i64)q0 * c.ldo + (i64)g * c.D, i1 - q0, L + S::HALF, mine + buf * S::STAGE + S::HALF, i0 - q0);
         // 64 floats each, inside the padded rows: q0 is a multiple of BN, a short tile's are read twice
         if (SMALL || wave == 0) {
             const uint32_t off = 4u * (uint32_t)(lane & (BN - 1));

@@ -121,7 +121,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
     const int doc = seeing && smp.docs != nullptr ? smp.docs[pos] : -1;
     const int head = kv * c.G + (row_ok ? g : 0);
     u32x4_t qf[KS];
-    TL::load_row((const T *)c.Q + ((i64)n * c.Tq + (row_ok ? i : 0)) * c.ldq + (i64)head * c.D, c.D, row_ok, VEC, lane, qf);
+    TL::load_row((const T *)c.Q + ((i64)n * c.Tq + (row_ok ? i : 0)) * c.ldq + (i64)head * c.D, c.D, seeing, VEC, lane, qf);
     const Scores<T, MOD> score(c);
     const float slope2 = (MOD & kSlope) != 0 && c.slopes != nullptr ? c.slopes[head] * kLog2e : 0.0f;
 

@@ -291,11 +291,12 @@ struct Stager {
         piece = (at - row * TL::PIECES) ^ TL::swz(row);
     }
     __device__ __forceinline__ uint32_t byte(int q) const { return 16u * (uint32_t)(q * TL::N < D ? q : 0); }
-    // rows behind `left` read the last of them (their weights are zeros)
-    __device__ __forceinline__ void issue(const T *base, int left, uint32_t lds, char *generic) const
+    // Rows from `left` on read the one before it, those before `skip` that one: their weights are zeros, and what lies in their own
+    // places (padding may hold anything) meets no product.
+    __device__ __forceinline__ void issue(const T *base, int left, uint32_t lds, char *generic, int skip = 0) const
     {
         if constexpr (VEC) {
-            if (left >= R) {
+            if (left >= R && skip <= 0) {
 #pragma unroll
                 for (int k = 0; k < LOADS; ++k)
                     dma16_off(reinterpret_cast<const char *>(base) + (i64)(k / PERIOD * PERIOD * STEP) * ld_bytes, off[k % PERIOD],
@@ -307,7 +308,7 @@ struct Stager {
         for (int k = 0; k < LOADS; ++k) {
             int row, q;
             place(k, row, q);
-            const int r = row < left ? row : left - 1;
+            const int in = row < skip ? skip : row, r = in < left ? in : left - 1;
             if constexpr (VEC) {
                 dma16_off(base, (uint32_t)r * ld_bytes + byte(q), lds + 1024u * (uint32_t)(wave + NW * k));
             } else {

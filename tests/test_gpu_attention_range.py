@@ -129,3 +129,40 @@ def test_gradients_where_keys_and_values_differ_little(shape, causal):
         assert k == "dK" or (np.abs(off[k] - want[k]) > 4 * b).any()
         wrong = np.abs(f64(out[k]) - want[k]) / b
         assert (wrong <= 1).all(), (k, float(wrong.max()), float((wrong > 1).mean()))
+
+
+# ---------------------------------------------------------------------------
+# padding
+# ---------------------------------------------------------------------------
+
+PADDED = {  # N, Tq, Tk, Hq, Hk, D: a workgroup's waves, queries split, blocks of 128 rows and keys, unaligned heads
+    "small": (3, 90, 90, 4, 2, 64), "split": (3, 300, 40, 4, 2, 80), "blocks": (16, 150, 150, 16, 16, 64), "blocks128": (9, 260, 260, 32, 32, 128),
+    "odd": (3, 70, 70, 4, 2, 33)}
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["plain", "cap", "causal", "last"])
+@pytest.mark.parametrize("shape", list(PADDED))
+def test_padding_holds_anything_at_no_cost(shape, kind, dt):
+    """What lies in padding (queries, their dO, keys, values) changes no bit: sums that it reached would not be finite, and would be
+    formed again in another order and at another speed."""
+    say("padding", shape, kind, dt)
+    N, Tq, Tk, Hq, Hk, D = PADDED[shape]
+    last = kind == "last"
+    lens = np.random.default_rng(41).integers(0, Tk + 1, N)
+    lens[0], lens[1] = Tk // 2 + 1, Tk
+    c = Case(N, Tq, Tk, Hq, Hk, D, dt, causal=kind in ("causal", "last"), last=last, lens=lens, cap=5.0 if kind == "cap" else 0.0, seed=42)
+    outs = []
+    for fill in (0.0, float("nan"), float("inf"), float(torch.finfo(c.tt).max)):
+        for n in range(N):
+            L = int(c.mask.L[n])
+            c.K[n, L:], c.V[n, L:] = fill, fill
+            pad = slice(0, max(0, Tq - L)) if last else slice(min(L, Tq), Tq)
+            c.Q[n, pad], c.dO[n, pad] = fill, fill
+        out, lse = c.run()
+        outs.append([lse, *out.values()])
+    bits = lambda x: x.contiguous().view(torch.int16 if x.dtype == torch.bfloat16 else torch.int32)  # noqa: E731
+    for other in outs[1:]:
+        for k, a, b in zip(("lse", "O", "dQ", "dK", "dV"), outs[0], other):
+            assert bool(torch.isfinite(b if k != "lse" else b.nan_to_num(neginf=0.0)).all()), k
+            assert torch.equal(bits(a), bits(b)), k
