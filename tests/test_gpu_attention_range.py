@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+import token_model_ref as ref
 from lm_ref import f64
 from paper_2109_12298_amd import binding as dp
 from test_gpu_attention import DEV, Case, ws_of
@@ -166,3 +167,113 @@ def test_padding_holds_anything_at_no_cost(shape, kind, dt):
         for k, a, b in zip(("lse", "O", "dQ", "dK", "dV"), outs[0], other):
             assert bool(torch.isfinite(b if k != "lse" else b.nan_to_num(neginf=0.0)).all()), k
             assert torch.equal(bits(a), bits(b)), k
+
+
+# ---------------------------------------------------------------------------
+# documents over more tiles than one list holds (1024 of 32 or 64 keys)
+# ---------------------------------------------------------------------------
+
+def documents(rng, T, lengths, again):
+    """[T]: documents of `lengths` in turn, every `again`-th one under an earlier one's number, some places without a document."""
+    row, k = np.empty(T, dtype=np.int64), 0
+    at = 0
+    while at < T:
+        n = int(rng.integers(*lengths))
+        row[at:at + n] = k if again == 0 or k % again else k // 2
+        at, k = at + n, k + 1
+    row[rng.integers(0, T, 20)] = -1
+    return row.astype(np.int32)
+
+
+def part_mask(see):
+    m = ref.Mask(1, *see.shape)
+    m.see = [see]
+    return m
+
+
+def compare(got, want, bound, what):
+    wrong = np.abs(f64(got) - want) > bound
+    assert not wrong.any(), (what, int(wrong.sum()))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_documents_in_several_lists_single_tokens(dt):
+    """One query a sample over 33500 keys, by a workgroup that is not split: 1047 tiles of 32."""
+    say("lists", "single", dt)
+    N, Tk, H, D, tt = 16, 33500, 64, 8, {"f32": torch.float32, "bf16": torch.bfloat16}[dt]
+    rng = np.random.default_rng(51)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(52)
+    Q, K, V = [torch.randn((N, T, H * D), generator=g, device=DEV, dtype=tt) for T in (1, Tk, Tk)]
+    lens = rng.integers(32700, Tk + 1, N).astype(np.int32)
+    lens[0], lens[1], lens[2] = Tk, 500, 32768
+    docs = np.stack([documents(rng, Tk, (10, 900), 3) for _ in range(N)])
+    for n in range(N):                                 # the last query's document: at its end, about the first list's, and at the start
+        p = int(lens[n]) - 1
+        docs[n, p - 40 - 10 * n:p + 1] = 7
+        docs[n, 5:60:7] = 7
+        docs[n, 32768 - 20:32768 + 20] = 7
+    dev = lambda x: torch.from_numpy(x).to(DEV)  # noqa: E731
+    a = dp.make_attention(dp.DP_F32 if dt == "f32" else dp.DP_BF16, N, 1, Tk, H, H, D, D ** -0.5,
+                          dp.DP_ATTENTION_CAUSAL | dp.DP_ATTENTION_LAST, lens=dev(lens), docs=dev(docs))
+    assert dp.dp_attention_forward_workspace_bytes(a) == 0
+    O, lse = torch.full_like(Q, float("nan")), torch.full((N, H, 1), float("nan"), device=DEV)
+    dp.dp_attention_forward(a, Q, K, V, O, lse)
+    for n in range(N):
+        L = int(lens[n])
+        at = torch.from_numpy(np.flatnonzero((docs[n, :L] == 7) & (docs[n, L - 1] == 7))).to(DEV)
+        part = lambda x: f64(x.reshape(1, -1, H, D))  # noqa: E731
+        (o, l), (eo, el) = ref.attention(part(Q[n]), part(K[n, at]), part(V[n, at]), part_mask(np.ones((1, len(at)), dtype=bool)),
+                                         float(np.float32(D ** -0.5)), dt=tt)
+        compare(O[n].reshape(1, 1, H, D), o, eo, ("O", n))
+        compare(lse[n:n + 1], l, el, ("lse", n))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("Tq,Tk,Hq,Hk", [(66100, 66100, 1, 1), (3, 33500, 4, 2), (200, 70000, 2, 2)])
+def test_documents_in_several_lists(Tq, Tk, Hq, Hk, dt):
+    """Forward and backward: all queries of a sample of 66100, and few over more keys than a list has."""
+    say("lists", Tq, Tk, Hq, Hk, dt)
+    last, D = Tq < Tk, 16
+    rng = np.random.default_rng(53)
+    docs = documents(rng, Tk, (50, 400), 5)
+    docs[32760:32780], docs[65500:65700] = docs[32759], docs[min(65499, Tk - 1)]      # across the lists' ends
+    if last:                                           # the queries' documents start and end all over the keys
+        ids = docs[Tk - Tq:][docs[Tk - Tq:] >= 0]
+        for k in np.unique(ids):
+            s = rng.integers(0, Tk - 60, 12)
+            for b in s:
+                docs[b:b + rng.integers(1, 50)] = k
+    tt = {"f32": torch.float32, "bf16": torch.bfloat16}[dt]
+    x = {k: torch.from_numpy(rng.standard_normal((1, T, H, D))).to(tt) for k, T, H in (("Q", Tq, Hq), ("K", Tk, Hk), ("V", Tk, Hk), ("dO", Tq, Hq))}
+    flags = dp.DP_ATTENTION_CAUSAL | (dp.DP_ATTENTION_LAST if last else 0)
+    a = dp.make_attention(dp.DP_F32 if dt == "f32" else dp.DP_BF16, 1, Tq, Tk, Hq, Hk, D, 0.25, flags,
+                          docs=torch.from_numpy(docs[None].copy()).to(DEV))
+    d = {k: v.reshape(1, v.shape[1], -1).to(DEV) for k, v in x.items()}
+    o = {k: torch.full_like(d[l], float("nan")) for k, l in (("O", "Q"), ("dQ", "Q"), ("dK", "K"), ("dV", "V"))}
+    lse = torch.full((1, Hq, Tq), float("nan"), device=DEV)
+    dp.dp_attention_forward(a, d["Q"], d["K"], d["V"], o["O"], lse, ws_of(dp.dp_attention_forward_workspace_bytes(a)))
+    dp.dp_attention_backward(a, d["Q"], d["K"], d["V"], o["O"], lse, d["dO"], o["dQ"], o["dK"], o["dV"],
+                             ws_of(dp.dp_attention_backward_workspace_bytes(a)))
+    got = {k: f64(v).reshape(1, v.shape[1], -1, D) for k, v in o.items()}
+    X = {k: f64(v) for k, v in x.items()}
+    first = Tk - Tq if last else 0
+    keys_left = np.ones(Tk, dtype=bool)
+    for k in np.unique(docs[docs >= 0]):
+        j = np.flatnonzero(docs == k)
+        i = j[j >= first] - first
+        if len(i) == 0:
+            continue
+        keys_left[j] = False
+        see = j[None, :] <= (i + first)[:, None]
+        args = (part_mask(see), 0.25, 0.0, None, tt)
+        q, kk, v, do = X["Q"][:, i], X["K"][:, j], X["V"][:, j], X["dO"][:, i]
+        (O, l), (eO, el) = ref.attention(q, kk, v, *args)
+        compare(torch.from_numpy(got["O"][:, i]), O, eO, ("O", k))
+        compare(lse[:, :, torch.from_numpy(i).to(DEV)], l, el, ("lse", k))
+        grads, errs = ref.attention_grads(q, kk, v, do, *args)
+        for name, at, want, err in zip(("dQ", "dK", "dV"), (i, j, j), grads, errs):
+            compare(torch.from_numpy(got[name][:, at]), want, err, (name, k))
+    none = docs[first:first + Tq] < 0
+    assert (got["O"][:, none] == 0).all() and (got["dQ"][:, none] == 0).all()
+    assert (got["dK"][:, keys_left] == 0).all() and (got["dV"][:, keys_left] == 0).all()
