@@ -418,8 +418,9 @@ dp_status dp_gated_ffn_backward(const void *dH, const void *G, const void *U, co
  * take one call.  Y may be X (with ldy = ldx); otherwise they do not overlap.
  * pos: int64 [axes][N][T], any values below 2^53 in size; freq: fp64 [P];
  * sections: a host array of `axes` counts >= 0, read during the call only.
- * Angles are formed and reduced in 64 bits (their error is 2^-53 of the
- * angle), sines, cosines and products in fp32, rounded once.
+ * Angles are formed and reduced in 64 bits (their error is at most 3 * 2^-53 of
+ * the angle: its product, 1 / (2 pi) and the product with that, each rounded),
+ * sines, cosines and products in fp32, rounded once.
  * N, T >= 0, H, D >= 1, 1 <= axes <= 4, 2P <= D, ldx, ldy >= H*D; needs
  * N*T < 2^31, D <= 1024, H < 2^20, ldx, ldy < 2^31 (else DP_EUNSUPPORTED). */
 typedef enum dp_rotary_layout { DP_ROTARY_HALVES = 0, DP_ROTARY_ADJACENT = 1 } dp_rotary_layout;
@@ -466,14 +467,16 @@ enum { DP_ATTENTION_CAUSAL = 1, DP_ATTENTION_LAST = 2 };
 
 /* O, and lse (fp32 [N][Hq][Tq], or NULL): the logarithm of a query's softmax
  * sum, -inf where it sees nothing.  Scores, sums and outputs are formed in
- * fp32; with bf16 inputs the softmax weights are rounded to bf16 (or to the sum
- * of two bf16 values) before their product with V.  N, Tq, Tk >= 0; Hq a multiple of Hk >= 1; 1 <= D <= 256;
+ * fp32; with bf16 inputs the softmax weights are rounded to bf16 (or, where there
+ * are few rows, to the sum of two bf16 values) before their product with V.
+ * N, Tq, Tk >= 0; Hq a multiple of Hk >= 1; 1 <= D <= 256;
  * ldq, ldo >= Hq*D, ldk, ldv >= Hk*D.  Needs Tq, Tk < 2^24,
  * N*Hq*ceil(Tq/32) and N*Hk*ceil(Tk/32) < 2^24, N*Hq < 2^31 and ld* < 2^22
  * (else DP_EUNSUPPORTED).  O overlaps no input.
  * Workspace: dp_attention_forward_workspace_bytes(a), 16-byte aligned (0 but
  * for few queries over many keys, whose keys are split over workgroups and
- * joined in a fixed order). */
+ * joined in a fixed order, and for long samples of documents, whose blocks run
+ * in the order of their work). */
 size_t dp_attention_forward_workspace_bytes(const dp_attention *a);
 dp_status dp_attention_forward(const dp_attention *a, const void *Q, const void *K, const void *V, void *O,
                                float *lse, void *ws, size_t ws_bytes, hipStream_t stream);
@@ -487,6 +490,9 @@ dp_status dp_attention_forward(const dp_attention *a, const void *Q, const void 
  * Padding queries and keys from L on get zeros.  Sums are formed in fp32; with
  * bf16 inputs p and g are rounded to bf16 (or to the sum of two bf16 values)
  * before their products.
+ * p takes lse as fp32 holds it, so that its error is some 2^-22 |lse| of itself:
+ * gradients lose digits where scores pass some thousands, and all of them from
+ * 2^21 on.
  * dO_i.O_i stands for sum_j p_ij dO_i.V_j: what the O given lacks of it, as it
  * is rounded to bf16, is made up for in dQ and dK.  Outputs
  * overlap nothing.  Sizes as the forward call; workspace:

@@ -5,8 +5,9 @@
 // and turns all heads by them; a thread keeps its pairs and has the loads of
 // kAhead heads in flight.  An angle is pos * freq / (2 pi) in 64 bits less the
 // nearest whole number of turns, then sine and cosine of what is left (within
-// half a turn) in fp32: the quotient's error is 2^-52 of the angle, so that
-// positions of 2^20 and more keep all of fp32's bits.
+// half a turn) in fp32: the quotient's error is at most 3 * 2^-53 of the angle
+// (the product, the constant and the quotient, each rounded), so that positions of
+// 2^20 and more keep all of fp32's bits.
 //
 // 4 x 4096 positions, 40 heads of 128 out of 56, three axes, bf16: 63 us, 5.3 TB/s
 // (a copy's rate is 4.9).  One position: 3 us, the angles' 64-bit arithmetic and
