@@ -58,9 +58,10 @@ __device__ __forceinline__ float score2(const Call &c, float x, float slope, int
     float s = c.scale * x;
     slope_of_cap = 1.0f;
     if (c.cap > 0.0f) {
-        const float t = tanhf(s / c.cap);
-        s = c.cap * t;
-        slope_of_cap = 1.0f - t * t;
+        // (1 - tanh^2 as a product: the difference would lose its digits where the cap is far exceeded)
+        const float y = s / c.cap, e = expf(-2.0f * fabsf(y)), r = 1.0f / (1.0f + e);
+        s = c.cap * tanhf(y);
+        slope_of_cap = 4.0f * e * r * r;
     }
     s -= slope * (float)far;
     return s * kLog2e;

@@ -224,7 +224,7 @@ __global__ __launch_bounds__((Shape<T, DP, SMALL>::THREADS), (SMALL || Tile<T, D
             for (int e = 0; e < 16; ++e) t = fmaxf(t, s[x][e]);
         t = fmaxf(t, other_half(t));
         if constexpr (MOD == kPlain) t *= score.scale2;
-        if constexpr (MOD == kCap) t = t == -INFINITY ? t : score.cap2 * tanh_for<T>(score.y_scale * t);
+        if constexpr (MOD == kCap) t = t == -INFINITY ? t : score.cap2 * tanh_for<T>(score.y_scale * t, unused);
         if (__any(t > top + 8.0f)) {
             const float was = top;
             top = fmaxf(top, t);

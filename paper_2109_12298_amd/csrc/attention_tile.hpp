@@ -328,7 +328,8 @@ enum { kPlain = 0, kCap = 1, kSlope = 2, kBoth = 3 };
 // tanh y = y P(y^2) up to |y| = 3/4 (least-maximum fits: five terms within 6e-7
 // of it for scores of bf16 inputs, whose rounding is 2^-9 of a score, seven within
 // 1.5e-9 for fp32 ones), from there 1 - 2 / (1 + exp 2|y|), whose subtrahend is at
-// most 0.37 and off by some 2^-23 of it.  Where no score of a bf16 wave's block
+// most 0.37 and off by some 2^-23 of it.  With r = 1 / (1 + exp 2|y|), 1 - tanh^2 is
+// 4 r (1 - r), which keeps its digits where tanh is all but 1.  Where no score of a bf16 wave's block
 // goes past 3/4, which a cap is chosen for, the polynomial alone is taken, with
 // the scales in its coefficients: five instructions a score, of which the last
 // forms the exponent.  No branches by lane: see wave_together.
@@ -338,14 +339,15 @@ constexpr float kTanh[5] = {0.999999435f, -0.333282516f, 0.132589834f, -0.050056
 constexpr float kTanh7[7] = {0.999999999f, -0.33333307f, 0.133325791f, -0.0538856315f, 0.0214308735f, -0.00762702948f, 0.00172035412f};
 
 template <typename T>
-__device__ __forceinline__ float tanh_for(float y)
+__device__ __forceinline__ float tanh_for(float y, float &bend)
 {
     constexpr int TERMS = sizeof(T) == 2 ? 5 : 7;
     const float a = __builtin_fabsf(y), u = y * y;
     float p = sizeof(T) == 2 ? kTanh[4] : kTanh7[6];
 #pragma unroll
     for (int k = TERMS - 2; k >= 0; --k) p = __builtin_fmaf(u, p, sizeof(T) == 2 ? kTanh[k] : kTanh7[k]);
-    const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * a));
+    const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kLog2e * a)), far = 1.0f - 2.0f * r;
+    bend = 4.0f * r * (1.0f - r);
     return a < kNear ? y * p : __builtin_copysignf(far, y);
 }
 
@@ -397,16 +399,13 @@ struct Scores {
                 bend = __builtin_fmaf(-t, t, 1.0f);
                 return __builtin_fmaf(x, p, -base);
             } else {
-                const float t = tanh_for<T>(y_scale * x);
-                bend = __builtin_fmaf(-t, t, 1.0f);
+                const float t = tanh_for<T>(y_scale * x, bend);
                 return __builtin_fmaf(cap2, t, -base);
             }
         } else {
             float v = scale2 * x;
             if (cap2 != 0.0f) {
-                const float t = tanh_for<T>(y_scale * x);
-                bend = __builtin_fmaf(-t, t, 1.0f);
-                v = cap2 * t;
+                v = cap2 * tanh_for<T>(y_scale * x, bend);
             }
             return v - slope2 * far - base;
         }

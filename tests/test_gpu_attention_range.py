@@ -277,3 +277,57 @@ def test_documents_in_several_lists(Tq, Tk, Hq, Hk, dt):
     none = docs[first:first + Tq] < 0
     assert (got["O"][:, none] == 0).all() and (got["dQ"][:, none] == 0).all()
     assert (got["dK"][:, keys_left] == 0).all() and (got["dV"][:, keys_left] == 0).all()
+
+
+# ---------------------------------------------------------------------------
+# scores far past their cap
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["cap", "both"])
+@pytest.mark.parametrize("shape", ["small", "blocks", "rows", "odd"])
+def test_gradients_of_scores_far_past_their_cap(shape, kind, dt):
+    """All scores 5 to 9 caps large, of either sign: 1 - tanh^2 is 2e-4 to 6e-8, and has to be right by itself, not as a difference."""
+    say("saturated", shape, kind, dt)
+    N, T, Hq, Hk, D = {"small": (2, 90, 2, 1, 64), "blocks": (16, 150, 16, 16, 64), "rows": (1, 50, 2, 2, 136), "odd": (2, 60, 2, 1, 33)}[shape]
+    c = Case(N, T, T, Hq, Hk, D, dt, causal=kind == "both", cap=1.0, slopes=kind == "both", scale=1.0, seed=61)
+    rng = np.random.default_rng(62)
+    u = rng.standard_normal(D)
+    u /= np.sqrt(u @ u)
+    put = lambda x: torch.from_numpy(x).to(c.tt)  # noqa: E731
+    c.Q = put(np.sqrt(7) * u + 0.03 * rng.standard_normal(c.Q.shape))
+    c.K = put(rng.choice([-1.0, 1.0], (N, T, Hk, 1)) * np.sqrt(7) * u + 0.03 * rng.standard_normal(c.K.shape))
+    out, _ = c.run()
+    Q, K, V, dO = [f64(getattr(c, k)) for k in ("Q", "K", "V", "dO")]
+    G, U, bf16 = Hq // Hk, 2.0 ** -24, dt == "bf16"
+    want = {k: np.zeros(x.shape) for k, x in (("dQ", Q), ("dK", K))}
+    bound = {k: np.zeros(x.shape) for k, x in want.items()}
+    for n in range(N):
+        see = c.mask.see[n]
+        for h in range(Hq):
+            q, k, v, d = Q[n, :, h], K[n, :, h // G], V[n, :, h // G], dO[n, :, h]
+            y = q @ k.T
+            assert np.abs(y).min() > 5 and np.abs(y).max() < 9
+            s = np.where(see, np.tanh(y) - (0.0 if c.slopes is None else c.slopes[h]) * c.mask.far[n], -np.inf)
+            w = np.exp(s - s.max(1, keepdims=True))
+            p = w / w.sum(1, keepdims=True)
+            r = 1 / (1 + np.exp(2 * np.abs(y)))
+            bend = 4 * r * (1 - r)
+            dP = d @ v.T
+            e = p * (dP - (p * dP).sum(1, keepdims=True)) * bend
+            # bend's logarithm has slope 2 at most: twice the score's error, a sum of D products; the exponential's argument, the quotient
+            # and the product 16 half steps in all.  p: the capped score, bias, lse and exp2, 64 half steps of sizes below 40
+            ey = U * (D + 8) * (np.abs(q) @ np.abs(k).T)
+            ep = 64 * 40 * U
+            size = np.where(see, np.abs(d) @ np.abs(v).T, 0.0).max(1, keepdims=True)
+            ee = np.abs(e) * (2 * ey * 1.01 + 16 * U + 36 * U + ep + (2.0 ** -16 if bf16 else 0)) + p * bend * size * (
+                2 * U * (2 * D + T + 8) + (2.0 ** -8 * ep if bf16 else 0))
+            ee += 2 * U * (T + T * G) * np.abs(e)
+            for x, z, kk, qq in ((want, e, k, q), (bound, ee, np.abs(k), np.abs(q))):
+                x["dQ"][n, :, h] = z @ kk
+                x["dK"][n, :, h // G] += z.T @ qq
+    half = 2.0 ** -8 if bf16 else U
+    for k in ("dQ", "dK"):
+        b = bound[k] + half * (np.abs(want[k]) + bound[k]) + 2.0 ** -126
+        wrong = np.abs(f64(out[k]) - want[k]) / b
+        assert (wrong <= 1).all(), (k, float(wrong.max()), float((wrong > 1).mean()))
