@@ -469,7 +469,8 @@ enum { DP_ATTENTION_CAUSAL = 1, DP_ATTENTION_LAST = 2 };
  * sum, -inf where it sees nothing.  Scores, sums and outputs are formed in
  * fp32; with bf16 inputs the softmax weights are rounded to bf16 (or, where there
  * are few rows, to the sum of two bf16 values) before their product with V.
- * N, Tq, Tk >= 0; Hq a multiple of Hk >= 1; 1 <= D <= 256;
+ * Heads wider than 128 are formed row by row, many times slower than narrower
+ * ones.  N, Tq, Tk >= 0; Hq a multiple of Hk >= 1; 1 <= D <= 256;
  * ldq, ldo >= Hq*D, ldk, ldv >= Hk*D.  Needs Tq, Tk < 2^24,
  * N*Hq*ceil(Tq/32) and N*Hk*ceil(Tk/32) < 2^24, N*Hq < 2^31 and ld* < 2^22
  * (else DP_EUNSUPPORTED).  O overlaps no input.

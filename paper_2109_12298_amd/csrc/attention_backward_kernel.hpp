@@ -25,9 +25,9 @@
 // all keys share drops out of dQ, as e adds up to 0, but not while delta lacks x:
 // dQ was then off by up to several times itself.  The second sum is a quarter more
 // matrix instructions, and for heads wider than 64 its registers leave one wave per
-// SIMD (two samples of 8192 in documents, 32 and 8 heads of 128: dQ 833 -> 1220 us;
-// going over the keys twice, x first, with two waves: 1290; 4 samples of 2048, 16
-// heads of 64, the whole step: 248 -> 261, going twice 297).
+// SIMD.  Steps, forward and backward: two samples of 8192 in documents, 32 and 8
+// heads of 128: 2590 -> 2990 us (dQ 833 -> 1310), 3060 by going over the keys twice,
+// x first, with two waves; 4 samples of 2048, 16 heads of 64: 248 -> 260, twice 297.
 //
 // e, which is small where it cancels, is taken as the sum of two bf16 values in its
 // products, p where workgroups are small: with one each, errors were 1.5 times the
@@ -35,10 +35,11 @@
 //
 // Bound by the vector unit's work on the scores (exponent, cap, e, its rounding)
 // and the matrix instructions, which take turns: 32 samples of 128, 12 heads of 64:
-// dQ 15, dK and dV 13 us.
+// dQ 16, dK and dV 13 us.
 //
 // As in the forward pass, a block whose sums are not finite is formed again row
-// by row, over visible pairs only.
+// by row, over visible pairs only.  Padding does not get there: rows that see nothing
+// are taken as zeros, and tiles of queries repeat a row that counts in their place.
 #pragma once
 
 #include "attention_backward.hpp"
