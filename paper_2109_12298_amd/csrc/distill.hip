@@ -287,9 +287,13 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
         return;
     }
 
-    // P in place of the teacher's logits; the loss
+    // P in place of the teacher's logits; the loss, by differences of logits (a fused power's factor log2 e would overflow for the
+    // lowest value) and the sums' logarithms less what the fused maximum's own power is off from 0
+    const auto log_sum = [&](float sum, float c) {
+        return logf(sum) - (is_fused ? kLn2 * power(std::true_type{}, zbase, zbase, c) : 0.0f);
+    };
     float part = 0.0f;
-    const float lq = logf(s_tau);
+    const float lq = log_sum(s_tau, c_tau);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int k = tid + i * THREADS;
@@ -298,7 +302,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
         if (soft && target_id[k] >= 0) {
             const float lp = (target[k] - tbase) * inv_tau - ltsum;
             P = expf(lp);
-            if (P != 0.0f) by(is_fused, [&](auto fused) { part += P * (lp - (kLn2 * power(fused, mine[i], zbase, c_tau) - lq)); });
+            if (P != 0.0f) part += P * (lp - ((mine[i] - zbase) * inv_tau - lq));
         }
         target[k] = P;
     }
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const T *Z, i64 M, Arg
     const float g_soft = soft ? a.alpha : 0.0f, g_hard = hard ? 1.0f - a.alpha : 0.0f;
     if (tid == 0) {
         float l = g_soft * a.tau * a.tau * parts[0];
-        if (hard) by(is_fused, [&](auto fused) { l += g_hard * (logf(s_1) - kLn2 * power(fused, z_label, zbase, kLog2e)); });
+        if (hard) l += g_hard * (log_sum(s_1, kLog2e) - (z_label - zbase));
         a.loss[m] = w * l;
     }
     if (dz == nullptr) return;

@@ -135,3 +135,19 @@ def test_labels_that_have_no_share_are_looked_at(V):
     assert none == 0 and torch.equal(loss, want) and torch.equal(dz, dwant)
     weight[1] = 0.0
     assert run(Z, ids, logits, labels, 1.0, 2.0, weight, "f32")[2] == 0
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [60, 9001, 100001])
+@pytest.mark.parametrize("top", [1.0, 1e9])
+def test_targets_at_the_lowest_value(top, V, dt):
+    """A teacher's class, or the label, that the row masks with the type's lowest value: a loss of that size, not an infinity."""
+    say("target", top, V, dt)
+    Z, ids, logits, labels, weight = draw(3, V, 4, dt, seed=6, ragged=False)
+    Z *= top
+    low = float(torch.finfo(TT[dt]).min)
+    ids[:], labels[:], weight[:] = [3, 9, 20, 30], 40, 0.5
+    Z[0, 9] = low
+    Z[1, 40] = low
+    Z[2, 3] = Z[2, 30] = Z[2, 40] = low
+    check(Z, ids, logits, labels, 0.5, 1.0, weight, dt)
